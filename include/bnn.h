@@ -298,6 +298,116 @@ BNN_API bnn_status bnn_conv2d_f32(const float *x, const float *w, int N, int C, 
 BNN_API bnn_status bnn_fc_f32(const float *x, const float *w, const float *bias, int64_t M, int64_t K,
                       int64_t N, int sign_input, float *out, void *stream);
 
+/* ---- 8-bit and gated layers ------------------------------------------------------------------
+ *
+ * Layers of more than one bit: an 8-bit linear layer, the gated feed-forward block (16-bit floating point with its
+ * backward pass, or 8-bit), and the norms around such a block.  Matrices are row-major, `_ld` is a row stride in elements.
+ * Rows may start at any address (only base pointers are checked for 16-byte alignment); operands whose rows and strides
+ * are multiples of 16 bytes are staged fastest.  Nothing is read or written beside the rows' elements.
+ */
+typedef enum { BNN_F32 = 0, BNN_BF16 = 1, BNN_F16 = 2 } bnn_float;  /* element type of a tensor */
+typedef enum { BNN_NORM_NONE = 0, BNN_NORM_RMS = 1, BNN_NORM_LAYER = 2 } bnn_norm;
+typedef enum { BNN_ACT_SILU = 0, BNN_ACT_GELU = 1, BNN_ACT_GELU_TANH = 2, BNN_ACT_RELU = 3 } bnn_act;
+
+/*
+ * bnn_quant_rows_i8 -- rows as 8-bit integers with one scale a row (dynamic quantization per token; weights are quantized
+ * by it per output channel).  With a = max |x[m, :]|, all in fp32:
+ *   scale[m] = a / 127,  q[m,k] = rint(x[m,k] * (127 / a))  (to nearest, ties to even: -127 .. 127).
+ *   A row with a < 2^-100 has scale 0 and q 0.  A row that holds an infinity or a NaN has q 0 and scale a (NaN if it
+ *   holds a NaN), so that products with it are NaN.
+ *   x [rows, K] of `type` (bnn_float), q [rows, K] int8, scale [rows] fp32.  rows and K below 2^31 - 65536.
+ */
+BNN_API bnn_status bnn_quant_rows_i8(const void *x, int type, int64_t rows, int64_t K, int64_t x_ld, int8_t *q,
+                                     int64_t q_ld, float *scale, void *stream);
+
+/*
+ * bnn_linear_i8 -- y[m,n] = a_scale[m] * b_scale[n] * sum_k a[m,k] * b[n,k] (+ bias[n]): the sum is exact in int32, then
+ * fp32, rounded once to `type`.
+ *   a [M, K], b [N, K] int8 (any value, -128 too), scales and bias (may be NULL) fp32, y [M, N] of `type` (bnn_float).
+ *   K at most 131071 (BNN_ERR_UNSUPPORTED beyond: the sum could pass 32 bits), M and N below 2^31 - 256.
+ */
+BNN_API bnn_status bnn_linear_i8(const int8_t *a, int64_t lda, const float *a_scale, const int8_t *b, int64_t ldb,
+                                 const float *b_scale, const float *bias, int64_t M, int64_t N, int64_t K, void *y,
+                                 int type, int64_t ldy, void *stream);
+
+/*
+ * bnn_norm_gate -- from one block of a residual network to the next in one pass:
+ *   p[t,c]  = norm_post(b[t,:])[c]                                    the norm after the block
+ *   r'[t,c] = r[t,c] + res_scale[c] * gate[t / gate_rows, c] * p[t,c]  the block's gate and residual scale
+ *   n[t,c]  = norm_pre(r'[t,:])[c]                                    the norm before the next block
+ * with  BNN_NORM_RMS:   x * (mean(x^2) + eps)^(-1/2) * w + bias
+ *       BNN_NORM_LAYER: (x - mean(x)) * (mean((x - mean(x))^2) + eps)^(-1/2) * w + bias
+ *       BNN_NORM_NONE:  x  (takes no w and no bias).
+ * fp32 inside; n is computed from r' before r' is rounded.  The struct is a HOST struct, its pointers device pointers:
+ *   b [rows, D] of `type` (bnn_float), r [rows, D] of r_type (`type` or BNN_F32); gate [ceil(rows / gate_rows), D] of
+ *   `type`: gate_rows consecutive rows share a row of it (1: a gate a token, rows: one for all); res_scale, w_post,
+ *   bias_post, w_pre, bias_pre [D] fp32.  Each vector and the gate may be NULL: 1, or 0 for a bias.
+ *   b NULL: no block yet, r' = r (r_out, post, gate and res_scale have to be absent too).
+ * Outputs: r_out [rows, D] of r_type (may be r itself); n_out [rows, D] of `type` and / or q_out [rows, D] int8 with
+ *   q_scale [rows], n's fp32 values as by bnn_quant_rows_i8.  pre BNN_NORM_NONE: neither n_out nor q_out.
+ * D at most 16384 (BNN_ERR_UNSUPPORTED beyond).
+ */
+typedef struct {
+  int64_t rows;
+  int D;
+  int type, r_type;
+  int post, pre; /* bnn_norm */
+  float eps;
+  const void *b;
+  int64_t b_ld;
+  const void *r;
+  int64_t r_ld;
+  const void *gate;
+  int64_t gate_ld, gate_rows;
+  const float *res_scale, *w_post, *bias_post, *w_pre, *bias_pre;
+} bnn_norm_gate_in;
+BNN_API bnn_status bnn_norm_gate(const bnn_norm_gate_in *in, void *r_out, int64_t r_out_ld, void *n_out, int64_t n_ld,
+                                 int8_t *q_out, int64_t q_ld, float *q_scale, void *stream);
+
+/*
+ * bnn_norm_gate_backward -- gradients of bnn_norm_gate from its inputs (`in` as in the forward call; r is the stream that
+ * went in, not r') and the gradients dn of n and dr_out of r' (either may be NULL: zero).
+ *   dr [rows, D] of r_type, db [rows, D] of `type` (iff b), dgate [groups, D] of `type`, and fp32 [D] sums over the rows:
+ *   dres_scale, dw_post, dbias_post, dw_pre, dbias_pre; each of these six may be NULL (not wanted).  Sums are in fp32, in
+ *   an order that depends on the sizes alone.  rows 0: the sums are 0.
+ *   workspace at least bnn_norm_gate_backward_workspace_bytes(rows, D, gate ? gate_rows : 0) bytes, needed where a
+ *   sum or dgate is wanted.
+ */
+BNN_API bnn_status bnn_norm_gate_backward(const bnn_norm_gate_in *in, const void *dn, int64_t dn_ld, const void *dr_out,
+                                          int64_t dr_out_ld, void *dr, int64_t dr_ld, void *db, int64_t db_ld, void *dgate,
+                                          int64_t dgate_ld, float *dres_scale, float *dw_post, float *dbias_post,
+                                          float *dw_pre, float *dbias_pre, void *workspace, size_t workspace_bytes,
+                                          void *stream);
+BNN_API size_t bnn_norm_gate_backward_workspace_bytes(int64_t rows, int D, int64_t gate_rows);
+
+/*
+ * bnn_gated_ff -- both projections, the activation and the product of a gated feed-forward block in one kernel:
+ *   h[t,f] = act(g) * u,  g = sum_k x[t,k] * wg[f,k],  u = sum_k x[t,k] * wu[f,k]   (fp32, rounded once)
+ *   act: BNN_ACT_SILU z / (1 + exp(-z)); BNN_ACT_GELU z * (1 + erf(z / sqrt 2)) / 2; BNN_ACT_GELU_TANH
+ *   z * (1 + tanh(sqrt(2 / pi) * (z + 0.044715 z^3))) / 2; BNN_ACT_RELU max(z, 0).
+ *   x [T, D], wg, wu [F, D], h [T, F] of `type`, BNN_BF16 or BNN_F16 (BNN_ERR_UNSUPPORTED for BNN_F32).
+ *   saved  NULL, or bnn_gated_ff_saved_bytes(T, F) bytes that the backward pass reads: [2, T, F] fp32, act'(g) * u and
+ *          act(g).
+ * bnn_gated_ff_i8: the same from 8-bit operands with scales (bnn_quant_rows_i8), g = x_scale[t] * wg_scale[f] * (exact
+ *   int32 sum), u likewise; h of any `type`.  D at most 131071.
+ * bnn_gated_ff_backward: from dh [T, F] the gradients dx [T, D], dwg, dwu [F, D], all of `type`.  The gradients of g and u
+ *   are rounded to `type` as operands of the products, sums are fp32.  T or F 0: zeros.
+ *   workspace at least bnn_gated_ff_backward_workspace_bytes(T, D, F) bytes.
+ * T, D and F below 2^22 - 64 (BNN_ERR_UNSUPPORTED beyond; bnn_gated_ff_i8: D as above).
+ */
+BNN_API size_t bnn_gated_ff_saved_bytes(int64_t T, int64_t F);
+BNN_API bnn_status bnn_gated_ff(const void *x, int64_t x_ld, const void *wg, int64_t wg_ld, const void *wu, int64_t wu_ld,
+                                int type, int64_t T, int64_t D, int64_t F, int act, void *h, int64_t h_ld, float *saved,
+                                void *stream);
+BNN_API bnn_status bnn_gated_ff_i8(const int8_t *x, int64_t x_ld, const float *x_scale, const int8_t *wg, int64_t wg_ld,
+                                   const float *wg_scale, const int8_t *wu, int64_t wu_ld, const float *wu_scale, int64_t T,
+                                   int64_t D, int64_t F, int act, void *h, int type, int64_t h_ld, void *stream);
+BNN_API size_t bnn_gated_ff_backward_workspace_bytes(int64_t T, int64_t D, int64_t F);
+BNN_API bnn_status bnn_gated_ff_backward(const void *x, int64_t x_ld, const void *wg, int64_t wg_ld, const void *wu,
+                                         int64_t wu_ld, int type, int64_t T, int64_t D, int64_t F, const float *saved,
+                                         const void *dh, int64_t dh_ld, void *dx, int64_t dx_ld, void *dwg, int64_t dwg_ld,
+                                         void *dwu, int64_t dwu_ld, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- ablation --------------------------------------------------------------------------- */
 
 /*

@@ -30,6 +30,13 @@ class ChainLayer(ctypes.Structure):
     _fields_ = [("w_chain", _p), ("scale", _p), ("bias", _p), ("D", _i32), ("pool", _i32)]
 
 
+class NormGateIn(ctypes.Structure):
+    """bnn_norm_gate_in"""
+    _fields_ = [("rows", _i64), ("D", _i32), ("type", _i32), ("r_type", _i32), ("post", _i32), ("pre", _i32),
+                ("eps", ctypes.c_float), ("b", _p), ("b_ld", _i64), ("r", _p), ("r_ld", _i64), ("gate", _p), ("gate_ld", _i64),
+                ("gate_rows", _i64), ("res_scale", _p), ("w_post", _p), ("bias_post", _p), ("w_pre", _p), ("bias_pre", _p)]
+
+
 # name -> (restype, argtypes); the list mirrors include/bnn.h one to one.
 SIGNATURES = {
     "bnn_status_str": (ctypes.c_char_p, [_i32]),
@@ -63,6 +70,18 @@ SIGNATURES = {
     "bnn_maxpool2x2": (_i32, [_p, _i32, _i32, _i32, _i32, _p, _p, _p, _p, _p]),
     "bnn_conv2d_f32": (_i32, [_p, _p] + [_i32] * 11 + [_p, _p, _p, _p]),
     "bnn_fc_f32": (_i32, [_p, _p, _p, _i64, _i64, _i64, _i32, _p, _p]),
+    "bnn_quant_rows_i8": (_i32, [_p, _i32, _i64, _i64, _i64, _p, _i64, _p, _p]),
+    "bnn_linear_i8": (_i32, [_p, _i64, _p, _p, _i64, _p, _p, _i64, _i64, _i64, _p, _i32, _i64, _p]),
+    "bnn_norm_gate": (_i32, [ctypes.POINTER(NormGateIn), _p, _i64, _p, _i64, _p, _i64, _p, _p]),
+    "bnn_norm_gate_backward": (_i32, [ctypes.POINTER(NormGateIn), _p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _p,
+                                      _p, _p, _p, _p, _sz, _p]),
+    "bnn_norm_gate_backward_workspace_bytes": (_sz, [_i64, _i32, _i64]),
+    "bnn_gated_ff_saved_bytes": (_sz, [_i64, _i64]),
+    "bnn_gated_ff": (_i32, [_p, _i64, _p, _i64, _p, _i64, _i32, _i64, _i64, _i64, _i32, _p, _i64, _p, _p]),
+    "bnn_gated_ff_i8": (_i32, [_p, _i64, _p, _p, _i64, _p, _p, _i64, _p, _i64, _i64, _i64, _i32, _p, _i32, _i64, _p]),
+    "bnn_gated_ff_backward_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "bnn_gated_ff_backward": (_i32, [_p, _i64, _p, _i64, _p, _i64, _i32, _i64, _i64, _i64, _p, _p, _i64, _p, _i64, _p, _i64,
+                                     _p, _i64, _p, _sz, _p]),
 }
 
 # include/bnn_testing.h: the same calls with the kernel variant chosen by the caller, the
@@ -665,6 +684,235 @@ def bnn_fc_f32(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = 
     _check(_c().bnn_fc_f32(_ptr(x), _ptr(w), _ptr(bias), M, K, N, int(sign_input), _ptr(out), _stream()),
            "bnn_fc_f32")
     return out
+
+
+# ---- 8-bit and gated layers ----------------------------------------------------------
+FLOATS = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
+
+
+def _float(t: torch.Tensor, name: str) -> int:
+    if not t.is_cuda or t.dtype not in FLOATS:
+        raise TypeError(f"{name} must be a GPU tensor of dtype {', '.join(map(str, FLOATS))}")
+    return FLOATS[t.dtype]
+
+
+def _rows(t: torch.Tensor, name: str, rows: Optional[int] = None, cols: Optional[int] = None) -> int:
+    """The row stride of a matrix (of the given size) whose rows are contiguous."""
+    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{name}: [{'any' if rows is None else rows}, {'any' if cols is None else cols}] expected, got {list(t.shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the values of a row have to be consecutive")
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+def _vector(t: Optional[torch.Tensor], name: str, n: int) -> Optional[int]:
+    if t is None:
+        return None
+    _dev(t, torch.float32, name)
+    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name}: {n} consecutive values expected")
+    return t.data_ptr()
+
+
+def _one_of(table, key, name: str) -> int:
+    if key not in table:
+        raise ValueError(f"{name}: one of {', '.join(table)}")
+    return table[key]
+
+
+def rows_i8(rows: int, K: int, device="cuda:0") -> torch.Tensor:
+    """Room for int8 [rows, K] whose rows start on 16 bytes, which the products read fastest."""
+    return torch.empty((rows, (K + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :K]
+
+
+def bnn_quant_rows_i8(x: torch.Tensor, q: Optional[torch.Tensor] = None,
+                      scale: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """x [rows, K] fp32, bf16 or fp16 -> (q int8 [rows, K], scale fp32 [rows])."""
+    kind, ld = _float(x, "x"), _rows(x, "x")
+    rows, K = x.shape
+    if q is None:
+        q = rows_i8(rows, K, x.device)
+    if scale is None:
+        scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
+    _dev(q, torch.int8, "q")
+    _check(_c().bnn_quant_rows_i8(_ptr(x), kind, rows, K, ld, _ptr(q), _rows(q, "q", rows, K), _vector(scale, "scale", rows),
+                                   _stream()), "bnn_quant_rows_i8")
+    return q, scale
+
+
+def bnn_linear_i8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor,
+                  bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                  dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """a int8 [M, K] and its scales [M], b int8 [N, K] and its scales [N] -> [M, N] of out's type, or of dtype."""
+    _dev(a, torch.int8, "a")
+    _dev(b, torch.int8, "b")
+    lda = _rows(a, "a")
+    (M, K), N = a.shape, b.shape[0]
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype, device=a.device)
+    _check(_c().bnn_linear_i8(_ptr(a), lda, _vector(a_scale, "a_scale", M), _ptr(b), _rows(b, "b", None, K),
+                               _vector(b_scale, "b_scale", N), _vector(bias, "bias", N), M, N, K, _ptr(out),
+                               _float(out, "out"), _rows(out, "out", M, N), _stream()), "bnn_linear_i8")
+    return out
+
+
+def _norm_in(b, r, gate, gate_rows, res_scale, w_post, bias_post, w_pre, bias_pre, post, pre, eps) -> NormGateIn:
+    r_type, r_ld = _float(r, "r"), _rows(r, "r")
+    rows, D = r.shape
+    kind, b_ld, gate_ld = r_type, 0, 0
+    if b is not None:
+        kind, b_ld = _float(b, "b"), _rows(b, "b", rows, D)
+    if gate is not None:
+        if gate_rows < 1:
+            raise ValueError("gate_rows: at least 1")
+        _dev(gate, b.dtype if b is not None else r.dtype, "gate")
+        gate_ld = _rows(gate, "gate", (rows + gate_rows - 1) // gate_rows, D)
+    return NormGateIn(rows, D, kind, r_type, _one_of(NORMS, post, "post"), _one_of(NORMS, pre, "pre"), eps, _ptr(b), b_ld, _ptr(r),
+                      r_ld, _ptr(gate), gate_ld, gate_rows if gate is not None else 0, _vector(res_scale, "res_scale", D),
+                      _vector(w_post, "w_post", D), _vector(bias_post, "bias_post", D), _vector(w_pre, "w_pre", D),
+                      _vector(bias_pre, "bias_pre", D))
+
+
+def bnn_norm_gate(b: Optional[torch.Tensor], r: torch.Tensor, *, gate: Optional[torch.Tensor] = None, gate_rows: int = 1,
+                  res_scale: Optional[torch.Tensor] = None, w_post: Optional[torch.Tensor] = None,
+                  bias_post: Optional[torch.Tensor] = None, w_pre: Optional[torch.Tensor] = None,
+                  bias_pre: Optional[torch.Tensor] = None, post: str = "rms", pre: str = "rms", eps: float = 1e-6,
+                  r_out: Optional[torch.Tensor] = None, n_out: Optional[torch.Tensor] = None,
+                  q_out: Optional[torch.Tensor] = None, q_scale: Optional[torch.Tensor] = None):
+    """b [rows, D] (a block's output, or None before the first), r [rows, D] (the residual stream) -> (r', n): the new stream
+    (None without b) and its norm, n_out.  With q_out and q_scale n goes out as int8 rows with scales; n_out is then written
+    only if given.  post, pre: "rms", "layer" or "none"."""
+    p = _norm_in(b, r, gate, gate_rows, res_scale, w_post, bias_post, w_pre, bias_pre, post, pre, eps)
+    rows, D = r.shape
+    if r_out is None and b is not None:
+        r_out = torch.empty((rows, D), dtype=r.dtype, device=r.device)
+    if n_out is None and q_out is None and pre != "none":
+        n_out = torch.empty((rows, D), dtype=r.dtype if b is None else b.dtype, device=r.device)
+    lds = [0, 0, 0]
+    for i, (t, dtype, name) in enumerate(((r_out, r.dtype, "r_out"), (n_out, r.dtype if b is None else b.dtype, "n_out"),
+                                          (q_out, torch.int8, "q_out"))):
+        if t is not None:
+            _dev(t, dtype, name)
+            lds[i] = _rows(t, name, rows, D)
+    _check(_c().bnn_norm_gate(ctypes.addressof(p), _ptr(r_out), lds[0], _ptr(n_out), lds[1], _ptr(q_out), lds[2],
+                               _vector(q_scale, "q_scale", rows), _stream()), "bnn_norm_gate")
+    return r_out, n_out
+
+
+def norm_gate_backward_workspace_bytes(rows: int, D: int, gate_rows: int) -> int:
+    return int(_c().bnn_norm_gate_backward_workspace_bytes(rows, D, gate_rows))
+
+
+def bnn_norm_gate_backward(b: Optional[torch.Tensor], r: torch.Tensor, dn: Optional[torch.Tensor],
+                           dr_out: Optional[torch.Tensor], *, gate: Optional[torch.Tensor] = None, gate_rows: int = 1,
+                           res_scale: Optional[torch.Tensor] = None, w_post: Optional[torch.Tensor] = None,
+                           bias_post: Optional[torch.Tensor] = None, w_pre: Optional[torch.Tensor] = None,
+                           bias_pre: Optional[torch.Tensor] = None, post: str = "rms", pre: str = "rms", eps: float = 1e-6,
+                           workspace: Optional[torch.Tensor] = None, out=None):
+    """Gradients of bnn_norm_gate from its inputs and those of its outputs (dn of n, dr_out of r'; None: zero), as a dict: dr,
+    and, for each of b, gate, res_scale, w_post, bias_post, w_pre and bias_pre that was given, its name with a d before it.
+    out: the same dict with tensors to write to, where a caller keeps them."""
+    p = _norm_in(b, r, gate, gate_rows, res_scale, w_post, bias_post, w_pre, bias_pre, post, pre, eps)
+    rows, D = r.shape
+    kind = r.dtype if b is None else b.dtype
+    got = dict(out or {})
+    wanted = {"dr": r, "db": b, "dgate": gate, "dres_scale": res_scale, "dw_post": w_post, "dbias_post": bias_post,
+              "dw_pre": w_pre, "dbias_pre": bias_pre}
+    for name, of in wanted.items():
+        if of is None:
+            got.pop(name, None)
+        elif name not in got:
+            got[name] = torch.empty(of.shape, dtype=of.dtype, device=r.device)
+    mats = [(dn, kind, "dn", rows), (dr_out, r.dtype, "dr_out", rows), (got["dr"], r.dtype, "dr", rows),
+            (got.get("db"), kind, "db", rows), (got.get("dgate"), kind, "dgate", gate.shape[0] if gate is not None else 0)]
+    args = []
+    for t, dtype, name, n in mats:
+        if t is not None:
+            _dev(t, dtype, name)
+        args += [_ptr(t), 0 if t is None else _rows(t, name, n, D)]
+    for name in ("dres_scale", "dw_post", "dbias_post", "dw_pre", "dbias_pre"):
+        args.append(_vector(got.get(name), name, D))
+    if workspace is None:
+        nbytes = norm_gate_backward_workspace_bytes(rows, D, gate_rows if gate is not None else 0)
+        workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=r.device)
+    _check(_c().bnn_norm_gate_backward(ctypes.addressof(p), *args, _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                        _stream()), "bnn_norm_gate_backward")
+    return got
+
+
+def gated_ff_saved(T: int, F: int, device="cuda:0") -> torch.Tensor:
+    """What bnn_gated_ff leaves for its backward pass, [2, T, F] fp32."""
+    return torch.empty((2, T, F), dtype=torch.float32, device=device)
+
+
+def _saved(saved: torch.Tensor, T: int, F: int) -> int:
+    _dev(saved, torch.float32, "saved")
+    if tuple(saved.shape) != (2, T, F) or not saved.is_contiguous():
+        raise ValueError(f"saved: contiguous [2, {T}, {F}] expected")
+    return saved.data_ptr()
+
+
+def _gated_in(x, wg, wu):
+    """(T, D, F, type, strides) of the operands of the two projections."""
+    kind, x_ld = _float(x, "x"), _rows(x, "x")
+    _dev(wg, x.dtype, "wg")
+    _dev(wu, x.dtype, "wu")
+    (T, D), F = x.shape, wg.shape[0]
+    return T, D, F, kind, (x_ld, _rows(wg, "wg", F, D), _rows(wu, "wu", F, D))
+
+
+def bnn_gated_ff(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str = "silu", out: Optional[torch.Tensor] = None,
+                 saved: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [T, D], wg and wu [F, D], all bf16 or all fp16 -> h [T, F] = act(x wg^T) * (x wu^T).  act: "silu", "gelu",
+    "gelu_tanh" or "relu".  saved (gated_ff_saved): written for bnn_gated_ff_backward."""
+    T, D, F, kind, (x_ld, g_ld, u_ld) = _gated_in(x, wg, wu)
+    if out is None:
+        out = torch.empty((T, F), dtype=x.dtype, device=x.device)
+    _dev(out, x.dtype, "out")
+    _check(_c().bnn_gated_ff(_ptr(x), x_ld, _ptr(wg), g_ld, _ptr(wu), u_ld, kind, T, D, F, _one_of(ACTS, act, "act"), _ptr(out),
+                              _rows(out, "out", T, F), None if saved is None else _saved(saved, T, F), _stream()), "bnn_gated_ff")
+    return out
+
+
+def bnn_gated_ff_i8(x: torch.Tensor, x_scale: torch.Tensor, wg: torch.Tensor, wg_scale: torch.Tensor, wu: torch.Tensor,
+                    wu_scale: torch.Tensor, act: str = "silu", out: Optional[torch.Tensor] = None,
+                    dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """bnn_gated_ff on int8 rows with their scales; h of out's type, or of dtype."""
+    for t, name in ((x, "x"), (wg, "wg"), (wu, "wu")):
+        _dev(t, torch.int8, name)
+    x_ld = _rows(x, "x")
+    (T, D), F = x.shape, wg.shape[0]
+    if out is None:
+        out = torch.empty((T, F), dtype=dtype, device=x.device)
+    _check(_c().bnn_gated_ff_i8(_ptr(x), x_ld, _vector(x_scale, "x_scale", T), _ptr(wg), _rows(wg, "wg", F, D),
+                                 _vector(wg_scale, "wg_scale", F), _ptr(wu), _rows(wu, "wu", F, D), _vector(wu_scale, "wu_scale", F),
+                                 T, D, F, _one_of(ACTS, act, "act"), _ptr(out), _float(out, "out"), _rows(out, "out", T, F),
+                                 _stream()), "bnn_gated_ff_i8")
+    return out
+
+
+def gated_ff_backward_workspace_bytes(T: int, D: int, F: int) -> int:
+    return int(_c().bnn_gated_ff_backward_workspace_bytes(T, D, F))
+
+
+def bnn_gated_ff_backward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, saved: torch.Tensor, dh: torch.Tensor,
+                          dx: Optional[torch.Tensor] = None, dwg: Optional[torch.Tensor] = None,
+                          dwu: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """(dx, dwg, dwu) from the operands of bnn_gated_ff, what it saved, and dh [T, F]."""
+    T, D, F, kind, (x_ld, g_ld, u_ld) = _gated_in(x, wg, wu)
+    dx, dwg, dwu = (torch.empty(of.shape, dtype=x.dtype, device=x.device) if t is None else t
+                    for t, of in ((dx, x), (dwg, wg), (dwu, wu)))
+    for t, name in ((dh, "dh"), (dx, "dx"), (dwg, "dwg"), (dwu, "dwu")):
+        _dev(t, x.dtype, name)
+    if workspace is None:
+        workspace = torch.empty(max(16, gated_ff_backward_workspace_bytes(T, D, F)), dtype=torch.uint8, device=x.device)
+    _check(_c().bnn_gated_ff_backward(_ptr(x), x_ld, _ptr(wg), g_ld, _ptr(wu), u_ld, kind, T, D, F, _saved(saved, T, F), _ptr(dh),
+                                       _rows(dh, "dh", T, F), _ptr(dx), _rows(dx, "dx", T, D), _ptr(dwg), _rows(dwg, "dwg", F, D),
+                                       _ptr(dwu), _rows(dwu, "dwu", F, D), _ptr(workspace),
+                                       workspace.numel() * workspace.element_size(), _stream()), "bnn_gated_ff_backward")
+    return dx, dwg, dwu
 
 
 # ---- measurement helpers (include/bnn_testing.h) -----------------------------------

@@ -128,6 +128,17 @@ extern "C" const char *bnn_kernel_name(int kernel_id) {
     case bnn::KID_CONV_F32: return "conv2d_f32";
     case bnn::KID_CONV_F32_SIGN: return "conv2d_f32_sign";
     case bnn::KID_FC_F32: return "fc_f32";
+    case bnn::KID_QUANT_ROWS: return "quant_rows_i8";
+    case bnn::KID_LINEAR_I8: return "linear_i8";
+    case bnn::KID_LINEAR_I8_FEW: return "linear_i8_few";
+    case bnn::KID_NORM_GATE: return "norm_gate";
+    case bnn::KID_NORM_GATE_BACKWARD: return "norm_gate_backward";
+    case bnn::KID_NORM_GATE_SUMS: return "norm_gate_sums";
+    case bnn::KID_GATED_FF: return "gated_ff";
+    case bnn::KID_GATED_FF_I8: return "gated_ff_i8";
+    case bnn::KID_GATED_GRADIENT: return "gated_gradient";
+    case bnn::KID_TRANSPOSE: return "transpose";
+    case bnn::KID_GATED_FF_BACKWARD: return "gated_ff_backward";
     case bnn::KID_VALU_PROBE: return "valu_probe";
     case bnn::KID_COPY_PROBE: return "copy_probe";
   }

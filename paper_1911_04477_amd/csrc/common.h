@@ -33,7 +33,18 @@ enum KernelId : int {
   KID_CONV_CHAIN = 22,
   KID_CONV_POINTWISE = 23,
   KID_XNOR_GEMM_FEWROWS = 24,
-  KID_COUNT = 25
+  KID_QUANT_ROWS = 25,
+  KID_LINEAR_I8 = 26,
+  KID_LINEAR_I8_FEW = 27,
+  KID_NORM_GATE = 28,
+  KID_NORM_GATE_BACKWARD = 29,
+  KID_NORM_GATE_SUMS = 30,
+  KID_GATED_FF = 31,
+  KID_GATED_FF_I8 = 32,
+  KID_GATED_GRADIENT = 33,
+  KID_TRANSPOSE = 34,
+  KID_GATED_FF_BACKWARD = 35,
+  KID_COUNT = 36
 };
 
 // Timing hook: records an event pair around a launch when profiling is on.

@@ -1,0 +1,48 @@
+// Floating-point element types of the quantised and gated layers: conversion to fp32 and, rounded to nearest even, back.
+#pragma once
+#include "common.h"
+
+namespace bnn {
+
+inline bool float_type(int t) { return t == BNN_F32 || t == BNN_BF16 || t == BNN_F16; }
+inline int float_size(int t) { return t == BNN_F32 ? 4 : 2; }
+
+template <int DT>
+struct Float;
+template <>
+struct Float<BNN_F32> { using type = float; };
+template <>
+struct Float<BNN_BF16> { using type = __bf16; };
+template <>
+struct Float<BNN_F16> { using type = _Float16; };
+
+// Calls f with the element type as a tag, f(Float<..>()).
+template <class F>
+inline auto with_float(int t, const F &f) {
+  if (t == BNN_F32) return f(Float<BNN_F32>());
+  if (t == BNN_BF16) return f(Float<BNN_BF16>());
+  return f(Float<BNN_F16>());
+}
+
+// Whether a matrix's rows may be read and written `count` elements of `size` bytes at a time.
+inline bool rows_by(const void *p, int64_t ld, int size, int count) {
+  return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) & (uintptr_t)(count * size - 1)) == 0;
+}
+
+// Four consecutive values of a row of N, from column n on; vec: whole groups of four may go out as one store.
+template <class E, class V>
+__device__ __forceinline__ void store4(E *row, int n, int N, const V &v, bool vec) {
+  typedef E E4 __attribute__((ext_vector_type(4)));
+  if (vec && n + 4 <= N) {
+    E4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = (E)v[i];
+    *reinterpret_cast<E4 *>(row + n) = o;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < N) row[n + i] = (E)v[i];
+  }
+}
+
+}  // namespace bnn

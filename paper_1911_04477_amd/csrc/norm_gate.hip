@@ -1,0 +1,438 @@
+// The norms after a block and before the next one, with the block's gate and residual scale between them
+// (bnn_norm_gate), and their backward pass.
+#include <algorithm>
+#include <cmath>
+
+#include "rows.h"
+
+namespace bnn {
+
+struct NormOut {
+  void *r, *n;
+  int64_t r_ld, n_ld, q_ld;
+  int8_t *q;
+  float *q_scale;
+};
+
+struct NormGrad {
+  const void *dn, *dr_out;
+  int64_t dn_ld, dr_out_ld;
+  void *dr, *db, *dgate;
+  int64_t dr_ld, db_ld, dgate_ld;
+  float *part;       // [6][workers][D]: w_pre, bias_pre, w_post, bias_post, res_scale, gate
+  int want;          // bit k: sum k is wanted
+  int workers, per;  // teams, rows a team takes at most
+  int segments;      // teams that share a group of rows with one gate; 0: a team has whole groups
+};
+
+__device__ __forceinline__ void fill8(float (&v)[8], float x) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = x;
+}
+// Values of a vector of D, or of a matrix row; `missing` where there is none.
+template <class E>
+__device__ __forceinline__ void load8_or(float (&v)[8], const E *row, int c, int D, float missing) {
+  if (row) load8(v, row, c, D);
+  else fill8(v, missing);
+}
+__device__ __forceinline__ void zero_past(float (&v)[8], int c, int D) {
+  if (c + 8 > D)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i >= D) v[i] = 0.0f;
+}
+
+// v: values before the norm, then normed (before weight and bias).  Returns the factor.  Centred values first, then the
+// mean of their squares: no difference of two large sums.  lds: two reductions' worth.
+template <int T, int NV>
+__device__ __forceinline__ float unit_rows(float (&v)[NV][8], int norm, int c0, int D, float eps, uint32_t *lds) {
+  if (norm == BNN_NORM_NONE) return 1.0f;
+  if (norm == BNN_NORM_LAYER) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += v[i][j];
+    const float mean = team_sum<T>(sum, lds) / (float)D;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] -= mean;
+      zero_past(v[i], c0 + i * T * 8, D);
+    }
+  }
+  float sq = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sq = fmaf(v[i][j], v[i][j], sq);
+  const float rs = 1.0f / sqrtf(team_sum<T>(sq, lds + T / 64) / (float)D + eps);
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] *= rs;
+  return rs;
+}
+
+// e: gradient of the normed values u, then of the values before the norm: rs * (e - mean(e) - u * mean(e * u)), the first
+// mean for centred norms only.
+template <int T, int NV>
+__device__ __forceinline__ void unit_rows_backward(float (&e)[NV][8], const float (&u)[NV][8], float rs, int norm, int D,
+                                                   uint32_t *lds) {
+  if (norm == BNN_NORM_NONE) return;
+  float along = 0.0f, level = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) along = fmaf(e[i][j], u[i][j], along), level += e[i][j];
+  along = team_sum<T>(along, lds) / (float)D;
+  level = norm == BNN_NORM_LAYER ? team_sum<T>(level, lds + T / 64) / (float)D : 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[i][j] = rs * (e[i][j] - level - u[i][j] * along);
+}
+
+// Which row of the gate; the host has cut gate_rows to at most 2^31 - 1 rows.
+__device__ __forceinline__ int64_t norm_group(const bnn_norm_gate_in &p, int64_t row) { return (uint32_t)row / (uint32_t)p.gate_rows; }
+
+// A team of T threads takes a row at a time, NV pieces of eight values a thread.
+template <class E, class R, int T, int NV>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_gate_kernel(bnn_norm_gate_in p, NormOut o, int teams) {
+  constexpr int TEAMS = T < 256 ? 256 / T : 1;
+  __shared__ uint32_t lds[2][5][T / 64];
+  const int t = threadIdx.x % T, c0 = t * 8, D = p.D;
+  float w_post[NV][8], w_pre[NV][8], scale[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    load8_or(w_post[i], p.w_post, c0 + i * T * 8, D, 1.0f);
+    load8_or(w_pre[i], p.w_pre, c0 + i * T * 8, D, 1.0f);
+    load8_or(scale[i], p.res_scale, c0 + i * T * 8, D, 1.0f);
+  }
+  int flip = 0;  // a row's reductions do not touch what the row before left for slower waves to read
+  for (int64_t row = (int64_t)blockIdx.x * TEAMS + (TEAMS > 1 ? threadIdx.x / T : 0); row < p.rows; row += teams, flip ^= 1) {
+    uint32_t *const mem = &lds[flip][0][0];
+    float v[NV][8], r[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      load8(r[i], static_cast<const R *>(p.r) + row * p.r_ld, c0 + i * T * 8, D);
+      if (p.b) load8(v[i], static_cast<const E *>(p.b) + row * p.b_ld, c0 + i * T * 8, D);
+    }
+    if (p.b) {
+      unit_rows<T, NV>(v, p.post, c0, D, p.eps, mem);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = c0 + i * T * 8;
+        float g[8], bias[8];
+        load8_or(bias, p.bias_post, c, D, 0.0f);
+        load8_or(g, p.gate ? static_cast<const E *>(p.gate) + norm_group(p, row) * p.gate_ld : nullptr, c, D, 1.0f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[i][j] += scale[i][j] * g[j] * (v[i][j] * w_post[i][j] + bias[j]);
+        if (o.r) store8(static_cast<R *>(o.r) + row * o.r_ld, c, D, r[i]);
+      }
+    }
+    if (p.pre == BNN_NORM_NONE) continue;
+    unit_rows<T, NV>(r, p.pre, c0, D, p.eps, mem + 2 * (T / 64));
+    uint32_t top = 0u;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = c0 + i * T * 8;
+      float bias[8];
+      load8_or(bias, p.bias_pre, c, D, 0.0f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r[i][j] = r[i][j] * w_pre[i][j] + bias[j];
+      zero_past(r[i], c, D);
+      if (o.n) store8(static_cast<E *>(o.n) + row * o.n_ld, c, D, r[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max(top, magnitude(r[i][j]));
+    }
+    if (o.q) {
+      const RowScale s = row_scale(team_max_magnitude<T>(top, mem + 4 * (T / 64)));
+#pragma unroll
+      for (int i = 0; i < NV; ++i) store_q8(o.q + row * o.q_ld, c0 + i * T * 8, D, r[i], s.inv);
+      if (t == 0) o.q_scale[row] = s.scale;
+    }
+  }
+}
+
+// Teams walk through contiguous rows and keep the sums over rows in registers; the sums of all teams meet in
+// norm_gate_sums_kernel, in the same order at every call.
+template <class E, class R, int T, int NV>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_gate_backward_kernel(bnn_norm_gate_in p, NormGrad q) {
+  constexpr int TEAMS = T < 256 ? 256 / T : 1;
+  __shared__ uint32_t lds[2][8][T / 64];
+  const int worker = blockIdx.x * TEAMS + (TEAMS > 1 ? threadIdx.x / T : 0);
+  if (worker >= q.workers) return;  // whole waves; only teams of one wave share a workgroup
+  const int t = threadIdx.x % T, c0 = t * 8, D = p.D;
+  int64_t row, end;
+  if (q.segments) {
+    const int64_t group = worker / q.segments, part = worker % q.segments;
+    row = group * p.gate_rows + part * q.per;
+    end = min(min(row + q.per, (group + 1) * p.gate_rows), p.rows);
+  } else {
+    row = (int64_t)worker * q.per;
+    end = min(row + q.per, p.rows);
+  }
+  float w_post[NV][8], w_pre[NV][8], scale[NV][8], sum[6][NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    load8_or(w_post[i], p.w_post, c0 + i * T * 8, D, 1.0f);
+    load8_or(w_pre[i], p.w_pre, c0 + i * T * 8, D, 1.0f);
+    load8_or(scale[i], p.res_scale, c0 + i * T * 8, D, 1.0f);
+#pragma unroll
+    for (int k = 0; k < 6; ++k) fill8(sum[k][i], 0.0f);
+  }
+  int64_t left = p.gate_rows;  // of the group with this gate
+  for (int flip = 0; row < end; ++row, flip ^= 1) {
+    uint32_t *const mem = &lds[flip][0][0];
+    float b[NV][8], r[NV][8], e[NV][8], dr[NV][8], g[NV][8], pv[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = c0 + i * T * 8;
+      load8(r[i], static_cast<const R *>(p.r) + row * p.r_ld, c, D);
+      load8_or(b[i], p.b ? static_cast<const E *>(p.b) + row * p.b_ld : nullptr, c, D, 0.0f);
+      load8_or(e[i], q.dn ? static_cast<const E *>(q.dn) + row * q.dn_ld : nullptr, c, D, 0.0f);
+      load8_or(dr[i], q.dr_out ? static_cast<const R *>(q.dr_out) + row * q.dr_out_ld : nullptr, c, D, 0.0f);
+      load8_or(g[i], p.gate ? static_cast<const E *>(p.gate) + norm_group(p, row) * p.gate_ld : nullptr, c, D, 1.0f);
+    }
+    // forward again: b normed, p, r' normed
+    const float rsb = p.b ? unit_rows<T, NV>(b, p.post, c0, D, p.eps, mem) : 1.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float bias[8];
+      load8_or(bias, p.bias_post, c0 + i * T * 8, D, 0.0f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        pv[i][j] = b[i][j] * w_post[i][j] + bias[j];
+        if (p.b) r[i][j] += scale[i][j] * g[i][j] * pv[i][j];
+      }
+      zero_past(r[i], c0 + i * T * 8, D);
+    }
+    if (p.pre != BNN_NORM_NONE) {
+      const float rsr = unit_rows<T, NV>(r, p.pre, c0, D, p.eps, mem + 2 * (T / 64));
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          sum[0][i][j] = fmaf(e[i][j], r[i][j], sum[0][i][j]);
+          sum[1][i][j] += e[i][j];
+          e[i][j] *= w_pre[i][j];
+        }
+      unit_rows_backward<T, NV>(e, r, rsr, p.pre, D, mem + 4 * (T / 64));
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dr[i][j] += e[i][j];
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      zero_past(dr[i], c0 + i * T * 8, D);
+      store8(static_cast<R *>(q.dr) + row * q.dr_ld, c0 + i * T * 8, D, dr[i]);
+    }
+    if (!p.b) continue;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float along = dr[i][j] * pv[i][j], dp = dr[i][j] * scale[i][j] * g[i][j];
+        sum[2][i][j] = fmaf(dp, b[i][j], sum[2][i][j]);
+        sum[3][i][j] += dp;
+        sum[4][i][j] = fmaf(along, g[i][j], sum[4][i][j]);
+        sum[5][i][j] = fmaf(along, scale[i][j], sum[5][i][j]);
+        e[i][j] = dp * w_post[i][j];
+      }
+    unit_rows_backward<T, NV>(e, b, rsb, p.post, D, mem + 6 * (T / 64));
+#pragma unroll
+    for (int i = 0; i < NV; ++i) store8(static_cast<E *>(q.db) + row * q.db_ld, c0 + i * T * 8, D, e[i]);
+    if (q.dgate && !q.segments && (--left == 0 || row + 1 == end)) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        store8(static_cast<E *>(q.dgate) + norm_group(p, row) * q.dgate_ld, c0 + i * T * 8, D, sum[5][i]);
+        fill8(sum[5][i], 0.0f);
+      }
+      left = p.gate_rows;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 6; ++k)
+    if (q.want >> k & 1)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) store8(q.part + ((int64_t)k * q.workers + worker) * D, c0 + i * T * 8, D, sum[k][i]);
+}
+
+struct NormSums {
+  const float *part;
+  float *out[5];
+  void *dgate;
+  int64_t dgate_ld;
+  int workers, segments, D;
+};
+// Sums of the teams' sums: 64 columns a workgroup, its 16 waves share the teams out.  blockIdx.y: which sum; from 5 on: the
+// gate of group blockIdx.y - 5.
+template <class E>
+__global__ __launch_bounds__(1024) void norm_gate_sums_kernel(NormSums q) {
+  __shared__ float lds[16][64];
+  const int which = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  if (which < 5 && !q.out[which]) return;
+  const int first = which < 5 ? 0 : (which - 5) * q.segments, last = which < 5 ? q.workers : first + q.segments;
+  const float *part = q.part + (int64_t)min(which, 5) * q.workers * q.D;
+  float sum = 0.0f;
+  if (c < q.D)
+    for (int w = first + wave; w < last; w += 16) sum += part[(int64_t)w * q.D + c];
+  lds[wave][lane] = sum;
+  __syncthreads();
+  if (wave || c >= q.D) return;
+  sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) sum += lds[w][lane];
+  if (which < 5) q.out[which][c] = sum;
+  else static_cast<E *>(q.dgate)[(which - 5) * q.dgate_ld + c] = (E)sum;
+}
+
+constexpr int NORM_MAX_D = 16384;
+
+struct NormPlan {
+  int workers, per, segments;
+};
+// About as many teams as the card has room for; each takes contiguous rows, of one group where a gate is shared by more rows
+// than that, else of whole groups.
+inline NormPlan norm_plan(int64_t rows, int D, int64_t gate_rows) {
+  const int64_t room = D <= 512 ? 2048 : D <= 2048 ? 1024 : 512;
+  int64_t per = (rows - 1) / room + 1;
+  if (gate_rows > rows) gate_rows = rows;
+  if (gate_rows > per) {
+    const int64_t segments = (gate_rows - 1) / per + 1, groups = (rows - 1) / gate_rows + 1;
+    return {(int)(segments * groups), (int)((gate_rows - 1) / segments + 1), (int)segments};
+  }
+  if (gate_rows > 0) per = ((per - 1) / gate_rows + 1) * gate_rows;
+  return {(int)((rows - 1) / per + 1), (int)per, 0};
+}
+
+// f with the element types and the team as tags.
+template <class F>
+void with_norm(const bnn_norm_gate_in &p, const F &f) {
+  const auto widths = [&](auto e, auto r) {
+    if (p.D <= 512) f(e, r, std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
+    else if (p.D <= 2048) f(e, r, std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
+    else if (p.D <= 4096) f(e, r, std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
+    else if (p.D <= 8192) f(e, r, std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
+    else f(e, r, std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
+  };
+  if (p.type == BNN_F32) widths(Float<BNN_F32>(), Float<BNN_F32>());
+  else if (p.type == BNN_BF16 && p.r_type == BNN_F32) widths(Float<BNN_BF16>(), Float<BNN_F32>());
+  else if (p.type == BNN_BF16) widths(Float<BNN_BF16>(), Float<BNN_BF16>());
+  else if (p.r_type == BNN_F32) widths(Float<BNN_F16>(), Float<BNN_F32>());
+  else widths(Float<BNN_F16>(), Float<BNN_F16>());
+}
+
+inline bool norm_known(int n) { return n >= BNN_NORM_NONE && n <= BNN_NORM_LAYER; }
+
+// No group is longer than the rows there are.
+inline bnn_norm_gate_in cut_groups(bnn_norm_gate_in p) {
+  p.gate_rows = p.gate ? std::min(p.gate_rows, p.rows) : 1;
+  return p;
+}
+
+bnn_status check_norm(const bnn_norm_gate_in *p) {
+  if (!p) return BNN_ERR_NULL;
+  if (p->rows < 0 || p->D <= 0 || !float_type(p->type) || !float_type(p->r_type) || !norm_known(p->post) || !norm_known(p->pre) ||
+      !(p->eps >= 0.0f) || !std::isfinite(p->eps))
+    return BNN_ERR_SHAPE;
+  if (p->gate && p->gate_rows < 1) return BNN_ERR_SHAPE;
+  if (p->rows > 0 && !p->b && (p->post != BNN_NORM_NONE || p->gate || p->res_scale)) return BNN_ERR_NULL;  // of nothing
+  if ((p->post == BNN_NORM_NONE && (p->w_post || p->bias_post)) || (p->pre == BNN_NORM_NONE && (p->w_pre || p->bias_pre)))
+    return BNN_ERR_SHAPE;
+  if (p->r_ld < p->D || (p->b && p->b_ld < p->D) || (p->gate && p->gate_ld < p->D)) return BNN_ERR_STRIDE;
+  if ((p->r_type != p->type && p->r_type != BNN_F32) || p->D > NORM_MAX_D || p->rows > INT32_MAX) return BNN_ERR_UNSUPPORTED;
+  if (!aligned16(p->b) || !aligned16(p->r) || !aligned16(p->gate) || !aligned16(p->res_scale) || !aligned16(p->w_post) ||
+      !aligned16(p->bias_post) || !aligned16(p->w_pre) || !aligned16(p->bias_pre))
+    return BNN_ERR_ALIGN;
+  return BNN_OK;
+}
+
+}  // namespace bnn
+
+extern "C" bnn_status bnn_norm_gate(const bnn_norm_gate_in *in, void *r_out, int64_t r_out_ld, void *n_out, int64_t n_ld, int8_t *q_out,
+                                    int64_t q_ld, float *q_scale, void *stream) {
+  using namespace bnn;
+  if (bnn_status st = check_norm(in)) return st;
+  const bnn_norm_gate_in &p = *in;
+  if (p.pre == BNN_NORM_NONE && (n_out || q_out)) return BNN_ERR_SHAPE;
+  if ((r_out && r_out_ld < p.D) || (n_out && n_ld < p.D) || (q_out && q_ld < p.D)) return BNN_ERR_STRIDE;
+  if (p.rows == 0) return BNN_OK;
+  if (!p.r || (p.b && !r_out) || (!p.b && r_out) || (p.pre != BNN_NORM_NONE && !n_out && !q_out) || (!q_out != !q_scale))
+    return BNN_ERR_NULL;
+  if (!aligned16(r_out) || !aligned16(n_out) || !aligned16(q_out) || !aligned16(q_scale)) return BNN_ERR_ALIGN;
+  if (!p.b && p.pre == BNN_NORM_NONE) return BNN_OK;  // nothing to write
+  const NormOut o = {r_out, n_out, r_out_ld, n_ld, q_ld, q_out, q_scale};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const bnn_norm_gate_in in_groups = cut_groups(p);
+  ProfScope ps(KID_NORM_GATE, s);
+  with_norm(p, [&](auto e, auto r, auto threads, auto pieces) {
+    constexpr int T = decltype(threads)::value, NV = decltype(pieces)::value, BLOCK = T < 256 ? 256 : T, TEAMS = BLOCK / T;
+    const int64_t room = 256 * (2048 / BLOCK);  // workgroups that run at once
+    const uint32_t grid = (uint32_t)std::min<int64_t>((p.rows - 1) / TEAMS + 1, room);
+    norm_gate_kernel<typename decltype(e)::type, typename decltype(r)::type, T, NV><<<grid, BLOCK, 0, s>>>(in_groups, o, (int)grid * TEAMS);
+  });
+  return launch_status();
+}
+
+extern "C" size_t bnn_norm_gate_backward_workspace_bytes(int64_t rows, int D, int64_t gate_rows) {
+  using namespace bnn;
+  if (rows <= 0 || D <= 0 || D > NORM_MAX_D || rows > INT32_MAX || gate_rows < 0) return 0;
+  return sizeof(float) * 6 * (size_t)norm_plan(rows, D, gate_rows).workers * (size_t)D;
+}
+
+extern "C" bnn_status bnn_norm_gate_backward(const bnn_norm_gate_in *in, const void *dn, int64_t dn_ld, const void *dr_out,
+                                             int64_t dr_out_ld, void *dr, int64_t dr_ld, void *db, int64_t db_ld, void *dgate,
+                                             int64_t dgate_ld, float *dres_scale, float *dw_post, float *dbias_post, float *dw_pre,
+                                             float *dbias_pre, void *workspace, size_t workspace_bytes, void *stream) {
+  using namespace bnn;
+  if (bnn_status st = check_norm(in)) return st;
+  const bnn_norm_gate_in &p = *in;
+  if (p.pre == BNN_NORM_NONE && (dn || dw_pre || dbias_pre)) return BNN_ERR_SHAPE;
+  if (p.rows > 0 && ((!p.b && (db || dres_scale || dw_post || dbias_post)) || (!p.gate && dgate))) return BNN_ERR_SHAPE;
+  if ((dn && dn_ld < p.D) || (dr_out && dr_out_ld < p.D) || (dr && dr_ld < p.D) || (db && db_ld < p.D) || (dgate && dgate_ld < p.D))
+    return BNN_ERR_STRIDE;
+  if (!aligned16(dn) || !aligned16(dr_out) || !aligned16(dr) || !aligned16(db) || !aligned16(dgate) || !aligned16(dres_scale) ||
+      !aligned16(dw_post) || !aligned16(dbias_post) || !aligned16(dw_pre) || !aligned16(dbias_pre) || !aligned16(workspace))
+    return BNN_ERR_ALIGN;
+  NormSums sums = {};
+  sums.D = p.D;
+  sums.out[0] = dw_pre, sums.out[1] = dbias_pre, sums.out[2] = dw_post, sums.out[3] = dbias_post, sums.out[4] = dres_scale;
+  NormGrad q = {};
+  for (int k = 0; k < 5; ++k) q.want |= (sums.out[k] ? 1 : 0) << k;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (p.rows > 0) {
+    if (!p.r || !dr || (p.b && !db)) return BNN_ERR_NULL;
+    const NormPlan plan = norm_plan(p.rows, p.D, p.gate ? p.gate_rows : 0);
+    q.dn = dn, q.dr_out = dr_out, q.dn_ld = dn_ld, q.dr_out_ld = dr_out_ld;
+    q.dr = dr, q.db = db, q.dgate = dgate, q.dr_ld = dr_ld, q.db_ld = db_ld, q.dgate_ld = dgate_ld;
+    q.workers = plan.workers, q.per = plan.per, q.segments = plan.segments;
+    if (dgate && plan.segments) q.want |= 1 << 5;
+    if (q.want) {
+      if (!workspace) return BNN_ERR_NULL;
+      if (workspace_bytes < bnn_norm_gate_backward_workspace_bytes(p.rows, p.D, p.gate ? p.gate_rows : 0)) return BNN_ERR_WORKSPACE;
+    }
+    q.part = static_cast<float *>(workspace);
+    const bnn_norm_gate_in in_groups = cut_groups(p);
+    ProfScope ps(KID_NORM_GATE_BACKWARD, s);
+    with_norm(p, [&](auto e, auto r, auto threads, auto pieces) {
+      constexpr int T = decltype(threads)::value, NV = decltype(pieces)::value, BLOCK = T < 256 ? 256 : T, TEAMS = BLOCK / T;
+      norm_gate_backward_kernel<typename decltype(e)::type, typename decltype(r)::type, T, NV>
+          <<<(uint32_t)((plan.workers - 1) / TEAMS + 1), BLOCK, 0, s>>>(in_groups, q);
+    });
+    if (bnn_status st = launch_status()) return st;
+  } else if (!q.want) {
+    return BNN_OK;
+  }
+  if (q.want) {
+    sums.part = q.part, sums.workers = q.workers, sums.segments = q.segments, sums.dgate = dgate, sums.dgate_ld = dgate_ld;
+    const uint32_t groups = q.want >> 5 & 1 ? (uint32_t)(q.workers / q.segments) : 0u;
+    ProfScope ps(KID_NORM_GATE_SUMS, s);
+    with_float(p.type, [&](auto tag) {
+      norm_gate_sums_kernel<typename decltype(tag)::type><<<dim3((uint32_t)(p.D - 1) / 64 + 1, 5 + groups), 1024, 0, s>>>(sums);
+    });
+  }
+  return launch_status();
+}

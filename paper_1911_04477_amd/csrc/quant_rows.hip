@@ -1,0 +1,85 @@
+// Rows of floating-point values as 8-bit integers with one scale a row (bnn_quant_rows_i8).
+#include "rows.h"
+
+namespace bnn {
+
+struct QuantParams {
+  const void *x;
+  int64_t x_ld, q_ld;
+  int8_t *q;
+  float *scale;
+  int64_t rows;
+  int K;
+};
+
+// T threads a row, NV pieces of eight values a thread, held in registers between the maximum and the rounding.
+// NV 0: rows of any length, read twice.
+template <class E, int T, int NV>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void quant_rows_kernel(QuantParams p) {
+  constexpr int TEAMS = T < 256 ? 256 / T : 1;
+  __shared__ uint32_t lds[T / 64];
+  const int64_t row = (int64_t)blockIdx.x * TEAMS + (TEAMS > 1 ? threadIdx.x / T : 0);
+  if (row >= p.rows) return;  // whole waves; only teams of one wave share a workgroup
+  const int t = threadIdx.x % T;
+  const E *x = static_cast<const E *>(p.x) + row * p.x_ld;
+  int8_t *q = p.q + row * p.q_ld;
+  uint32_t top = 0u;
+  if constexpr (NV > 0) {
+    float v[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) load8(v[i], x, (i * T + t) * 8, p.K);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[i][j]));
+    const RowScale s = row_scale(team_max_magnitude<T>(top, lds));
+#pragma unroll
+    for (int i = 0; i < NV; ++i) store_q8(q, (i * T + t) * 8, p.K, v[i], s.inv);
+    if (t == 0) p.scale[row] = s.scale;
+  } else {
+    for (int c = t * 8; c < p.K; c += T * 8) {
+      float v[8];
+      load8(v, x, c, p.K);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[j]));
+    }
+    const RowScale s = row_scale(team_max_magnitude<T>(top, lds));
+    for (int c = t * 8; c < p.K; c += T * 8) {
+      float v[8];
+      load8(v, x, c, p.K);
+      store_q8(q, c, p.K, v, s.inv);
+    }
+    if (t == 0) p.scale[row] = s.scale;
+  }
+}
+
+template <class E, int T, int NV>
+void launch_quant(const QuantParams &p, hipStream_t s) {
+  constexpr int TEAMS = T < 256 ? 256 / T : 1;
+  quant_rows_kernel<E, T, NV><<<(uint32_t)((p.rows - 1) / TEAMS + 1), T < 256 ? 256 : T, 0, s>>>(p);
+}
+
+}  // namespace bnn
+
+extern "C" bnn_status bnn_quant_rows_i8(const void *x, int type, int64_t rows, int64_t K, int64_t x_ld, int8_t *q,
+                                        int64_t q_ld, float *scale, void *stream) {
+  using namespace bnn;
+  if (rows < 0 || K <= 0 || !float_type(type)) return BNN_ERR_SHAPE;
+  if (x_ld < K || q_ld < K) return BNN_ERR_STRIDE;
+  if (K > INT32_MAX - 65536 || rows > INT32_MAX) return BNN_ERR_UNSUPPORTED;
+  if (rows == 0) return BNN_OK;
+  if (!x || !q || !scale) return BNN_ERR_NULL;
+  if (!aligned16(x) || !aligned16(q) || !aligned16(scale)) return BNN_ERR_ALIGN;
+  const QuantParams p = {x, x_ld, q_ld, q, scale, rows, (int)K};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  ProfScope ps(KID_QUANT_ROWS, s);
+  with_float(type, [&](auto tag) {
+    using E = typename decltype(tag)::type;
+    if (K <= 512) launch_quant<E, 64, 1>(p, s);
+    else if (K <= 2048) launch_quant<E, 256, 1>(p, s);
+    else if (K <= 8192) launch_quant<E, 256, 4>(p, s);
+    else if (K <= 32768) launch_quant<E, 1024, 4>(p, s);
+    else launch_quant<E, 1024, 0>(p, s);
+  });
+  return launch_status();
+}

@@ -1,0 +1,229 @@
+// Matrix-core product of two row-major operands, out[m][n] = sum over k of A[m][k] * B[n][k], on 8-bit integers (32-bit
+// sums) or 16-bit floating point (fp32 sums), in the form that the quantised and the gated layers share: a workgroup
+// computes BM x BN outputs, both operands go through LDS in steps of 128 bytes of k, and an epilogue takes sums of four
+// consecutive columns at a time.
+#pragma once
+#include <type_traits>
+
+#include "common.h"
+
+namespace bnn {
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(1)));  // global loads take any byte address
+
+enum MmType : int { MM_I8 = 0, MM_BF16 = 1, MM_F16 = 2 };
+template <int TY>
+struct MmTraits;
+template <>
+struct MmTraits<MM_I8> {
+  using elem = int8_t;
+  using acc = v4i;
+  static __device__ __forceinline__ acc mfma(u32x4 a, u32x4 b, acc c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, a), __builtin_bit_cast(v4i, b), c, 0, 0, 0);
+  }
+};
+template <>
+struct MmTraits<MM_BF16> {
+  using elem = __bf16;
+  using acc = v4f;
+  static __device__ __forceinline__ acc mfma(u32x4 a, u32x4 b, acc c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+  }
+};
+template <>
+struct MmTraits<MM_F16> {
+  using elem = _Float16;
+  using acc = v4f;
+  static __device__ __forceinline__ acc mfma(u32x4 a, u32x4 b, acc c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+  }
+};
+
+// Operands of a product.  DUAL kernels multiply A with two matrices B0 and B1 of N rows each; others have B0 alone.
+struct MmOperands {
+  const char *A, *B0, *B1;
+  int64_t lda, ldb0, ldb1;  // bytes between rows
+  int M, N, kbytes;
+  int dma;                  // rows and strides are multiples of 16 bytes (mm_dma)
+  int tilesM, tilesN;
+};
+
+// Whether an operand's tiles can go straight to LDS: 16-byte pieces that start on 16 bytes, 32-bit offsets in a tile.
+inline bool mm_dma(const void *p, int64_t ld_bytes) {
+  return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)ld_bytes) & 15u) == 0 && ld_bytes < (1 << 22);
+}
+
+// 16 bytes of a row at byte k, zeros from byte `end` on (end > k), any alignment, nothing read at or past the end.
+template <class E>
+__device__ __forceinline__ u32x4 mm_piece(const char *row, int k, int end) {
+  if (k + 16 <= end) return *reinterpret_cast<const u32x4_any *>(row + k);
+  u32x4 v = {0u, 0u, 0u, 0u};
+  if (k >= end) return v;
+#pragma unroll
+  for (int e = 0; e < 16 / (int)sizeof(E); ++e) {
+    if (k + e * (int)sizeof(E) < end) {
+      uint32_t x;
+      if constexpr (sizeof(E) == 1) x = *reinterpret_cast<const uint8_t *>(row + k + e);
+      else x = *reinterpret_cast<const uint16_t *>(row + k + 2 * e);
+      v[e * sizeof(E) / 4] |= x << (8 * (e * sizeof(E) % 4));
+    }
+  }
+  return v;
+}
+
+// Tiles in an order in which the workgroups that run at the same time on one XCD (ids go round the eight of them) read few
+// different rows: each XCD has a contiguous share of the tiles, and goes through it in bands of 8 tile rows.
+__device__ __forceinline__ void mm_tile(int id, int tilesM, int tilesN, int &tm, int &tn) {
+  const int total = tilesM * tilesN, xcd = id & 7, share = total >> 3, rest = total & 7;
+  const int t = xcd * share + min(xcd, rest) + (id >> 3);
+  constexpr int BAND = 8;
+  const int band = t / (BAND * tilesN), in = t - band * BAND * tilesN, rows = min(BAND, tilesM - band * BAND);
+  tn = in / rows;
+  tm = band * BAND + (in - tn * rows);
+}
+
+constexpr int MM_STEP = 128;  // bytes of k a step
+
+// LDS: rows of 128 bytes, 16-byte piece c of row r in slot c ^ (r % 8), so that the 16 rows of a fragment spread over all
+// banks.  A wave's load fills 8 rows: lane i slot i % 8 of row i / 8.  WGM x WGN waves, each (BM / WGM) x (BN / WGN)
+// outputs; with DUAL half of a wave's columns are B0's and half the same columns of B1.
+template <int TY, int BM, int BN, int WGM, int WGN, bool DUAL, bool DMA, class Epilogue>
+__device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilogue &epi, int tm, int tn, char *lds0, char *lds1) {
+  using T = MmTraits<TY>;
+  using E = typename T::elem;
+  constexpr int WAVES = WGM * WGN, ROWS = BM + BN, LOADS = ROWS / 8 / WAVES, LOADS_A = BM / 8 / WAVES;
+  static_assert(ROWS % (8 * WAVES) == 0 && BM % (8 * WAVES) == 0 && BM % (16 * WGM) == 0 && BN % (16 * WGN * (DUAL ? 2 : 1)) == 0, "");
+  constexpr int TM = BM / WGM / 16, TN = BN / WGN / 16, NB = DUAL ? BN / 2 : BN;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WGN, wn = wave % WGN;
+  const int m0 = tm * BM, n0 = tn * NB;
+  const int piece = ((lane & 7) ^ (lane >> 3)) * 16;  // of the 128 bytes of a step, that this lane's loads bring
+
+  // where this lane's loads start: rows beyond the operands repeat the last one, their outputs are not stored
+  const char *baseA = p.A + (int64_t)m0 * p.lda, *base0 = p.B0 + (int64_t)n0 * p.ldb0;
+  const char *base1 = DUAL ? p.B1 + (int64_t)n0 * p.ldb1 : base0;
+  int at[LOADS];         // byte offset (DMA)
+  const char *src[LOADS];  // row (otherwise)
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int row = (i * WAVES + wave) * 8 + (lane >> 3);
+    const bool inA = i < LOADS_A;
+    const int nrow = row - BM;
+    const bool second = DUAL && nrow >= NB;
+    const int r = inA ? min(row, p.M - 1 - m0) : min(second ? nrow - NB : nrow, p.N - 1 - n0);
+    const int64_t ld = inA ? p.lda : second ? p.ldb1 : p.ldb0;
+    at[i] = (int)(r * ld) + piece;
+    src[i] = (inA ? baseA : second ? base1 : base0) + r * ld;
+  }
+  const auto resA = __builtin_amdgcn_make_buffer_rsrc((void *)baseA, 0, 0xffffffffu, 0x00020000);
+  const auto res0 = __builtin_amdgcn_make_buffer_rsrc((void *)base0, 0, 0xffffffffu, 0x00020000);
+  const auto res1 = __builtin_amdgcn_make_buffer_rsrc((void *)base1, 0, 0xffffffffu, 0x00020000);
+
+  typename T::acc acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = typename T::acc{0, 0, 0, 0};
+
+  u32x4 held[LOADS];
+  const auto request = [&](int k, char *lds) {  // step k into lds, or into registers
+    if (DMA && k + MM_STEP <= p.kbytes) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int row = (i * WAVES + wave) * 8;
+        const auto to = (__attribute__((address_space(3))) void *)(lds + row * MM_STEP);
+        if (i < LOADS_A) __builtin_amdgcn_raw_ptr_buffer_load_lds(resA, to, 16, at[i], k, 0, 0);
+        else if (DUAL && row - BM >= NB) __builtin_amdgcn_raw_ptr_buffer_load_lds(res1, to, 16, at[i], k, 0, 0);
+        else __builtin_amdgcn_raw_ptr_buffer_load_lds(res0, to, 16, at[i], k, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) held[i] = mm_piece<E>(src[i], k + piece, p.kbytes);
+    }
+  };
+  const auto deliver = [&](int k, char *lds) {  // what request left in registers
+    if (!(DMA && k + MM_STEP <= p.kbytes)) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        *reinterpret_cast<u32x4 *>(lds + (i * WAVES + wave) * 8 * MM_STEP + lane * 16) = held[i];
+    }
+  };
+  const int slot = ((lane >> 4) ^ (lane & 7)) * 16;  // of this lane's piece of the first 64 bytes; ^ 64: of the second
+  const int fragA = (wm * (BM / WGM) + (lane & 15)) * MM_STEP + slot;
+  const int fragB = (BM + wn * (NB / WGN) + (lane & 15)) * MM_STEP + slot;
+  const auto multiply = [&](const char *lds) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      u32x4 a[TM], b[TN];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int row = !DUAL ? j * 16 : j < TN / 2 ? j * 16 : NB + (j - TN / 2) * 16;
+        b[j] = *reinterpret_cast<const u32x4 *>(lds + (fragB ^ (kk * 64)) + row * MM_STEP);
+      }
+#pragma unroll
+      for (int i = 0; i < TM; ++i) a[i] = *reinterpret_cast<const u32x4 *>(lds + (fragA ^ (kk * 64)) + i * 16 * MM_STEP);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = T::mfma(b[j], a[i], acc[i][j]);  // rows of the result: n
+    }
+  };
+
+  const int K = p.kbytes;
+  request(0, lds0);
+  deliver(0, lds0);
+  for (int k = 0; k < K; k += 2 * MM_STEP) {
+    __syncthreads();  // step k has arrived, and lds1 is free
+    if (k + MM_STEP < K) request(k + MM_STEP, lds1);
+    multiply(lds0);
+    if (k + MM_STEP >= K) break;
+    deliver(k + MM_STEP, lds1);
+    __syncthreads();
+    if (k + 2 * MM_STEP < K) request(k + 2 * MM_STEP, lds0);
+    multiply(lds1);
+    if (k + 2 * MM_STEP < K) deliver(k + 2 * MM_STEP, lds0);
+  }
+
+  const int m = m0 + wm * (BM / WGM) + (lane & 15), n = n0 + wn * (NB / WGN) + (lane >> 4) * 4;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    if (m + i * 16 >= p.M) continue;
+    if constexpr (DUAL) {
+#pragma unroll
+      for (int j = 0; j < TN / 2; ++j)
+        if (n + j * 16 < p.N) epi(m + i * 16, n + j * 16, p.N, acc[i][j], acc[i][TN / 2 + j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        if (n + j * 16 < p.N) epi(m + i * 16, n + j * 16, p.N, acc[i][j]);
+    }
+  }
+}
+
+template <int TY, int BM, int BN, int WGM, int WGN, bool DUAL, class Epilogue>
+__global__ __launch_bounds__(64 * WGM *WGN, (BM + BN) * 4 * MM_STEP <= 163840 ? 2 : 1) void mm_tile_kernel(MmOperands p, Epilogue epi) {
+  __shared__ __attribute__((aligned(16))) char lds0[(BM + BN) * MM_STEP];
+  __shared__ __attribute__((aligned(16))) char lds1[(BM + BN) * MM_STEP];
+  int tm, tn;
+  mm_tile(blockIdx.x, p.tilesM, p.tilesN, tm, tn);
+  if (p.dma) mm_tile_product<TY, BM, BN, WGM, WGN, DUAL, true>(p, epi, tm, tn, lds0, lds1);
+  else mm_tile_product<TY, BM, BN, WGM, WGN, DUAL, false>(p, epi, tm, tn, lds0, lds1);
+}
+
+template <int TY, int BM, int BN, int WGM, int WGN, bool DUAL, class Epilogue>
+bnn_status launch_mm_tile(MmOperands p, const Epilogue &epi, int kid, hipStream_t s) {
+  p.tilesM = (p.M - 1) / BM + 1;
+  p.tilesN = (p.N - 1) / (DUAL ? BN / 2 : BN) + 1;
+  const int64_t tiles = (int64_t)p.tilesM * p.tilesN;
+  if (tiles > 0x7fffffff) return BNN_ERR_UNSUPPORTED;
+  ProfScope ps(kid, s);
+  mm_tile_kernel<TY, BM, BN, WGM, WGN, DUAL, Epilogue><<<(uint32_t)tiles, 64 * WGM * WGN, 0, s>>>(p, epi);
+  return launch_status();
+}
+
+}  // namespace bnn
