@@ -77,23 +77,24 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void mm_few_kernel(MmOperand
   }
 }
 
-// Which kernel takes a product: by rows up to 64 the one that streams B, else tiles, the large ones where they occupy the
-// compute units.
-enum MmForm { MM_FEW16, MM_FEW64, MM_TILE128, MM_TILE256 };
-inline MmForm mm_form(int M, int N, bool dual) {
-  if (M <= 16) return MM_FEW16;
-  if (M <= 64) return MM_FEW64;
-  const int64_t columns = dual ? 128 : 256;
-  const int64_t large = (int64_t)((M - 1) / 256 + 1) * ((N - 1) / columns + 1);
-  return large >= device_cu_count() ? MM_TILE256 : MM_TILE128;
-}
-
 template <int TY, int MT, int WAVES, bool DUAL, class Epilogue>
 bnn_status launch_mm_few(const MmOperands &p, const Epilogue &epi, int kid, hipStream_t s) {
   const dim3 grid((uint32_t)((p.N - 1) / 16 + 1), (uint32_t)((p.M - 1) / (16 * MT) + 1));
   ProfScope ps(kid, s);
   mm_few_kernel<TY, MT, WAVES, DUAL, Epilogue><<<grid, 64 * WAVES, 0, s>>>(p, epi);
   return launch_status();
+}
+
+// Which kernel takes a product: up to 64 rows the one that streams B, else tiles, the large ones where they occupy the
+// compute units.
+template <int TY, bool DUAL, class Epilogue>
+bnn_status run_product(const MmOperands &p, const Epilogue &epi, int kid_few, int kid, hipStream_t s) {
+  if (p.M <= 16) return launch_mm_few<TY, 1, 8, DUAL>(p, epi, kid_few, s);
+  if (p.M <= 64) return launch_mm_few<TY, 4, 8, DUAL>(p, epi, kid_few, s);
+  if (!p.dma) return launch_mm_tile<TY, 128, 128, 2, 2, DUAL, false>(p, epi, kid, s);
+  const int64_t large = (int64_t)((p.M - 1) / 256 + 1) * ((p.N - 1) / (DUAL ? 128 : 256) + 1);
+  if (large < device_cu_count()) return launch_mm_tile<TY, 128, 128, 2, 2, DUAL, true>(p, epi, kid, s);
+  return launch_mm_tile<TY, 256, 256, 2, 4, DUAL, true>(p, epi, kid, s);
 }
 
 }  // namespace bnn

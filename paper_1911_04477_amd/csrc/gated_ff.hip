@@ -132,15 +132,6 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(E *y, int64_t ld, int64_
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < rows * cols; i += gridDim.x * 256ll) y[i / cols * ld + i % cols] = (E)0.0f;
 }
 
-template <int TY, bool DUAL, class Epilogue>
-bnn_status run_product(const MmOperands &p, const Epilogue &epi, int kid, hipStream_t s) {
-  const MmForm form = mm_form(p.M, p.N, DUAL);
-  if (form == MM_FEW16) return launch_mm_few<TY, 1, 8, DUAL>(p, epi, kid, s);
-  if (form == MM_FEW64) return launch_mm_few<TY, 4, 8, DUAL>(p, epi, kid, s);
-  if (form == MM_TILE128) return launch_mm_tile<TY, 128, 128, 2, 2, DUAL>(p, epi, kid, s);
-  return launch_mm_tile<TY, 256, 256, 2, 4, DUAL>(p, epi, kid, s);
-}
-
 inline bool half_type(int t) { return t == BNN_BF16 || t == BNN_F16; }
 inline bool act_known(int a) { return a >= BNN_ACT_SILU && a <= BNN_ACT_RELU; }
 inline int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
@@ -175,14 +166,14 @@ bnn_status gated_backward(const char *x, int64_t x_ld, const char *wg, int64_t w
   p.M = T, p.N = D, p.kbytes = 4 * Fp;
   p.dma = mm_dma(p.A, p.lda) && mm_dma(p.B0, p.ldb0);
   const ProductEpilogue<E> ex = {static_cast<E *>(dx), nullptr, dx_ld, 0, T, T, rows_by(dx, dx_ld, 2, 4)};
-  if (bnn_status st = run_product<TY, false>(p, ex, KID_GATED_FF_BACKWARD, s)) return st;
+  if (bnn_status st = run_product<TY, false>(p, ex, KID_GATED_FF_BACKWARD, KID_GATED_FF_BACKWARD, s)) return st;
   p.A = reinterpret_cast<const char *>(gradT), p.lda = 2ll * Tp;
   p.B0 = p.B1 = reinterpret_cast<const char *>(xT), p.ldb0 = p.ldb1 = 2ll * Tp;
   p.M = 2 * Fp, p.N = D, p.kbytes = 2 * Tp;
   p.dma = mm_dma(p.A, p.lda) && mm_dma(p.B0, p.ldb0);
   const ProductEpilogue<E> ew = {static_cast<E *>(dwg), static_cast<E *>(dwu), dwg_ld, dwu_ld, F, Fp,
                                  rows_by(dwg, dwg_ld, 2, 4) && rows_by(dwu, dwu_ld, 2, 4)};
-  return run_product<TY, false>(p, ew, KID_GATED_FF_BACKWARD, s);
+  return run_product<TY, false>(p, ew, KID_GATED_FF_BACKWARD, KID_GATED_FF_BACKWARD, s);
 }
 
 // Gradients of an empty product.
@@ -216,8 +207,8 @@ extern "C" bnn_status bnn_gated_ff(const void *x, int64_t x_ld, const void *wg, 
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int vec = rows_by(h, h_ld, 2, 4), savedVec = F % 4 == 0;
   if (type == BNN_BF16)
-    return run_product<MM_BF16, true>(p, GatedEpilogue<__bf16>{static_cast<__bf16 *>(h), h_ld, saved, T * F, act, vec, savedVec}, KID_GATED_FF, s);
-  return run_product<MM_F16, true>(p, GatedEpilogue<_Float16>{static_cast<_Float16 *>(h), h_ld, saved, T * F, act, vec, savedVec}, KID_GATED_FF, s);
+    return run_product<MM_BF16, true>(p, GatedEpilogue<__bf16>{static_cast<__bf16 *>(h), h_ld, saved, T * F, act, vec, savedVec}, KID_GATED_FF, KID_GATED_FF, s);
+  return run_product<MM_F16, true>(p, GatedEpilogue<_Float16>{static_cast<_Float16 *>(h), h_ld, saved, T * F, act, vec, savedVec}, KID_GATED_FF, KID_GATED_FF, s);
 }
 
 extern "C" bnn_status bnn_gated_ff_i8(const int8_t *x, int64_t x_ld, const float *x_scale, const int8_t *wg, int64_t wg_ld,
@@ -239,7 +230,7 @@ extern "C" bnn_status bnn_gated_ff_i8(const int8_t *x, int64_t x_ld, const float
   p.M = (int)T, p.N = (int)F, p.kbytes = (int)D;
   p.dma = mm_dma(x, x_ld) && mm_dma(wg, wg_ld) && mm_dma(wu, wu_ld);
   const GatedI8Epilogue epi = {x_scale, wg_scale, wu_scale, h, h_ld, type, act, rows_by(h, h_ld, float_size(type), 4)};
-  return run_product<MM_I8, true>(p, epi, KID_GATED_FF_I8, static_cast<hipStream_t>(stream));
+  return run_product<MM_I8, true>(p, epi, KID_GATED_FF_I8, KID_GATED_FF_I8, static_cast<hipStream_t>(stream));
 }
 
 extern "C" size_t bnn_gated_ff_backward_workspace_bytes(int64_t T, int64_t D, int64_t F) {

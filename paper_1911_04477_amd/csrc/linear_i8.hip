@@ -45,10 +45,5 @@ extern "C" bnn_status bnn_linear_i8(const int8_t *a, int64_t lda, const float *a
   p.M = (int)M, p.N = (int)N, p.kbytes = (int)K;
   p.dma = mm_dma(a, lda) && mm_dma(b, ldb);
   const LinearEpilogue epi = {a_scale, b_scale, bias, y, ldy, type, rows_by(y, ldy, float_size(type), 4)};
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  const MmForm form = mm_form(p.M, p.N, false);
-  if (form == MM_FEW16) return launch_mm_few<MM_I8, 1, 8, false>(p, epi, KID_LINEAR_I8_FEW, s);
-  if (form == MM_FEW64) return launch_mm_few<MM_I8, 4, 8, false>(p, epi, KID_LINEAR_I8_FEW, s);
-  if (form == MM_TILE128) return launch_mm_tile<MM_I8, 128, 128, 2, 2, false>(p, epi, KID_LINEAR_I8, s);
-  return launch_mm_tile<MM_I8, 256, 256, 2, 4, false>(p, epi, KID_LINEAR_I8, s);
+  return run_product<MM_I8, false>(p, epi, KID_LINEAR_I8_FEW, KID_LINEAR_I8, static_cast<hipStream_t>(stream));
 }

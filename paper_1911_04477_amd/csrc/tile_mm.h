@@ -104,25 +104,22 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
   const int m0 = tm * BM, n0 = tn * NB;
   const int piece = ((lane & 7) ^ (lane >> 3)) * 16;  // of the 128 bytes of a step, that this lane's loads bring
 
-  // where this lane's loads start: rows beyond the operands repeat the last one, their outputs are not stored
+  // Where the pieces of this lane's loads come from: rows beyond the operands repeat the last one, their outputs are not
+  // stored.
   const char *baseA = p.A + (int64_t)m0 * p.lda, *base0 = p.B0 + (int64_t)n0 * p.ldb0;
   const char *base1 = DUAL ? p.B1 + (int64_t)n0 * p.ldb1 : base0;
-  int at[LOADS];         // byte offset (DMA)
-  const char *src[LOADS];  // row (otherwise)
-#pragma unroll
-  for (int i = 0; i < LOADS; ++i) {
-    const int row = (i * WAVES + wave) * 8 + (lane >> 3);
-    const bool inA = i < LOADS_A;
-    const int nrow = row - BM;
+  const auto row_of = [&](int i, int64_t &ld) {  // of load i, in its operand's tile
+    const int row = (i * WAVES + wave) * 8 + (lane >> 3), nrow = row - BM;
     const bool second = DUAL && nrow >= NB;
-    const int r = inA ? min(row, p.M - 1 - m0) : min(second ? nrow - NB : nrow, p.N - 1 - n0);
-    const int64_t ld = inA ? p.lda : second ? p.ldb1 : p.ldb0;
-    at[i] = (int)(r * ld) + piece;
-    src[i] = (inA ? baseA : second ? base1 : base0) + r * ld;
-  }
-  const auto resA = __builtin_amdgcn_make_buffer_rsrc((void *)baseA, 0, 0xffffffffu, 0x00020000);
-  const auto res0 = __builtin_amdgcn_make_buffer_rsrc((void *)base0, 0, 0xffffffffu, 0x00020000);
-  const auto res1 = __builtin_amdgcn_make_buffer_rsrc((void *)base1, 0, 0xffffffffu, 0x00020000);
+    ld = i < LOADS_A ? p.lda : second ? p.ldb1 : p.ldb0;
+    return i < LOADS_A ? min(row, p.M - 1 - m0) : min(second ? nrow - NB : nrow, p.N - 1 - n0);
+  };
+  const auto source = [&](int i) {
+    int64_t ld;
+    const int r = row_of(i, ld);
+    return (i < LOADS_A ? baseA : DUAL && (i * WAVES + wave) * 8 - BM >= NB ? base1 : base0) + r * ld;
+  };
+  const auto room = [&](char *lds, int i) { return reinterpret_cast<u32x4 *>(lds + (i * WAVES + wave) * 8 * MM_STEP + lane * 16); };
 
   typename T::acc acc[TM][TN];
 #pragma unroll
@@ -130,29 +127,6 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = typename T::acc{0, 0, 0, 0};
 
-  u32x4 held[LOADS];
-  const auto request = [&](int k, char *lds) {  // step k into lds, or into registers
-    if (DMA && k + MM_STEP <= p.kbytes) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int row = (i * WAVES + wave) * 8;
-        const auto to = (__attribute__((address_space(3))) void *)(lds + row * MM_STEP);
-        if (i < LOADS_A) __builtin_amdgcn_raw_ptr_buffer_load_lds(resA, to, 16, at[i], k, 0, 0);
-        else if (DUAL && row - BM >= NB) __builtin_amdgcn_raw_ptr_buffer_load_lds(res1, to, 16, at[i], k, 0, 0);
-        else __builtin_amdgcn_raw_ptr_buffer_load_lds(res0, to, 16, at[i], k, 0, 0);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) held[i] = mm_piece<E>(src[i], k + piece, p.kbytes);
-    }
-  };
-  const auto deliver = [&](int k, char *lds) {  // what request left in registers
-    if (!(DMA && k + MM_STEP <= p.kbytes)) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i)
-        *reinterpret_cast<u32x4 *>(lds + (i * WAVES + wave) * 8 * MM_STEP + lane * 16) = held[i];
-    }
-  };
   const int slot = ((lane >> 4) ^ (lane & 7)) * 16;  // of this lane's piece of the first 64 bytes; ^ 64: of the second
   const int fragA = (wm * (BM / WGM) + (lane & 15)) * MM_STEP + slot;
   const int fragB = (BM + wn * (NB / WGN) + (lane & 15)) * MM_STEP + slot;
@@ -175,18 +149,76 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
   };
 
   const int K = p.kbytes;
-  request(0, lds0);
-  deliver(0, lds0);
-  for (int k = 0; k < K; k += 2 * MM_STEP) {
-    __syncthreads();  // step k has arrived, and lds1 is free
-    if (k + MM_STEP < K) request(k + MM_STEP, lds1);
-    multiply(lds0);
-    if (k + MM_STEP >= K) break;
-    deliver(k + MM_STEP, lds1);
-    __syncthreads();
-    if (k + 2 * MM_STEP < K) request(k + 2 * MM_STEP, lds0);
-    multiply(lds1);
-    if (k + 2 * MM_STEP < K) deliver(k + 2 * MM_STEP, lds0);
+  if constexpr (DMA) {
+    const auto resA = __builtin_amdgcn_make_buffer_rsrc((void *)baseA, 0, 0xffffffffu, 0x00020000);
+    const auto res0 = __builtin_amdgcn_make_buffer_rsrc((void *)base0, 0, 0xffffffffu, 0x00020000);
+    const auto res1 = __builtin_amdgcn_make_buffer_rsrc((void *)base1, 0, 0xffffffffu, 0x00020000);
+    int at[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      int64_t ld;
+      const int r = row_of(i, ld);
+      at[i] = (int)(r * ld) + piece;
+    }
+    const auto request = [&](int k, char *lds) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int row = (i * WAVES + wave) * 8;
+        const auto to = (__attribute__((address_space(3))) void *)(lds + row * MM_STEP);
+        if (i < LOADS_A) __builtin_amdgcn_raw_ptr_buffer_load_lds(resA, to, 16, at[i], k, 0, 0);
+        else if (DUAL && row - BM >= NB) __builtin_amdgcn_raw_ptr_buffer_load_lds(res1, to, 16, at[i], k, 0, 0);
+        else __builtin_amdgcn_raw_ptr_buffer_load_lds(res0, to, 16, at[i], k, 0, 0);
+      }
+    };
+    const int whole = K / MM_STEP * MM_STEP;
+    if (whole) request(0, lds0);
+    for (int k = 0; k < whole; k += 2 * MM_STEP) {
+      __syncthreads();  // step k has arrived, and lds1 is free
+      if (k + MM_STEP < whole) request(k + MM_STEP, lds1);
+      multiply(lds0);
+      if (k + MM_STEP >= whole) break;
+      __syncthreads();
+      if (k + 2 * MM_STEP < whole) request(k + 2 * MM_STEP, lds0);
+      multiply(lds1);
+    }
+    if (whole < K) {  // what is left of k, with zeros behind it
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) *room(lds0, i) = mm_piece<E>(source(i), whole + piece, K);
+      __syncthreads();
+      multiply(lds0);
+    }
+  } else {
+    const char *src[LOADS];
+    u32x4 held[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) src[i] = source(i);
+    const auto request = [&](int k) {
+      if (k + MM_STEP <= K) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) held[i] = *reinterpret_cast<const u32x4_any *>(src[i] + k + piece);
+      } else {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) held[i] = mm_piece<E>(src[i], k + piece, K);
+      }
+    };
+    const auto deliver = [&](char *lds) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) *room(lds, i) = held[i];
+    };
+    request(0);
+    deliver(lds0);
+    for (int k = 0; k < K; k += 2 * MM_STEP) {
+      __syncthreads();  // step k has arrived, and lds1 is free
+      if (k + MM_STEP < K) request(k + MM_STEP);
+      multiply(lds0);
+      if (k + MM_STEP >= K) break;
+      deliver(lds1);
+      __syncthreads();
+      if (k + 2 * MM_STEP < K) request(k + 2 * MM_STEP);
+      multiply(lds1);
+      if (k + 2 * MM_STEP < K) deliver(lds0);
+    }
   }
 
   const int m = m0 + wm * (BM / WGM) + (lane & 15), n = n0 + wn * (NB / WGN) + (lane >> 4) * 4;
@@ -205,24 +237,23 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
   }
 }
 
-template <int TY, int BM, int BN, int WGM, int WGN, bool DUAL, class Epilogue>
-__global__ __launch_bounds__(64 * WGM *WGN, (BM + BN) * 4 * MM_STEP <= 163840 ? 2 : 1) void mm_tile_kernel(MmOperands p, Epilogue epi) {
+template <int TY, int BM, int BN, int WGM, int WGN, bool DUAL, bool DMA, class Epilogue>
+__global__ __launch_bounds__(64 * WGM *WGN, 2) void mm_tile_kernel(MmOperands p, Epilogue epi) {
   __shared__ __attribute__((aligned(16))) char lds0[(BM + BN) * MM_STEP];
   __shared__ __attribute__((aligned(16))) char lds1[(BM + BN) * MM_STEP];
   int tm, tn;
   mm_tile(blockIdx.x, p.tilesM, p.tilesN, tm, tn);
-  if (p.dma) mm_tile_product<TY, BM, BN, WGM, WGN, DUAL, true>(p, epi, tm, tn, lds0, lds1);
-  else mm_tile_product<TY, BM, BN, WGM, WGN, DUAL, false>(p, epi, tm, tn, lds0, lds1);
+  mm_tile_product<TY, BM, BN, WGM, WGN, DUAL, DMA>(p, epi, tm, tn, lds0, lds1);
 }
 
-template <int TY, int BM, int BN, int WGM, int WGN, bool DUAL, class Epilogue>
+template <int TY, int BM, int BN, int WGM, int WGN, bool DUAL, bool DMA, class Epilogue>
 bnn_status launch_mm_tile(MmOperands p, const Epilogue &epi, int kid, hipStream_t s) {
   p.tilesM = (p.M - 1) / BM + 1;
   p.tilesN = (p.N - 1) / (DUAL ? BN / 2 : BN) + 1;
   const int64_t tiles = (int64_t)p.tilesM * p.tilesN;
   if (tiles > 0x7fffffff) return BNN_ERR_UNSUPPORTED;
   ProfScope ps(kid, s);
-  mm_tile_kernel<TY, BM, BN, WGM, WGN, DUAL, Epilogue><<<(uint32_t)tiles, 64 * WGM * WGN, 0, s>>>(p, epi);
+  mm_tile_kernel<TY, BM, BN, WGM, WGN, DUAL, DMA, Epilogue><<<(uint32_t)tiles, 64 * WGM * WGN, 0, s>>>(p, epi);
   return launch_status();
 }
 
