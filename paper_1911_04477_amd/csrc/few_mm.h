@@ -4,14 +4,15 @@
 
 namespace bnn {
 
-// A workgroup owns 16 columns and up to 16 * MT rows; its waves deal the k axis out in runs of 256 bytes, straight from
-// memory into matrix operands (any order of k is right as long as both operands have it), and their sums meet in LDS.
-template <int TY, int MT, int WAVES, bool DUAL, class Epilogue>
+// A workgroup owns 16 columns and up to 16 * MT rows; its waves deal the k axis out in runs of RUN * 64 bytes, straight from
+// memory into matrix operands (any order of k is right as long as both operands have it), and their sums meet in LDS.  The
+// next run is requested before the products of the present one.
+template <int TY, int MT, int WAVES, int RUN, bool DUAL, class Epilogue>
 __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void mm_few_kernel(MmOperands p, Epilogue epi) {
   using T = MmTraits<TY>;
   using E = typename T::elem;
   using Acc = typename T::acc;
-  constexpr int NB = DUAL ? 2 : 1, RUN = 4;
+  constexpr int NB = DUAL ? 2 : 1, BYTES = RUN * 64;
   __shared__ Acc sums[WAVES][MT][NB][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT;
@@ -28,33 +29,54 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void mm_few_kernel(MmOperand
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int d = 0; d < NB; ++d) acc[i][d] = Acc{0, 0, 0, 0};
+  struct Run {
+    u32x4 b[RUN][NB], a[RUN][MT];
+  };
   const int K = p.kbytes;
-  constexpr int STRIDE = WAVES * RUN * 64;
-  for (int k = wave * RUN * 64; k < K; k += STRIDE) {
-    u32x4 vb[RUN][NB], va[RUN][MT];
-    if (k + RUN * 64 <= K) {
+  const auto request = [&](Run &v, int k) {
 #pragma unroll
-      for (int r = 0; r < RUN; ++r) {
+    for (int r = 0; r < RUN; ++r)
 #pragma unroll
-        for (int d = 0; d < NB; ++d) vb[r][d] = *reinterpret_cast<const u32x4_any *>(b[d] + k + r * 64 + piece);
+      for (int d = 0; d < NB; ++d) v.b[r][d] = *reinterpret_cast<const u32x4_any *>(b[d] + k + r * 64 + piece);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) va[r][i] = *reinterpret_cast<const u32x4_any *>(a[i] + k + r * 64 + piece);
-      }
-    } else {
+    for (int r = 0; r < RUN; ++r)
 #pragma unroll
-      for (int r = 0; r < RUN; ++r) {
-#pragma unroll
-        for (int d = 0; d < NB; ++d) vb[r][d] = mm_piece<E>(b[d], k + r * 64 + piece, K);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) va[r][i] = mm_piece<E>(a[i], k + r * 64 + piece, K);
-      }
-    }
+      for (int i = 0; i < MT; ++i) v.a[r][i] = *reinterpret_cast<const u32x4_any *>(a[i] + k + r * 64 + piece);
+  };
+  const auto multiply = [&](const Run &v) {
 #pragma unroll
     for (int r = 0; r < RUN; ++r)
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int d = 0; d < NB; ++d) acc[i][d] = T::mfma(vb[r][d], va[r][i], acc[i][d]);
+        for (int d = 0; d < NB; ++d) acc[i][d] = T::mfma(v.b[r][d], v.a[r][i], acc[i][d]);
+  };
+  constexpr int STRIDE = WAVES * BYTES;
+  int k = wave * BYTES;
+  if (k + BYTES <= K) {
+    Run v[2];
+    request(v[0], k);
+    for (;;) {
+      if (k + STRIDE + BYTES <= K) request(v[1], k + STRIDE);
+      multiply(v[0]);
+      k += STRIDE;
+      if (k + BYTES > K) break;
+      if (k + STRIDE + BYTES <= K) request(v[0], k + STRIDE);
+      multiply(v[1]);
+      k += STRIDE;
+      if (k + BYTES > K) break;
+    }
+  }
+  for (const int end = min(K, k + BYTES); k < end; k += 64) {  // the last run, cut short
+    u32x4 vb[NB], va[MT];
+#pragma unroll
+    for (int d = 0; d < NB; ++d) vb[d] = mm_piece<E>(b[d], k + piece, K);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) va[i] = mm_piece<E>(a[i], k + piece, K);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int d = 0; d < NB; ++d) acc[i][d] = T::mfma(vb[d], va[i], acc[i][d]);
   }
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -71,30 +93,61 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void mm_few_kernel(MmOperand
     }
     const int m = m0 + i * 16 + (lane & 15), nn = n0 + (lane >> 4) * 4;
     if (m < p.M && nn < p.N) {
-      if constexpr (DUAL) epi(m, nn, p.N, t[0], t[1]);
-      else epi(m, nn, p.N, t[0]);
+      if constexpr (DUAL) epi(m, nn, p.N, epi.row(m), epi.columns(nn, p.N), t[0], t[1]);
+      else epi(m, nn, p.N, epi.row(m), epi.columns(nn, p.N), t[0]);
     }
   }
 }
 
-template <int TY, int MT, int WAVES, bool DUAL, class Epilogue>
+template <int TY, int MT, int WAVES, int RUN, bool DUAL, class Epilogue>
 bnn_status launch_mm_few(const MmOperands &p, const Epilogue &epi, int kid, hipStream_t s) {
   const dim3 grid((uint32_t)((p.N - 1) / 16 + 1), (uint32_t)((p.M - 1) / (16 * MT) + 1));
   ProfScope ps(kid, s);
-  mm_few_kernel<TY, MT, WAVES, DUAL, Epilogue><<<grid, 64 * WAVES, 0, s>>>(p, epi);
+  mm_few_kernel<TY, MT, WAVES, RUN, DUAL, Epilogue><<<grid, 64 * WAVES, 0, s>>>(p, epi);
   return launch_status();
 }
 
-// Which kernel takes a product: up to 64 rows the one that streams B, else tiles, the large ones where they occupy the
-// compute units.
+// Which kernel takes a product of more than 16 rows: the cheapest by the rounds of tiles that the compute units go through,
+// in hundredths of a round of 256 x 256 tiles.  `one`: every unit has one tile at most; `two`: a round of two tiles a unit
+// (256 x 256: one at a time).  Measured in 8 bits, k 4096, of 256 x 256 tiles 45 us a round: 128 x 128 tiles 15.4 us a round
+// of one, two a unit 35; 64 x 64 10.0; 64 x 32 and 32 x 32 7.7 (64 to 100 rows by 4096).
+struct MmForm {
+  int bm, bn, one, two;
+};
+constexpr MmForm MM_FORMS[] = {{256, 256, 100, 200}, {128, 128, 45, 66}, {64, 64, 22, 30}, {64, 32, 17, 25}, {32, 32, 17, 20}};
+inline int mm_form(int M, int N, bool dual, bool dma) {
+  const int64_t units = device_cu_count();
+  int best = 1;
+  int64_t least = INT64_MAX;
+  for (int f = dma ? 0 : 1; f < (dma ? 5 : 3); ++f) {
+    const MmForm &t = MM_FORMS[f];
+    const int64_t tiles = (int64_t)((M - 1) / t.bm + 1) * ((N - 1) / (dual ? t.bn / 2 : t.bn) + 1);
+    const int64_t cost = f == 0 ? (tiles + units - 1) / units * t.one : tiles <= units ? t.one : (tiles + 2 * units - 1) / (2 * units) * t.two;
+    if (cost <= least) least = cost, best = f;
+  }
+  return best;
+}
+
 template <int TY, bool DUAL, class Epilogue>
 bnn_status run_product(const MmOperands &p, const Epilogue &epi, int kid_few, int kid, hipStream_t s) {
-  if (p.M <= 16) return launch_mm_few<TY, 1, 8, DUAL>(p, epi, kid_few, s);
-  if (p.M <= 64) return launch_mm_few<TY, 4, 8, DUAL>(p, epi, kid_few, s);
-  if (!p.dma) return launch_mm_tile<TY, 128, 128, 2, 2, DUAL, false>(p, epi, kid, s);
-  const int64_t large = (int64_t)((p.M - 1) / 256 + 1) * ((p.N - 1) / (DUAL ? 128 : 256) + 1);
-  if (large < device_cu_count()) return launch_mm_tile<TY, 128, 128, 2, 2, DUAL, true>(p, epi, kid, s);
-  return launch_mm_tile<TY, 256, 256, 2, 4, DUAL, true>(p, epi, kid, s);
+  if (p.M <= 16) return launch_mm_few<TY, 1, 8, 4, DUAL>(p, epi, kid_few, s);
+  const int form = mm_form(p.M, p.N, DUAL, p.dma);
+  if (!p.dma) {
+    if (form == 1) return launch_mm_tile<TY, 128, 128, 2, 2, 2, DUAL, false>(p, epi, kid, s);
+    return launch_mm_tile<TY, 64, 64, 2, 2, 2, DUAL, false>(p, epi, kid, s);
+  }
+  switch (form) {
+    case 0: return launch_mm_tile<TY, 256, 256, 4, 2, 2, DUAL, true>(p, epi, kid, s);
+    case 1: {
+      const int64_t tiles = (int64_t)((p.M - 1) / 128 + 1) * ((p.N - 1) / (DUAL ? 64 : 128) + 1);
+      // one tile a unit: eight waves and four steps ahead (256 x 4096 by 4096 to 8192 gated 61 -> 44 us); else two
+      if (tiles <= device_cu_count()) return launch_mm_tile<TY, 128, 128, 2, 4, 4, DUAL, true>(p, epi, kid, s);
+      return launch_mm_tile<TY, 128, 128, 2, 2, 2, DUAL, true>(p, epi, kid, s);
+    }
+    case 2: return launch_mm_tile<TY, 64, 64, 2, 2, 4, DUAL, true>(p, epi, kid, s);
+    case 3: return launch_mm_tile<TY, 64, 32, 4, 1, 5, DUAL, true>(p, epi, kid, s);
+    default: return launch_mm_tile<TY, 32, 32, 2, 1, 8, DUAL, true>(p, epi, kid, s);
+  }
 }
 
 }  // namespace bnn

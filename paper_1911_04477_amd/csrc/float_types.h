@@ -29,6 +29,14 @@ inline bool rows_by(const void *p, int64_t ld, int size, int count) {
   return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) & (uintptr_t)(count * size - 1)) == 0;
 }
 
+// Values n .. n + 3 of an aligned vector of N, zeros past its end; n is a multiple of 4.
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ f32x4 load4(const float *v, int n, int N) {
+  if (n + 4 <= N) return *reinterpret_cast<const f32x4 *>(v + n);
+  return f32x4{v[n], n + 1 < N ? v[n + 1] : 0.0f, n + 2 < N ? v[n + 2] : 0.0f, 0.0f};
+}
+struct NoConstants {};
+
 // Four consecutive values of a row of N, from column n on; vec: whole groups of four may go out as one store.
 template <class E, class V>
 __device__ __forceinline__ void store4(E *row, int n, int N, const V &v, bool vec) {

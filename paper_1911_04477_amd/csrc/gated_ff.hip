@@ -7,25 +7,30 @@
 
 namespace bnn {
 
-// The activation and its derivative.
-__device__ __forceinline__ void activation(int act, float z, float &a, float &slope) {
+// The activation, or with SLOPE also its derivative.  exp and the quotient are the hardware's (relative error of a few
+// 2^-24; what exp loses for large arguments belongs to values next to zero).
+template <bool SLOPE>
+__device__ __forceinline__ float activation(int act, float z, float &slope) {
+  constexpr float LOG2E = 1.44269504088896341f;
+  float a;
   if (act == BNN_ACT_SILU) {
-    const float t = 1.0f / (1.0f + expf(-z));
+    const float t = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -LOG2E));
     a = z * t;
-    slope = t * (1.0f + z * (1.0f - t));
+    if (SLOPE) slope = t * (1.0f + z * (1.0f - t));
   } else if (act == BNN_ACT_GELU) {
     const float t = 0.5f * erfcf(z * -0.70710678118654752f);  // of the normal distribution, without cancellation below 0
     a = z * t;
-    slope = t + z * 0.39894228040143268f * expf(-0.5f * z * z);
+    if (SLOPE) slope = t + z * 0.39894228040143268f * __builtin_amdgcn_exp2f(z * z * (-0.5f * LOG2E));
   } else if (act == BNN_ACT_GELU_TANH) {
     const float k = 0.79788456080286536f, c = 0.044715f;
-    const float t = 1.0f / (1.0f + expf(-2.0f * k * (z + c * z * z * z)));  // (1 + tanh) / 2
+    const float t = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-2.0f * LOG2E * k * (z + c * z * z * z)));  // (1 + tanh) / 2
     a = z * t;
-    slope = t + 2.0f * z * t * (1.0f - t) * k * (1.0f + 3.0f * c * fminf(z * z, 1e30f));
+    if (SLOPE) slope = t + 2.0f * z * t * (1.0f - t) * k * (1.0f + 3.0f * c * fminf(z * z, 1e30f));
   } else {
     a = z > 0.0f || z != z ? z : 0.0f;
-    slope = z > 0.0f ? 1.0f : 0.0f;
+    if (SLOPE) slope = z > 0.0f ? 1.0f : 0.0f;
   }
+  return a;
 }
 
 // Where a backward pass will follow, `saved` takes what it multiplies the gradient of h with, in fp32 (16 bits would round
@@ -37,20 +42,29 @@ struct GatedEpilogue {
   float *saved;
   int64_t plane;  // values in one of the two
   int act, vec, savedVec;
-  __device__ __forceinline__ void operator()(int m, int n, int N, const v4f &g, const v4f &u) const {
+  using Row = NoConstants;
+  __device__ __forceinline__ Row row(int) const { return {}; }
+  __device__ __forceinline__ NoConstants columns(int, int) const { return {}; }
+  __device__ __forceinline__ void operator()(int m, int n, int N, Row, NoConstants, const v4f &g, const v4f &u) const {
     float o[4], dg[4], du[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float slope;
-      activation(act, g[i], du[i], slope);
-      dg[i] = slope * u[i];
-      o[i] = du[i] * u[i];
-    }
-    store4(h + m * ldh, n, N, o, vec);
     if (saved) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float slope;
+        du[i] = activation<true>(act, g[i], slope);
+        dg[i] = slope * u[i];
+        o[i] = du[i] * u[i];
+      }
       store4(saved + (int64_t)m * N, n, N, dg, savedVec);
       store4(saved + plane + (int64_t)m * N, n, N, du, savedVec);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float none;
+        o[i] = activation<false>(act, g[i], none) * u[i];
+      }
     }
+    store4(h + m * ldh, n, N, o, vec);
   }
 };
 
@@ -59,15 +73,18 @@ struct GatedI8Epilogue {
   void *h;
   int64_t ldh;
   int type, act, vec;
-  __device__ __forceinline__ void operator()(int m, int n, int N, const v4i &g, const v4i &u) const {
-    const float a = sx[m];
+  using Row = float;
+  struct Columns {
+    f32x4 g, u;
+  };
+  __device__ __forceinline__ Row row(int m) const { return sx[m]; }
+  __device__ __forceinline__ Columns columns(int n, int N) const { return {load4(sg, n, N), load4(su, n, N)}; }
+  __device__ __forceinline__ void operator()(int m, int n, int N, Row a, const Columns &c, const v4i &g, const v4i &u) const {
     float o[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int c = min(n + i, N - 1);
-      float z, slope;
-      activation(act, (float)g[i] * a * sg[c], z, slope);
-      o[i] = z * ((float)u[i] * a * su[c]);
+      float none;
+      o[i] = activation<false>(act, (float)g[i] * a * c.g[i], none) * ((float)u[i] * a * c.u[i]);
     }
     if (type == BNN_BF16) store4(static_cast<__bf16 *>(h) + m * ldh, n, N, o, vec);
     else if (type == BNN_F16) store4(static_cast<_Float16 *>(h) + m * ldh, n, N, o, vec);
@@ -81,7 +98,10 @@ struct ProductEpilogue {
   E *y0, *y1;
   int64_t ld0, ld1;
   int rows0, split, vec;  // rows0 <= split: rows between them are padding
-  __device__ __forceinline__ void operator()(int m, int n, int N, const v4f &v) const {
+  using Row = NoConstants;
+  __device__ __forceinline__ Row row(int) const { return {}; }
+  __device__ __forceinline__ NoConstants columns(int, int) const { return {}; }
+  __device__ __forceinline__ void operator()(int m, int n, int N, Row, NoConstants, const v4f &v) const {
     if (m < rows0) store4(y0 + m * ld0, n, N, v, vec);
     else if (m >= split && m - split < rows0) store4(y1 + (m - split) * ld1, n, N, v, vec);
   }

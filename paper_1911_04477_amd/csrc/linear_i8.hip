@@ -10,15 +10,18 @@ struct LinearEpilogue {
   void *y;
   int64_t ldy;
   int type, vec;
-  __device__ __forceinline__ void operator()(int m, int n, int N, const v4i &sum) const {
-    const float a = sa[m];
+  using Row = float;
+  struct Columns {
+    f32x4 scale, bias;
+  };
+  __device__ __forceinline__ Row row(int m) const { return sa[m]; }
+  __device__ __forceinline__ Columns columns(int n, int N) const {
+    return {load4(sb, n, N), bias ? load4(bias, n, N) : f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+  }
+  __device__ __forceinline__ void operator()(int m, int n, int N, Row a, const Columns &c, const v4i &sum) const {
     float v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int c = min(n + i, N - 1);
-      const float t = (float)sum[i] * a;
-      v[i] = bias ? fmaf(t, sb[c], bias[c]) : t * sb[c];
-    }
+    for (int i = 0; i < 4; ++i) v[i] = fmaf((float)sum[i] * a, c.scale[i], c.bias[i]);
     if (type == BNN_BF16) store4(static_cast<__bf16 *>(y) + m * ldy, n, N, v, vec);
     else if (type == BNN_F16) store4(static_cast<_Float16 *>(y) + m * ldy, n, N, v, vec);
     else store4(static_cast<float *>(y) + m * ldy, n, N, v, vec);

@@ -1,7 +1,7 @@
 // Matrix-core product of two row-major operands, out[m][n] = sum over k of A[m][k] * B[n][k], on 8-bit integers (32-bit
 // sums) or 16-bit floating point (fp32 sums), in the form that the quantised and the gated layers share: a workgroup
 // computes BM x BN outputs, both operands go through LDS in steps of 128 bytes of k, and an epilogue takes sums of four
-// consecutive columns at a time.
+// consecutive columns at a time: epi(m, n, N, epi.row(m), epi.columns(n, N), sums..), with n a multiple of 4 below N.
 #pragma once
 #include <type_traits>
 
@@ -89,11 +89,17 @@ __device__ __forceinline__ void mm_tile(int id, int tilesM, int tilesN, int &tm,
 
 constexpr int MM_STEP = 128;  // bytes of k a step
 
+// All but this wave's last N loads have arrived, its reads of LDS have ended, and every wave of the workgroup is here.
+template <int N>
+__device__ __forceinline__ void mm_sync() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
 // LDS: rows of 128 bytes, 16-byte piece c of row r in slot c ^ (r % 8), so that the 16 rows of a fragment spread over all
 // banks.  A wave's load fills 8 rows: lane i slot i % 8 of row i / 8.  WGM x WGN waves, each (BM / WGM) x (BN / WGN)
 // outputs; with DUAL half of a wave's columns are B0's and half the same columns of B1.
-template <int TY, int BM, int BN, int WGM, int WGN, bool DUAL, bool DMA, class Epilogue>
-__device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilogue &epi, int tm, int tn, char *lds0, char *lds1) {
+template <int TY, int BM, int BN, int WGM, int WGN, int STAGES, bool DUAL, bool DMA, class Epilogue>
+__device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilogue &epi, int tm, int tn, char *lds) {
   using T = MmTraits<TY>;
   using E = typename T::elem;
   constexpr int WAVES = WGM * WGN, ROWS = BM + BN, LOADS = ROWS / 8 / WAVES, LOADS_A = BM / 8 / WAVES;
@@ -119,33 +125,56 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
     const int r = row_of(i, ld);
     return (i < LOADS_A ? baseA : DUAL && (i * WAVES + wave) * 8 - BM >= NB ? base1 : base0) + r * ld;
   };
+  constexpr int STAGE = ROWS * MM_STEP;  // bytes of LDS
   const auto room = [&](char *lds, int i) { return reinterpret_cast<u32x4 *>(lds + (i * WAVES + wave) * 8 * MM_STEP + lane * 16); };
 
-  typename T::acc acc[TM][TN];
+  using Acc = typename T::acc;
+  Acc acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = typename T::acc{0, 0, 0, 0};
+    for (int j = 0; j < TN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
 
   const int slot = ((lane >> 4) ^ (lane & 7)) * 16;  // of this lane's piece of the first 64 bytes; ^ 64: of the second
   const int fragA = (wm * (BM / WGM) + (lane & 15)) * MM_STEP + slot;
   const int fragB = (BM + wn * (NB / WGN) + (lane & 15)) * MM_STEP + slot;
-  const auto multiply = [&](const char *lds) {
+  struct Half {  // fragments of 64 bytes of k
+    u32x4 a[TM], b[TN];
+  };
+  const auto fetch = [&](Half &f, const char *lds, int half) {
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      u32x4 a[TM], b[TN];
-#pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int row = !DUAL ? j * 16 : j < TN / 2 ? j * 16 : NB + (j - TN / 2) * 16;
-        b[j] = *reinterpret_cast<const u32x4 *>(lds + (fragB ^ (kk * 64)) + row * MM_STEP);
-      }
-#pragma unroll
-      for (int i = 0; i < TM; ++i) a[i] = *reinterpret_cast<const u32x4 *>(lds + (fragA ^ (kk * 64)) + i * 16 * MM_STEP);
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = T::mfma(b[j], a[i], acc[i][j]);  // rows of the result: n
+    for (int j = 0; j < TN; ++j) {
+      const int row = !DUAL ? j * 16 : j < TN / 2 ? j * 16 : NB + (j - TN / 2) * 16;
+      f.b[j] = *reinterpret_cast<const u32x4 *>(lds + (fragB ^ (half * 64)) + row * MM_STEP);
     }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) f.a[i] = *reinterpret_cast<const u32x4 *>(lds + (fragA ^ (half * 64)) + i * 16 * MM_STEP);
+  };
+  const auto multiply = [&](const Half &f) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = T::mfma(f.b[j], f.a[i], acc[i][j]);  // rows of the result: n
+  };
+  const auto whole_step = [&](const char *lds) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      Half f;
+      fetch(f, lds, half);
+      multiply(f);
+    }
+  };
+  // Reads of LDS and requests between matrix instructions, not all in front of them (8192^3 bf16 841 -> 818 us).
+  constexpr int PER = TM * TN / (TM + TN) ? TM * TN / (TM + TN) : 1;
+  const auto interleave = [&](auto loads) {
+    constexpr int N = decltype(loads)::value;
+#pragma unroll
+    for (int i = 0; i < TM + TN; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      if (i < N) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   };
 
   const int K = p.kbytes;
@@ -170,23 +199,47 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
         else __builtin_amdgcn_raw_ptr_buffer_load_lds(res0, to, 16, at[i], k, 0, 0);
       }
     };
-    const int whole = K / MM_STEP * MM_STEP;
-    if (whole) request(0, lds0);
-    for (int k = 0; k < whole; k += 2 * MM_STEP) {
-      __syncthreads();  // step k has arrived, and lds1 is free
-      if (k + MM_STEP < whole) request(k + MM_STEP, lds1);
-      multiply(lds0);
-      if (k + MM_STEP >= whole) break;
-      __syncthreads();
-      if (k + 2 * MM_STEP < whole) request(k + 2 * MM_STEP, lds0);
-      multiply(lds1);
+    // Both halves of a step's fragments are in registers before the workgroup meets in the middle of the step; from there
+    // on its place in LDS takes the step STAGES ahead, and the first half of the next step is read under the products of
+    // the second half of this one.
+    const int steps = K / MM_STEP;
+    for (int i = 0; i < min(steps, STAGES); ++i) request(i * MM_STEP, lds + i * STAGE);
+    if (steps) {
+      Half first, second;
+      if (steps >= STAGES) mm_sync<(STAGES - 1) * LOADS>();
+      else mm_sync<0>();
+      fetch(first, lds, 0);
+      int now = 0;
+      const auto turn = [&](int i, auto loads) {
+        __builtin_amdgcn_sched_barrier(0);
+        const int next = now + 1 == STAGES ? 0 : now + 1;
+        fetch(second, lds + now * STAGE, 1);
+        multiply(first);
+        interleave(std::integral_constant<int, 0>());
+        if (i + STAGES - 1 < steps) mm_sync<(STAGES - 2) * LOADS>();
+        else mm_sync<0>();
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (decltype(loads)::value > 0) {
+          request((i + STAGES) * MM_STEP, lds + now * STAGE);
+        }
+        fetch(first, lds + next * STAGE, 0);
+        multiply(second);
+        interleave(loads);
+        now = next;
+      };
+      int i = 0;
+      for (; i + STAGES < steps; ++i) turn(i, std::integral_constant<int, LOADS>());
+      for (; i + 1 < steps; ++i) turn(i, std::integral_constant<int, 0>());
+      fetch(second, lds + now * STAGE, 1);
+      multiply(first);
+      multiply(second);
     }
-    if (whole < K) {  // what is left of k, with zeros behind it
+    if (steps * MM_STEP < K) {  // what is left of k, with zeros behind it
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) *room(lds0, i) = mm_piece<E>(source(i), whole + piece, K);
+      for (int i = 0; i < LOADS; ++i) *room(lds, i) = mm_piece<E>(source(i), steps * MM_STEP + piece, K);
       __syncthreads();
-      multiply(lds0);
+      whole_step(lds);
     }
   } else {
     const char *src[LOADS];
@@ -207,53 +260,53 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
       for (int i = 0; i < LOADS; ++i) *room(lds, i) = held[i];
     };
     request(0);
-    deliver(lds0);
+    deliver(lds);
     for (int k = 0; k < K; k += 2 * MM_STEP) {
-      __syncthreads();  // step k has arrived, and lds1 is free
+      __syncthreads();  // step k has arrived, and the other half is free
       if (k + MM_STEP < K) request(k + MM_STEP);
-      multiply(lds0);
+      whole_step(lds);
       if (k + MM_STEP >= K) break;
-      deliver(lds1);
+      deliver(lds + STAGE);
       __syncthreads();
       if (k + 2 * MM_STEP < K) request(k + 2 * MM_STEP);
-      multiply(lds1);
-      if (k + 2 * MM_STEP < K) deliver(lds0);
+      whole_step(lds + STAGE);
+      if (k + 2 * MM_STEP < K) deliver(lds);
     }
   }
 
   const int m = m0 + wm * (BM / WGM) + (lane & 15), n = n0 + wn * (NB / WGN) + (lane >> 4) * 4;
+  typename Epilogue::Row rows[TM];  // what the epilogue needs to know of them, all requested at once
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    if (m + i * 16 >= p.M) continue;
-    if constexpr (DUAL) {
+  for (int i = 0; i < TM; ++i) rows[i] = epi.row(min(m + i * 16, p.M - 1));
 #pragma unroll
-      for (int j = 0; j < TN / 2; ++j)
-        if (n + j * 16 < p.N) epi(m + i * 16, n + j * 16, p.N, acc[i][j], acc[i][TN / 2 + j]);
-    } else {
+  for (int j = 0; j < (DUAL ? TN / 2 : TN); ++j) {
+    if (n + j * 16 >= p.N) continue;
+    const auto columns = epi.columns(n + j * 16, p.N);
 #pragma unroll
-      for (int j = 0; j < TN; ++j)
-        if (n + j * 16 < p.N) epi(m + i * 16, n + j * 16, p.N, acc[i][j]);
+    for (int i = 0; i < TM; ++i) {
+      if (m + i * 16 >= p.M) continue;
+      if constexpr (DUAL) epi(m + i * 16, n + j * 16, p.N, rows[i], columns, acc[i][j], acc[i][TN / 2 + j]);
+      else epi(m + i * 16, n + j * 16, p.N, rows[i], columns, acc[i][j]);
     }
   }
 }
 
-template <int TY, int BM, int BN, int WGM, int WGN, bool DUAL, bool DMA, class Epilogue>
-__global__ __launch_bounds__(64 * WGM *WGN, 2) void mm_tile_kernel(MmOperands p, Epilogue epi) {
-  __shared__ __attribute__((aligned(16))) char lds0[(BM + BN) * MM_STEP];
-  __shared__ __attribute__((aligned(16))) char lds1[(BM + BN) * MM_STEP];
+template <int TY, int BM, int BN, int WGM, int WGN, int STAGES, bool DUAL, bool DMA, class Epilogue>
+__global__ __launch_bounds__(64 * WGM *WGN, WGM *WGN < 4 ? 1 : WGM *WGN / 4) void mm_tile_kernel(MmOperands p, Epilogue epi) {
+  __shared__ __attribute__((aligned(16))) char lds[STAGES * (BM + BN) * MM_STEP];
   int tm, tn;
   mm_tile(blockIdx.x, p.tilesM, p.tilesN, tm, tn);
-  mm_tile_product<TY, BM, BN, WGM, WGN, DUAL, DMA>(p, epi, tm, tn, lds0, lds1);
+  mm_tile_product<TY, BM, BN, WGM, WGN, STAGES, DUAL, DMA>(p, epi, tm, tn, lds);
 }
 
-template <int TY, int BM, int BN, int WGM, int WGN, bool DUAL, bool DMA, class Epilogue>
+template <int TY, int BM, int BN, int WGM, int WGN, int STAGES, bool DUAL, bool DMA, class Epilogue>
 bnn_status launch_mm_tile(MmOperands p, const Epilogue &epi, int kid, hipStream_t s) {
   p.tilesM = (p.M - 1) / BM + 1;
   p.tilesN = (p.N - 1) / (DUAL ? BN / 2 : BN) + 1;
   const int64_t tiles = (int64_t)p.tilesM * p.tilesN;
   if (tiles > 0x7fffffff) return BNN_ERR_UNSUPPORTED;
   ProfScope ps(kid, s);
-  mm_tile_kernel<TY, BM, BN, WGM, WGN, DUAL, DMA, Epilogue><<<(uint32_t)tiles, 64 * WGM * WGN, 0, s>>>(p, epi);
+  mm_tile_kernel<TY, BM, BN, WGM, WGN, STAGES, DUAL, DMA, Epilogue><<<(uint32_t)tiles, 64 * WGM * WGN, 0, s>>>(p, epi);
   return launch_status();
 }
 
