@@ -137,7 +137,8 @@ extern "C" const char *bnn_kernel_name(int kernel_id) {
     case bnn::KID_GATED_FF: return "gated_ff";
     case bnn::KID_GATED_FF_I8: return "gated_ff_i8";
     case bnn::KID_GATED_GRADIENT: return "gated_gradient";
-    case bnn::KID_TRANSPOSE: return "transpose";
+    case bnn::KID_REALIGN: return "realign";
+    case bnn::KID_PRODUCT_SUMS: return "product_sums";
     case bnn::KID_GATED_FF_BACKWARD: return "gated_ff_backward";
     case bnn::KID_VALU_PROBE: return "valu_probe";
     case bnn::KID_COPY_PROBE: return "copy_probe";

@@ -42,9 +42,10 @@ enum KernelId : int {
   KID_GATED_FF = 31,
   KID_GATED_FF_I8 = 32,
   KID_GATED_GRADIENT = 33,
-  KID_TRANSPOSE = 34,
+  KID_REALIGN = 34,
   KID_GATED_FF_BACKWARD = 35,
-  KID_COUNT = 36
+  KID_PRODUCT_SUMS = 36,
+  KID_COUNT = 37
 };
 
 // Timing hook: records an event pair around a launch when profiling is on.

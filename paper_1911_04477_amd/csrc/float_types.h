@@ -24,11 +24,6 @@ inline auto with_float(int t, const F &f) {
   return f(Float<BNN_F16>());
 }
 
-// Whether a matrix's rows may be read and written `count` elements of `size` bytes at a time.
-inline bool rows_by(const void *p, int64_t ld, int size, int count) {
-  return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) & (uintptr_t)(count * size - 1)) == 0;
-}
-
 // Values n .. n + 3 of an aligned vector of N, zeros past its end; n is a multiple of 4.
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ f32x4 load4(const float *v, int n, int N) {
@@ -37,15 +32,16 @@ __device__ __forceinline__ f32x4 load4(const float *v, int n, int N) {
 }
 struct NoConstants {};
 
-// Four consecutive values of a row of N, from column n on; vec: whole groups of four may go out as one store.
+// Four consecutive values of a row of N, from column n on; whole groups go out as one store, which takes any alignment.
 template <class E, class V>
-__device__ __forceinline__ void store4(E *row, int n, int N, const V &v, bool vec) {
+__device__ __forceinline__ void store4(E *row, int n, int N, const V &v) {
   typedef E E4 __attribute__((ext_vector_type(4)));
-  if (vec && n + 4 <= N) {
+  typedef uint32_t Words __attribute__((ext_vector_type(sizeof(E)), aligned(1)));
+  if (n + 4 <= N) {
     E4 o;
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = (E)v[i];
-    *reinterpret_cast<E4 *>(row + n) = o;
+    *reinterpret_cast<Words *>(row + n) = __builtin_bit_cast(Words, o);
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)

@@ -1,9 +1,11 @@
 // Gated feed-forward, h = act(x Wg^T) * (x Wu^T): both projections, the activation and the product in one kernel, from
 // 16-bit floating-point operands (with its backward pass) or from 8-bit ones with scales.
 #include <algorithm>
+#include <cmath>
 
 #include "few_mm.h"
-#include "float_types.h"
+#include "kmajor_mm.h"
+#include "rows.h"
 
 namespace bnn {
 
@@ -41,7 +43,7 @@ struct GatedEpilogue {
   int64_t ldh;
   float *saved;
   int64_t plane;  // values in one of the two
-  int act, vec, savedVec;
+  int act;
   using Row = NoConstants;
   __device__ __forceinline__ Row row(int) const { return {}; }
   __device__ __forceinline__ NoConstants columns(int, int) const { return {}; }
@@ -55,8 +57,8 @@ struct GatedEpilogue {
         dg[i] = slope * u[i];
         o[i] = du[i] * u[i];
       }
-      store4(saved + (int64_t)m * N, n, N, dg, savedVec);
-      store4(saved + plane + (int64_t)m * N, n, N, du, savedVec);
+      store4(saved + (int64_t)m * N, n, N, dg);
+      store4(saved + plane + (int64_t)m * N, n, N, du);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -64,7 +66,7 @@ struct GatedEpilogue {
         o[i] = activation<false>(act, g[i], none) * u[i];
       }
     }
-    store4(h + m * ldh, n, N, o, vec);
+    store4(h + m * ldh, n, N, o);
   }
 };
 
@@ -72,7 +74,7 @@ struct GatedI8Epilogue {
   const float *sx, *sg, *su;
   void *h;
   int64_t ldh;
-  int type, act, vec;
+  int type, act;
   using Row = float;
   struct Columns {
     f32x4 g, u;
@@ -86,65 +88,74 @@ struct GatedI8Epilogue {
       float none;
       o[i] = activation<false>(act, (float)g[i] * a * c.g[i], none) * ((float)u[i] * a * c.u[i]);
     }
-    if (type == BNN_BF16) store4(static_cast<__bf16 *>(h) + m * ldh, n, N, o, vec);
-    else if (type == BNN_F16) store4(static_cast<_Float16 *>(h) + m * ldh, n, N, o, vec);
-    else store4(static_cast<float *>(h) + m * ldh, n, N, o, vec);
+    if (type == BNN_BF16) store4(static_cast<__bf16 *>(h) + m * ldh, n, N, o);
+    else if (type == BNN_F16) store4(static_cast<_Float16 *>(h) + m * ldh, n, N, o);
+    else store4(static_cast<float *>(h) + m * ldh, n, N, o);
   }
 };
 
-// A plain product, rounded to the operands' type; rows from `split` on go to a second matrix.
+// A product rounded to the operands' type; rows from `split` on go to a second matrix.  part: sums of a share of k go there
+// instead, in fp32, [shares][M][ld].
 template <class E>
 struct ProductEpilogue {
   E *y0, *y1;
   int64_t ld0, ld1;
-  int rows0, split, vec;  // rows0 <= split: rows between them are padding
-  using Row = NoConstants;
-  __device__ __forceinline__ Row row(int) const { return {}; }
-  __device__ __forceinline__ NoConstants columns(int, int) const { return {}; }
-  __device__ __forceinline__ void operator()(int m, int n, int N, Row, NoConstants, const v4f &v) const {
-    if (m < rows0) store4(y0 + m * ld0, n, N, v, vec);
-    else if (m >= split && m - split < rows0) store4(y1 + (m - split) * ld1, n, N, v, vec);
+  int rows0, split;  // rows0 <= split: rows between them are padding
+  int D;             // columns that are stored
+  float *part;
+  int64_t plane, part_ld;
+  template <class V>
+  __device__ __forceinline__ void store(int m, int n, const V &v) const {
+    if (m < rows0) store4(y0 + m * ld0, n, D, v);
+    else if (m >= split && m - split < rows0) store4(y1 + (m - split) * ld1, n, D, v);
+  }
+  __device__ __forceinline__ void operator()(int m, int n, int, int share, const v4f &v) const {
+    if (part) *reinterpret_cast<v4f *>(part + share * plane + m * part_ld + n) = v;
+    else store(m, n, v);
   }
 };
 
-// 64 x 64 blocks of 16-bit values, transposed through LDS.
-constexpr int TRB = 64;
 template <class E>
-__device__ __forceinline__ void transposed_block(E (*t)[TRB + 2], E *out, int64_t ld, int r0, int c0, int rows, int cols) {
-  __syncthreads();
-  for (int i = threadIdx.x; i < TRB * TRB; i += 256) {
-    const int c = i / TRB, r = i % TRB;  // out[c][r]
-    if (c0 + c < cols && r0 + r < rows) out[(int64_t)(c0 + c) * ld + r0 + r] = t[r][c];
-  }
+__global__ __launch_bounds__(256) void product_sums_kernel(ProductEpilogue<E> epi, int M, int shares) {
+  const int64_t quads = epi.part_ld / 4, i = blockIdx.x * 256ll + threadIdx.x;
+  if (i >= M * quads) return;
+  const int m = (int)(i / quads), n = (int)(i - m * quads) * 4;
+  v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < shares; ++s) sum += *reinterpret_cast<const v4f *>(epi.part + s * epi.plane + m * epi.part_ld + n);
+  if (n < epi.D) epi.store(m, n, sum);
 }
 
-// out[c][r] = in[r][c] for r below `rows`, zeros up to outCols; in has `cols` columns.
+// Gradients of the projections, dG = dh * saved[0] and dU = dh * saved[1], side by side in rows of 2 Fp (zeros beside F):
+// eight values a thread.  Bound by memory (14 B a value).
 template <class E>
-__global__ __launch_bounds__(256) void transpose_kernel(const E *in, int64_t ldi, int rows, int cols, E *out, int64_t ldo,
-                                                        int outCols) {
-  __shared__ E t[TRB][TRB + 2];
-  const int r0 = blockIdx.y * TRB, c0 = blockIdx.x * TRB;
-  for (int i = threadIdx.x; i < TRB * TRB; i += 256) {
-    const int r = i / TRB, c = i % TRB;
-    t[r][c] = r0 + r < rows && c0 + c < cols ? in[(int64_t)(r0 + r) * ldi + c0 + c] : (E)0.0f;
-  }
-  transposed_block(t, out, ldo, r0, c0, outCols, cols);
+__global__ __launch_bounds__(256) void gated_gradient_kernel(const E *dh, int64_t ldh, const float *saved, int64_t plane, int64_t groups,
+                                                             int F, int Fp, E *out) {
+  const int64_t i = blockIdx.x * 256ll + threadIdx.x;
+  if (i >= groups) return;
+  const int per = Fp / 8;
+  const int64_t r = i / per;
+  const int c = (int)(i - r * per) * 8;
+  float d[8], g[8], u[8];
+  load8(d, dh + r * ldh, c, F);
+  load8(g, saved + r * F, c, F);
+  load8(u, saved + plane + r * F, c, F);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) g[j] *= d[j], u[j] *= d[j];
+  store8(out + r * 2 * Fp, c, Fp, g);
+  store8(out + r * 2 * Fp + Fp, c, Fp, u);
 }
 
-// Gradients of the projections, dG = dh * saved[0] and dU = dh * saved[1], side by side in rows of 2 Fp (zeros beside F),
-// and the same transposed with zeros beside T.
+// Rows of D values as rows of Dp that start on 16 bytes, zeros behind them.
 template <class E>
-__global__ __launch_bounds__(256) void gated_gradient_kernel(const E *dh, int64_t ldh, const float *saved, int64_t plane, int T,
-                                                             int F, int Fp, int Tp, E *out, E *outT) {
-  __shared__ E t[TRB][TRB + 2];
-  const int r0 = blockIdx.y * TRB, c0 = blockIdx.x * TRB, which = blockIdx.z;
-  for (int i = threadIdx.x; i < TRB * TRB; i += 256) {
-    const int r = r0 + i / TRB, c = c0 + i % TRB;
-    const E v = r < T && c < F ? (E)((float)dh[r * ldh + c] * saved[which * plane + (int64_t)r * F + c]) : (E)0.0f;
-    t[i / TRB][i % TRB] = v;
-    if (r < T && c < Fp) out[(int64_t)r * 2 * Fp + which * Fp + c] = v;
-  }
-  transposed_block(t, outT + (int64_t)which * Fp * Tp, Tp, r0, c0, Tp, Fp);
+__global__ __launch_bounds__(256) void realign_kernel(const E *in, int64_t ld, int64_t groups, int D, int Dp, E *out) {
+  const int64_t i = blockIdx.x * 256ll + threadIdx.x;
+  if (i >= groups) return;
+  const int per = Dp / 8;
+  const int64_t r = i / per;
+  const int c = (int)(i - r * per) * 8;
+  float v[8];
+  load8(v, in + r * ld, c, D);
+  store8(out + r * Dp, c, Dp, v);
 }
 
 template <class E>
@@ -154,46 +165,107 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(E *y, int64_t ld, int64_
 
 inline bool half_type(int t) { return t == BNN_BF16 || t == BNN_F16; }
 inline bool act_known(int a) { return a >= BNN_ACT_SILU && a <= BNN_ACT_RELU; }
-inline int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
-constexpr int64_t MAX_DIM = (1 << 22) - 64;  // blocks of 64 rows within a launch's 65535; in bytes, doubled, 32 bits
+inline int64_t pad(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+constexpr int64_t MAX_DIM = (1 << 22) - 64;  // in bytes and doubled, 32 bits
+
+// Which kernel takes a k-major product, and into how many shares its k is split: the cheapest by microseconds a step and a
+// round of tiles, measured in bf16 (256 x 256: 8192 x 4096 by k 16384 828 us; 128 x 128 with one tile a unit: 256 x 4096
+// by k 16384 117 us, two a unit 8192 x 4096 1040; 64 x 64: 80 and 1896), what a round costs beside its steps (16384 x 4096
+// by k 256: 83, 85, 62 and 101 us), and the shares' way through memory.
+struct KmPlan {
+  int form, shares;
+};
+inline KmPlan km_plan(int64_t M, int64_t N, int64_t steps) {
+  constexpr struct {
+    int tile, slots;
+    double step, round;
+  } forms[] = {{256, 256, 1.62, 14.0}, {128, 256, 0.457, 3.5}, {128, 512, 1.016, 3.6}, {64, 256, 0.31, 1.3}, {64, 512, 0.463, 1.3}};
+  KmPlan best = {0, 1};
+  double least = 1e300;
+  for (int f = 0; f < 5; ++f)
+    for (int shares = 1; shares <= 32 && (shares == 1 || shares * 4 <= steps); shares *= 2) {
+      const double tiles = (double)((M - 1) / forms[f].tile + 1) * (double)((N - 1) / forms[f].tile + 1) * shares;
+      if (f % 2 && tiles > forms[f].slots) continue;  // one tile a unit
+      const double rounds = std::ceil(tiles / forms[f].slots);
+      const double cost = rounds * ((steps + shares - 1) / shares * forms[f].step + forms[f].round) +
+                          (shares > 1 ? 4.0 + 8e-6 / 4.0 * shares * (double)M * (double)N : 0.0);
+      if (cost < least) least = cost, best = {f, shares};
+    }
+  return best;
+}
+
+// The parts of the backward pass's workspace, in bytes from its start.
+struct GatedSpace {
+  int64_t Fp, Dp, wg, wu, x, part, end;
+};
+inline GatedSpace gated_space(int64_t T, int64_t D, int64_t F) {
+  GatedSpace g;
+  g.Fp = pad(F, KM_STEP), g.Dp = pad(D, 8);
+  g.wg = pad(T * 2 * g.Fp * 2, 256);  // gradients of the projections before it
+  g.wu = g.wg + pad(F * g.Dp * 2, 256);
+  g.x = g.wu + pad(F * g.Dp * 2, 256);
+  g.part = g.x + pad(T * g.Dp * 2, 256);
+  const KmPlan x = km_plan(T, g.Dp, 2 * (F / KM_STEP)), w = km_plan(2 * g.Fp, g.Dp, T / KM_STEP);
+  g.end = g.part + 4 * std::max(x.shares > 1 ? x.shares * T * g.Dp : 0, w.shares > 1 ? w.shares * 2 * g.Fp * g.Dp : 0);
+  return g;
+}
+
+template <int TY, bool A_ROWS, class E>
+bnn_status km_product(KmOperands p, ProductEpilogue<E> epi, float *part, hipStream_t s) {
+  const KmPlan plan = km_plan(p.M, p.N, (int64_t)p.K / KM_STEP * p.segments);
+  p.splits = plan.shares;
+  if (plan.shares > 1) epi.part = part, epi.part_ld = p.N, epi.plane = (int64_t)p.M * p.N;
+  bnn_status st;
+  switch (plan.form) {
+    case 0: st = launch_km_tile<TY, 256, 256, 4, 2, 2, A_ROWS>(p, epi, KID_GATED_FF_BACKWARD, s); break;
+    case 1: st = launch_km_tile<TY, 128, 128, 2, 4, 4, A_ROWS>(p, epi, KID_GATED_FF_BACKWARD, s); break;
+    case 2: st = launch_km_tile<TY, 128, 128, 2, 2, 2, A_ROWS>(p, epi, KID_GATED_FF_BACKWARD, s); break;
+    default: st = launch_km_tile<TY, 64, 64, 2, 2, 4, A_ROWS>(p, epi, KID_GATED_FF_BACKWARD, s);
+  }
+  if (st || plan.shares == 1) return st;
+  ProfScope ps(KID_PRODUCT_SUMS, s);
+  product_sums_kernel<E><<<(uint32_t)(((int64_t)p.M * p.N / 4 + 255) / 256), 256, 0, s>>>(epi, p.M, plan.shares);
+  return launch_status();
+}
 
 template <int TY>
 bnn_status gated_backward(const char *x, int64_t x_ld, const char *wg, int64_t wg_ld, const char *wu, int64_t wu_ld,
-                          const float *saved, const void *dh_, int64_t dh_ld, int T, int D, int F, void *dx, int64_t dx_ld,
+                          const float *saved, const void *dh, int64_t dh_ld, int T, int D, int F, void *dx, int64_t dx_ld,
                           void *dwg, int64_t dwg_ld, void *dwu, int64_t dwu_ld, char *workspace, hipStream_t s) {
   using E = typename MmTraits<TY>::elem;
-  const int Fp = (int)pad8(F), Tp = (int)pad8(T);
-  E *grad = reinterpret_cast<E *>(workspace);              // [T, 2 Fp]
-  E *gradT = grad + (int64_t)T * 2 * Fp;                   // [2 Fp, Tp]
-  E *wT = gradT + (int64_t)2 * Fp * Tp;                    // [D, 2 Fp]
-  E *xT = wT + (int64_t)D * 2 * Fp;                        // [D, Tp]
-  const E *dh = static_cast<const E *>(dh_);
-  const auto blocks = [](int64_t n) { return (uint32_t)((n + TRB - 1) / TRB); };
+  const GatedSpace g = gated_space(T, D, F);
+  const int Fp = (int)g.Fp, Dp = (int)g.Dp;
+  E *const grad = reinterpret_cast<E *>(workspace);
+  float *const part = reinterpret_cast<float *>(workspace + g.part);
+  const auto blocks = [](int64_t n) { return (uint32_t)((n + 255) / 256); };
   {
     ProfScope ps(KID_GATED_GRADIENT, s);
-    gated_gradient_kernel<E><<<dim3(blocks(Fp), blocks(Tp), 2), 256, 0, s>>>(dh, dh_ld, saved, (int64_t)T * F, T, F, Fp, Tp, grad, gradT);
+    const int64_t n = (int64_t)T * Fp / 8;
+    gated_gradient_kernel<E><<<blocks(n), 256, 0, s>>>(static_cast<const E *>(dh), dh_ld, saved, (int64_t)T * F, n, F, Fp, grad);
   }
-  {
-    ProfScope ps(KID_TRANSPOSE, s);
-    transpose_kernel<E><<<dim3(blocks(D), blocks(Fp)), 256, 0, s>>>(reinterpret_cast<const E *>(wg), wg_ld, F, D, wT, 2 * Fp, Fp);
-    transpose_kernel<E><<<dim3(blocks(D), blocks(Fp)), 256, 0, s>>>(reinterpret_cast<const E *>(wu), wu_ld, F, D, wT + Fp, 2 * Fp, Fp);
-    transpose_kernel<E><<<dim3(blocks(D), blocks(Tp)), 256, 0, s>>>(reinterpret_cast<const E *>(x), x_ld, T, D, xT, Tp, Tp);
-  }
+  // the products take columns eight at a time, from rows that start on 16 bytes
+  const auto aligned = [&](const char *&m, int64_t &ld, int64_t rows, int64_t at) {
+    if (D == Dp && mm_dma(m, 2 * ld)) return;
+    E *const to = reinterpret_cast<E *>(workspace + at);
+    const int64_t n = rows * Dp / 8;
+    ProfScope ps(KID_REALIGN, s);
+    realign_kernel<E><<<blocks(n), 256, 0, s>>>(reinterpret_cast<const E *>(m), ld, n, D, Dp, to);
+    m = workspace + at, ld = Dp;
+  };
+  aligned(wg, wg_ld, F, g.wg);
+  aligned(wu, wu_ld, F, g.wu);
+  aligned(x, x_ld, T, g.x);
   if (bnn_status st = launch_status()) return st;
-  MmOperands p = {};
-  p.A = reinterpret_cast<const char *>(grad), p.lda = 4ll * Fp;
-  p.B0 = p.B1 = reinterpret_cast<const char *>(wT), p.ldb0 = p.ldb1 = 4ll * Fp;
-  p.M = T, p.N = D, p.kbytes = 4 * Fp;
-  p.dma = mm_dma(p.A, p.lda) && mm_dma(p.B0, p.ldb0);
-  const ProductEpilogue<E> ex = {static_cast<E *>(dx), nullptr, dx_ld, 0, T, T, rows_by(dx, dx_ld, 2, 4)};
-  if (bnn_status st = run_product<TY, false>(p, ex, KID_GATED_FF_BACKWARD, KID_GATED_FF_BACKWARD, s)) return st;
-  p.A = reinterpret_cast<const char *>(gradT), p.lda = 2ll * Tp;
-  p.B0 = p.B1 = reinterpret_cast<const char *>(xT), p.ldb0 = p.ldb1 = 2ll * Tp;
-  p.M = 2 * Fp, p.N = D, p.kbytes = 2 * Tp;
-  p.dma = mm_dma(p.A, p.lda) && mm_dma(p.B0, p.ldb0);
-  const ProductEpilogue<E> ew = {static_cast<E *>(dwg), static_cast<E *>(dwu), dwg_ld, dwu_ld, F, Fp,
-                                 rows_by(dwg, dwg_ld, 2, 4) && rows_by(dwu, dwu_ld, 2, 4)};
-  return run_product<TY, false>(p, ew, KID_GATED_FF_BACKWARD, KID_GATED_FF_BACKWARD, s);
+  KmOperands p = {};
+  p.A = workspace, p.lda = 4ll * Fp, p.segA = Fp;
+  p.B0 = wg, p.B1 = wu, p.ldb0 = 2 * wg_ld, p.ldb1 = 2 * wu_ld;
+  p.M = T, p.N = Dp, p.K = F, p.segments = 2;
+  ProductEpilogue<E> epi = {static_cast<E *>(dx), nullptr, dx_ld, 0, T, T, D, nullptr, 0, 0};
+  if (bnn_status st = km_product<TY, true>(p, epi, part, s)) return st;
+  p.B0 = p.B1 = x, p.ldb0 = p.ldb1 = 2 * x_ld, p.segA = 0;
+  p.M = 2 * Fp, p.K = T, p.segments = 1;
+  epi = {static_cast<E *>(dwg), static_cast<E *>(dwu), dwg_ld, dwu_ld, F, Fp, D, nullptr, 0, 0};
+  return km_product<TY, false>(p, epi, part, s);
 }
 
 // Gradients of an empty product.
@@ -225,10 +297,9 @@ extern "C" bnn_status bnn_gated_ff(const void *x, int64_t x_ld, const void *wg, 
   p.M = (int)T, p.N = (int)F, p.kbytes = (int)(2 * D);
   p.dma = mm_dma(x, p.lda) && mm_dma(wg, p.ldb0) && mm_dma(wu, p.ldb1);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int vec = rows_by(h, h_ld, 2, 4), savedVec = F % 4 == 0;
   if (type == BNN_BF16)
-    return run_product<MM_BF16, true>(p, GatedEpilogue<__bf16>{static_cast<__bf16 *>(h), h_ld, saved, T * F, act, vec, savedVec}, KID_GATED_FF, KID_GATED_FF, s);
-  return run_product<MM_F16, true>(p, GatedEpilogue<_Float16>{static_cast<_Float16 *>(h), h_ld, saved, T * F, act, vec, savedVec}, KID_GATED_FF, KID_GATED_FF, s);
+    return run_product<MM_BF16, true>(p, GatedEpilogue<__bf16>{static_cast<__bf16 *>(h), h_ld, saved, T * F, act}, KID_GATED_FF, KID_GATED_FF, s);
+  return run_product<MM_F16, true>(p, GatedEpilogue<_Float16>{static_cast<_Float16 *>(h), h_ld, saved, T * F, act}, KID_GATED_FF, KID_GATED_FF, s);
 }
 
 extern "C" bnn_status bnn_gated_ff_i8(const int8_t *x, int64_t x_ld, const float *x_scale, const int8_t *wg, int64_t wg_ld,
@@ -249,15 +320,14 @@ extern "C" bnn_status bnn_gated_ff_i8(const int8_t *x, int64_t x_ld, const float
   p.B1 = reinterpret_cast<const char *>(wu), p.ldb1 = wu_ld;
   p.M = (int)T, p.N = (int)F, p.kbytes = (int)D;
   p.dma = mm_dma(x, x_ld) && mm_dma(wg, wg_ld) && mm_dma(wu, wu_ld);
-  const GatedI8Epilogue epi = {x_scale, wg_scale, wu_scale, h, h_ld, type, act, rows_by(h, h_ld, float_size(type), 4)};
+  const GatedI8Epilogue epi = {x_scale, wg_scale, wu_scale, h, h_ld, type, act};
   return run_product<MM_I8, true>(p, epi, KID_GATED_FF_I8, KID_GATED_FF_I8, static_cast<hipStream_t>(stream));
 }
 
 extern "C" size_t bnn_gated_ff_backward_workspace_bytes(int64_t T, int64_t D, int64_t F) {
   using namespace bnn;
   if (T <= 0 || D <= 0 || F <= 0 || T > MAX_DIM || D > MAX_DIM || F > MAX_DIM) return 0;
-  const size_t Fp = (size_t)pad8(F), Tp = (size_t)pad8(T);
-  return 2 * (2 * Fp * (size_t)T + 2 * Fp * Tp + 2 * Fp * (size_t)D + Tp * (size_t)D);
+  return (size_t)gated_space(T, D, F).end;
 }
 
 extern "C" bnn_status bnn_gated_ff_backward(const void *x, int64_t x_ld, const void *wg, int64_t wg_ld, const void *wu,

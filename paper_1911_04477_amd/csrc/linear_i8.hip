@@ -9,7 +9,7 @@ struct LinearEpilogue {
   const float *sa, *sb, *bias;
   void *y;
   int64_t ldy;
-  int type, vec;
+  int type;
   using Row = float;
   struct Columns {
     f32x4 scale, bias;
@@ -22,9 +22,9 @@ struct LinearEpilogue {
     float v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = fmaf((float)sum[i] * a, c.scale[i], c.bias[i]);
-    if (type == BNN_BF16) store4(static_cast<__bf16 *>(y) + m * ldy, n, N, v, vec);
-    else if (type == BNN_F16) store4(static_cast<_Float16 *>(y) + m * ldy, n, N, v, vec);
-    else store4(static_cast<float *>(y) + m * ldy, n, N, v, vec);
+    if (type == BNN_BF16) store4(static_cast<__bf16 *>(y) + m * ldy, n, N, v);
+    else if (type == BNN_F16) store4(static_cast<_Float16 *>(y) + m * ldy, n, N, v);
+    else store4(static_cast<float *>(y) + m * ldy, n, N, v);
   }
 };
 
@@ -47,6 +47,6 @@ extern "C" bnn_status bnn_linear_i8(const int8_t *a, int64_t lda, const float *a
   p.lda = lda, p.ldb0 = p.ldb1 = ldb;
   p.M = (int)M, p.N = (int)N, p.kbytes = (int)K;
   p.dma = mm_dma(a, lda) && mm_dma(b, ldb);
-  const LinearEpilogue epi = {a_scale, b_scale, bias, y, ldy, type, rows_by(y, ldy, float_size(type), 4)};
+  const LinearEpilogue epi = {a_scale, b_scale, bias, y, ldy, type};
   return run_product<MM_I8, false>(p, epi, KID_LINEAR_I8_FEW, KID_LINEAR_I8, static_cast<hipStream_t>(stream));
 }
