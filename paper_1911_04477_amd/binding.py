@@ -161,7 +161,8 @@ class _Tensors:
     function of this module has to look at it.  Where the extension has not been built, or for another torch, every call is of that
     kind."""
 
-    FUNCTIONS = ("gemm", "epilogue", "encode", "conv2d", "conv2d_packed", "im2col", "f32_sign", "conv2d_f32", "maxpool", "fc")
+    FUNCTIONS = ("gemm", "epilogue", "encode", "conv2d", "conv2d_packed", "im2col", "f32_sign", "conv2d_f32", "maxpool", "fc",
+                 "quant_rows", "linear_i8", "norm_gate", "norm_gate_backward", "gated_ff", "gated_ff_i8", "gated_ff_backward")
 
     def __init__(self, L: ctypes.CDLL, path: str):
         module = None
@@ -730,6 +731,11 @@ def rows_i8(rows: int, K: int, device="cuda:0") -> torch.Tensor:
 def bnn_quant_rows_i8(x: torch.Tensor, q: Optional[torch.Tensor] = None,
                       scale: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """x [rows, K] fp32, bf16 or fp16 -> (q int8 [rows, K], scale fp32 [rows])."""
+    if q is not None and scale is not None:
+        st = _t().quant_rows(x, q, scale)
+        if st is not None:
+            _check(st, "bnn_quant_rows_i8")
+            return q, scale
     kind, ld = _float(x, "x"), _rows(x, "x")
     rows, K = x.shape
     if q is None:
@@ -746,6 +752,11 @@ def bnn_linear_i8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_sca
                   bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                   dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """a int8 [M, K] and its scales [M], b int8 [N, K] and its scales [N] -> [M, N] of out's type, or of dtype."""
+    if out is not None:
+        st = _t().linear_i8(a, a_scale, b, b_scale, bias, out)
+        if st is not None:
+            _check(st, "bnn_linear_i8")
+            return out
     _dev(a, torch.int8, "a")
     _dev(b, torch.int8, "b")
     lda = _rows(a, "a")
@@ -784,12 +795,17 @@ def bnn_norm_gate(b: Optional[torch.Tensor], r: torch.Tensor, *, gate: Optional[
     """b [rows, D] (a block's output, or None before the first), r [rows, D] (the residual stream) -> (r', n): the new stream
     (None without b) and its norm, n_out.  With q_out and q_scale n goes out as int8 rows with scales; n_out is then written
     only if given.  post, pre: "rms", "layer" or "none"."""
+    if r_out is None and b is not None:
+        r_out = torch.empty(r.shape, dtype=r.dtype, device=r.device)
+    if n_out is None and q_out is None and pre != "none":
+        n_out = torch.empty(r.shape, dtype=r.dtype if b is None else b.dtype, device=r.device)
+    st = _t().norm_gate(b, r, gate, gate_rows, res_scale, w_post, bias_post, w_pre, bias_pre, NORMS.get(post), NORMS.get(pre), eps,
+                        r_out, n_out, q_out, q_scale)
+    if st is not None:
+        _check(st, "bnn_norm_gate")
+        return r_out, n_out
     p = _norm_in(b, r, gate, gate_rows, res_scale, w_post, bias_post, w_pre, bias_pre, post, pre, eps)
     rows, D = r.shape
-    if r_out is None and b is not None:
-        r_out = torch.empty((rows, D), dtype=r.dtype, device=r.device)
-    if n_out is None and q_out is None and pre != "none":
-        n_out = torch.empty((rows, D), dtype=r.dtype if b is None else b.dtype, device=r.device)
     lds = [0, 0, 0]
     for i, (t, dtype, name) in enumerate(((r_out, r.dtype, "r_out"), (n_out, r.dtype if b is None else b.dtype, "n_out"),
                                           (q_out, torch.int8, "q_out"))):
@@ -814,9 +830,9 @@ def bnn_norm_gate_backward(b: Optional[torch.Tensor], r: torch.Tensor, dn: Optio
     """Gradients of bnn_norm_gate from its inputs and those of its outputs (dn of n, dr_out of r'; None: zero), as a dict: dr,
     and, for each of b, gate, res_scale, w_post, bias_post, w_pre and bias_pre that was given, its name with a d before it.
     out: the same dict with tensors to write to, where a caller keeps them."""
-    p = _norm_in(b, r, gate, gate_rows, res_scale, w_post, bias_post, w_pre, bias_pre, post, pre, eps)
+    if r.dim() != 2:
+        raise ValueError("r: a matrix expected")
     rows, D = r.shape
-    kind = r.dtype if b is None else b.dtype
     got = dict(out or {})
     wanted = {"dr": r, "db": b, "dgate": gate, "dres_scale": res_scale, "dw_post": w_post, "dbias_post": bias_post,
               "dw_pre": w_pre, "dbias_pre": bias_pre}
@@ -825,6 +841,16 @@ def bnn_norm_gate_backward(b: Optional[torch.Tensor], r: torch.Tensor, dn: Optio
             got.pop(name, None)
         elif name not in got:
             got[name] = torch.empty(of.shape, dtype=of.dtype, device=r.device)
+    if workspace is None:
+        nbytes = norm_gate_backward_workspace_bytes(rows, D, gate_rows if gate is not None else 0)
+        workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=r.device)
+    st = _t().norm_gate_backward(b, r, gate, gate_rows, res_scale, w_post, bias_post, w_pre, bias_pre, NORMS.get(post), NORMS.get(pre),
+                                 eps, dn, dr_out, *[got.get(name) for name in wanted], workspace)
+    if st is not None:
+        _check(st, "bnn_norm_gate_backward")
+        return got
+    p = _norm_in(b, r, gate, gate_rows, res_scale, w_post, bias_post, w_pre, bias_pre, post, pre, eps)
+    kind = r.dtype if b is None else b.dtype
     mats = [(dn, kind, "dn", rows), (dr_out, r.dtype, "dr_out", rows), (got["dr"], r.dtype, "dr", rows),
             (got.get("db"), kind, "db", rows), (got.get("dgate"), kind, "dgate", gate.shape[0] if gate is not None else 0)]
     args = []
@@ -834,9 +860,6 @@ def bnn_norm_gate_backward(b: Optional[torch.Tensor], r: torch.Tensor, dn: Optio
         args += [_ptr(t), 0 if t is None else _rows(t, name, n, D)]
     for name in ("dres_scale", "dw_post", "dbias_post", "dw_pre", "dbias_pre"):
         args.append(_vector(got.get(name), name, D))
-    if workspace is None:
-        nbytes = norm_gate_backward_workspace_bytes(rows, D, gate_rows if gate is not None else 0)
-        workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=r.device)
     _check(_c().bnn_norm_gate_backward(ctypes.addressof(p), *args, _ptr(workspace), workspace.numel() * workspace.element_size(),
                                         _stream()), "bnn_norm_gate_backward")
     return got
@@ -867,6 +890,11 @@ def bnn_gated_ff(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str =
                  saved: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [T, D], wg and wu [F, D], all bf16 or all fp16 -> h [T, F] = act(x wg^T) * (x wu^T).  act: "silu", "gelu",
     "gelu_tanh" or "relu".  saved (gated_ff_saved): written for bnn_gated_ff_backward."""
+    if out is not None:
+        st = _t().gated_ff(x, wg, wu, ACTS.get(act), out, saved)
+        if st is not None:
+            _check(st, "bnn_gated_ff")
+            return out
     T, D, F, kind, (x_ld, g_ld, u_ld) = _gated_in(x, wg, wu)
     if out is None:
         out = torch.empty((T, F), dtype=x.dtype, device=x.device)
@@ -880,6 +908,11 @@ def bnn_gated_ff_i8(x: torch.Tensor, x_scale: torch.Tensor, wg: torch.Tensor, wg
                     wu_scale: torch.Tensor, act: str = "silu", out: Optional[torch.Tensor] = None,
                     dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """bnn_gated_ff on int8 rows with their scales; h of out's type, or of dtype."""
+    if out is not None:
+        st = _t().gated_ff_i8(x, x_scale, wg, wg_scale, wu, wu_scale, ACTS.get(act), out)
+        if st is not None:
+            _check(st, "bnn_gated_ff_i8")
+            return out
     for t, name in ((x, "x"), (wg, "wg"), (wu, "wu")):
         _dev(t, torch.int8, name)
     x_ld = _rows(x, "x")
@@ -901,13 +934,20 @@ def bnn_gated_ff_backward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, s
                           dx: Optional[torch.Tensor] = None, dwg: Optional[torch.Tensor] = None,
                           dwu: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """(dx, dwg, dwu) from the operands of bnn_gated_ff, what it saved, and dh [T, F]."""
-    T, D, F, kind, (x_ld, g_ld, u_ld) = _gated_in(x, wg, wu)
+    if x.dim() != 2 or wg.dim() != 2:
+        raise ValueError("x, wg: matrices expected")
     dx, dwg, dwu = (torch.empty(of.shape, dtype=x.dtype, device=x.device) if t is None else t
                     for t, of in ((dx, x), (dwg, wg), (dwu, wu)))
+    if workspace is None:
+        nbytes = gated_ff_backward_workspace_bytes(x.shape[0], x.shape[1], wg.shape[0])
+        workspace = torch.empty(max(16, nbytes), dtype=torch.uint8, device=x.device)
+    st = _t().gated_ff_backward(x, wg, wu, saved, dh, dx, dwg, dwu, workspace)
+    if st is not None:
+        _check(st, "bnn_gated_ff_backward")
+        return dx, dwg, dwu
+    T, D, F, kind, (x_ld, g_ld, u_ld) = _gated_in(x, wg, wu)
     for t, name in ((dh, "dh"), (dx, "dx"), (dwg, "dwg"), (dwu, "dwu")):
         _dev(t, x.dtype, name)
-    if workspace is None:
-        workspace = torch.empty(max(16, gated_ff_backward_workspace_bytes(T, D, F)), dtype=torch.uint8, device=x.device)
     _check(_c().bnn_gated_ff_backward(_ptr(x), x_ld, _ptr(wg), g_ld, _ptr(wu), u_ld, kind, T, D, F, _saved(saved, T, F), _ptr(dh),
                                        _rows(dh, "dh", T, F), _ptr(dx), _rows(dx, "dx", T, D), _ptr(dwg), _rows(dwg, "dwg", F, D),
                                        _ptr(dwu), _rows(dwu, "dwu", F, D), _ptr(workspace),

@@ -43,65 +43,60 @@ __device__ __forceinline__ void zero_past(float (&v)[8], int c, int D) {
 }
 
 // v: values before the norm, then normed (before weight and bias).  Returns the factor.  Centred values first, then the
-// mean of their squares: no difference of two large sums.  lds: two reductions' worth.
-template <int T, int NV>
-__device__ __forceinline__ float unit_rows(float (&v)[NV][8], int norm, int c0, int D, float eps, uint32_t *lds) {
-  if (norm == BNN_NORM_NONE) return 1.0f;
-  if (norm == BNN_NORM_LAYER) {
-    float sum = 0.0f;
+// mean of their squares: no difference of two large sums.  lds: two reductions' worth.  T: threads of the team.
+template <bool BLOCK, int NV>
+__device__ __forceinline__ void centre_rows(float (&v)[NV][8], float mean, int c0, int T, int D) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+  for (int i = 0; i < NV; ++i) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum += v[i][j];
-    const float mean = team_sum<T>(sum, lds) / (float)D;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] -= mean;
-      zero_past(v[i], c0 + i * T * 8, D);
-    }
+    for (int j = 0; j < 8; ++j) v[i][j] -= mean;
+    zero_past(v[i], c0 + i * T * 8, D);
   }
-  float sq = 0.0f;
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sq = fmaf(v[i][j], v[i][j], sq);
-  const float rs = 1.0f / sqrtf(team_sum<T>(sq, lds + T / 64) / (float)D + eps);
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] *= rs;
-  return rs;
 }
+template <int NV>
+__device__ __forceinline__ float sum_of(const float (&v)[NV][8]) {
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += v[i][j];
+  return s;
+}
+template <int NV>
+__device__ __forceinline__ float dot_of(const float (&v)[NV][8], const float (&u)[NV][8]) {
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = fmaf(v[i][j], u[i][j], s);
+  return s;
+}
+template <int NV>
+__device__ __forceinline__ void times(float (&v)[NV][8], float x) {
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] *= x;
+}
+__device__ __forceinline__ float row_factor(float squares, int D, float eps) { return 1.0f / sqrtf(squares / (float)D + eps); }
 
-// e: gradient of the normed values u, then of the values before the norm: rs * (e - mean(e) - u * mean(e * u)), the first
-// mean for centred norms only.
-template <int T, int NV>
-__device__ __forceinline__ void unit_rows_backward(float (&e)[NV][8], const float (&u)[NV][8], float rs, int norm, int D,
-                                                   uint32_t *lds) {
+template <bool BLOCK, int NV>
+__device__ __forceinline__ void unit_rows(float (&v)[NV][8], int norm, int c0, int T, int D, float eps, uint32_t *lds) {
   if (norm == BNN_NORM_NONE) return;
-  float along = 0.0f, level = 0.0f;
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) along = fmaf(e[i][j], u[i][j], along), level += e[i][j];
-  along = team_sum<T>(along, lds) / (float)D;
-  level = norm == BNN_NORM_LAYER ? team_sum<T>(level, lds + T / 64) / (float)D : 0.0f;
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) e[i][j] = rs * (e[i][j] - level - u[i][j] * along);
+  if (norm == BNN_NORM_LAYER) centre_rows<BLOCK, NV>(v, team_sum<BLOCK>(sum_of(v), lds) / (float)D, c0, T, D);
+  times(v, row_factor(team_sum<BLOCK>(dot_of(v, v), lds + 16), D, eps));
 }
 
 // Which row of the gate; the host has cut gate_rows to at most 2^31 - 1 rows.
 __device__ __forceinline__ int64_t norm_group(const bnn_norm_gate_in &p, int64_t row) { return (uint32_t)row / (uint32_t)p.gate_rows; }
 
-// A team of T threads takes a row at a time, NV pieces of eight values a thread.
-template <class E, class R, int T, int NV>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_gate_kernel(bnn_norm_gate_in p, NormOut o, int teams) {
-  constexpr int TEAMS = T < 256 ? 256 / T : 1;
-  __shared__ uint32_t lds[2][5][T / 64];
-  const int t = threadIdx.x % T, c0 = t * 8, D = p.D;
+// A team (a wave, or with BLOCK a workgroup) takes a row at a time, NV pieces of eight values a thread.  Bound by memory
+// (8192 x 4096 bf16 with a gate a token 74 us, 4.5 TB/s).
+template <class E, class R, bool BLOCK, int MAXT, int NV>
+__global__ __launch_bounds__(MAXT) void norm_gate_kernel(bnn_norm_gate_in p, NormOut o, int teams) {
+  __shared__ uint32_t lds[2 * 5 * 16];
+  if constexpr (BLOCK) clear_words(lds);
+  const int T = BLOCK ? blockDim.x : 64, t = BLOCK ? threadIdx.x : threadIdx.x & 63, c0 = t * 8, D = p.D;
   float w_post[NV][8], w_pre[NV][8], scale[NV][8];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -110,8 +105,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_gate_kernel(bnn_norm_g
     load8_or(scale[i], p.res_scale, c0 + i * T * 8, D, 1.0f);
   }
   int flip = 0;  // a row's reductions do not touch what the row before left for slower waves to read
-  for (int64_t row = (int64_t)blockIdx.x * TEAMS + (TEAMS > 1 ? threadIdx.x / T : 0); row < p.rows; row += teams, flip ^= 1) {
-    uint32_t *const mem = &lds[flip][0][0];
+  for (int64_t row = BLOCK ? blockIdx.x : blockIdx.x * 4ll + (threadIdx.x >> 6); row < p.rows; row += teams, flip ^= 1) {
+    uint32_t *const mem = lds + flip * 5 * 16;
     float v[NV][8], r[NV][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -119,7 +114,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_gate_kernel(bnn_norm_g
       if (p.b) load8(v[i], static_cast<const E *>(p.b) + row * p.b_ld, c0 + i * T * 8, D);
     }
     if (p.b) {
-      unit_rows<T, NV>(v, p.post, c0, D, p.eps, mem);
+      unit_rows<BLOCK, NV>(v, p.post, c0, T, D, p.eps, mem);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int c = c0 + i * T * 8;
@@ -132,7 +127,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_gate_kernel(bnn_norm_g
       }
     }
     if (p.pre == BNN_NORM_NONE) continue;
-    unit_rows<T, NV>(r, p.pre, c0, D, p.eps, mem + 2 * (T / 64));
+    unit_rows<BLOCK, NV>(r, p.pre, c0, T, D, p.eps, mem + 32);
     uint32_t top = 0u;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -147,7 +142,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_gate_kernel(bnn_norm_g
       for (int j = 0; j < 8; ++j) top = max(top, magnitude(r[i][j]));
     }
     if (o.q) {
-      const RowScale s = row_scale(team_max_magnitude<T>(top, mem + 4 * (T / 64)));
+      const RowScale s = row_scale(team_max_magnitude<BLOCK>(top, mem + 64));
 #pragma unroll
       for (int i = 0; i < NV; ++i) store_q8(o.q + row * o.q_ld, c0 + i * T * 8, D, r[i], s.inv);
       if (t == 0) o.q_scale[row] = s.scale;
@@ -156,105 +151,215 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_gate_kernel(bnn_norm_g
 }
 
 // Teams walk through contiguous rows and keep the sums over rows in registers; the sums of all teams meet in
-// norm_gate_sums_kernel, in the same order at every call.
-template <class E, class R, int T, int NV>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_gate_backward_kernel(bnn_norm_gate_in p, NormGrad q) {
-  constexpr int TEAMS = T < 256 ? 256 / T : 1;
-  __shared__ uint32_t lds[2][8][T / 64];
-  const int worker = blockIdx.x * TEAMS + (TEAMS > 1 ? threadIdx.x / T : 0);
-  if (worker >= q.workers) return;  // whole waves; only teams of one wave share a workgroup
-  const int t = threadIdx.x % T, c0 = t * 8, D = p.D;
-  int64_t row, end;
+// norm_gate_sums_kernel, in the same order at every call.  A row's loads are in flight while the row before is worked on,
+// and its first sum is taken along with that row's last: between rms norms a row meets twice (8192 x 4096 bf16, a workgroup
+// a unit: 214 us without either, 173 with the loads ahead).  The vectors are in LDS, where there is room.  CENTRED: a norm
+// with a mean or a bias takes part.
+template <class E, class R, bool BLOCK, int MAXT, int NV, bool CENTRED>
+__global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_in p, NormGrad q) {
+  constexpr int WIDTH = (BLOCK ? MAXT : 64) * NV * 8;
+  constexpr bool NEAR = WIDTH <= 8192;
+  constexpr int SUMS = 6, MEM = 8 * 16;
+  __shared__ __attribute__((aligned(16))) uint32_t lds[2 * MEM];
+  __shared__ __attribute__((aligned(16))) float near_[3][NEAR ? WIDTH : 4];  // w_post, w_pre, res_scale
+  const int D = p.D;
+  if constexpr (NEAR) {
+    const float *from[3] = {p.w_post, p.w_pre, p.res_scale};
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      for (int c = threadIdx.x; c < WIDTH; c += blockDim.x) near_[k][c] = c >= D ? 0.0f : from[k] ? from[k][c] : 1.0f;
+  }
+  clear_words(lds);
+  const int T = BLOCK ? blockDim.x : 64, t = BLOCK ? threadIdx.x : threadIdx.x & 63, c0 = t * 8;
+  const int worker = BLOCK ? blockIdx.x : blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (worker >= q.workers) return;  // whole waves, of workgroups without barriers from here on
+  const auto vector = [&](float (&v)[8], int k, int i) {
+    if constexpr (NEAR) {
+      const float *from = &near_[k][c0 + i * T * 8];
+      const f32x4 lo = *reinterpret_cast<const f32x4 *>(from), hi = *reinterpret_cast<const f32x4 *>(from + 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
+    } else {
+      load8_or(v, k == 0 ? p.w_post : k == 1 ? p.w_pre : p.res_scale, c0 + i * T * 8, D, 1.0f);
+    }
+  };
+  const auto bias = [&](float (&v)[8], const float *from, int i) {
+    if (CENTRED) load8_or(v, from, c0 + i * T * 8, D, 0.0f);
+    else fill8(v, 0.0f);
+  };
+  int row, end;
   if (q.segments) {
-    const int64_t group = worker / q.segments, part = worker % q.segments;
-    row = group * p.gate_rows + part * q.per;
-    end = min(min(row + q.per, (group + 1) * p.gate_rows), p.rows);
+    const int group = worker / q.segments, part = worker % q.segments;
+    const int64_t first = group * p.gate_rows + (int64_t)part * q.per;
+    row = (int)min(first, p.rows);
+    end = (int)min(min(first + q.per, (group + 1) * p.gate_rows), p.rows);
   } else {
-    row = (int64_t)worker * q.per;
-    end = min(row + q.per, p.rows);
+    const int64_t first = (int64_t)worker * q.per;
+    row = (int)min(first, p.rows);
+    end = (int)min(first + q.per, p.rows);
   }
-  float w_post[NV][8], w_pre[NV][8], scale[NV][8], sum[6][NV][8];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    load8_or(w_post[i], p.w_post, c0 + i * T * 8, D, 1.0f);
-    load8_or(w_pre[i], p.w_pre, c0 + i * T * 8, D, 1.0f);
-    load8_or(scale[i], p.res_scale, c0 + i * T * 8, D, 1.0f);
-#pragma unroll
-    for (int k = 0; k < 6; ++k) fill8(sum[k][i], 0.0f);
-  }
-  int64_t left = p.gate_rows;  // of the group with this gate
-  for (int flip = 0; row < end; ++row, flip ^= 1) {
-    uint32_t *const mem = &lds[flip][0][0];
-    float b[NV][8], r[NV][8], e[NV][8], dr[NV][8], g[NV][8], pv[NV][8];
+  struct Raw {
+    Piece8<E> b[NV], dn[NV], g[NV];
+    Piece8<R> r[NV], dro[NV];
+  };
+  const auto request = [&](Raw &w, int row) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = c0 + i * T * 8;
-      load8(r[i], static_cast<const R *>(p.r) + row * p.r_ld, c, D);
-      load8_or(b[i], p.b ? static_cast<const E *>(p.b) + row * p.b_ld : nullptr, c, D, 0.0f);
-      load8_or(e[i], q.dn ? static_cast<const E *>(q.dn) + row * q.dn_ld : nullptr, c, D, 0.0f);
-      load8_or(dr[i], q.dr_out ? static_cast<const R *>(q.dr_out) + row * q.dr_out_ld : nullptr, c, D, 0.0f);
-      load8_or(g[i], p.gate ? static_cast<const E *>(p.gate) + norm_group(p, row) * p.gate_ld : nullptr, c, D, 1.0f);
+      w.r[i].load(static_cast<const R *>(p.r) + row * p.r_ld, c, D);
+      if (p.b) w.b[i].load(static_cast<const E *>(p.b) + row * p.b_ld, c, D);
+      else w.b[i].fill(0.0f);
+      if (q.dn) w.dn[i].load(static_cast<const E *>(q.dn) + row * q.dn_ld, c, D);
+      else w.dn[i].fill(0.0f);
+      if (q.dr_out) w.dro[i].load(static_cast<const R *>(q.dr_out) + row * q.dr_out_ld, c, D);
+      else w.dro[i].fill(0.0f);
+      if (p.gate) w.g[i].load(static_cast<const E *>(p.gate) + norm_group(p, row) * p.gate_ld, c, D);
+      else w.g[i].fill(1.0f);
     }
-    // forward again: b normed, p, r' normed
-    const float rsb = p.b ? unit_rows<T, NV>(b, p.post, c0, D, p.eps, mem) : 1.0f;
+  };
+  float sum[SUMS][NV][8];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      float bias[8];
-      load8_or(bias, p.bias_post, c0 + i * T * 8, D, 0.0f);
+  for (int k = 0; k < SUMS; ++k)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        pv[i][j] = b[i][j] * w_post[i][j] + bias[j];
-        if (p.b) r[i][j] += scale[i][j] * g[i][j] * pv[i][j];
-      }
-      zero_past(r[i], c0 + i * T * 8, D);
-    }
-    if (p.pre != BNN_NORM_NONE) {
-      const float rsr = unit_rows<T, NV>(r, p.pre, c0, D, p.eps, mem + 2 * (T / 64));
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          sum[0][i][j] = fmaf(e[i][j], r[i][j], sum[0][i][j]);
-          sum[1][i][j] += e[i][j];
-          e[i][j] *= w_pre[i][j];
-        }
-      unit_rows_backward<T, NV>(e, r, rsr, p.pre, D, mem + 4 * (T / 64));
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dr[i][j] += e[i][j];
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      zero_past(dr[i], c0 + i * T * 8, D);
-      store8(static_cast<R *>(q.dr) + row * q.dr_ld, c0 + i * T * 8, D, dr[i]);
-    }
-    if (!p.b) continue;
+    for (int i = 0; i < NV; ++i) fill8(sum[k][i], 0.0f);
+  int left = (int)p.gate_rows;  // of the group with this gate
+  // A row's first sum: of its squares, or (centred) of its values.
+  const auto values = [&](float (&v)[NV][8], const Raw &w) {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float along = dr[i][j] * pv[i][j], dp = dr[i][j] * scale[i][j] * g[i][j];
-        sum[2][i][j] = fmaf(dp, b[i][j], sum[2][i][j]);
-        sum[3][i][j] += dp;
-        sum[4][i][j] = fmaf(along, g[i][j], sum[4][i][j]);
-        sum[5][i][j] = fmaf(along, scale[i][j], sum[5][i][j]);
-        e[i][j] = dp * w_post[i][j];
-      }
-    unit_rows_backward<T, NV>(e, b, rsb, p.post, D, mem + 6 * (T / 64));
+      for (int j = 0; j < 8; ++j) v[i][j] = (float)w.b[i].v[j];
+  };
+  const bool layer_post = CENTRED && p.post == BNN_NORM_LAYER, layer_pre = CENTRED && p.pre == BNN_NORM_LAYER;
+  const auto first_sum = [&](const float (&v)[NV][8]) { return layer_post ? sum_of(v) : dot_of(v, v); };
+  Raw w;
+  float b[NV][8], opening = 0.0f;  // of the row at hand
+  if (row < end) {
+    request(w, row);
+    values(b, w);
+    opening = team_sum<BLOCK>(first_sum(b), lds + MEM);
+  }
+  for (int flip = 0; row < end; ++row, flip ^= 1) {
+    uint32_t *const mem = lds + flip * MEM;
+    Raw ahead = w;
+    if (row + 1 < end) request(ahead, row + 1);
+    float r[NV][8], e[NV][8], v[8], m[8];
+    // forward again: b normed, r' normed
+    values(b, w);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) store8(static_cast<E *>(q.db) + row * q.db_ld, c0 + i * T * 8, D, e[i]);
-    if (q.dgate && !q.segments && (--left == 0 || row + 1 == end)) {
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r[i][j] = (float)w.r[i].v[j], e[i][j] = (float)w.dn[i].v[j];
+    float rsb = 1.0f;
+    if (p.post != BNN_NORM_NONE) {
+      float squares = opening;
+      if (layer_post) {
+        centre_rows<BLOCK, NV>(b, opening / (float)D, c0, T, D);
+        squares = team_sum<BLOCK>(dot_of(b, b), mem);
+      }
+      rsb = row_factor(squares, D, p.eps);
+      times(b, rsb);
+    }
+    const auto block = [&](float (&pv)[8], int i) {  // p of this row
+      float add[8];
+      vector(pv, 0, i);
+      bias(add, p.bias_post, i);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) pv[j] = b[i][j] * pv[j] + add[j];
+    };
+    if (p.b) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        store8(static_cast<E *>(q.dgate) + norm_group(p, row) * q.dgate_ld, c0 + i * T * 8, D, sum[5][i]);
-        fill8(sum[5][i], 0.0f);
+        block(v, i);
+        vector(m, 2, i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[i][j] += m[j] * (float)w.g[i].v[j] * v[j];
+        zero_past(r[i], c0 + i * T * 8, D);
       }
-      left = p.gate_rows;
     }
+    // gradient through the norm of r': rs (e - mean(e) - u mean(e u)), u the normed values, the first mean if centred
+    if (p.pre != BNN_NORM_NONE) {
+      if (layer_pre) centre_rows<BLOCK, NV>(r, team_sum<BLOCK>(sum_of(r), mem + 16) / (float)D, c0, T, D);
+      float s[3] = {dot_of(r, r), 0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        vector(v, 1, i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float ew = e[i][j] * v[j];
+          s[1] = fmaf(ew, r[i][j], s[1]);
+          if (CENTRED) s[2] += ew;
+        }
+      }
+      team_sum<BLOCK>(s, mem + 32);
+      const float rsr = row_factor(s[0], D, p.eps), along = s[1] * rsr / (float)D, level = layer_pre ? s[2] / (float)D : 0.0f;
+      times(r, rsr);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        vector(v, 1, i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          sum[0][i][j] = fmaf(e[i][j], r[i][j], sum[0][i][j]);
+          if (CENTRED) sum[1][i][j] += e[i][j];
+          e[i][j] = rsr * (e[i][j] * v[j] - level - r[i][j] * along);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) fill8(e[i], 0.0f);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {  // r from here on: the gradient of r'
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r[i][j] = (float)w.dro[i].v[j] + e[i][j];
+      zero_past(r[i], c0 + i * T * 8, D);
+      store8(static_cast<R *>(q.dr) + row * q.dr_ld, c0 + i * T * 8, D, r[i]);
+    }
+    if (p.b) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        block(v, i);
+        vector(m, 2, i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float g = (float)w.g[i].v[j], along = r[i][j] * v[j], dp = r[i][j] * m[j] * g;
+          sum[2][i][j] = fmaf(dp, b[i][j], sum[2][i][j]);
+          if (CENTRED) sum[3][i][j] += dp;
+          sum[4][i][j] = fmaf(along, g, sum[4][i][j]);
+          sum[5][i][j] = fmaf(along, m[j], sum[5][i][j]);
+          e[i][j] = dp;
+        }
+        vector(v, 0, i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[i][j] *= v[j];
+      }
+      float next[NV][8];
+      values(next, ahead);
+      float s[3] = {dot_of(e, b), first_sum(next), CENTRED ? sum_of(e) : 0.0f};
+      team_sum<BLOCK>(s, mem + 80);
+      opening = s[1];
+      if (p.post != BNN_NORM_NONE) {
+        const float along = s[0] / (float)D, level = layer_post ? s[2] / (float)D : 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) e[i][j] = rsb * (e[i][j] - level - b[i][j] * along);
+      }
+#pragma unroll
+      for (int i = 0; i < NV; ++i) store8(static_cast<E *>(q.db) + row * q.db_ld, c0 + i * T * 8, D, e[i]);
+      if (q.dgate && !q.segments && (--left == 0 || row + 1 == end)) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          store8(static_cast<E *>(q.dgate) + norm_group(p, row) * q.dgate_ld, c0 + i * T * 8, D, sum[5][i]);
+          fill8(sum[5][i], 0.0f);
+        }
+        left = (int)p.gate_rows;
+      }
+    }
+    w = ahead;
   }
 #pragma unroll
-  for (int k = 0; k < 6; ++k)
+  for (int k = 0; k < SUMS; ++k)
     if (q.want >> k & 1)
 #pragma unroll
       for (int i = 0; i < NV; ++i) store8(q.part + ((int64_t)k * q.workers + worker) * D, c0 + i * T * 8, D, sum[k][i]);
@@ -277,8 +382,16 @@ __global__ __launch_bounds__(1024) void norm_gate_sums_kernel(NormSums q) {
   const int first = which < 5 ? 0 : (which - 5) * q.segments, last = which < 5 ? q.workers : first + q.segments;
   const float *part = q.part + (int64_t)min(which, 5) * q.workers * q.D;
   float sum = 0.0f;
-  if (c < q.D)
-    for (int w = first + wave; w < last; w += 16) sum += part[(int64_t)w * q.D + c];
+  if (c < q.D) {
+    int w = first + wave;
+    for (; w + 48 < last; w += 64) {  // four in flight
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = part[(int64_t)(w + 16 * i) * q.D + c];
+      sum += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    for (; w < last; w += 16) sum += part[(int64_t)w * q.D + c];
+  }
   lds[wave][lane] = sum;
   __syncthreads();
   if (wave || c >= q.D) return;
@@ -297,7 +410,7 @@ struct NormPlan {
 // About as many teams as the card has room for; each takes contiguous rows, of one group where a gate is shared by more rows
 // than that, else of whole groups.
 inline NormPlan norm_plan(int64_t rows, int D, int64_t gate_rows) {
-  const int64_t room = D <= 512 ? 2048 : D <= 2048 ? 1024 : 512;
+  const int64_t waves = (D + 511) / 512, room = 256 * std::max<int64_t>(1, 12 / waves);  // three waves a SIMD have room
   int64_t per = (rows - 1) / room + 1;
   if (gate_rows > rows) gate_rows = rows;
   if (gate_rows > per) {
@@ -308,21 +421,14 @@ inline NormPlan norm_plan(int64_t rows, int D, int64_t gate_rows) {
   return {(int)((rows - 1) / per + 1), (int)per, 0};
 }
 
-// f with the element types and the team as tags.
+// f with the element types as tags.
 template <class F>
 void with_norm(const bnn_norm_gate_in &p, const F &f) {
-  const auto widths = [&](auto e, auto r) {
-    if (p.D <= 512) f(e, r, std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
-    else if (p.D <= 2048) f(e, r, std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
-    else if (p.D <= 4096) f(e, r, std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
-    else if (p.D <= 8192) f(e, r, std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
-    else f(e, r, std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
-  };
-  if (p.type == BNN_F32) widths(Float<BNN_F32>(), Float<BNN_F32>());
-  else if (p.type == BNN_BF16 && p.r_type == BNN_F32) widths(Float<BNN_BF16>(), Float<BNN_F32>());
-  else if (p.type == BNN_BF16) widths(Float<BNN_BF16>(), Float<BNN_BF16>());
-  else if (p.r_type == BNN_F32) widths(Float<BNN_F16>(), Float<BNN_F32>());
-  else widths(Float<BNN_F16>(), Float<BNN_F16>());
+  if (p.type == BNN_F32) f(0.0f, 0.0f);
+  else if (p.type == BNN_BF16 && p.r_type == BNN_F32) f((__bf16)0.0f, 0.0f);
+  else if (p.type == BNN_BF16) f((__bf16)0.0f, (__bf16)0.0f);
+  else if (p.r_type == BNN_F32) f((_Float16)0.0f, 0.0f);
+  else f((_Float16)0.0f, (_Float16)0.0f);
 }
 
 inline bool norm_known(int n) { return n >= BNN_NORM_NONE && n <= BNN_NORM_LAYER; }
@@ -368,11 +474,17 @@ extern "C" bnn_status bnn_norm_gate(const bnn_norm_gate_in *in, void *r_out, int
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bnn_norm_gate_in in_groups = cut_groups(p);
   ProfScope ps(KID_NORM_GATE, s);
-  with_norm(p, [&](auto e, auto r, auto threads, auto pieces) {
-    constexpr int T = decltype(threads)::value, NV = decltype(pieces)::value, BLOCK = T < 256 ? 256 : T, TEAMS = BLOCK / T;
-    const int64_t room = 256 * (2048 / BLOCK);  // workgroups that run at once
-    const uint32_t grid = (uint32_t)std::min<int64_t>((p.rows - 1) / TEAMS + 1, room);
-    norm_gate_kernel<typename decltype(e)::type, typename decltype(r)::type, T, NV><<<grid, BLOCK, 0, s>>>(in_groups, o, (int)grid * TEAMS);
+  with_norm(p, [&](auto e, auto r) {
+    using E = decltype(e);
+    using R = decltype(r);
+    const auto run = [&](auto kernel, int block, int teams) {  // as many workgroups as run at once, at most
+      const uint32_t grid = (uint32_t)std::min<int64_t>((p.rows - 1) / teams + 1, 256 * (2048 / block));
+      kernel<<<grid, block, 0, s>>>(in_groups, o, (int)grid * teams);
+    };
+    if (p.D <= 512) run(norm_gate_kernel<E, R, false, 256, 1>, 256, 4);
+    else if (p.D <= 4096) run(norm_gate_kernel<E, R, true, 512, 1>, row_threads(p.D, 1), 1);
+    else if (p.D <= 8192) run(norm_gate_kernel<E, R, true, 1024, 1>, row_threads(p.D, 1), 1);
+    else run(norm_gate_kernel<E, R, true, 1024, 2>, row_threads(p.D, 2), 1);
   });
   return launch_status();
 }
@@ -417,10 +529,20 @@ extern "C" bnn_status bnn_norm_gate_backward(const bnn_norm_gate_in *in, const v
     q.part = static_cast<float *>(workspace);
     const bnn_norm_gate_in in_groups = cut_groups(p);
     ProfScope ps(KID_NORM_GATE_BACKWARD, s);
-    with_norm(p, [&](auto e, auto r, auto threads, auto pieces) {
-      constexpr int T = decltype(threads)::value, NV = decltype(pieces)::value, BLOCK = T < 256 ? 256 : T, TEAMS = BLOCK / T;
-      norm_gate_backward_kernel<typename decltype(e)::type, typename decltype(r)::type, T, NV>
-          <<<(uint32_t)((plan.workers - 1) / TEAMS + 1), BLOCK, 0, s>>>(in_groups, q);
+    const bool centred = p.post == BNN_NORM_LAYER || p.pre == BNN_NORM_LAYER || p.bias_post || p.bias_pre;
+    with_norm(p, [&](auto e, auto r) {
+      using E = decltype(e);
+      using R = decltype(r);
+      const auto run = [&](auto plain, auto with_means, int block, int teams) {
+        (centred ? with_means : plain)<<<(uint32_t)((plan.workers - 1) / teams + 1), block, 0, s>>>(in_groups, q);
+      };
+      if (p.D <= 512) run(norm_gate_backward_kernel<E, R, false, 256, 1, false>, norm_gate_backward_kernel<E, R, false, 256, 1, true>, 256, 4);
+      else if (p.D <= 4096)
+        run(norm_gate_backward_kernel<E, R, true, 512, 1, false>, norm_gate_backward_kernel<E, R, true, 512, 1, true>, row_threads(p.D, 1), 1);
+      else if (p.D <= 8192)
+        run(norm_gate_backward_kernel<E, R, true, 512, 2, false>, norm_gate_backward_kernel<E, R, true, 512, 2, true>, row_threads(p.D, 2), 1);
+      else
+        run(norm_gate_backward_kernel<E, R, true, 1024, 2, false>, norm_gate_backward_kernel<E, R, true, 1024, 2, true>, row_threads(p.D, 2), 1);
     });
     if (bnn_status st = launch_status()) return st;
   } else if (!q.want) {

@@ -12,15 +12,16 @@ struct QuantParams {
   int K;
 };
 
-// T threads a row, NV pieces of eight values a thread, held in registers between the maximum and the rounding.
-// NV 0: rows of any length, read twice.
-template <class E, int T, int NV>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void quant_rows_kernel(QuantParams p) {
-  constexpr int TEAMS = T < 256 ? 256 / T : 1;
-  __shared__ uint32_t lds[T / 64];
-  const int64_t row = (int64_t)blockIdx.x * TEAMS + (TEAMS > 1 ? threadIdx.x / T : 0);
-  if (row >= p.rows) return;  // whole waves; only teams of one wave share a workgroup
-  const int t = threadIdx.x % T;
+// A row a wave (four of them a workgroup), or (BLOCK) a row a workgroup; NV pieces of eight values a thread, held in
+// registers between the maximum and the rounding.  NV 0: rows of any length, read twice.  Bound by memory (8192 x 4096
+// bf16 20 us, 5.0 TB/s).
+template <class E, bool BLOCK, int MAXT, int NV>
+__global__ __launch_bounds__(MAXT) void quant_rows_kernel(QuantParams p) {
+  __shared__ uint32_t lds[16];
+  if constexpr (BLOCK) clear_words(lds);
+  const int T = BLOCK ? blockDim.x : 64, t = BLOCK ? threadIdx.x : threadIdx.x & 63;
+  const int64_t row = BLOCK ? blockIdx.x : blockIdx.x * 4ll + (threadIdx.x >> 6);
+  if (row >= p.rows) return;  // whole waves, of workgroups without barriers
   const E *x = static_cast<const E *>(p.x) + row * p.x_ld;
   int8_t *q = p.q + row * p.q_ld;
   uint32_t top = 0u;
@@ -32,7 +33,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void quant_rows_kernel(QuantPara
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[i][j]));
-    const RowScale s = row_scale(team_max_magnitude<T>(top, lds));
+    const RowScale s = row_scale(team_max_magnitude<BLOCK>(top, lds));
 #pragma unroll
     for (int i = 0; i < NV; ++i) store_q8(q, (i * T + t) * 8, p.K, v[i], s.inv);
     if (t == 0) p.scale[row] = s.scale;
@@ -43,7 +44,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void quant_rows_kernel(QuantPara
 #pragma unroll
       for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[j]));
     }
-    const RowScale s = row_scale(team_max_magnitude<T>(top, lds));
+    const RowScale s = row_scale(team_max_magnitude<BLOCK>(top, lds));
     for (int c = t * 8; c < p.K; c += T * 8) {
       float v[8];
       load8(v, x, c, p.K);
@@ -51,12 +52,6 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void quant_rows_kernel(QuantPara
     }
     if (t == 0) p.scale[row] = s.scale;
   }
-}
-
-template <class E, int T, int NV>
-void launch_quant(const QuantParams &p, hipStream_t s) {
-  constexpr int TEAMS = T < 256 ? 256 / T : 1;
-  quant_rows_kernel<E, T, NV><<<(uint32_t)((p.rows - 1) / TEAMS + 1), T < 256 ? 256 : T, 0, s>>>(p);
 }
 
 }  // namespace bnn
@@ -75,11 +70,11 @@ extern "C" bnn_status bnn_quant_rows_i8(const void *x, int type, int64_t rows, i
   ProfScope ps(KID_QUANT_ROWS, s);
   with_float(type, [&](auto tag) {
     using E = typename decltype(tag)::type;
-    if (K <= 512) launch_quant<E, 64, 1>(p, s);
-    else if (K <= 2048) launch_quant<E, 256, 1>(p, s);
-    else if (K <= 8192) launch_quant<E, 256, 4>(p, s);
-    else if (K <= 32768) launch_quant<E, 1024, 4>(p, s);
-    else launch_quant<E, 1024, 0>(p, s);
+    const uint32_t n = (uint32_t)rows;
+    if (K <= 512) quant_rows_kernel<E, false, 256, 1><<<(n - 1) / 4 + 1, 256, 0, s>>>(p);
+    else if (K <= 4096) quant_rows_kernel<E, true, 512, 1><<<n, row_threads(K, 1), 0, s>>>(p);
+    else if (K <= 32768) quant_rows_kernel<E, true, 1024, 4><<<n, row_threads(K, 4), 0, s>>>(p);
+    else quant_rows_kernel<E, true, 1024, 0><<<n, 1024, 0, s>>>(p);
   });
   return launch_status();
 }

@@ -30,6 +30,32 @@ __device__ __forceinline__ void load8(float (&v)[8], const E *row, int c, int D)
   }
 }
 
+// The same eight values as they lie, for rows that are requested before they are needed.
+template <class E>
+struct Piece8 {
+  typedef E E8 __attribute__((ext_vector_type(8)));
+  E8 v;
+  __device__ __forceinline__ void load(const E *row, int c, int D) {
+    if (c + 8 <= D) {
+      if constexpr (sizeof(E) == 4) {
+        typedef E E4 __attribute__((ext_vector_type(4)));
+        const auto lo = __builtin_bit_cast(E4, *reinterpret_cast<const u32x4_row *>(row + c));
+        const auto hi = __builtin_bit_cast(E4, *reinterpret_cast<const u32x4_row *>(row + c + 4));
+        v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      } else {
+        v = __builtin_bit_cast(E8, *reinterpret_cast<const u32x4_row *>(row + c));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = c + i < D ? row[c + i] : (E)0.0f;
+    }
+  }
+  __device__ __forceinline__ void fill(float x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (E)x;
+  }
+};
+
 template <class E>
 __device__ __forceinline__ void store8(E *row, int c, int D, const float (&v)[8]) {
   typedef E E8 __attribute__((ext_vector_type(8)));
@@ -51,32 +77,75 @@ __device__ __forceinline__ void store8(E *row, int c, int D, const float (&v)[8]
   }
 }
 
-// Sum or maximum over a team of T threads (a wave, or a whole workgroup), the same order at every call.  `lds` holds
-// T / 64 values and is not used by another reduction that threads could still be reading.
-template <int T, class Op>
-__device__ __forceinline__ uint32_t team_reduce(uint32_t x, uint32_t *lds, const Op &op) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) x = op(x, (uint32_t)__shfl_xor((int)x, d));
-  if constexpr (T > 64) {
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = lds[0];
-#pragma unroll
-    for (int w = 1; w < T / 64; ++w) x = op(x, lds[w]);
-  }
-  return x;
+// Sums and maxima over a team: one wave, or (BLOCK) all waves of a workgroup, the same order at every call.  Within a wave
+// by lane exchanges of the vector unit: rows of 16 lanes, then the rows, the result from the last lane.  0 is neutral.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t other_lane(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
 }
-template <int T>
+template <class Op>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t x, const Op &op) {
+  x = op(x, other_lane<0x111, 0xf>(x));
+  x = op(x, other_lane<0x112, 0xf>(x));
+  x = op(x, other_lane<0x114, 0xf>(x));
+  x = op(x, other_lane<0x118, 0xf>(x));
+  x = op(x, other_lane<0x142, 0xa>(x));
+  x = op(x, other_lane<0x143, 0xc>(x));
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+// V values at once.  lds: V * 16 words that no other reduction uses that threads could still be reading; words of waves
+// that the workgroup does not have are 0 (clear_words).
+template <bool BLOCK, int V, class Op>
+__device__ __forceinline__ void team_reduce(uint32_t (&x)[V], uint32_t *lds, const Op &op) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) x[k] = wave_reduce(x[k], op);
+  if constexpr (BLOCK) {
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int k = 0; k < V; ++k) lds[k * 16 + (threadIdx.x >> 6)] = x[k];
+    __syncthreads();
+    typedef uint32_t Words __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      x[k] = 0u;
+      for (int w = 0; w < (int)(blockDim.x >> 6); w += 4) {
+        const Words v = *reinterpret_cast<const Words *>(lds + k * 16 + w);
+        x[k] = op(x[k], op(op(v[0], v[1]), op(v[2], v[3])));
+      }
+    }
+  }
+}
+template <bool BLOCK, int V>
+__device__ __forceinline__ void team_sum(float (&x)[V], uint32_t *lds) {
+  uint32_t u[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) u[k] = __float_as_uint(x[k]);
+  team_reduce<BLOCK>(u, lds, [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); });
+#pragma unroll
+  for (int k = 0; k < V; ++k) x[k] = __uint_as_float(u[k]);
+}
+template <bool BLOCK>
 __device__ __forceinline__ float team_sum(float x, uint32_t *lds) {
-  return __uint_as_float(team_reduce<T>(__float_as_uint(x), lds, [](uint32_t a, uint32_t b) {
-    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
-  }));
+  float v[1] = {x};
+  team_sum<BLOCK>(v, lds);
+  return v[0];
 }
 // Of magnitudes, as bit patterns: a NaN is larger than infinity, and stays.
-template <int T>
+template <bool BLOCK>
 __device__ __forceinline__ float team_max_magnitude(uint32_t bits, uint32_t *lds) {
-  return __uint_as_float(team_reduce<T>(bits, lds, [](uint32_t a, uint32_t b) { return a > b ? a : b; }));
+  uint32_t v[1] = {bits};
+  team_reduce<BLOCK>(v, lds, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+  return __uint_as_float(v[0]);
 }
+template <int N>
+__device__ __forceinline__ void clear_words(uint32_t (&lds)[N]) {
+  for (int i = threadIdx.x; i < N; i += blockDim.x) lds[i] = 0u;
+  __syncthreads();
+}
+
+// Threads a row of D values, NV pieces of eight each: whole waves.
+inline int row_threads(int64_t D, int NV) { return (int)((D + 8ll * NV * 64 - 1) / (8ll * NV * 64)) * 64; }
+
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
 // A row's 8-bit form: s = a / 127 and q = rint(x * (127 / a)) with a the row's largest magnitude, both quotients

@@ -29,9 +29,17 @@ struct Library {
   decltype(&bnn_conv2d_f32) f32;
   decltype(&bnn_maxpool2x2) maxpool;
   decltype(&bnn_fc_f32) fc;
+  decltype(&bnn_quant_rows_i8) quant;
+  decltype(&bnn_linear_i8) linear;
+  decltype(&bnn_norm_gate) norm;
+  decltype(&bnn_norm_gate_backward) norm_backward;
+  decltype(&bnn_gated_ff) gated;
+  decltype(&bnn_gated_ff_i8) gated_i8;
+  decltype(&bnn_gated_ff_backward) gated_backward;
 };
 constexpr const char *names[] = {"bnn_xnor_gemm", "bnn_xnor_gemm_epilogue", "bnn_encode", "bnn_conv2d", "bnn_conv2d_packed",
-                                 "bnn_im2col_packed", "bnn_conv2d_f32_sign", "bnn_conv2d_f32", "bnn_maxpool2x2", "bnn_fc_f32"};
+                                 "bnn_im2col_packed", "bnn_conv2d_f32_sign", "bnn_conv2d_f32", "bnn_maxpool2x2", "bnn_fc_f32", "bnn_quant_rows_i8", "bnn_linear_i8",
+                                 "bnn_norm_gate", "bnn_norm_gate_backward", "bnn_gated_ff", "bnn_gated_ff_i8", "bnn_gated_ff_backward"};
 Library lib = {};
 
 struct Other {};  // not the plain case
@@ -64,6 +72,18 @@ class Args {
       return nullptr;
     }
     return tensor().data_ptr();
+  }
+  const at::Tensor *tensor_or_none() {
+    if (*a_ == Py_None) {
+      ++a_;
+      return nullptr;
+    }
+    return &tensor();
+  }
+  float real() {
+    PyObject *o = *a_++;
+    if (!PyFloat_CheckExact(o)) throw Other();
+    return (float)PyFloat_AS_DOUBLE(o);
   }
   int64_t integer() { return integer(*a_++); }
   int small() { return as_int(integer()); }
@@ -288,6 +308,183 @@ PyObject *fc(PyObject *, PyObject *const *a, Py_ssize_t n) {  // x, w, bias, sig
   });
 }
 
+// ---- 8-bit and gated layers: matrices with rows of consecutive values, of given sizes and types, as the binding's checks ask ----
+struct Matrix {
+  char *p = nullptr;
+  int64_t ld = 0, rows = 0, cols = 0;
+};
+Matrix matrix(const at::Tensor &t, at::ScalarType type) {
+  if (!t.is_cuda() || t.scalar_type() != type || t.dim() != 2) throw Other();
+  Matrix m;
+  m.rows = t.size(0), m.cols = t.size(1);
+  if (m.cols > 1 && t.stride(1) != 1) throw Other();
+  m.ld = m.rows > 1 ? t.stride(0) : std::max(m.cols, t.stride(0));
+  m.p = static_cast<char *>(t.data_ptr());
+  return m;
+}
+Matrix matrix(const at::Tensor &t, at::ScalarType type, int64_t rows, int64_t cols) {
+  const Matrix m = matrix(t, type);
+  if (m.rows != rows || m.cols != cols) throw Other();
+  return m;
+}
+Matrix matrix(const at::Tensor *t, at::ScalarType type, int64_t rows, int64_t cols) {
+  return t ? matrix(*t, type, rows, cols) : Matrix();
+}
+float *vector(const at::Tensor *t, int64_t n) {
+  if (!t) return nullptr;
+  if (!t->is_cuda() || t->scalar_type() != kFloat || t->dim() != 1 || t->size(0) != n || (n > 1 && t->stride(0) != 1)) throw Other();
+  return f32(t->data_ptr());
+}
+int float_type(at::ScalarType t) {
+  if (t == kFloat) return BNN_F32;
+  if (t == at::kBFloat16) return BNN_BF16;
+  if (t == at::kHalf) return BNN_F16;
+  throw Other();
+}
+int8_t *i8(const Matrix &m) { return reinterpret_cast<int8_t *>(m.p); }
+using at::kChar;
+
+PyObject *quant_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {  // x, q, scale
+  return guarded(a, n, 3, [](Args &v) {
+    const at::Tensor &t = v.tensor();
+    const int type = float_type(t.scalar_type());
+    const Matrix x = matrix(t, t.scalar_type()), q = matrix(v.tensor(), kChar, x.rows, x.cols);
+    float *const scale = vector(&v.tensor(), x.rows);
+    return launch([&](void *s) { return lib.quant(x.p, type, x.rows, x.cols, x.ld, i8(q), q.ld, scale, s); });
+  });
+}
+
+PyObject *linear_i8(PyObject *, PyObject *const *args, Py_ssize_t n) {  // a, a_scale, b, b_scale, bias, out
+  return guarded(args, n, 6, [](Args &v) {
+    const Matrix a = matrix(v.tensor(), kChar);
+    const float *const sa = vector(&v.tensor(), a.rows);
+    const Matrix b = matrix(v.tensor(), kChar);
+    const float *const sb = vector(&v.tensor(), b.rows), *const bias = vector(v.tensor_or_none(), b.rows);
+    const at::Tensor &out = v.tensor();
+    const Matrix y = matrix(out, out.scalar_type(), a.rows, b.rows);
+    if (b.cols != a.cols) throw Other();
+    const int type = float_type(out.scalar_type());
+    return launch([&](void *s) { return lib.linear(i8(a), a.ld, sa, i8(b), b.ld, sb, bias, a.rows, b.rows, a.cols, y.p, type, y.ld, s); });
+  });
+}
+
+// b, r, gate, gate_rows, res_scale, w_post, bias_post, w_pre, bias_pre, post, pre, eps
+bnn_norm_gate_in norm_in(Args &v, at::ScalarType &type, at::ScalarType &r_type) {
+  const at::Tensor *const b = v.tensor_or_none();
+  const at::Tensor &r = v.tensor();
+  const at::Tensor *const gate = v.tensor_or_none();
+  const int64_t gate_rows = v.integer();
+  r_type = r.scalar_type();
+  type = b ? b->scalar_type() : r_type;
+  const Matrix mr = matrix(r, r_type), mb = matrix(b, type, mr.rows, mr.cols);
+  if (gate && gate_rows < 1) throw Other();
+  const Matrix mg = matrix(gate, type, gate ? (mr.rows - 1) / gate_rows + 1 : 0, mr.cols);
+  if (mr.rows < 1 || mr.cols > (1 << 30)) throw Other();
+  bnn_norm_gate_in in = {};
+  in.rows = mr.rows, in.D = (int)mr.cols;
+  in.type = float_type(type), in.r_type = float_type(r_type);
+  in.b = mb.p, in.b_ld = mb.ld, in.r = mr.p, in.r_ld = mr.ld, in.gate = mg.p, in.gate_ld = mg.ld, in.gate_rows = gate ? gate_rows : 0;
+  const float **const vectors[] = {&in.res_scale, &in.w_post, &in.bias_post, &in.w_pre, &in.bias_pre};
+  for (const float **to : vectors) *to = vector(v.tensor_or_none(), mr.cols);
+  in.post = v.small(), in.pre = v.small();
+  in.eps = v.real();
+  return in;
+}
+
+PyObject *norm_gate(PyObject *, PyObject *const *a, Py_ssize_t n) {  // norm_in's, r_out, n_out, q_out, q_scale
+  return guarded(a, n, 16, [](Args &v) {
+    at::ScalarType type, r_type;
+    const bnn_norm_gate_in in = norm_in(v, type, r_type);
+    const Matrix r = matrix(v.tensor_or_none(), r_type, in.rows, in.D), out = matrix(v.tensor_or_none(), type, in.rows, in.D),
+                 q = matrix(v.tensor_or_none(), kChar, in.rows, in.D);
+    float *const scale = vector(v.tensor_or_none(), in.rows);
+    return launch([&](void *s) { return lib.norm(&in, r.p, r.ld, out.p, out.ld, i8(q), q.ld, scale, s); });
+  });
+}
+
+// norm_in's, dn, dr_out, dr, db, dgate, dres_scale, dw_post, dbias_post, dw_pre, dbias_pre, workspace
+PyObject *norm_gate_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 23, [](Args &v) {
+    at::ScalarType type, r_type;
+    const bnn_norm_gate_in in = norm_in(v, type, r_type);
+    const Matrix dn = matrix(v.tensor_or_none(), type, in.rows, in.D), dro = matrix(v.tensor_or_none(), r_type, in.rows, in.D),
+                 dr = matrix(v.tensor(), r_type, in.rows, in.D), db = matrix(v.tensor_or_none(), type, in.rows, in.D),
+                 dg = matrix(v.tensor_or_none(), type, in.gate ? (in.rows - 1) / in.gate_rows + 1 : 0, in.D);
+    float *sums[5];
+    for (float *&p : sums) p = vector(v.tensor_or_none(), in.D);
+    const at::Tensor &ws = v.tensor();
+    void *const pws = ws.data_ptr();
+    const size_t nws = (size_t)ws.numel() * ws.element_size();
+    return launch([&](void *s) {
+      return lib.norm_backward(&in, dn.p, dn.ld, dro.p, dro.ld, dr.p, dr.ld, db.p, db.ld, dg.p, dg.ld, sums[0], sums[1], sums[2], sums[3],
+                               sums[4], pws, nws, s);
+    });
+  });
+}
+
+float *saved_of(const at::Tensor *t, int64_t T, int64_t F) {
+  if (!t) return nullptr;
+  if (!t->is_cuda() || t->scalar_type() != kFloat || t->dim() != 3 || t->size(0) != 2 || t->size(1) != T || t->size(2) != F || !t->is_contiguous())
+    throw Other();
+  return f32(t->data_ptr());
+}
+
+PyObject *gated_ff(PyObject *, PyObject *const *a, Py_ssize_t n) {  // x, wg, wu, act, out, saved
+  return guarded(a, n, 6, [](Args &v) {
+    const at::Tensor &t = v.tensor();
+    const at::ScalarType type = t.scalar_type();
+    const Matrix x = matrix(t, type), wg = matrix(v.tensor(), type);
+    if (wg.cols != x.cols) throw Other();
+    const Matrix wu = matrix(v.tensor(), type, wg.rows, x.cols);
+    const int act = v.small();
+    const Matrix h = matrix(v.tensor(), type, x.rows, wg.rows);
+    float *const saved = saved_of(v.tensor_or_none(), x.rows, wg.rows);
+    const int code = float_type(type);
+    return launch([&](void *s) { return lib.gated(x.p, x.ld, wg.p, wg.ld, wu.p, wu.ld, code, x.rows, x.cols, wg.rows, act, h.p, h.ld, saved, s); });
+  });
+}
+
+PyObject *gated_ff_i8(PyObject *, PyObject *const *a, Py_ssize_t n) {  // x, x_scale, wg, wg_scale, wu, wu_scale, act, out
+  return guarded(a, n, 8, [](Args &v) {
+    const Matrix x = matrix(v.tensor(), kChar);
+    const float *const sx = vector(&v.tensor(), x.rows);
+    const Matrix wg = matrix(v.tensor(), kChar);
+    const float *const sg = vector(&v.tensor(), wg.rows);
+    if (wg.cols != x.cols) throw Other();
+    const Matrix wu = matrix(v.tensor(), kChar, wg.rows, x.cols);
+    const float *const su = vector(&v.tensor(), wg.rows);
+    const int act = v.small();
+    const at::Tensor &out = v.tensor();
+    const Matrix h = matrix(out, out.scalar_type(), x.rows, wg.rows);
+    const int code = float_type(out.scalar_type());
+    return launch([&](void *s) {
+      return lib.gated_i8(i8(x), x.ld, sx, i8(wg), wg.ld, sg, i8(wu), wu.ld, su, x.rows, x.cols, wg.rows, act, h.p, code, h.ld, s);
+    });
+  });
+}
+
+PyObject *gated_ff_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {  // x, wg, wu, saved, dh, dx, dwg, dwu, workspace
+  return guarded(a, n, 9, [](Args &v) {
+    const at::Tensor &t = v.tensor();
+    const at::ScalarType type = t.scalar_type();
+    const Matrix x = matrix(t, type), wg = matrix(v.tensor(), type);
+    if (wg.cols != x.cols) throw Other();
+    const int64_t T = x.rows, D = x.cols, F = wg.rows;
+    const Matrix wu = matrix(v.tensor(), type, F, D);
+    const float *const saved = saved_of(&v.tensor(), T, F);
+    const Matrix dh = matrix(v.tensor(), type, T, F), dx = matrix(v.tensor(), type, T, D), dwg = matrix(v.tensor(), type, F, D),
+                 dwu = matrix(v.tensor(), type, F, D);
+    const at::Tensor &ws = v.tensor();
+    void *const pws = ws.data_ptr();
+    const size_t nws = (size_t)ws.numel() * ws.element_size();
+    const int code = float_type(type);
+    return launch([&](void *s) {
+      return lib.gated_backward(x.p, x.ld, wg.p, wg.ld, wu.p, wu.ld, code, T, D, F, saved, dh.p, dh.ld, dx.p, dx.ld, dwg.p, dwg.ld, dwu.p,
+                                dwu.ld, pws, nws, s);
+    });
+  });
+}
+
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
   constexpr Py_ssize_t want = sizeof(Library) / sizeof(void *);
   static_assert(want == sizeof(names) / sizeof(names[0]), "an address for every name");
@@ -310,7 +507,9 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
 #define BNN_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {BNN_METHOD(bind), BNN_METHOD(gemm), BNN_METHOD(epilogue), BNN_METHOD(encode), BNN_METHOD(conv2d),
                          BNN_METHOD(conv2d_packed), BNN_METHOD(im2col), BNN_METHOD(f32_sign), BNN_METHOD(conv2d_f32),
-                         BNN_METHOD(maxpool), BNN_METHOD(fc), {nullptr, nullptr, 0, nullptr}};
+                         BNN_METHOD(maxpool), BNN_METHOD(fc), BNN_METHOD(quant_rows), BNN_METHOD(linear_i8),
+                         BNN_METHOD(norm_gate), BNN_METHOD(norm_gate_backward), BNN_METHOD(gated_ff), BNN_METHOD(gated_ff_i8),
+                         BNN_METHOD(gated_ff_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensorcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
