@@ -315,7 +315,7 @@ typedef enum { BNN_ACT_SILU = 0, BNN_ACT_GELU = 1, BNN_ACT_GELU_TANH = 2, BNN_AC
  *   scale[m] = a / 127,  q[m,k] = rint(x[m,k] * (127 / a))  (to nearest, ties to even: -127 .. 127).
  *   A row with a < 2^-100 has scale 0 and q 0.  A row that holds an infinity or a NaN has q 0 and scale a (NaN if it
  *   holds a NaN), so that products with it are NaN.
- *   x [rows, K] of `type` (bnn_float), q [rows, K] int8, scale [rows] fp32.  rows and K below 2^31 - 65536.
+ *   x [rows, K] of `type` (bnn_float), q [rows, K] int8, scale [rows] fp32.  rows below 2^31, K at most 2^28.
  */
 BNN_API bnn_status bnn_quant_rows_i8(const void *x, int type, int64_t rows, int64_t K, int64_t x_ld, int8_t *q,
                                      int64_t q_ld, float *scale, void *stream);

@@ -70,9 +70,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void mm_few_kernel(MmOperand
   for (const int end = min(K, k + BYTES); k < end; k += 64) {  // the last run, cut short
     u32x4 vb[NB], va[MT];
 #pragma unroll
-    for (int d = 0; d < NB; ++d) vb[d] = mm_piece<E>(b[d], k + piece, K);
+    for (int d = 0; d < NB; ++d) vb[d] = bytes16<E>(b[d], k + piece, K);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) va[i] = mm_piece<E>(a[i], k + piece, K);
+    for (int i = 0; i < MT; ++i) va[i] = bytes16<E>(a[i], k + piece, K);
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll

@@ -24,6 +24,38 @@ inline auto with_float(int t, const F &f) {
   return f(Float<BNN_F16>());
 }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(1)));  // global loads and stores take any byte address
+
+// 16 bytes of a row of `end` bytes from byte k on, zeros past its end, any alignment; nothing is read outside the row.  Of a
+// row's last piece the 16 bytes that end with the row, moved (element by element only in rows of less than 16 bytes: loads
+// under a mask each wait for the one before).
+template <class E>
+__device__ __forceinline__ u32x4 bytes16(const char *row, int k, int end) {
+  if (k + 16 <= end) return *reinterpret_cast<const u32x4_any *>(row + k);
+  u32x4 v = {0u, 0u, 0u, 0u};
+  if (k >= end) return v;
+  if (end >= 16) {
+    const u32x4 last = *reinterpret_cast<const u32x4_any *>(row + end - 16);
+    uint64_t lo = last[0] | (uint64_t)last[1] << 32, hi = last[2] | (uint64_t)last[3] << 32;
+    const int bits = 8 * (k + 16 - end);  // 8 .. 120
+    lo = bits < 64 ? lo >> bits | hi << (64 - bits) : hi >> (bits - 64);
+    hi = bits < 64 ? hi >> bits : 0u;
+    return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+  }
+#pragma unroll
+  for (int e = 0; e < 16 / (int)sizeof(E); ++e) {
+    if (k + e * (int)sizeof(E) < end) {
+      uint32_t x;
+      if constexpr (sizeof(E) == 1) x = *reinterpret_cast<const uint8_t *>(row + k + e);
+      else if constexpr (sizeof(E) == 2) x = *reinterpret_cast<const uint16_t *>(row + k + 2 * e);
+      else x = *reinterpret_cast<const uint32_t *>(row + k + 4 * e);
+      v[e * sizeof(E) / 4] |= x << (8 * (e * sizeof(E) % 4));
+    }
+  }
+  return v;
+}
+
 // Values n .. n + 3 of an aligned vector of N, zeros past its end; n is a multiple of 4.
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ f32x4 load4(const float *v, int n, int N) {

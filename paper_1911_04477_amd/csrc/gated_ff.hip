@@ -9,6 +9,18 @@
 
 namespace bnn {
 
+// The normal distribution's function: erfc by Abramowitz and Stegun 7.1.26 (absolute error of at most 1.5e-7, so of a GELU
+// of z 0.75e-7 |z|), with the density exp(-z^2 / 2) that it contains.  (erfcf: 1000 x 1024 to 2321 24.8 us instead of 21.)
+__device__ __forceinline__ float normal_function(float z, float &density) {
+  constexpr float LOG2E = 1.44269504088896341f;
+  const float x = fabsf(z) * 0.70710678118654752f;
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+  density = __builtin_amdgcn_exp2f(x * x * -LOG2E);
+  const float tail = 0.5f * density * t *
+                     fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  return z < 0.0f ? tail : 1.0f - tail;
+}
+
 // The activation, or with SLOPE also its derivative.  exp and the quotient are the hardware's (relative error of a few
 // 2^-24; what exp loses for large arguments belongs to values next to zero).
 template <bool SLOPE>
@@ -20,9 +32,10 @@ __device__ __forceinline__ float activation(int act, float z, float &slope) {
     a = z * t;
     if (SLOPE) slope = t * (1.0f + z * (1.0f - t));
   } else if (act == BNN_ACT_GELU) {
-    const float t = 0.5f * erfcf(z * -0.70710678118654752f);  // of the normal distribution, without cancellation below 0
+    float density;
+    const float t = normal_function(z, density);
     a = z * t;
-    if (SLOPE) slope = t + z * 0.39894228040143268f * __builtin_amdgcn_exp2f(z * z * (-0.5f * LOG2E));
+    if (SLOPE) slope = t + z * 0.39894228040143268f * density;
   } else if (act == BNN_ACT_GELU_TANH) {
     const float k = 0.79788456080286536f, c = 0.044715f;
     const float t = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-2.0f * LOG2E * k * (z + c * z * z * z)));  // (1 + tanh) / 2

@@ -144,6 +144,30 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
   // The loop of mm_tile_product, over this workgroup's share of the whole steps.
   const int all = whole * p.segments, split = blockIdx.y;
   const int from = (int)((int64_t)all * split / p.splits), steps = (int)((int64_t)all * (split + 1) / p.splits) - from;
+  // What is left of k in a stretch, with zeros behind it, by the last share: requested first and held, where registers allow.
+  const int left = p.K - whole * KM_STEP;
+  const bool rest = left > 0 && split == p.splits - 1;
+  struct Rest {
+    u32x4 a[LOADS_A], b[LOADS_B];
+  };
+  const auto request_rest = [&](Rest &r, int s) {
+    const int64_t k = (int64_t)whole * KM_STEP, ka = k + s * p.segA, ldb = s ? p.ldb1 : p.ldb0;
+    const char *const a = baseA + (A_ROWS ? 2 * ka : ka * p.lda), *const b = (s ? p.B1 : p.B0) + k * ldb;
+    const u32x4 none = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int l = 0; l < LOADS_A; ++l) {
+      if constexpr (A_ROWS) r.a[l] = bytes16<E>(a + atA[l] - piece, piece, 2 * left);
+      else r.a[l] = row_k(l, XA()) < left ? *reinterpret_cast<const u32x4 *>(a + atA[l]) : none;
+    }
+#pragma unroll
+    for (int l = 0; l < LOADS_B; ++l) r.b[l] = rowB[l] < left ? *reinterpret_cast<const u32x4 *>(b + rowB[l] * ldb + colB[l]) : none;
+  };
+  constexpr bool HELD = BM * BN < 256 * 256;
+  Rest held[2];
+  if (HELD && rest) {
+    request_rest(held[0], 0);
+    if (p.segments > 1) request_rest(held[1], 1);
+  }
   for (int i = 0; i < min(steps, STAGES); ++i) request(from + i, lds + i * STAGE);
   if (steps) {
     Half first, second;
@@ -173,24 +197,16 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
     multiply(first);
     multiply(second);
   }
-  if (split == p.splits - 1 && whole * KM_STEP < p.K) {  // what is left of k in every stretch, with zeros behind it
-    const int left = p.K - whole * KM_STEP;
-    for (int s = 0; s < p.segments; ++s) {
-      const int64_t k = (int64_t)whole * KM_STEP, ka = k + s * p.segA, ldb = s ? p.ldb1 : p.ldb0;
-      const char *const a = baseA + (A_ROWS ? 2 * ka : ka * p.lda), *const b = (s ? p.B1 : p.B0) + k * ldb;
-      const u32x4 none = {0u, 0u, 0u, 0u};
+  if (rest) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (s >= p.segments) break;
+      if (!HELD) request_rest(held[s], s);
       __syncthreads();
 #pragma unroll
-      for (int l = 0; l < LOADS_A; ++l) {
-        u32x4 v;
-        if constexpr (A_ROWS) v = mm_piece<E>(a + atA[l] - piece, piece, 2 * left);
-        else v = row_k(l, XA()) < left ? *reinterpret_cast<const u32x4 *>(a + atA[l]) : none;
-        *reinterpret_cast<u32x4 *>(lds + (l * WAVES + wave) * 1024 + lane * 16) = v;
-      }
+      for (int l = 0; l < LOADS_A; ++l) *reinterpret_cast<u32x4 *>(lds + (l * WAVES + wave) * 1024 + lane * 16) = held[s].a[l];
 #pragma unroll
-      for (int l = 0; l < LOADS_B; ++l)
-        *reinterpret_cast<u32x4 *>(lds + STAGE_A + (l * WAVES + wave) * 1024 + lane * 16) =
-            rowB[l] < left ? *reinterpret_cast<const u32x4 *>(b + rowB[l] * ldb + colB[l]) : none;
+      for (int l = 0; l < LOADS_B; ++l) *reinterpret_cast<u32x4 *>(lds + STAGE_A + (l * WAVES + wave) * 1024 + lane * 16) = held[s].b[l];
       __syncthreads();
 #pragma unroll
       for (int half = 0; half < 2; ++half) {

@@ -29,12 +29,19 @@ __device__ __forceinline__ void fill8(float (&v)[8], float x) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = x;
 }
-// Values of a vector of D, or of a matrix row; `missing` where there is none.
-template <class E>
-__device__ __forceinline__ void load8_or(float (&v)[8], const E *row, int c, int D, float missing) {
-  if (row) load8(v, row, c, D);
-  else fill8(v, missing);
+// A vector of D or a matrix row, `missing` where there is none: requested, and taken once it is needed.
+template <class E, bool SMALL>
+__device__ __forceinline__ void request8(Piece8<E> &w, const E *row, const Place8<SMALL> &at, int D, float missing) {
+  if (row) w.load(row, at, D);
+  else w.fill(missing);
 }
+template <class E>
+__device__ __forceinline__ void take8(float (&v)[8], Piece8<E> &w, int shift) {
+  if (shift) w.settle(shift);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (float)w.v[j];
+}
+
 __device__ __forceinline__ void zero_past(float (&v)[8], int c, int D) {
   if (c + 8 > D)
 #pragma unroll
@@ -78,70 +85,88 @@ __device__ __forceinline__ void times(float (&v)[NV][8], float x) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[i][j] *= x;
 }
-__device__ __forceinline__ float row_factor(float squares, int D, float eps) { return 1.0f / sqrtf(squares / (float)D + eps); }
+__device__ __forceinline__ float row_factor(float squares, float per, float eps) { return __builtin_amdgcn_rsqf(fmaf(squares, per, eps)); }
 
-template <bool BLOCK, int NV>
-__device__ __forceinline__ void unit_rows(float (&v)[NV][8], int norm, int c0, int T, int D, float eps, uint32_t *lds) {
+template <bool BLOCK, bool CENTRED, int NV>
+__device__ __forceinline__ void unit_rows(float (&v)[NV][8], int norm, int c0, int T, int D, float per, float eps, uint32_t *lds) {
   if (norm == BNN_NORM_NONE) return;
-  if (norm == BNN_NORM_LAYER) centre_rows<BLOCK, NV>(v, team_sum<BLOCK>(sum_of(v), lds) / (float)D, c0, T, D);
-  times(v, row_factor(team_sum<BLOCK>(dot_of(v, v), lds + 16), D, eps));
+  if (CENTRED && norm == BNN_NORM_LAYER) centre_rows<BLOCK, NV>(v, team_sum<BLOCK>(sum_of(v), lds) * per, c0, T, D);
+  times(v, row_factor(team_sum<BLOCK>(dot_of(v, v), lds + 16), per, eps));
 }
 
 // Which row of the gate; the host has cut gate_rows to at most 2^31 - 1 rows.
 __device__ __forceinline__ int64_t norm_group(const bnn_norm_gate_in &p, int64_t row) { return (uint32_t)row / (uint32_t)p.gate_rows; }
 
-// A team (a wave, or with BLOCK a workgroup) takes a row at a time, NV pieces of eight values a thread.  Bound by memory
-// (8192 x 4096 bf16 with a gate a token 74 us, 4.5 TB/s).
-template <class E, class R, bool BLOCK, int MAXT, int NV>
+// A team (a wave, or with BLOCK a workgroup) takes a row at a time, NV pieces of eight values a thread; all that a row needs
+// is requested before its first sum.  CENTRED: a norm with a mean or a bias takes part.  Bound by memory (8192 x 4096 bf16
+// with a gate a token 74 us, 4.5 TB/s), a few rows by the chain of request, sum, sum.
+template <class E, class R, bool BLOCK, int MAXT, int NV, bool CENTRED, bool SMALL>
 __global__ __launch_bounds__(MAXT) void norm_gate_kernel(bnn_norm_gate_in p, NormOut o, int teams) {
   __shared__ uint32_t lds[2 * 5 * 16];
-  if constexpr (BLOCK) clear_words(lds);
   const int T = BLOCK ? blockDim.x : 64, t = BLOCK ? threadIdx.x : threadIdx.x & 63, c0 = t * 8, D = p.D;
-  float w_post[NV][8], w_pre[NV][8], scale[NV][8];
+  const float per = 1.0f / (float)D;
+  const auto place = [&](int i) { return Place8<SMALL>(c0 + i * T * 8, D); };
+  constexpr int VECTORS = CENTRED ? 5 : 3;
+  const float *const from[5] = {p.w_post, p.w_pre, p.res_scale, p.bias_post, p.bias_pre};
+  Piece8<float> vec[VECTORS][NV];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    load8_or(w_post[i], p.w_post, c0 + i * T * 8, D, 1.0f);
-    load8_or(w_pre[i], p.w_pre, c0 + i * T * 8, D, 1.0f);
-    load8_or(scale[i], p.res_scale, c0 + i * T * 8, D, 1.0f);
-  }
+  for (int k = 0; k < VECTORS; ++k)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) request8(vec[k][i], from[k], place(i), D, k < 3 ? 1.0f : 0.0f);
+  bool settled = false;
   int flip = 0;  // a row's reductions do not touch what the row before left for slower waves to read
   for (int64_t row = BLOCK ? blockIdx.x : blockIdx.x * 4ll + (threadIdx.x >> 6); row < p.rows; row += teams, flip ^= 1) {
     uint32_t *const mem = lds + flip * 5 * 16;
+    Piece8<E> vb[NV], vg[NV];
+    Piece8<R> vr[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      request8(vb[i], p.b ? static_cast<const E *>(p.b) + row * p.b_ld : nullptr, place(i), D, 0.0f);
+      vr[i].load(static_cast<const R *>(p.r) + row * p.r_ld, place(i), D);
+      request8(vg[i], p.gate ? static_cast<const E *>(p.gate) + norm_group(p, row) * p.gate_ld : nullptr, place(i), D, 1.0f);
+    }
+    if (!settled) {  // while the first row comes
+      if (BLOCK) clear_words(lds);
+#pragma unroll
+      for (int k = 0; k < VECTORS; ++k)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (place(i).shift) vec[k][i].settle(place(i).shift);
+      settled = true;
+    }
     float v[NV][8], r[NV][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      load8(r[i], static_cast<const R *>(p.r) + row * p.r_ld, c0 + i * T * 8, D);
-      if (p.b) load8(v[i], static_cast<const E *>(p.b) + row * p.b_ld, c0 + i * T * 8, D);
+      if (place(i).shift) vg[i].settle(place(i).shift);
+      take8(v[i], vb[i], place(i).shift);
+      take8(r[i], vr[i], place(i).shift);
     }
     if (p.b) {
-      unit_rows<BLOCK, NV>(v, p.post, c0, T, D, p.eps, mem);
+      unit_rows<BLOCK, CENTRED, NV>(v, p.post, c0, T, D, per, p.eps, mem);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int c = c0 + i * T * 8;
-        float g[8], bias[8];
-        load8_or(bias, p.bias_post, c, D, 0.0f);
-        load8_or(g, p.gate ? static_cast<const E *>(p.gate) + norm_group(p, row) * p.gate_ld : nullptr, c, D, 1.0f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r[i][j] += scale[i][j] * g[j] * (v[i][j] * w_post[i][j] + bias[j]);
-        if (o.r) store8(static_cast<R *>(o.r) + row * o.r_ld, c, D, r[i]);
+        for (int j = 0; j < 8; ++j) {
+          const float n = CENTRED ? fmaf(v[i][j], vec[0][i].v[j], vec[VECTORS - 2][i].v[j]) : v[i][j] * vec[0][i].v[j];
+          r[i][j] = fmaf(vec[2][i].v[j] * (float)vg[i].v[j], n, r[i][j]);
+        }
+        if (o.r) store8(static_cast<R *>(o.r) + row * o.r_ld, c0 + i * T * 8, D, r[i]);
       }
     }
     if (p.pre == BNN_NORM_NONE) continue;
-    unit_rows<BLOCK, NV>(r, p.pre, c0, T, D, p.eps, mem + 32);
-    uint32_t top = 0u;
+    unit_rows<BLOCK, CENTRED, NV>(r, p.pre, c0, T, D, per, p.eps, mem + 32);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = c0 + i * T * 8;
-      float bias[8];
-      load8_or(bias, p.bias_pre, c, D, 0.0f);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) r[i][j] = r[i][j] * w_pre[i][j] + bias[j];
-      zero_past(r[i], c, D);
-      if (o.n) store8(static_cast<E *>(o.n) + row * o.n_ld, c, D, r[i]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = max(top, magnitude(r[i][j]));
+      for (int j = 0; j < 8; ++j) r[i][j] = CENTRED ? fmaf(r[i][j], vec[1][i].v[j], vec[VECTORS - 1][i].v[j]) : r[i][j] * vec[1][i].v[j];
+      if (o.n) store8(static_cast<E *>(o.n) + row * o.n_ld, c0 + i * T * 8, D, r[i]);
     }
-    if (o.q) {
+    if (o.q) {  // values past the end of the row are 0 in every vector
+      uint32_t top = 0u;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, magnitude(r[i][j]));
       const RowScale s = row_scale(team_max_magnitude<BLOCK>(top, mem + 64));
 #pragma unroll
       for (int i = 0; i < NV; ++i) store_q8(o.q + row * o.q_ld, c0 + i * T * 8, D, r[i], s.inv);
@@ -155,7 +180,7 @@ __global__ __launch_bounds__(MAXT) void norm_gate_kernel(bnn_norm_gate_in p, Nor
 // and its first sum is taken along with that row's last: between rms norms a row meets twice (8192 x 4096 bf16, a workgroup
 // a unit: 214 us without either, 173 with the loads ahead).  The vectors are in LDS, where there is room.  CENTRED: a norm
 // with a mean or a bias takes part.
-template <class E, class R, bool BLOCK, int MAXT, int NV, bool CENTRED>
+template <class E, class R, bool BLOCK, int MAXT, int NV, bool CENTRED, bool SMALL>
 __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_in p, NormGrad q) {
   constexpr int WIDTH = (BLOCK ? MAXT : 64) * NV * 8;
   constexpr bool NEAR = WIDTH <= 8192;
@@ -163,6 +188,7 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
   __shared__ __attribute__((aligned(16))) uint32_t lds[2 * MEM];
   __shared__ __attribute__((aligned(16))) float near_[3][NEAR ? WIDTH : 4];  // w_post, w_pre, res_scale
   const int D = p.D;
+  const float per = 1.0f / (float)D;
   if constexpr (NEAR) {
     const float *from[3] = {p.w_post, p.w_pre, p.res_scale};
 #pragma unroll
@@ -173,6 +199,12 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
   const int T = BLOCK ? blockDim.x : 64, t = BLOCK ? threadIdx.x : threadIdx.x & 63, c0 = t * 8;
   const int worker = BLOCK ? blockIdx.x : blockIdx.x * 4 + (threadIdx.x >> 6);
   if (worker >= q.workers) return;  // whole waves, of workgroups without barriers from here on
+  const auto place = [&](int i) { return Place8<SMALL>(c0 + i * T * 8, D); };
+  const auto far = [&](float (&v)[8], const float *from, int i, float missing) {
+    Piece8<float> w;
+    request8(w, from, place(i), D, missing);
+    take8(v, w, place(i).shift);
+  };
   const auto vector = [&](float (&v)[8], int k, int i) {
     if constexpr (NEAR) {
       const float *from = &near_[k][c0 + i * T * 8];
@@ -180,11 +212,11 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
     } else {
-      load8_or(v, k == 0 ? p.w_post : k == 1 ? p.w_pre : p.res_scale, c0 + i * T * 8, D, 1.0f);
+      far(v, k == 0 ? p.w_post : k == 1 ? p.w_pre : p.res_scale, i, 1.0f);
     }
   };
   const auto bias = [&](float (&v)[8], const float *from, int i) {
-    if (CENTRED) load8_or(v, from, c0 + i * T * 8, D, 0.0f);
+    if (CENTRED) far(v, from, i, 0.0f);
     else fill8(v, 0.0f);
   };
   int row, end;
@@ -205,17 +237,19 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
   const auto request = [&](Raw &w, int row) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = c0 + i * T * 8;
-      w.r[i].load(static_cast<const R *>(p.r) + row * p.r_ld, c, D);
-      if (p.b) w.b[i].load(static_cast<const E *>(p.b) + row * p.b_ld, c, D);
-      else w.b[i].fill(0.0f);
-      if (q.dn) w.dn[i].load(static_cast<const E *>(q.dn) + row * q.dn_ld, c, D);
-      else w.dn[i].fill(0.0f);
-      if (q.dr_out) w.dro[i].load(static_cast<const R *>(q.dr_out) + row * q.dr_out_ld, c, D);
-      else w.dro[i].fill(0.0f);
-      if (p.gate) w.g[i].load(static_cast<const E *>(p.gate) + norm_group(p, row) * p.gate_ld, c, D);
-      else w.g[i].fill(1.0f);
+      const Place8<SMALL> at = place(i);
+      w.r[i].load(static_cast<const R *>(p.r) + row * p.r_ld, at, D);
+      request8(w.b[i], p.b ? static_cast<const E *>(p.b) + row * p.b_ld : nullptr, at, D, 0.0f);
+      request8(w.dn[i], q.dn ? static_cast<const E *>(q.dn) + row * q.dn_ld : nullptr, at, D, 0.0f);
+      request8(w.dro[i], q.dr_out ? static_cast<const R *>(q.dr_out) + row * q.dr_out_ld : nullptr, at, D, 0.0f);
+      request8(w.g[i], p.gate ? static_cast<const E *>(p.gate) + norm_group(p, row) * p.gate_ld : nullptr, at, D, 1.0f);
     }
+  };
+  const auto settle = [&](Raw &w) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (const int shift = place(i).shift)
+        w.r[i].settle(shift), w.b[i].settle(shift), w.dn[i].settle(shift), w.dro[i].settle(shift), w.g[i].settle(shift);
   };
   float sum[SUMS][NV][8];
 #pragma unroll
@@ -236,6 +270,7 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
   float b[NV][8], opening = 0.0f;  // of the row at hand
   if (row < end) {
     request(w, row);
+    settle(w);
     values(b, w);
     opening = team_sum<BLOCK>(first_sum(b), lds + MEM);
   }
@@ -254,10 +289,10 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
     if (p.post != BNN_NORM_NONE) {
       float squares = opening;
       if (layer_post) {
-        centre_rows<BLOCK, NV>(b, opening / (float)D, c0, T, D);
+        centre_rows<BLOCK, NV>(b, opening * per, c0, T, D);
         squares = team_sum<BLOCK>(dot_of(b, b), mem);
       }
-      rsb = row_factor(squares, D, p.eps);
+      rsb = row_factor(squares, per, p.eps);
       times(b, rsb);
     }
     const auto block = [&](float (&pv)[8], int i) {  // p of this row
@@ -279,7 +314,7 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
     }
     // gradient through the norm of r': rs (e - mean(e) - u mean(e u)), u the normed values, the first mean if centred
     if (p.pre != BNN_NORM_NONE) {
-      if (layer_pre) centre_rows<BLOCK, NV>(r, team_sum<BLOCK>(sum_of(r), mem + 16) / (float)D, c0, T, D);
+      if (layer_pre) centre_rows<BLOCK, NV>(r, team_sum<BLOCK>(sum_of(r), mem + 16) * per, c0, T, D);
       float s[3] = {dot_of(r, r), 0.0f, 0.0f};
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
@@ -292,7 +327,7 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
         }
       }
       team_sum<BLOCK>(s, mem + 32);
-      const float rsr = row_factor(s[0], D, p.eps), along = s[1] * rsr / (float)D, level = layer_pre ? s[2] / (float)D : 0.0f;
+      const float rsr = row_factor(s[0], per, p.eps), along = s[1] * rsr * per, level = layer_pre ? s[2] * per : 0.0f;
       times(r, rsr);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
@@ -333,13 +368,14 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
 #pragma unroll
         for (int j = 0; j < 8; ++j) e[i][j] *= v[j];
       }
+      if (row + 1 < end) settle(ahead);
       float next[NV][8];
       values(next, ahead);
       float s[3] = {dot_of(e, b), first_sum(next), CENTRED ? sum_of(e) : 0.0f};
       team_sum<BLOCK>(s, mem + 80);
       opening = s[1];
       if (p.post != BNN_NORM_NONE) {
-        const float along = s[0] / (float)D, level = layer_post ? s[2] / (float)D : 0.0f;
+        const float along = s[0] * per, level = layer_post ? s[2] * per : 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -355,6 +391,9 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
         }
         left = (int)p.gate_rows;
       }
+    }
+    else if (row + 1 < end) {
+      settle(ahead);
     }
     w = ahead;
   }
@@ -439,6 +478,10 @@ inline bnn_norm_gate_in cut_groups(bnn_norm_gate_in p) {
   return p;
 }
 
+inline bool has_means(const bnn_norm_gate_in &p) {
+  return p.post == BNN_NORM_LAYER || p.pre == BNN_NORM_LAYER || p.bias_post || p.bias_pre;
+}
+
 bnn_status check_norm(const bnn_norm_gate_in *p) {
   if (!p) return BNN_ERR_NULL;
   if (p->rows < 0 || p->D <= 0 || !float_type(p->type) || !float_type(p->r_type) || !norm_known(p->post) || !norm_known(p->pre) ||
@@ -473,18 +516,21 @@ extern "C" bnn_status bnn_norm_gate(const bnn_norm_gate_in *in, void *r_out, int
   const NormOut o = {r_out, n_out, r_out_ld, n_ld, q_ld, q_out, q_scale};
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bnn_norm_gate_in in_groups = cut_groups(p);
+  const bool centred = has_means(p);
   ProfScope ps(KID_NORM_GATE, s);
   with_norm(p, [&](auto e, auto r) {
     using E = decltype(e);
     using R = decltype(r);
-    const auto run = [&](auto kernel, int block, int teams) {  // as many workgroups as run at once, at most
+    const auto run = [&](auto plain, auto with_means, int block, int teams) {  // as many workgroups as run at once, at most
       const uint32_t grid = (uint32_t)std::min<int64_t>((p.rows - 1) / teams + 1, 256 * (2048 / block));
-      kernel<<<grid, block, 0, s>>>(in_groups, o, (int)grid * teams);
+      (centred ? with_means : plain)<<<grid, block, 0, s>>>(in_groups, o, (int)grid * teams);
     };
-    if (p.D <= 512) run(norm_gate_kernel<E, R, false, 256, 1>, 256, 4);
-    else if (p.D <= 4096) run(norm_gate_kernel<E, R, true, 512, 1>, row_threads(p.D, 1), 1);
-    else if (p.D <= 8192) run(norm_gate_kernel<E, R, true, 1024, 1>, row_threads(p.D, 1), 1);
-    else run(norm_gate_kernel<E, R, true, 1024, 2>, row_threads(p.D, 2), 1);
+#define BNN_FORMS(kernel, ...) kernel<E, R, __VA_ARGS__, false, false>, kernel<E, R, __VA_ARGS__, true, false>
+    if (p.D < 8) run(norm_gate_kernel<E, R, false, 256, 1, true, true>, norm_gate_kernel<E, R, false, 256, 1, true, true>, 256, 4);
+    else if (p.D <= 512) run(BNN_FORMS(norm_gate_kernel, false, 256, 1), 256, 4);
+    else if (p.D <= 4096) run(BNN_FORMS(norm_gate_kernel, true, 512, 1), row_threads(p.D, 1), 1);
+    else if (p.D <= 8192) run(BNN_FORMS(norm_gate_kernel, true, 1024, 1), row_threads(p.D, 1), 1);
+    else run(BNN_FORMS(norm_gate_kernel, true, 1024, 2), row_threads(p.D, 2), 1);
   });
   return launch_status();
 }
@@ -529,20 +575,19 @@ extern "C" bnn_status bnn_norm_gate_backward(const bnn_norm_gate_in *in, const v
     q.part = static_cast<float *>(workspace);
     const bnn_norm_gate_in in_groups = cut_groups(p);
     ProfScope ps(KID_NORM_GATE_BACKWARD, s);
-    const bool centred = p.post == BNN_NORM_LAYER || p.pre == BNN_NORM_LAYER || p.bias_post || p.bias_pre;
+    const bool centred = has_means(p);
     with_norm(p, [&](auto e, auto r) {
       using E = decltype(e);
       using R = decltype(r);
       const auto run = [&](auto plain, auto with_means, int block, int teams) {
         (centred ? with_means : plain)<<<(uint32_t)((plan.workers - 1) / teams + 1), block, 0, s>>>(in_groups, q);
       };
-      if (p.D <= 512) run(norm_gate_backward_kernel<E, R, false, 256, 1, false>, norm_gate_backward_kernel<E, R, false, 256, 1, true>, 256, 4);
-      else if (p.D <= 4096)
-        run(norm_gate_backward_kernel<E, R, true, 512, 1, false>, norm_gate_backward_kernel<E, R, true, 512, 1, true>, row_threads(p.D, 1), 1);
-      else if (p.D <= 8192)
-        run(norm_gate_backward_kernel<E, R, true, 512, 2, false>, norm_gate_backward_kernel<E, R, true, 512, 2, true>, row_threads(p.D, 2), 1);
-      else
-        run(norm_gate_backward_kernel<E, R, true, 1024, 2, false>, norm_gate_backward_kernel<E, R, true, 1024, 2, true>, row_threads(p.D, 2), 1);
+      if (p.D < 8) run(norm_gate_backward_kernel<E, R, false, 256, 1, true, true>, norm_gate_backward_kernel<E, R, false, 256, 1, true, true>, 256, 4);
+      else if (p.D <= 512) run(BNN_FORMS(norm_gate_backward_kernel, false, 256, 1), 256, 4);
+      else if (p.D <= 4096) run(BNN_FORMS(norm_gate_backward_kernel, true, 512, 1), row_threads(p.D, 1), 1);
+      else if (p.D <= 8192) run(BNN_FORMS(norm_gate_backward_kernel, true, 512, 2), row_threads(p.D, 2), 1);
+      else run(BNN_FORMS(norm_gate_backward_kernel, true, 1024, 2), row_threads(p.D, 2), 1);
+#undef BNN_FORMS
     });
     if (bnn_status st = launch_status()) return st;
   } else if (!q.want) {

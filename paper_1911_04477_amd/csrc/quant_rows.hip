@@ -15,7 +15,7 @@ struct QuantParams {
 // A row a wave (four of them a workgroup), or (BLOCK) a row a workgroup; NV pieces of eight values a thread, held in
 // registers between the maximum and the rounding.  NV 0: rows of any length, read twice.  Bound by memory (8192 x 4096
 // bf16 20 us, 5.0 TB/s).
-template <class E, bool BLOCK, int MAXT, int NV>
+template <class E, bool BLOCK, int MAXT, int NV, bool SMALL>
 __global__ __launch_bounds__(MAXT) void quant_rows_kernel(QuantParams p) {
   __shared__ uint32_t lds[16];
   if constexpr (BLOCK) clear_words(lds);
@@ -26,13 +26,17 @@ __global__ __launch_bounds__(MAXT) void quant_rows_kernel(QuantParams p) {
   int8_t *q = p.q + row * p.q_ld;
   uint32_t top = 0u;
   if constexpr (NV > 0) {
+    Piece8<E> w[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) w[i].load(x, Place8<SMALL>((i * T + t) * 8, p.K), p.K);
     float v[NV][8];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) load8(v[i], x, (i * T + t) * 8, p.K);
+    for (int i = 0; i < NV; ++i) {
+      const Place8<SMALL> at((i * T + t) * 8, p.K);
+      if (at.shift) w[i].settle(at.shift);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[i][j]));
+      for (int j = 0; j < 8; ++j) v[i][j] = (float)w[i].v[j], top = max(top, magnitude(v[i][j]));
+    }
     const RowScale s = row_scale(team_max_magnitude<BLOCK>(top, lds));
 #pragma unroll
     for (int i = 0; i < NV; ++i) store_q8(q, (i * T + t) * 8, p.K, v[i], s.inv);
@@ -61,7 +65,7 @@ extern "C" bnn_status bnn_quant_rows_i8(const void *x, int type, int64_t rows, i
   using namespace bnn;
   if (rows < 0 || K <= 0 || !float_type(type)) return BNN_ERR_SHAPE;
   if (x_ld < K || q_ld < K) return BNN_ERR_STRIDE;
-  if (K > INT32_MAX - 65536 || rows > INT32_MAX) return BNN_ERR_UNSUPPORTED;
+  if (K > (1 << 28) || rows > INT32_MAX) return BNN_ERR_UNSUPPORTED;
   if (rows == 0) return BNN_OK;
   if (!x || !q || !scale) return BNN_ERR_NULL;
   if (!aligned16(x) || !aligned16(q) || !aligned16(scale)) return BNN_ERR_ALIGN;
@@ -71,10 +75,11 @@ extern "C" bnn_status bnn_quant_rows_i8(const void *x, int type, int64_t rows, i
   with_float(type, [&](auto tag) {
     using E = typename decltype(tag)::type;
     const uint32_t n = (uint32_t)rows;
-    if (K <= 512) quant_rows_kernel<E, false, 256, 1><<<(n - 1) / 4 + 1, 256, 0, s>>>(p);
-    else if (K <= 4096) quant_rows_kernel<E, true, 512, 1><<<n, row_threads(K, 1), 0, s>>>(p);
-    else if (K <= 32768) quant_rows_kernel<E, true, 1024, 4><<<n, row_threads(K, 4), 0, s>>>(p);
-    else quant_rows_kernel<E, true, 1024, 0><<<n, 1024, 0, s>>>(p);
+    if (K < 8) quant_rows_kernel<E, false, 256, 1, true><<<(n - 1) / 4 + 1, 256, 0, s>>>(p);
+    else if (K <= 512) quant_rows_kernel<E, false, 256, 1, false><<<(n - 1) / 4 + 1, 256, 0, s>>>(p);
+    else if (K <= 4096) quant_rows_kernel<E, true, 512, 1, false><<<n, row_threads(K, 1), 0, s>>>(p);
+    else if (K <= 32768) quant_rows_kernel<E, true, 1024, 4, false><<<n, row_threads(K, 4), 0, s>>>(p);
+    else quant_rows_kernel<E, true, 1024, 0, false><<<n, 1024, 0, s>>>(p);
   });
   return launch_status();
 }

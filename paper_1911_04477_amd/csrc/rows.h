@@ -6,55 +6,66 @@
 namespace bnn {
 
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
-typedef uint32_t u32x4_row __attribute__((ext_vector_type(4), aligned(1)));
 
-// Values c .. c + 7 of a row of D, zeros past its end.
-template <class E>
-__device__ __forceinline__ void load8(float (&v)[8], const E *row, int c, int D) {
-  typedef E E8 __attribute__((ext_vector_type(8)));
-  typedef E E4 __attribute__((ext_vector_type(4)));
-  if (c + 8 <= D) {
-    if constexpr (sizeof(E) == 4) {
-      const auto lo = __builtin_bit_cast(E4, *reinterpret_cast<const u32x4_row *>(row + c));
-      const auto hi = __builtin_bit_cast(E4, *reinterpret_cast<const u32x4_row *>(row + c + 4));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = (float)lo[i], v[4 + i] = (float)hi[i];
-    } else {
-      const auto x = __builtin_bit_cast(E8, *reinterpret_cast<const u32x4_row *>(row + c));
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = (float)x[i];
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < D ? (float)row[c + i] : 0.0f;
-  }
-}
-
-// The same eight values as they lie, for rows that are requested before they are needed.
+// Where a thread's eight values of a row of D lie: values c .. c + 7, read from `at` on, inside the row, and then moved down
+// by `shift` (8 and more: none is left).  Loads under a condition of their own would each wait for the one before; so all of
+// a row's loads are issued first, without one, and only threads at the end of a row move what they got.  SMALL: D < 8, read
+// one by one.
+template <bool SMALL>
+struct Place8 {
+  int c, at, shift;
+  __device__ __forceinline__ Place8(int c_, int D) : c(c_), at(SMALL ? 0 : min(c_, D - 8)), shift(c_ - at) {}
+};
 template <class E>
 struct Piece8 {
   typedef E E8 __attribute__((ext_vector_type(8)));
   E8 v;
-  __device__ __forceinline__ void load(const E *row, int c, int D) {
-    if (c + 8 <= D) {
-      if constexpr (sizeof(E) == 4) {
-        typedef E E4 __attribute__((ext_vector_type(4)));
-        const auto lo = __builtin_bit_cast(E4, *reinterpret_cast<const u32x4_row *>(row + c));
-        const auto hi = __builtin_bit_cast(E4, *reinterpret_cast<const u32x4_row *>(row + c + 4));
-        v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      } else {
-        v = __builtin_bit_cast(E8, *reinterpret_cast<const u32x4_row *>(row + c));
-      }
-    } else {
+  template <bool SMALL>
+  __device__ __forceinline__ void load(const E *row, const Place8<SMALL> &p, int D) {
+    if constexpr (SMALL) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = c + i < D ? row[c + i] : (E)0.0f;
+      for (int i = 0; i < 8; ++i) v[i] = row[min(i, D - 1)];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i >= D) v[i] = (E)0.0f;
+    } else if constexpr (sizeof(E) == 4) {
+      typedef E E4 __attribute__((ext_vector_type(4)));
+      const auto lo = __builtin_bit_cast(E4, *reinterpret_cast<const u32x4_any *>(row + p.at));
+      const auto hi = __builtin_bit_cast(E4, *reinterpret_cast<const u32x4_any *>(row + p.at + 4));
+      v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      v = __builtin_bit_cast(E8, *reinterpret_cast<const u32x4_any *>(row + p.at));
     }
+  }
+  // After the loads: the values that belong here, zeros behind them.
+  __device__ __forceinline__ void settle(int shift) {
+    const E8 none = {};
+    if (shift & 4) v = __builtin_shufflevector(v, none, 4, 5, 6, 7, 8, 9, 10, 11);
+    if (shift & 2) v = __builtin_shufflevector(v, none, 2, 3, 4, 5, 6, 7, 8, 9);
+    if (shift & 1) v = __builtin_shufflevector(v, none, 1, 2, 3, 4, 5, 6, 7, 8);
+    if (shift >= 8) v = none;
   }
   __device__ __forceinline__ void fill(float x) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (E)x;
   }
 };
+// The same where nothing else is to be requested at once.
+template <class E>
+__device__ __forceinline__ void load8(float (&v)[8], const E *row, int c, int D) {
+  Piece8<E> x;
+  if (D >= 8) {
+    const Place8<false> p(c, D);
+    x.load(row, p, D);
+    if (p.shift) x.settle(p.shift);
+  } else {
+    const Place8<true> p(c, D);
+    x.load(row, p, D);
+    if (p.shift) x.settle(p.shift);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)x.v[i];
+}
 
 template <class E>
 __device__ __forceinline__ void store8(E *row, int c, int D, const float (&v)[8]) {
@@ -62,13 +73,13 @@ __device__ __forceinline__ void store8(E *row, int c, int D, const float (&v)[8]
   typedef E E4 __attribute__((ext_vector_type(4)));
   if (c + 8 <= D) {
     if constexpr (sizeof(E) == 4) {
-      *reinterpret_cast<u32x4_row *>(row + c) = __builtin_bit_cast(u32x4_row, (E4{(E)v[0], (E)v[1], (E)v[2], (E)v[3]}));
-      *reinterpret_cast<u32x4_row *>(row + c + 4) = __builtin_bit_cast(u32x4_row, (E4{(E)v[4], (E)v[5], (E)v[6], (E)v[7]}));
+      *reinterpret_cast<u32x4_any *>(row + c) = __builtin_bit_cast(u32x4, (E4{(E)v[0], (E)v[1], (E)v[2], (E)v[3]}));
+      *reinterpret_cast<u32x4_any *>(row + c + 4) = __builtin_bit_cast(u32x4, (E4{(E)v[4], (E)v[5], (E)v[6], (E)v[7]}));
     } else {
       E8 x;
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = (E)v[i];
-      *reinterpret_cast<u32x4_row *>(row + c) = __builtin_bit_cast(u32x4_row, x);
+      *reinterpret_cast<u32x4_any *>(row + c) = __builtin_bit_cast(u32x4, x);
     }
   } else {
 #pragma unroll
