@@ -30,14 +30,14 @@ __device__ __forceinline__ void fill8(float (&v)[8], float x) {
   for (int i = 0; i < 8; ++i) v[i] = x;
 }
 // A vector of D or a matrix row, `missing` where there is none: requested, and taken once it is needed.
-template <class E, bool SMALL>
-__device__ __forceinline__ void request8(Piece8<E> &w, const E *row, const Place8<SMALL> &at, int D, float missing) {
+template <class E, int EDGE>
+__device__ __forceinline__ void request8(Piece8<E> &w, const E *row, const Place8<EDGE> &at, int D, float missing) {
   if (row) w.load(row, at, D);
   else w.fill(missing);
 }
-template <class E>
-__device__ __forceinline__ void take8(float (&v)[8], Piece8<E> &w, int shift) {
-  if (shift) w.settle(shift);
+template <class E, int EDGE>
+__device__ __forceinline__ void take8(float (&v)[8], Piece8<E> &w, const Place8<EDGE> &at) {
+  if (at.shift) w.settle(at);
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = (float)w.v[j];
 }
@@ -100,12 +100,12 @@ __device__ __forceinline__ int64_t norm_group(const bnn_norm_gate_in &p, int64_t
 // A team (a wave, or with BLOCK a workgroup) takes a row at a time, NV pieces of eight values a thread; all that a row needs
 // is requested before its first sum.  CENTRED: a norm with a mean or a bias takes part.  Bound by memory (8192 x 4096 bf16
 // with a gate a token 74 us, 4.5 TB/s), a few rows by the chain of request, sum, sum.
-template <class E, class R, bool BLOCK, int MAXT, int NV, bool CENTRED, bool SMALL>
+template <class E, class R, bool BLOCK, int MAXT, int NV, bool CENTRED, int EDGE>
 __global__ __launch_bounds__(MAXT) void norm_gate_kernel(bnn_norm_gate_in p, NormOut o, int teams) {
   __shared__ uint32_t lds[2 * 5 * 16];
   const int T = BLOCK ? blockDim.x : 64, t = BLOCK ? threadIdx.x : threadIdx.x & 63, c0 = t * 8, D = p.D;
   const float per = 1.0f / (float)D;
-  const auto place = [&](int i) { return Place8<SMALL>(c0 + i * T * 8, D); };
+  const auto place = [&](int i) { return Place8<EDGE>(c0 + i * T * 8, D); };
   constexpr int VECTORS = CENTRED ? 5 : 3;
   const float *const from[5] = {p.w_post, p.w_pre, p.res_scale, p.bias_post, p.bias_pre};
   Piece8<float> vec[VECTORS][NV];
@@ -131,15 +131,15 @@ __global__ __launch_bounds__(MAXT) void norm_gate_kernel(bnn_norm_gate_in p, Nor
       for (int k = 0; k < VECTORS; ++k)
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-          if (place(i).shift) vec[k][i].settle(place(i).shift);
+          if (place(i).shift) vec[k][i].settle(place(i));
       settled = true;
     }
     float v[NV][8], r[NV][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      if (place(i).shift) vg[i].settle(place(i).shift);
-      take8(v[i], vb[i], place(i).shift);
-      take8(r[i], vr[i], place(i).shift);
+      if (place(i).shift) vg[i].settle(place(i));
+      take8(v[i], vb[i], place(i));
+      take8(r[i], vr[i], place(i));
     }
     if (p.b) {
       unit_rows<BLOCK, CENTRED, NV>(v, p.post, c0, T, D, per, p.eps, mem);
@@ -180,8 +180,8 @@ __global__ __launch_bounds__(MAXT) void norm_gate_kernel(bnn_norm_gate_in p, Nor
 // and its first sum is taken along with that row's last: between rms norms a row meets twice (8192 x 4096 bf16, a workgroup
 // a unit: 214 us without either, 173 with the loads ahead).  The vectors are in LDS, where there is room.  CENTRED: a norm
 // with a mean or a bias takes part.
-template <class E, class R, bool BLOCK, int MAXT, int NV, bool CENTRED, bool SMALL>
-__global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_in p, NormGrad q) {
+template <class E, class R, bool BLOCK, int MAXT, int NV, bool CENTRED, int EDGE>
+__global__ __launch_bounds__(MAXT, NV > 1 || CENTRED ? 2 : 3) void norm_gate_backward_kernel(bnn_norm_gate_in p, NormGrad q) {
   constexpr int WIDTH = (BLOCK ? MAXT : 64) * NV * 8;
   constexpr bool NEAR = WIDTH <= 8192;
   constexpr int SUMS = 6, MEM = 8 * 16;
@@ -199,11 +199,11 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
   const int T = BLOCK ? blockDim.x : 64, t = BLOCK ? threadIdx.x : threadIdx.x & 63, c0 = t * 8;
   const int worker = BLOCK ? blockIdx.x : blockIdx.x * 4 + (threadIdx.x >> 6);
   if (worker >= q.workers) return;  // whole waves, of workgroups without barriers from here on
-  const auto place = [&](int i) { return Place8<SMALL>(c0 + i * T * 8, D); };
+  const auto place = [&](int i) { return Place8<EDGE>(c0 + i * T * 8, D); };
   const auto far = [&](float (&v)[8], const float *from, int i, float missing) {
     Piece8<float> w;
     request8(w, from, place(i), D, missing);
-    take8(v, w, place(i).shift);
+    take8(v, w, place(i));
   };
   const auto vector = [&](float (&v)[8], int k, int i) {
     if constexpr (NEAR) {
@@ -237,19 +237,13 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
   const auto request = [&](Raw &w, int row) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const Place8<SMALL> at = place(i);
+      const Place8<EDGE> at = place(i);
       w.r[i].load(static_cast<const R *>(p.r) + row * p.r_ld, at, D);
       request8(w.b[i], p.b ? static_cast<const E *>(p.b) + row * p.b_ld : nullptr, at, D, 0.0f);
       request8(w.dn[i], q.dn ? static_cast<const E *>(q.dn) + row * q.dn_ld : nullptr, at, D, 0.0f);
       request8(w.dro[i], q.dr_out ? static_cast<const R *>(q.dr_out) + row * q.dr_out_ld : nullptr, at, D, 0.0f);
       request8(w.g[i], p.gate ? static_cast<const E *>(p.gate) + norm_group(p, row) * p.gate_ld : nullptr, at, D, 1.0f);
     }
-  };
-  const auto settle = [&](Raw &w) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (const int shift = place(i).shift)
-        w.r[i].settle(shift), w.b[i].settle(shift), w.dn[i].settle(shift), w.dro[i].settle(shift), w.g[i].settle(shift);
   };
   float sum[SUMS][NV][8];
 #pragma unroll
@@ -260,9 +254,10 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
   // A row's first sum: of its squares, or (centred) of its values.
   const auto values = [&](float (&v)[NV][8], const Raw &w) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = (float)w.b[i].v[j];
+    for (int i = 0; i < NV; ++i) {
+      Piece8<E> x = w.b[i];
+      take8(v[i], x, place(i));
+    }
   };
   const bool layer_post = CENTRED && p.post == BNN_NORM_LAYER, layer_pre = CENTRED && p.pre == BNN_NORM_LAYER;
   const auto first_sum = [&](const float (&v)[NV][8]) { return layer_post ? sum_of(v) : dot_of(v, v); };
@@ -270,7 +265,6 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
   float b[NV][8], opening = 0.0f;  // of the row at hand
   if (row < end) {
     request(w, row);
-    settle(w);
     values(b, w);
     opening = team_sum<BLOCK>(first_sum(b), lds + MEM);
   }
@@ -282,9 +276,11 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
     // forward again: b normed, r' normed
     values(b, w);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) r[i][j] = (float)w.r[i].v[j], e[i][j] = (float)w.dn[i].v[j];
+    for (int i = 0; i < NV; ++i) {
+      take8(r[i], w.r[i], place(i));
+      take8(e[i], w.dn[i], place(i));
+      if (place(i).shift) w.g[i].settle(place(i)), w.dro[i].settle(place(i));
+    }
     float rsb = 1.0f;
     if (p.post != BNN_NORM_NONE) {
       float squares = opening;
@@ -368,7 +364,6 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
 #pragma unroll
         for (int j = 0; j < 8; ++j) e[i][j] *= v[j];
       }
-      if (row + 1 < end) settle(ahead);
       float next[NV][8];
       values(next, ahead);
       float s[3] = {dot_of(e, b), first_sum(next), CENTRED ? sum_of(e) : 0.0f};
@@ -391,9 +386,6 @@ __global__ __launch_bounds__(MAXT) void norm_gate_backward_kernel(bnn_norm_gate_
         }
         left = (int)p.gate_rows;
       }
-    }
-    else if (row + 1 < end) {
-      settle(ahead);
     }
     w = ahead;
   }
@@ -517,16 +509,20 @@ extern "C" bnn_status bnn_norm_gate(const bnn_norm_gate_in *in, void *r_out, int
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bnn_norm_gate_in in_groups = cut_groups(p);
   const bool centred = has_means(p);
+  const RowEdge edge = row_edge(p.D);
   ProfScope ps(KID_NORM_GATE, s);
   with_norm(p, [&](auto e, auto r) {
     using E = decltype(e);
     using R = decltype(r);
-    const auto run = [&](auto plain, auto with_means, int block, int teams) {  // as many workgroups as run at once, at most
+    const auto run = [&](auto plain, auto with_means, auto ragged, int block, int teams) {  // as many workgroups as run at once, at most
       const uint32_t grid = (uint32_t)std::min<int64_t>((p.rows - 1) / teams + 1, 256 * (2048 / block));
-      (centred ? with_means : plain)<<<grid, block, 0, s>>>(in_groups, o, (int)grid * teams);
+      (edge != EDGE_WHOLE ? ragged : centred ? with_means : plain)<<<grid, block, 0, s>>>(in_groups, o, (int)grid * teams);
     };
-#define BNN_FORMS(kernel, ...) kernel<E, R, __VA_ARGS__, false, false>, kernel<E, R, __VA_ARGS__, true, false>
-    if (p.D < 8) run(norm_gate_kernel<E, R, false, 256, 1, true, true>, norm_gate_kernel<E, R, false, 256, 1, true, true>, 256, 4);
+// rows of a multiple of eight values without and with means, and any others
+#define BNN_FORMS(kernel, ...) \
+  kernel<E, R, __VA_ARGS__, false, EDGE_WHOLE>, kernel<E, R, __VA_ARGS__, true, EDGE_WHOLE>, kernel<E, R, __VA_ARGS__, true, EDGE_RAGGED>
+#define BNN_SMALL(kernel) kernel<E, R, false, 256, 1, true, EDGE_SMALL>
+    if (edge == EDGE_SMALL) run(BNN_SMALL(norm_gate_kernel), BNN_SMALL(norm_gate_kernel), BNN_SMALL(norm_gate_kernel), 256, 4);
     else if (p.D <= 512) run(BNN_FORMS(norm_gate_kernel, false, 256, 1), 256, 4);
     else if (p.D <= 4096) run(BNN_FORMS(norm_gate_kernel, true, 512, 1), row_threads(p.D, 1), 1);
     else if (p.D <= 8192) run(BNN_FORMS(norm_gate_kernel, true, 1024, 1), row_threads(p.D, 1), 1);
@@ -576,18 +572,21 @@ extern "C" bnn_status bnn_norm_gate_backward(const bnn_norm_gate_in *in, const v
     const bnn_norm_gate_in in_groups = cut_groups(p);
     ProfScope ps(KID_NORM_GATE_BACKWARD, s);
     const bool centred = has_means(p);
+    const RowEdge edge = row_edge(p.D);
     with_norm(p, [&](auto e, auto r) {
       using E = decltype(e);
       using R = decltype(r);
-      const auto run = [&](auto plain, auto with_means, int block, int teams) {
-        (centred ? with_means : plain)<<<(uint32_t)((plan.workers - 1) / teams + 1), block, 0, s>>>(in_groups, q);
+      const auto run = [&](auto plain, auto with_means, auto ragged, int block, int teams) {
+        (edge != EDGE_WHOLE ? ragged : centred ? with_means : plain)<<<(uint32_t)((plan.workers - 1) / teams + 1), block, 0, s>>>(in_groups, q);
       };
-      if (p.D < 8) run(norm_gate_backward_kernel<E, R, false, 256, 1, true, true>, norm_gate_backward_kernel<E, R, false, 256, 1, true, true>, 256, 4);
+      if (edge == EDGE_SMALL)
+        run(BNN_SMALL(norm_gate_backward_kernel), BNN_SMALL(norm_gate_backward_kernel), BNN_SMALL(norm_gate_backward_kernel), 256, 4);
       else if (p.D <= 512) run(BNN_FORMS(norm_gate_backward_kernel, false, 256, 1), 256, 4);
       else if (p.D <= 4096) run(BNN_FORMS(norm_gate_backward_kernel, true, 512, 1), row_threads(p.D, 1), 1);
       else if (p.D <= 8192) run(BNN_FORMS(norm_gate_backward_kernel, true, 512, 2), row_threads(p.D, 2), 1);
       else run(BNN_FORMS(norm_gate_backward_kernel, true, 1024, 2), row_threads(p.D, 2), 1);
 #undef BNN_FORMS
+#undef BNN_SMALL
     });
     if (bnn_status st = launch_status()) return st;
   } else if (!q.want) {

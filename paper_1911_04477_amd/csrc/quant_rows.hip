@@ -15,7 +15,7 @@ struct QuantParams {
 // A row a wave (four of them a workgroup), or (BLOCK) a row a workgroup; NV pieces of eight values a thread, held in
 // registers between the maximum and the rounding.  NV 0: rows of any length, read twice.  Bound by memory (8192 x 4096
 // bf16 20 us, 5.0 TB/s).
-template <class E, bool BLOCK, int MAXT, int NV, bool SMALL>
+template <class E, bool BLOCK, int MAXT, int NV, int EDGE>
 __global__ __launch_bounds__(MAXT) void quant_rows_kernel(QuantParams p) {
   __shared__ uint32_t lds[16];
   if constexpr (BLOCK) clear_words(lds);
@@ -28,12 +28,12 @@ __global__ __launch_bounds__(MAXT) void quant_rows_kernel(QuantParams p) {
   if constexpr (NV > 0) {
     Piece8<E> w[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) w[i].load(x, Place8<SMALL>((i * T + t) * 8, p.K), p.K);
+    for (int i = 0; i < NV; ++i) w[i].load(x, Place8<EDGE>((i * T + t) * 8, p.K), p.K);
     float v[NV][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const Place8<SMALL> at((i * T + t) * 8, p.K);
-      if (at.shift) w[i].settle(at.shift);
+      const Place8<EDGE> at((i * T + t) * 8, p.K);
+      if (at.shift) w[i].settle(at);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] = (float)w[i].v[j], top = max(top, magnitude(v[i][j]));
     }
@@ -75,11 +75,16 @@ extern "C" bnn_status bnn_quant_rows_i8(const void *x, int type, int64_t rows, i
   with_float(type, [&](auto tag) {
     using E = typename decltype(tag)::type;
     const uint32_t n = (uint32_t)rows;
-    if (K < 8) quant_rows_kernel<E, false, 256, 1, true><<<(n - 1) / 4 + 1, 256, 0, s>>>(p);
-    else if (K <= 512) quant_rows_kernel<E, false, 256, 1, false><<<(n - 1) / 4 + 1, 256, 0, s>>>(p);
-    else if (K <= 4096) quant_rows_kernel<E, true, 512, 1, false><<<n, row_threads(K, 1), 0, s>>>(p);
-    else if (K <= 32768) quant_rows_kernel<E, true, 1024, 4, false><<<n, row_threads(K, 4), 0, s>>>(p);
-    else quant_rows_kernel<E, true, 1024, 0, false><<<n, 1024, 0, s>>>(p);
+    const auto run = [&](auto whole, auto ragged, int block, int teams) {
+      (row_edge(K) == EDGE_WHOLE ? whole : ragged)<<<(n - 1) / teams + 1, block, 0, s>>>(p);
+    };
+#define BNN_FORMS(...) quant_rows_kernel<E, __VA_ARGS__, EDGE_WHOLE>, quant_rows_kernel<E, __VA_ARGS__, EDGE_RAGGED>
+    if (K < 8) quant_rows_kernel<E, false, 256, 1, EDGE_SMALL><<<(n - 1) / 4 + 1, 256, 0, s>>>(p);
+    else if (K <= 512) run(BNN_FORMS(false, 256, 1), 256, 4);
+    else if (K <= 4096) run(BNN_FORMS(true, 512, 1), row_threads(K, 1), 1);
+    else if (K <= 32768) run(BNN_FORMS(true, 1024, 4), row_threads(K, 4), 1);
+    else quant_rows_kernel<E, true, 1024, 0, EDGE_RAGGED><<<n, 1024, 0, s>>>(p);
+#undef BNN_FORMS
   });
   return launch_status();
 }

@@ -9,20 +9,25 @@ typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 
 // Where a thread's eight values of a row of D lie: values c .. c + 7, read from `at` on, inside the row, and then moved down
 // by `shift` (8 and more: none is left).  Loads under a condition of their own would each wait for the one before; so all of
-// a row's loads are issued first, without one, and only threads at the end of a row move what they got.  SMALL: D < 8, read
-// one by one.
-template <bool SMALL>
+// a row's loads are issued first, without one, and only threads at the end of a row move what they got.
+enum RowEdge : int {
+  EDGE_WHOLE = 0,   // D a multiple of eight: a thread has all of its values or none
+  EDGE_RAGGED = 1,  // D > 8
+  EDGE_SMALL = 2    // D < 8, read one by one
+};
+inline RowEdge row_edge(int64_t D) { return D % 8 == 0 ? EDGE_WHOLE : D > 8 ? EDGE_RAGGED : EDGE_SMALL; }
+template <int EDGE>
 struct Place8 {
   int c, at, shift;
-  __device__ __forceinline__ Place8(int c_, int D) : c(c_), at(SMALL ? 0 : min(c_, D - 8)), shift(c_ - at) {}
+  __device__ __forceinline__ Place8(int c_, int D) : c(c_), at(EDGE == EDGE_SMALL ? 0 : min(c_, D - 8)), shift(c_ - at) {}
 };
 template <class E>
 struct Piece8 {
   typedef E E8 __attribute__((ext_vector_type(8)));
   E8 v;
-  template <bool SMALL>
-  __device__ __forceinline__ void load(const E *row, const Place8<SMALL> &p, int D) {
-    if constexpr (SMALL) {
+  template <int EDGE>
+  __device__ __forceinline__ void load(const E *row, const Place8<EDGE> &p, int D) {
+    if constexpr (EDGE == EDGE_SMALL) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = row[min(i, D - 1)];
 #pragma unroll
@@ -38,12 +43,14 @@ struct Piece8 {
     }
   }
   // After the loads: the values that belong here, zeros behind them.
-  __device__ __forceinline__ void settle(int shift) {
+  template <int EDGE>
+  __device__ __forceinline__ void settle(const Place8<EDGE> &p) {
     const E8 none = {};
+    const int shift = EDGE == EDGE_RAGGED ? p.shift : 0;
     if (shift & 4) v = __builtin_shufflevector(v, none, 4, 5, 6, 7, 8, 9, 10, 11);
     if (shift & 2) v = __builtin_shufflevector(v, none, 2, 3, 4, 5, 6, 7, 8, 9);
     if (shift & 1) v = __builtin_shufflevector(v, none, 1, 2, 3, 4, 5, 6, 7, 8);
-    if (shift >= 8) v = none;
+    if (p.shift >= 8) v = none;
   }
   __device__ __forceinline__ void fill(float x) {
 #pragma unroll
@@ -55,13 +62,13 @@ template <class E>
 __device__ __forceinline__ void load8(float (&v)[8], const E *row, int c, int D) {
   Piece8<E> x;
   if (D >= 8) {
-    const Place8<false> p(c, D);
+    const Place8<EDGE_RAGGED> p(c, D);
     x.load(row, p, D);
-    if (p.shift) x.settle(p.shift);
+    if (p.shift) x.settle(p);
   } else {
-    const Place8<true> p(c, D);
+    const Place8<EDGE_SMALL> p(c, D);
     x.load(row, p, D);
-    if (p.shift) x.settle(p.shift);
+    if (p.shift) x.settle(p);
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = (float)x.v[i];
