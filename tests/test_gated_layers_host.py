@@ -142,3 +142,21 @@ def test_gated_backward_refusals(L):
     assert f(nbytes=L.bnn_gated_ff_backward_workspace_bytes(4, 8, 16) - 1) == WORKSPACE
     assert f(T=0, F=0, dx=None, dwg=None, dwu=None) == OK
     assert L.bnn_gated_ff_backward_workspace_bytes(0, 8, 8) == L.bnn_gated_ff_backward_workspace_bytes(8, 8, 1 << 22) == 0
+
+
+def test_calls_from_tensors_decline_what_is_not_plain():
+    """CPU tensors, wrong counts and kinds of arguments are left to the binding, which raises."""
+    import torch
+    t = B._t()
+    x, v, q = torch.zeros(4, 8), torch.zeros(4), torch.zeros(4, 8, dtype=torch.int8)
+    none = [None] * 7
+    for name, args in (("quant_rows", (x, q, v)), ("quant_rows", (x, q)), ("linear_i8", (q, v, q, v, None, x)),
+                       ("norm_gate", (x, x, None, 1, *none[:5], 1, 1, 1e-6, x, x, None, None)), ("norm_gate", (x, x)),
+                       ("norm_gate_backward", (x, x, None, 1, *none[:5], 1, 1, 1e-6, x, x, x, x, *none[:6], x)),
+                       ("gated_ff", (x, x, x, 0, x, None)), ("gated_ff", (x, x, x, "silu", x, None)),
+                       ("gated_ff_i8", (q, v, q, v, q, v, 0, x)), ("gated_ff_backward", (x, x, x, x, x, x, x, x, x))):
+        assert getattr(t, name)(*args) is None, name
+    with pytest.raises(TypeError):
+        B.bnn_quant_rows_i8(x)
+    with pytest.raises(TypeError):
+        B.bnn_gated_ff(x, x, x)
