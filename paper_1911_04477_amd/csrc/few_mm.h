@@ -137,7 +137,8 @@ bnn_status run_product(const MmOperands &p, const Epilogue &epi, int kid_few, in
     return launch_mm_tile<TY, 64, 64, 2, 2, 2, DUAL, false>(p, epi, kid, s);
   }
   switch (form) {
-    case 0: return launch_mm_tile<TY, 256, 256, 4, 2, 2, DUAL, true>(p, epi, kid, s);
+    case 0:  // 128 outputs a thread: what the epilogue does is compiled for the call
+      return epi.fixed([&](const auto &known) { return launch_mm_tile<TY, 256, 256, 2, 2, 2, DUAL, true>(p, known, kid, s); });
     case 1: {
       const int64_t tiles = (int64_t)((p.M - 1) / 128 + 1) * ((p.N - 1) / (DUAL ? 64 : 128) + 1);
       // one tile a unit: eight waves and four steps ahead (256 x 4096 by 4096 to 8192 gated 61 -> 44 us); else two

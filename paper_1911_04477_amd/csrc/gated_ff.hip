@@ -48,9 +48,21 @@ __device__ __forceinline__ float activation(int act, float z, float &slope) {
   return a;
 }
 
+// f with the activation as a tag.
+template <class F>
+bnn_status with_act(int act, const F &f) {
+  switch (act) {
+    case BNN_ACT_SILU: return f(std::integral_constant<int, BNN_ACT_SILU>());
+    case BNN_ACT_GELU: return f(std::integral_constant<int, BNN_ACT_GELU>());
+    case BNN_ACT_GELU_TANH: return f(std::integral_constant<int, BNN_ACT_GELU_TANH>());
+    default: return f(std::integral_constant<int, BNN_ACT_RELU>());
+  }
+}
+
 // Where a backward pass will follow, `saved` takes what it multiplies the gradient of h with, in fp32 (16 bits would round
 // the gradients of the projections twice): act'(g) * u for that of g = x Wg^T, act(g) for that of u = x Wu^T.
-template <class E>
+// ACT, SAVE: known when the kernel is compiled, or -1; then they are looked at for every group of columns.
+template <class E, int ACT = -1, int SAVE = -1>
 struct GatedEpilogue {
   E *h;
   int64_t ldh;
@@ -62,7 +74,8 @@ struct GatedEpilogue {
   __device__ __forceinline__ NoConstants columns(int, int) const { return {}; }
   __device__ __forceinline__ void operator()(int m, int n, int N, Row, NoConstants, const v4f &g, const v4f &u) const {
     float o[4], dg[4], du[4];
-    if (saved) {
+    const int act = ACT < 0 ? this->act : ACT;
+    if (SAVE < 0 ? saved != nullptr : SAVE) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float slope;
@@ -81,8 +94,16 @@ struct GatedEpilogue {
     }
     store4(h + m * ldh, n, N, o);
   }
+  template <class F>
+  bnn_status fixed(const F &f) const {
+    return with_act(act, [&](auto a) {
+      constexpr int A = decltype(a)::value;
+      return saved ? f(GatedEpilogue<E, A, 1>{h, ldh, saved, plane, act}) : f(GatedEpilogue<E, A, 0>{h, ldh, saved, plane, act});
+    });
+  }
 };
 
+template <int ACT = -1>
 struct GatedI8Epilogue {
   const float *sx, *sg, *su;
   void *h;
@@ -99,11 +120,15 @@ struct GatedI8Epilogue {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float none;
-      o[i] = activation<false>(act, (float)g[i] * a * c.g[i], none) * ((float)u[i] * a * c.u[i]);
+      o[i] = activation<false>(ACT < 0 ? act : ACT, (float)g[i] * a * c.g[i], none) * ((float)u[i] * a * c.u[i]);
     }
     if (type == BNN_BF16) store4(static_cast<__bf16 *>(h) + m * ldh, n, N, o);
     else if (type == BNN_F16) store4(static_cast<_Float16 *>(h) + m * ldh, n, N, o);
     else store4(static_cast<float *>(h) + m * ldh, n, N, o);
+  }
+  template <class F>
+  bnn_status fixed(const F &f) const {
+    return with_act(act, [&](auto a) { return f(GatedI8Epilogue<decltype(a)::value>{sx, sg, su, h, ldh, type, act}); });
   }
 };
 
@@ -230,7 +255,7 @@ bnn_status km_product(KmOperands p, ProductEpilogue<E> epi, float *part, hipStre
   if (plan.shares > 1) epi.part = part, epi.part_ld = p.N, epi.plane = (int64_t)p.M * p.N;
   bnn_status st;
   switch (plan.form) {
-    case 0: st = launch_km_tile<TY, 256, 256, 4, 2, 2, A_ROWS>(p, epi, KID_GATED_FF_BACKWARD, s); break;
+    case 0: st = launch_km_tile<TY, 256, 256, 2, 2, 2, A_ROWS>(p, epi, KID_GATED_FF_BACKWARD, s); break;
     case 1: st = launch_km_tile<TY, 128, 128, 2, 4, 4, A_ROWS>(p, epi, KID_GATED_FF_BACKWARD, s); break;
     case 2: st = launch_km_tile<TY, 128, 128, 2, 2, 2, A_ROWS>(p, epi, KID_GATED_FF_BACKWARD, s); break;
     default: st = launch_km_tile<TY, 64, 64, 2, 2, 4, A_ROWS>(p, epi, KID_GATED_FF_BACKWARD, s);
@@ -333,7 +358,7 @@ extern "C" bnn_status bnn_gated_ff_i8(const int8_t *x, int64_t x_ld, const float
   p.B1 = reinterpret_cast<const char *>(wu), p.ldb1 = wu_ld;
   p.M = (int)T, p.N = (int)F, p.kbytes = (int)D;
   p.dma = mm_dma(x, x_ld) && mm_dma(wg, wg_ld) && mm_dma(wu, wu_ld);
-  const GatedI8Epilogue epi = {x_scale, wg_scale, wu_scale, h, h_ld, type, act};
+  const GatedI8Epilogue<> epi = {x_scale, wg_scale, wu_scale, h, h_ld, type, act};
   return run_product<MM_I8, true>(p, epi, KID_GATED_FF_I8, KID_GATED_FF_I8, static_cast<hipStream_t>(stream));
 }
 

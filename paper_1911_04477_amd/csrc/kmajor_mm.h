@@ -78,15 +78,17 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
     ldb = s ? p.ldb1 : p.ldb0;
     b = (s ? p.B1 : p.B0) + k * ldb;
   };
-  const auto request = [&](int i, char *to) {
+  const auto request = [&](int i, char *to, int only = -1) {  // all loads of step i, or one
     const char *a, *b;
     int64_t ldb;
     step_of(i, a, b, ldb);
     const uint32_t dst = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)to + wave * 1024;
 #pragma unroll
-    for (int l = 0; l < LOADS_A; ++l) km_load(a, atA[l], dst + l * WAVES * 1024);
-#pragma unroll
-    for (int l = 0; l < LOADS_B; ++l) km_load(b, rowB[l] * (int)ldb + colB[l], dst + STAGE_A + l * WAVES * 1024);
+    for (int l = 0; l < LOADS; ++l)
+      if (only < 0 || l == only) {
+        if (l < LOADS_A) km_load(a, atA[l < LOADS_A ? l : 0], dst + l * WAVES * 1024);
+        else km_load(b, rowB[l < LOADS_A ? 0 : l - LOADS_A] * (int)ldb + colB[l < LOADS_A ? 0 : l - LOADS_A], dst + l * WAVES * 1024);
+      }
   };
 
   Acc acc[TM][TN];
@@ -94,6 +96,9 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+  if constexpr (TM * TN == 64)
+#pragma unroll
+    for (int i = 0; i < TM; ++i) mm_settle(acc[i]);
 
   // Fragments of 32 values of k.  k-major: lane l of 16 reads four values of row l / 4, and receives column l of four rows.
   const int slot = ((lane >> 4) ^ (lane & 7)) * 16;
@@ -115,15 +120,23 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
     const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(lds + at + 8 * X)));
     return u32x4{lo[0], lo[1], hi[0], hi[1]};
   };
+  const auto fetch_one = [&](Half &f, int stage, int half, int k) {  // B's first
+    const int j = k < TN ? k : 0, i = k < TN ? 0 : k - TN;
+    if (k < TN) f.b[j] = read8((stage + fragB ^ j * 32) + half * 64 * BN, XB());
+    else if constexpr (A_ROWS) f.a[i] = *reinterpret_cast<const u32x4 *>(lds + (stage + fragA ^ half * 64) + i * 2048);
+    else f.a[i] = read8((stage + fragA ^ i * 32) + half * 64 * BM, XA());
+  };
   const auto fetch = [&](Half &f, int stage, int half) {
 #pragma unroll
-    for (int j = 0; j < TN; ++j) f.b[j] = read8((stage + fragB ^ j * 32) + half * 64 * BN, XB());
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-      f.a[i] = A_ROWS ? *reinterpret_cast<const u32x4 *>(lds + (stage + fragA ^ half * 64) + i * 2048)
-                      : read8((stage + fragA ^ i * 32) + half * 64 * BM, XA());
+    for (int k = 0; k < TM + TN; ++k) fetch_one(f, stage, half, k);
   };
+  constexpr bool IN_PLACE = TM * TN == 64;
+  const auto nothing = [](int) {};
   const auto multiply = [&](const Half &f) {
+    if constexpr (IN_PLACE) {
+      mm_weave<T, 0>(f, acc, nothing, nothing);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -176,8 +189,19 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
     fetch(first, 0, 0);
     int now = 0;
     const auto turn = [&](int i, auto loads) {
-      __builtin_amdgcn_sched_barrier(0);
       const int next = now + 1 == STAGES ? 0 : now + 1;
+      if constexpr (IN_PLACE) {
+        mm_weave<T, TM + TN>(first, acc, [&](int k) { fetch_one(second, now * STAGE, 1, k); }, nothing);
+        if (i + STAGES - 1 < steps) mm_sync<(STAGES - 2) * LOADS>();
+        else mm_sync<0>();
+        mm_weave<T, TM + TN>(second, acc, [&](int k) { fetch_one(first, next * STAGE, 0, k); }, [&](int k) {
+          if constexpr (decltype(loads)::value > 0)
+            if (k < LOADS) request(from + i + STAGES, lds + now * STAGE, k);
+        });
+        now = next;
+        return;
+      }
+      __builtin_amdgcn_sched_barrier(0);
       fetch(second, now * STAGE, 1);
       multiply(first);
       interleave(std::integral_constant<int, 0>());
@@ -217,6 +241,9 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
     }
   }
 
+  if constexpr (IN_PLACE)
+#pragma unroll
+    for (int i = 0; i < TM; ++i) mm_settle(acc[i]);
   const int m = m0 + wm * (BM / WGM) + (lane & 15), n = n0 + wn * (BN / WGN) + (lane >> 4) * 4;
 #pragma unroll
   for (int j = 0; j < TN; ++j) {

@@ -26,6 +26,8 @@ struct LinearEpilogue {
     else if (type == BNN_F16) store4(static_cast<_Float16 *>(y) + m * ldy, n, N, v);
     else store4(static_cast<float *>(y) + m * ldy, n, N, v);
   }
+  template <class F>
+  bnn_status fixed(const F &f) const { return f(*this); }
 };
 
 }  // namespace bnn

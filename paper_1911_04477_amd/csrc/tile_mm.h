@@ -24,6 +24,10 @@ struct MmTraits<MM_I8> {
   static __device__ __forceinline__ acc mfma(u32x4 a, u32x4 b, acc c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, a), __builtin_bit_cast(v4i, b), c, 0, 0, 0);
   }
+  // c in accumulation registers and nowhere else (mm_settle)
+  static __device__ __forceinline__ void mfma_in_place(u32x4 a, u32x4 b, acc &c) {
+    asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  }
 };
 template <>
 struct MmTraits<MM_BF16> {
@@ -32,6 +36,10 @@ struct MmTraits<MM_BF16> {
   static __device__ __forceinline__ acc mfma(u32x4 a, u32x4 b, acc c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
   }
+  // c in accumulation registers and nowhere else (mm_settle)
+  static __device__ __forceinline__ void mfma_in_place(u32x4 a, u32x4 b, acc &c) {
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  }
 };
 template <>
 struct MmTraits<MM_F16> {
@@ -39,6 +47,10 @@ struct MmTraits<MM_F16> {
   using acc = v4f;
   static __device__ __forceinline__ acc mfma(u32x4 a, u32x4 b, acc c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+  }
+  // c in accumulation registers and nowhere else (mm_settle)
+  static __device__ __forceinline__ void mfma_in_place(u32x4 a, u32x4 b, acc &c) {
+    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
   }
 };
 
@@ -54,6 +66,27 @@ struct MmOperands {
 // Whether an operand's tiles can go straight to LDS: 16-byte pieces that start on 16 bytes, 32-bit offsets in a tile.
 inline bool mm_dma(const void *p, int64_t ld_bytes) {
   return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)ld_bytes) & 15u) == 0 && ld_bytes < (1 << 22);
+}
+
+// A wave's 64 accumulators of a 128 x 128 tile fill the accumulation registers.  The compiler then has none left to rotate
+// them through and copies about 200 of them a step, so these products are written out, each in place.  What the compiler
+// does not know of them is waited for here: before the first one reads, and after the last one has written (a matrix
+// instruction of eight passes needs eleven wait states before anything else reads its result).
+template <class Acc>
+__device__ __forceinline__ void mm_settle(Acc (&c)[8]) {
+  asm volatile("s_nop 15" : "+a"(c[0]), "+a"(c[1]), "+a"(c[2]), "+a"(c[3]), "+a"(c[4]), "+a"(c[5]), "+a"(c[6]), "+a"(c[7]));
+}
+// Products of one half step with the next half's reads of LDS between them: first(k) issues the k-th read, second(k) the k-th
+// request, if there are so many.
+template <class T, int READS, class Half, class Acc, class First, class Second>
+__device__ __forceinline__ void mm_weave(const Half &has, Acc (&acc)[8][8], const First &first, const Second &second) {
+  constexpr int PER = READS ? 64 / READS : 64;
+#pragma unroll
+  for (int q = 0; q < 64; ++q) {
+    if (q % PER == 0 && q / PER < READS) first(q / PER);
+    if (q % 4 == 2) second(q / 4);
+    T::mfma_in_place(has.b[q % 8], has.a[q / 8], acc[q / 8][q % 8]);  // rows of the result: n
+  }
 }
 
 // Tiles in an order in which the workgroups that run at the same time on one XCD (ids go round the eight of them) read few
@@ -114,6 +147,9 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+  if constexpr (TM * TN == 64)
+#pragma unroll
+    for (int i = 0; i < TM; ++i) mm_settle(acc[i]);
 
   const int slot = ((lane >> 4) ^ (lane & 7)) * 16;  // of this lane's piece of the first 64 bytes; ^ 64: of the second
   const int fragA = (wm * (BM / WGM) + (lane & 15)) * MM_STEP + slot;
@@ -121,16 +157,23 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
   struct Half {  // fragments of 64 bytes of k
     u32x4 a[TM], b[TN];
   };
+  const auto fetch_one = [&](Half &f, const char *lds, int half, int k) {  // B's first
+    const int j = k < TN ? k : 0, i = k < TN ? 0 : k - TN;
+    const int row = !DUAL ? j * 16 : j < TN / 2 ? j * 16 : NB + (j - TN / 2) * 16;
+    if (k < TN) f.b[j] = *reinterpret_cast<const u32x4 *>(lds + (fragB ^ (half * 64)) + row * MM_STEP);
+    else f.a[i] = *reinterpret_cast<const u32x4 *>(lds + (fragA ^ (half * 64)) + i * 16 * MM_STEP);
+  };
   const auto fetch = [&](Half &f, const char *lds, int half) {
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int row = !DUAL ? j * 16 : j < TN / 2 ? j * 16 : NB + (j - TN / 2) * 16;
-      f.b[j] = *reinterpret_cast<const u32x4 *>(lds + (fragB ^ (half * 64)) + row * MM_STEP);
-    }
-#pragma unroll
-    for (int i = 0; i < TM; ++i) f.a[i] = *reinterpret_cast<const u32x4 *>(lds + (fragA ^ (half * 64)) + i * 16 * MM_STEP);
+    for (int k = 0; k < TM + TN; ++k) fetch_one(f, lds, half, k);
   };
+  constexpr bool IN_PLACE = TM * TN == 64;
+  const auto nothing = [](int) {};
   const auto multiply = [&](const Half &f) {
+    if constexpr (IN_PLACE) {
+      mm_weave<T, 0>(f, acc, nothing, nothing);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -169,15 +212,17 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
       const int r = row_of(i, ld);
       at[i] = (int)(r * ld) + piece;
     }
+    constexpr bool BY_LOAD = NB % (8 * WAVES) == 0;  // a load of all waves is of one matrix
+    const auto request_one = [&](int i, int k, char *lds) {
+      const int row = (i * WAVES + wave) * 8;
+      const auto to = (__attribute__((address_space(3))) void *)(lds + row * MM_STEP);
+      if (i < LOADS_A) __builtin_amdgcn_raw_ptr_buffer_load_lds(resA, to, 16, at[i], k, 0, 0);
+      else if (DUAL && (BY_LOAD ? i * WAVES : i * WAVES + wave) * 8 - BM >= NB) __builtin_amdgcn_raw_ptr_buffer_load_lds(res1, to, 16, at[i], k, 0, 0);
+      else __builtin_amdgcn_raw_ptr_buffer_load_lds(res0, to, 16, at[i], k, 0, 0);
+    };
     const auto request = [&](int k, char *lds) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int row = (i * WAVES + wave) * 8;
-        const auto to = (__attribute__((address_space(3))) void *)(lds + row * MM_STEP);
-        if (i < LOADS_A) __builtin_amdgcn_raw_ptr_buffer_load_lds(resA, to, 16, at[i], k, 0, 0);
-        else if (DUAL && row - BM >= NB) __builtin_amdgcn_raw_ptr_buffer_load_lds(res1, to, 16, at[i], k, 0, 0);
-        else __builtin_amdgcn_raw_ptr_buffer_load_lds(res0, to, 16, at[i], k, 0, 0);
-      }
+      for (int i = 0; i < LOADS; ++i) request_one(i, k, lds);
     };
     // Both halves of a step's fragments are in registers before the workgroup meets in the middle of the step; from there
     // on its place in LDS takes the step STAGES ahead, and the first half of the next step is read under the products of
@@ -200,8 +245,19 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
       fetch(first, lds, 0);
       int now = 0;
       const auto turn = [&](int i, auto loads) {
-        __builtin_amdgcn_sched_barrier(0);
         const int next = now + 1 == STAGES ? 0 : now + 1;
+        if constexpr (IN_PLACE) {
+          mm_weave<T, TM + TN>(first, acc, [&](int k) { fetch_one(second, lds + now * STAGE, 1, k); }, nothing);
+          if (i + STAGES - 1 < steps) mm_sync<(STAGES - 2) * LOADS>();
+          else mm_sync<0>();
+          mm_weave<T, TM + TN>(second, acc, [&](int k) { fetch_one(first, lds + next * STAGE, 0, k); }, [&](int k) {
+            if constexpr (decltype(loads)::value > 0)
+              if (k < LOADS) request_one(k, (i + STAGES) * MM_STEP, lds + now * STAGE);
+          });
+          now = next;
+          return;
+        }
+        __builtin_amdgcn_sched_barrier(0);
         fetch(second, lds + now * STAGE, 1);
         multiply(first);
         interleave(std::integral_constant<int, 0>());
@@ -263,6 +319,9 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
     }
   }
 
+  if constexpr (IN_PLACE)
+#pragma unroll
+    for (int i = 0; i < TM; ++i) mm_settle(acc[i]);
   const int m = m0 + wm * (BM / WGM) + (lane & 15), n = n0 + wn * (NB / WGN) + (lane >> 4) * 4;
   typename Epilogue::Row rows[TM];  // what the epilogue needs to know of them, all requested at once
 #pragma unroll
