@@ -282,25 +282,24 @@ bnn_status gated_backward(const char *x, int64_t x_ld, const char *wg, int64_t w
     gated_gradient_kernel<E><<<blocks(n), 256, 0, s>>>(static_cast<const E *>(dh), dh_ld, saved, (int64_t)T * F, n, F, Fp, grad);
   }
   // the products take columns eight at a time, from rows that start on 16 bytes
-  const auto aligned = [&](const char *&m, int64_t &ld, int64_t rows, int64_t at) {
-    if (D == Dp && mm_dma(m, 2 * ld)) return;
-    E *const to = reinterpret_cast<E *>(workspace + at);
+  const auto fits = [&](const char *m, int64_t ld) { return D == Dp && mm_dma(m, 2 * ld); };
+  const auto realign = [&](const char *&m, int64_t &ld, int64_t rows, int64_t at) {
     const int64_t n = rows * Dp / 8;
     ProfScope ps(KID_REALIGN, s);
-    realign_kernel<E><<<blocks(n), 256, 0, s>>>(reinterpret_cast<const E *>(m), ld, n, D, Dp, to);
+    realign_kernel<E><<<blocks(n), 256, 0, s>>>(reinterpret_cast<const E *>(m), ld, n, D, Dp, reinterpret_cast<E *>(workspace + at));
     m = workspace + at, ld = Dp;
   };
-  aligned(wg, wg_ld, F, g.wg);
-  aligned(wu, wu_ld, F, g.wu);
-  aligned(x, x_ld, T, g.x);
+  const bool as_they_are = fits(wg, wg_ld) && fits(wu, wu_ld) && wg_ld == wu_ld;  // one row stride for both
+  if (!as_they_are) realign(wg, wg_ld, F, g.wg), realign(wu, wu_ld, F, g.wu);
+  if (!fits(x, x_ld)) realign(x, x_ld, T, g.x);
   if (bnn_status st = launch_status()) return st;
   KmOperands p = {};
   p.A = workspace, p.lda = 4ll * Fp, p.segA = Fp;
-  p.B0 = wg, p.B1 = wu, p.ldb0 = 2 * wg_ld, p.ldb1 = 2 * wu_ld;
+  p.B0 = wg, p.B1 = wu, p.ldb = 2 * wg_ld;
   p.M = T, p.N = Dp, p.K = F, p.segments = 2;
   ProductEpilogue<E> epi = {static_cast<E *>(dx), nullptr, dx_ld, 0, T, T, D, nullptr, 0, 0};
   if (bnn_status st = km_product<TY, true>(p, epi, part, s)) return st;
-  p.B0 = p.B1 = x, p.ldb0 = p.ldb1 = 2 * x_ld, p.segA = 0;
+  p.B0 = p.B1 = x, p.ldb = 2 * x_ld, p.segA = 0;
   p.M = 2 * Fp, p.K = T, p.segments = 1;
   epi = {static_cast<E *>(dwg), static_cast<E *>(dwu), dwg_ld, dwu_ld, F, Fp, D, nullptr, 0, 0};
   return km_product<TY, false>(p, epi, part, s);

@@ -9,7 +9,7 @@ namespace bnn {
 // k runs over `segments` stretches of K: stretch s reads B0 or B1, and A from s * segA values of k on.
 struct KmOperands {
   const char *A, *B0, *B1;
-  int64_t lda, ldb0, ldb1;  // bytes between rows
+  int64_t lda, ldb;  // bytes between rows
   int64_t segA;
   int M, N, K, segments;
   int tilesM, tilesN, splits;  // the steps of k are dealt out to `splits` workgroups a tile
@@ -26,15 +26,12 @@ __device__ __forceinline__ int km_turn(int k) {
 
 // 16 bytes a lane from base + at straight to LDS at `to`, lane after lane.  Written out: for the builtin the compiler lets
 // every transposing read wait for all loads in flight (8192 x 4096 by k 16384: 1008 -> 828 us without).  It has no result
-// register, and mm_sync, not the compiler, waits for it; m0 takes a wait state before the load reads it, and keeps what the
-// compiler may have there.
+// register, and mm_sync, not the compiler, waits for it; m0 takes a wait state before the load reads it.  Nothing else in
+// these kernels uses m0 (no builtin load to LDS, no indexed register), so it is not kept.
 __device__ __forceinline__ void km_load(const char *base, int at, uint32_t to) {
   const uint64_t b = reinterpret_cast<uint64_t>(base);
   const v4i res = {(int)(uint32_t)b, (int)((uint32_t)(b >> 32) & 0xffffu), -1, 0x00020000};
-  uint32_t kept;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
-               : "=&s"(kept)
-               : "s"(to), "v"(at), "s"(res));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(res));
 }
 
 template <int TY, int BM, int BN, int WGM, int WGN, int STAGES, bool A_ROWS, class Epilogue>
@@ -61,33 +58,31 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
   using XA = std::integral_constant<int, BM>;
   using XB = std::integral_constant<int, BN>;
   const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
-  int atA[LOADS_A], rowB[LOADS_B], colB[LOADS_B];
+  int atA[LOADS_A], atB[LOADS_B];
 #pragma unroll
   for (int i = 0; i < LOADS_A; ++i)
     atA[i] = A_ROWS ? (int)(min((i * WAVES + wave) * 8 + (lane >> 3), p.M - 1 - m0) * p.lda) + piece
                     : (int)(row_k(i, XA()) * p.lda) + columns(i, XA(), m0, p.M);
 #pragma unroll
-  for (int i = 0; i < LOADS_B; ++i) rowB[i] = row_k(i, XB()), colB[i] = columns(i, XB(), n0, p.N);
+  for (int i = 0; i < LOADS_B; ++i) atB[i] = (int)(row_k(i, XB()) * p.ldb) + columns(i, XB(), n0, p.N);
 
   const char *const baseA = A_ROWS ? p.A + (int64_t)m0 * p.lda : p.A;
   const int whole = p.K / KM_STEP;  // steps of a stretch
-  const auto step_of = [&](int i, const char *&a, const char *&b, int64_t &ldb) {
+  const auto step_of = [&](int i, const char *&a, const char *&b) {
     const int s = i >= whole ? 1 : 0;
     const int64_t k = (int64_t)(i - s * whole) * KM_STEP, ka = k + s * p.segA;
     a = baseA + (A_ROWS ? 2 * ka : ka * p.lda);
-    ldb = s ? p.ldb1 : p.ldb0;
-    b = (s ? p.B1 : p.B0) + k * ldb;
+    b = (s ? p.B1 : p.B0) + k * p.ldb;
   };
   const auto request = [&](int i, char *to, int only = -1) {  // all loads of step i, or one
     const char *a, *b;
-    int64_t ldb;
-    step_of(i, a, b, ldb);
+    step_of(i, a, b);
     const uint32_t dst = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)to + wave * 1024;
 #pragma unroll
     for (int l = 0; l < LOADS; ++l)
       if (only < 0 || l == only) {
         if (l < LOADS_A) km_load(a, atA[l < LOADS_A ? l : 0], dst + l * WAVES * 1024);
-        else km_load(b, rowB[l < LOADS_A ? 0 : l - LOADS_A] * (int)ldb + colB[l < LOADS_A ? 0 : l - LOADS_A], dst + l * WAVES * 1024);
+        else km_load(b, atB[l < LOADS_A ? 0 : l - LOADS_A], dst + l * WAVES * 1024);
       }
   };
 
@@ -164,8 +159,8 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
     u32x4 a[LOADS_A], b[LOADS_B];
   };
   const auto request_rest = [&](Rest &r, int s) {
-    const int64_t k = (int64_t)whole * KM_STEP, ka = k + s * p.segA, ldb = s ? p.ldb1 : p.ldb0;
-    const char *const a = baseA + (A_ROWS ? 2 * ka : ka * p.lda), *const b = (s ? p.B1 : p.B0) + k * ldb;
+    const int64_t k = (int64_t)whole * KM_STEP, ka = k + s * p.segA;
+    const char *const a = baseA + (A_ROWS ? 2 * ka : ka * p.lda), *const b = (s ? p.B1 : p.B0) + k * p.ldb;
     const u32x4 none = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int l = 0; l < LOADS_A; ++l) {
@@ -173,7 +168,7 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
       else r.a[l] = row_k(l, XA()) < left ? *reinterpret_cast<const u32x4 *>(a + atA[l]) : none;
     }
 #pragma unroll
-    for (int l = 0; l < LOADS_B; ++l) r.b[l] = rowB[l] < left ? *reinterpret_cast<const u32x4 *>(b + rowB[l] * ldb + colB[l]) : none;
+    for (int l = 0; l < LOADS_B; ++l) r.b[l] = row_k(l, XB()) < left ? *reinterpret_cast<const u32x4 *>(b + atB[l]) : none;
   };
   constexpr bool HELD = BM * BN < 256 * 256;
   Rest held[2];
@@ -215,6 +210,16 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
       now = next;
     };
     int i = 0;
+    if constexpr (IN_PLACE) {  // both stages' addresses in registers
+      static_assert(STAGES == 2, "");
+      for (; i + 1 + STAGES < steps; i += 2) {
+        now = 0;
+        turn(i, std::integral_constant<int, LOADS>());
+        now = 1;
+        turn(i + 1, std::integral_constant<int, LOADS>());
+      }
+      now = 0;
+    }
     for (; i + STAGES < steps; ++i) turn(i, std::integral_constant<int, LOADS>());
     for (; i + 1 < steps; ++i) turn(i, std::integral_constant<int, 0>());
     fetch(second, now * STAGE, 1);
