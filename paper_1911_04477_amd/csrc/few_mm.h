@@ -109,20 +109,29 @@ bnn_status launch_mm_few(const MmOperands &p, const Epilogue &epi, int kid, hipS
 
 // Which kernel takes a product of more than 16 rows: the cheapest by the rounds of tiles that the compute units go through,
 // in hundredths of a round of 256 x 256 tiles.  `one`: every unit has one tile at most; `two`: a round of two tiles a unit
-// (256 x 256: one at a time).  Measured in 8 bits, k 4096, of 256 x 256 tiles 45 us a round: 128 x 128 tiles 15.4 us a round
-// of one, two a unit 35; 64 x 64 10.0; 64 x 32 and 32 x 32 7.7 (64 to 100 rows by 4096).
+// (256 x 256 and 256 x 128: one at a time).  What the small tiles wait for is their operands' way into LDS, so that times
+// measured in 8 bits at k 4096 hold for 16 bits at k 2048.  In 8 bits, k 4096, by 4096, us:
+//   rows   256x256  256x128  128x128  128x64  64x64  64x32  32x32
+//   2048     45       33       35      42      53
+//    512              25       17      12.7    15     20     25
+//    256              25       17      12       9.8   10.9   12 to 16
+//    100              23       15      11.4     9.2    9.1    9.1
+//     64              23       15      10.6     8.9    8.7    7.8
 struct MmForm {
   int bm, bn, one, two;
 };
-constexpr MmForm MM_FORMS[] = {{256, 256, 100, 200}, {128, 128, 45, 66}, {64, 64, 22, 30}, {64, 32, 17, 25}, {32, 32, 17, 20}};
+enum : int { MM_256, MM_256_128, MM_128, MM_128_64, MM_64, MM_64_32, MM_32, MM_FORM_COUNT };
+constexpr MmForm MM_FORMS[MM_FORM_COUNT] = {{256, 256, 100, 200}, {256, 128, 70, 140}, {128, 128, 45, 74}, {128, 64, 28, 46},
+                                            {64, 64, 22, 32},     {64, 32, 19, 28},    {32, 32, 17, 24}};
 inline int mm_form(int M, int N, bool dual, bool dma) {
   const int64_t units = device_cu_count();
-  int best = 1;
+  int best = MM_128;
   int64_t least = INT64_MAX;
-  for (int f = dma ? 0 : 1; f < (dma ? 5 : 3); ++f) {
+  for (int f = 0; f < MM_FORM_COUNT; ++f) {
+    if (!dma && f != MM_128 && f != MM_64) continue;
     const MmForm &t = MM_FORMS[f];
     const int64_t tiles = (int64_t)((M - 1) / t.bm + 1) * ((N - 1) / (dual ? t.bn / 2 : t.bn) + 1);
-    const int64_t cost = f == 0 ? (tiles + units - 1) / units * t.one : tiles <= units ? t.one : (tiles + 2 * units - 1) / (2 * units) * t.two;
+    const int64_t cost = t.bm == 256 ? (tiles + units - 1) / units * t.one : tiles <= units ? t.one : (tiles + 2 * units - 1) / (2 * units) * t.two;
     if (cost <= least) least = cost, best = f;
   }
   return best;
@@ -133,21 +142,25 @@ bnn_status run_product(const MmOperands &p, const Epilogue &epi, int kid_few, in
   if (p.M <= 16) return launch_mm_few<TY, 1, 8, 4, DUAL>(p, epi, kid_few, s);
   const int form = mm_form(p.M, p.N, DUAL, p.dma);
   if (!p.dma) {
-    if (form == 1) return launch_mm_tile<TY, 128, 128, 2, 2, 2, DUAL, false>(p, epi, kid, s);
+    if (form == MM_128) return launch_mm_tile<TY, 128, 128, 2, 2, 2, DUAL, false>(p, epi, kid, s);
     return launch_mm_tile<TY, 64, 64, 2, 2, 2, DUAL, false>(p, epi, kid, s);
   }
   switch (form) {
-    case 0:  // 128 outputs a thread: what the epilogue does is compiled for the call
+    case MM_256:  // 128 outputs a thread: what the epilogue does is compiled for the call
       return epi.fixed([&](const auto &known) { return launch_mm_tile<TY, 256, 256, 2, 2, 2, DUAL, true>(p, known, kid, s); });
-    case 1: {
+    case MM_256_128: return launch_mm_tile<TY, 256, 128, 4, 2, 3, DUAL, true>(p, epi, kid, s);
+    case MM_128: {
       const int64_t tiles = (int64_t)((p.M - 1) / 128 + 1) * ((p.N - 1) / (DUAL ? 64 : 128) + 1);
-      // one tile a unit: eight waves and four steps ahead (256 x 4096 by 4096 to 8192 gated 61 -> 44 us); else two
+      // one tile a unit: four steps ahead (1024 x 4096 by k 1024 in 8 bits 8.9 us, with two 9.6); else two tiles a unit
+      // (2048 x 4096 by 4096 35 us, 41 with four steps)
       if (tiles <= device_cu_count()) return launch_mm_tile<TY, 128, 128, 2, 4, 4, DUAL, true>(p, epi, kid, s);
-      return launch_mm_tile<TY, 128, 128, 2, 2, 2, DUAL, true>(p, epi, kid, s);
+      return launch_mm_tile<TY, 128, 128, 4, 2, 2, DUAL, true>(p, epi, kid, s);
     }
-    case 2: return launch_mm_tile<TY, 64, 64, 2, 2, 4, DUAL, true>(p, epi, kid, s);
-    case 3: return launch_mm_tile<TY, 64, 32, 4, 1, 5, DUAL, true>(p, epi, kid, s);
-    default: return launch_mm_tile<TY, 32, 32, 2, 1, 8, DUAL, true>(p, epi, kid, s);
+    // eight waves a tile where its columns allow: 256 x 4096 by 4096 in 8 bits takes 9.8 us on 64 x 64, with four waves 11.8
+    case MM_128_64: return launch_mm_tile<TY, 128, 64, 4, 2, 3, DUAL, true>(p, epi, kid, s);
+    case MM_64: return launch_mm_tile<TY, 64, 64, 4, 2, 4, DUAL, true>(p, epi, kid, s);
+    case MM_64_32: return launch_mm_tile<TY, 64, 32, 4, 1, 4, DUAL, true>(p, epi, kid, s);
+    default: return launch_mm_tile<TY, 32, 32, 2, 1, 6, DUAL, true>(p, epi, kid, s);
   }
 }
 

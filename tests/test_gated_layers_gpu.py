@@ -110,7 +110,7 @@ def test_quant_rows_of_special_values(dtype):
 # ---------------------------------------------------------------- int8 linear layer
 LINEAR = [(1, 1, 1), (1, 17, 5), (3, 64, 64), (16, 16, 256), (16, 40, 2321), (17, 33, 100), (64, 65, 129), (50, 1000, 3000), (65, 130, 127),
           (128, 128, 128), (129, 257, 384), (256, 512, 1000), (300, 520, 2064), (513, 1030, 641), (4101, 4105, 144), (2000, 16400, 300),
-          (1, 4096, 4096)]
+          (600, 3000, 400), (1000, 4500, 272), (1, 4096, 4096)]
 
 
 def linear_ref(a, sa, b, sb, bias):
@@ -401,7 +401,7 @@ def act_ref(z, act):
 
 
 GATED = [(1, 1, 1), (1, 40, 17), (3, 200, 64), (16, 64, 33), (17, 65, 130), (64, 520, 100), (65, 127, 129), (128, 128, 256), (200, 1000, 321),
-         (257, 257, 513), (1030, 72, 2100), (4100, 64, 2321)]
+         (257, 257, 513), (1030, 72, 2100), (600, 72, 1500), (4100, 64, 2321)]
 
 
 def gated_inputs(T, D, F, dtype):
