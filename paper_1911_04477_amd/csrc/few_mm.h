@@ -128,7 +128,7 @@ inline int mm_form(int M, int N, bool dual, bool dma) {
   int best = MM_64;
   int64_t least = INT64_MAX;
   for (int f = 0; f < MM_FORM_COUNT; ++f) {
-    if (!dma && f != MM_128_64 && f != MM_64 && f != MM_32) continue;
+    if (!dma && f != MM_256_128 && f != MM_128 && f != MM_64) continue;
     const MmForm &t = MM_FORMS[f];
     const int64_t tiles = (int64_t)((M - 1) / t.bm + 1) * ((N - 1) / (dual ? t.bn / 2 : t.bn) + 1);
     const int64_t cost = t.bm == 256 ? (tiles + units - 1) / units * t.one : tiles <= units ? t.one : (tiles + 2 * units - 1) / (2 * units) * t.two;
@@ -141,10 +141,10 @@ template <int TY, bool DUAL, class Epilogue>
 bnn_status run_product(const MmOperands &p, const Epilogue &epi, int kid_few, int kid, hipStream_t s) {
   if (p.M <= 16) return launch_mm_few<TY, 1, 8, 4, DUAL>(p, epi, kid_few, s);
   const int form = mm_form(p.M, p.N, DUAL, p.dma);
-  if (!p.dma) {  // through registers; 128 x 128 tiles are never faster (4096 x 2321 to 4096 gated, bf16, 364 and 388 us)
-    if (form == MM_128_64) return launch_mm_tile<TY, 128, 64, 4, 2, 2, DUAL, false>(p, epi, kid, s);
-    if (form == MM_64) return launch_mm_tile<TY, 64, 64, 4, 2, 2, DUAL, false>(p, epi, kid, s);
-    return launch_mm_tile<TY, 32, 32, 2, 1, 2, DUAL, false>(p, epi, kid, s);
+  if (!p.dma) {  // through registers
+    if (form == MM_256_128) return launch_mm_tile<TY, 256, 128, 4, 2, 2, DUAL, false>(p, epi, kid, s);
+    if (form == MM_128) return launch_mm_tile<TY, 128, 128, 4, 2, 2, DUAL, false>(p, epi, kid, s);
+    return launch_mm_tile<TY, 64, 64, 4, 2, 2, DUAL, false>(p, epi, kid, s);
   }
   switch (form) {
     case MM_256:  // 128 outputs a thread: what the epilogue does is compiled for the call

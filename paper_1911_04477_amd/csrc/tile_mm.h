@@ -108,6 +108,9 @@ __device__ __forceinline__ void mm_sync() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// This wave's reads and writes of LDS have ended, and every wave of the workgroup is here.
+__device__ __forceinline__ void mm_meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // LDS: rows of 128 bytes, 16-byte piece c of row r in slot c ^ (r % 8), so that the 16 rows of a fragment spread over all
 // banks.  A wave's load fills 8 rows: lane i slot i % 8 of row i / 8.  WGM x WGN waves, each (BM / WGM) x (BN / WGN)
 // outputs; with DUAL half of a wave's columns are B0's and half the same columns of B1.
@@ -287,35 +290,52 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
       whole_step(lds);
     }
   } else {
+    // Two steps in LDS, and the two behind them on their way through registers (four are no faster: the vector caches'
+    // rate for pieces that do not start on 16 bytes bounds this form, so large tiles count more).  4096 x 2321 to 4096 gated,
+    // bf16: with one step on its way 388 us on 128 x 128 tiles, with two 259, on 256 x 128 221.
+    static_assert(STAGES == 2, "");
+    const int steps = K / MM_STEP;
+    const bool rest = steps * MM_STEP < K;
     const char *src[LOADS];
-    u32x4 held[LOADS];
+    u32x4 last[LOADS], held[2][LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) src[i] = source(i);
-    const auto request = [&](int k) {
-      if (k + MM_STEP <= K) {
+    if (rest) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) held[i] = *reinterpret_cast<const u32x4_any *>(src[i] + k + piece);
-      } else {
+      for (int i = 0; i < LOADS; ++i) last[i] = bytes16<E>(src[i], steps * MM_STEP + piece, K);
+    }
+    const auto request = [&](int step, u32x4 (&to)[LOADS]) {  // beyond the last step: that one once more, not used
+      const int k = min(step, steps - 1) * MM_STEP + piece;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) held[i] = bytes16<E>(src[i], k + piece, K);
+      for (int i = 0; i < LOADS; ++i) to[i] = *reinterpret_cast<const u32x4_any *>(src[i] + k);
+    };
+    const auto deliver = [&](const u32x4 (&from)[LOADS], char *lds) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) *room(lds, i) = from[i];
+    };
+    const auto turn = [&](int i, u32x4 (&next)[LOADS], char *now, char *other) {
+      mm_meet();  // step i has arrived, and the other half is free
+      if (i + 1 < steps) {
+        deliver(next, other);
+        request(i + 3, next);
       }
+      whole_step(now);
     };
-    const auto deliver = [&](char *lds) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) *room(lds, i) = held[i];
-    };
-    request(0);
-    deliver(lds);
-    for (int k = 0; k < K; k += 2 * MM_STEP) {
-      __syncthreads();  // step k has arrived, and the other half is free
-      if (k + MM_STEP < K) request(k + MM_STEP);
+    if (steps) {
+      request(0, held[0]);
+      request(1, held[1]);
+      deliver(held[0], lds);
+      request(2, held[0]);
+      for (int i = 0; i < steps; i += 2) {
+        turn(i, held[1], lds, lds + STAGE);
+        if (i + 1 < steps) turn(i + 1, held[0], lds + STAGE, lds);
+      }
+    }
+    if (rest) {
+      mm_meet();
+      deliver(last, lds);
+      mm_meet();
       whole_step(lds);
-      if (k + MM_STEP >= K) break;
-      deliver(lds + STAGE);
-      __syncthreads();
-      if (k + 2 * MM_STEP < K) request(k + 2 * MM_STEP);
-      whole_step(lds + STAGE);
-      if (k + 2 * MM_STEP < K) deliver(lds);
     }
   }
 
