@@ -157,12 +157,13 @@ def _c() -> _Calls:
 
 
 class _Tensors:
-    """Calls from the tensors themselves (csrc/tensorcall.cpp): a status, or None where the call is not a plain one and the
-    function of this module has to look at it.  Where the extension has not been built, or for another torch, every call is of that
-    kind."""
+    """Calls from the tensors themselves (csrc/tensorcall.cpp): a status (the gradients: their tensors, or a status), or None where
+    the call is not a plain one and the function of this module has to look at it.  Where the extension has not been built, or for
+    another torch, every call is of that kind."""
 
     FUNCTIONS = ("gemm", "epilogue", "encode", "conv2d", "conv2d_packed", "im2col", "f32_sign", "conv2d_f32", "maxpool", "fc",
-                 "quant_rows", "linear_i8", "norm_gate", "norm_gate_backward", "gated_ff", "gated_ff_i8", "gated_ff_backward")
+                 "quant_rows", "linear_i8", "norm_gate", "norm_gate_backward", "norm_gate_gradients", "gated_ff", "gated_ff_i8",
+                 "gated_ff_backward", "gated_ff_gradients")
 
     def __init__(self, L: ctypes.CDLL, path: str):
         module = None
@@ -821,6 +822,9 @@ def norm_gate_backward_workspace_bytes(rows: int, D: int, gate_rows: int) -> int
     return int(_c().bnn_norm_gate_backward_workspace_bytes(rows, D, gate_rows))
 
 
+NORM_GRADIENTS = ("dr", "db", "dgate", "dres_scale", "dw_post", "dbias_post", "dw_pre", "dbias_pre")
+
+
 def bnn_norm_gate_backward(b: Optional[torch.Tensor], r: torch.Tensor, dn: Optional[torch.Tensor],
                            dr_out: Optional[torch.Tensor], *, gate: Optional[torch.Tensor] = None, gate_rows: int = 1,
                            res_scale: Optional[torch.Tensor] = None, w_post: Optional[torch.Tensor] = None,
@@ -830,12 +834,18 @@ def bnn_norm_gate_backward(b: Optional[torch.Tensor], r: torch.Tensor, dn: Optio
     """Gradients of bnn_norm_gate from its inputs and those of its outputs (dn of n, dr_out of r'; None: zero), as a dict: dr,
     and, for each of b, gate, res_scale, w_post, bias_post, w_pre and bias_pre that was given, its name with a d before it.
     out: the same dict with tensors to write to, where a caller keeps them."""
+    if out is None and workspace is None:
+        made = _t().norm_gate_gradients(b, r, gate, gate_rows, res_scale, w_post, bias_post, w_pre, bias_pre, NORMS.get(post),
+                                        NORMS.get(pre), eps, dn, dr_out)
+        if made is not None:
+            if type(made) is int:
+                _check(made, "bnn_norm_gate_backward")
+            return {name: t for name, t in zip(NORM_GRADIENTS, made) if t is not None}
     if r.dim() != 2:
         raise ValueError("r: a matrix expected")
     rows, D = r.shape
     got = dict(out or {})
-    wanted = {"dr": r, "db": b, "dgate": gate, "dres_scale": res_scale, "dw_post": w_post, "dbias_post": bias_post,
-              "dw_pre": w_pre, "dbias_pre": bias_pre}
+    wanted = dict(zip(NORM_GRADIENTS, (r, b, gate, res_scale, w_post, bias_post, w_pre, bias_pre)))
     for name, of in wanted.items():
         if of is None:
             got.pop(name, None)
@@ -934,6 +944,12 @@ def bnn_gated_ff_backward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, s
                           dx: Optional[torch.Tensor] = None, dwg: Optional[torch.Tensor] = None,
                           dwu: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """(dx, dwg, dwu) from the operands of bnn_gated_ff, what it saved, and dh [T, F]."""
+    if dx is None and dwg is None and dwu is None and workspace is None:
+        made = _t().gated_ff_gradients(x, wg, wu, saved, dh)
+        if made is not None:
+            if type(made) is int:
+                _check(made, "bnn_gated_ff_backward")
+            return made
     if x.dim() != 2 or wg.dim() != 2:
         raise ValueError("x, wg: matrices expected")
     dx, dwg, dwu = (torch.empty(of.shape, dtype=x.dtype, device=x.device) if t is None else t

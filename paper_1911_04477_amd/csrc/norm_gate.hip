@@ -186,14 +186,14 @@ __global__ __launch_bounds__(MAXT, NV > 1 || CENTRED ? 2 : 3) void norm_gate_bac
   constexpr bool NEAR = WIDTH <= 8192;
   constexpr int SUMS = 6, MEM = 8 * 16;
   __shared__ __attribute__((aligned(16))) uint32_t lds[2 * MEM];
-  __shared__ __attribute__((aligned(16))) float near_[3][NEAR ? WIDTH : 4];  // w_post, w_pre, res_scale
-  const int D = p.D;
+  extern __shared__ __attribute__((aligned(16))) float near_[];  // w_post, w_pre, res_scale: as many as the teams' threads take
+  const int D = p.D, width = (BLOCK ? blockDim.x : 64) * NV * 8;
   const float per = 1.0f / (float)D;
   if constexpr (NEAR) {
     const float *from[3] = {p.w_post, p.w_pre, p.res_scale};
 #pragma unroll
     for (int k = 0; k < 3; ++k)
-      for (int c = threadIdx.x; c < WIDTH; c += blockDim.x) near_[k][c] = c >= D ? 0.0f : from[k] ? from[k][c] : 1.0f;
+      for (int c = threadIdx.x; c < width; c += blockDim.x) near_[k * width + c] = c >= D ? 0.0f : from[k] ? from[k][c] : 1.0f;
   }
   clear_words(lds);
   const int T = BLOCK ? blockDim.x : 64, t = BLOCK ? threadIdx.x : threadIdx.x & 63, c0 = t * 8;
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(MAXT, NV > 1 || CENTRED ? 2 : 3) void norm_gate_bac
   };
   const auto vector = [&](float (&v)[8], int k, int i) {
     if constexpr (NEAR) {
-      const float *from = &near_[k][c0 + i * T * 8];
+      const float *from = &near_[k * width + c0 + i * T * 8];
       const f32x4 lo = *reinterpret_cast<const f32x4 *>(from), hi = *reinterpret_cast<const f32x4 *>(from + 4);
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
@@ -577,7 +577,8 @@ extern "C" bnn_status bnn_norm_gate_backward(const bnn_norm_gate_in *in, const v
       using E = decltype(e);
       using R = decltype(r);
       const auto run = [&](auto plain, auto with_means, auto ragged, int block, int teams) {
-        (edge != EDGE_WHOLE ? ragged : centred ? with_means : plain)<<<(uint32_t)((plan.workers - 1) / teams + 1), block, 0, s>>>(in_groups, q);
+        const size_t near_bytes = p.D <= 8192 ? 3 * sizeof(float) * (size_t)(p.D <= 512 ? 512 : p.D <= 4096 ? row_threads(p.D, 1) * 8 : row_threads(p.D, 2) * 16) : 0;
+        (edge != EDGE_WHOLE ? ragged : centred ? with_means : plain)<<<(uint32_t)((plan.workers - 1) / teams + 1), block, near_bytes, s>>>(in_groups, q);
       };
       if (edge == EDGE_SMALL)
         run(BNN_SMALL(norm_gate_backward_kernel), BNN_SMALL(norm_gate_backward_kernel), BNN_SMALL(norm_gate_backward_kernel), 256, 4);

@@ -2,7 +2,8 @@
 //
 // A layer on a few thousand values is a launch of 2.4 us, and checking and converting its tensors through Python's attribute
 // calls (about 50 ns each, 20 to 30 of them) was 1.6 to 2 us beside it.  Here it is 0.2: one call from the binding with the
-// tensors themselves.  Each function returns the status of the call, or None for anything but the plain case (tensors of
+// tensors themselves.  Each function returns the status of the call (the
+// two of gradients their tensors, where the call went through), or None for anything but the plain case (tensors of
 // the binding's types on the GPU, given outputs, integers, pairs of integers); the binding's own code then takes the call,
 // and raises what it raises.  bind(): addresses of the library's functions, in the order of `names`.  built_for: the torch and the
 // Python of whose objects this file's accessors know the layout; the binding uses it with no other.
@@ -12,6 +13,7 @@
 #include <cstring>
 
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
 
 #include "bnn.h"
@@ -36,10 +38,13 @@ struct Library {
   decltype(&bnn_gated_ff) gated;
   decltype(&bnn_gated_ff_i8) gated_i8;
   decltype(&bnn_gated_ff_backward) gated_backward;
+  decltype(&bnn_norm_gate_backward_workspace_bytes) norm_workspace;
+  decltype(&bnn_gated_ff_backward_workspace_bytes) gated_workspace;
 };
 constexpr const char *names[] = {"bnn_xnor_gemm", "bnn_xnor_gemm_epilogue", "bnn_encode", "bnn_conv2d", "bnn_conv2d_packed",
                                  "bnn_im2col_packed", "bnn_conv2d_f32_sign", "bnn_conv2d_f32", "bnn_maxpool2x2", "bnn_fc_f32", "bnn_quant_rows_i8", "bnn_linear_i8",
-                                 "bnn_norm_gate", "bnn_norm_gate_backward", "bnn_gated_ff", "bnn_gated_ff_i8", "bnn_gated_ff_backward"};
+                                 "bnn_norm_gate", "bnn_norm_gate_backward", "bnn_gated_ff", "bnn_gated_ff_i8", "bnn_gated_ff_backward",
+                                 "bnn_norm_gate_backward_workspace_bytes", "bnn_gated_ff_backward_workspace_bytes"};
 Library lib = {};
 
 struct Other {};  // not the plain case
@@ -422,6 +427,52 @@ PyObject *norm_gate_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// Room for a call of its own, and its results: eight tensors made one by one from Python are 14 us, here 5.
+at::Tensor room(size_t bytes, const at::Tensor &on) {
+  return at::empty({(int64_t)std::max<size_t>(bytes, 16)}, on.options().dtype(at::kByte));
+}
+at::Tensor like(const at::Tensor &t) { return at::empty(t.sizes(), t.options(), at::MemoryFormat::Contiguous); }
+
+// The tensors of a call that went through, None for those that are not there; else its status.
+template <size_t N>
+PyObject *results(PyObject *status, const at::Tensor (&made)[N]) {
+  if (!status || PyLong_AsLong(status) != BNN_OK) return status;
+  Py_DECREF(status);
+  PyObject *const all = PyTuple_New(N);
+  if (!all) return nullptr;
+  for (size_t i = 0; i < N; ++i) {
+    PyObject *const o = made[i].defined() ? THPVariable_Wrap(made[i]) : Py_NewRef(Py_None);
+    if (!o) {
+      Py_DECREF(all);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(all, i, o);
+  }
+  return all;
+}
+
+// norm_in's, dn, dr_out -> dr, db, dgate, dres_scale, dw_post, dbias_post, dw_pre, dbias_pre
+PyObject *norm_gate_gradients(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 14, [&](Args &v) {
+    at::ScalarType type, r_type;
+    const bnn_norm_gate_in in = norm_in(v, type, r_type);
+    const Matrix dn = matrix(v.tensor_or_none(), type, in.rows, in.D), dro = matrix(v.tensor_or_none(), r_type, in.rows, in.D);
+    constexpr int of[] = {1, 0, 2, 4, 5, 6, 7, 8};  // whose gradient each is
+    at::Tensor made[8];
+    void *p[8];
+    for (int i = 0; i < 8; ++i) {
+      if (a[of[i]] != Py_None) made[i] = like(THPVariable_Unpack(a[of[i]]));
+      p[i] = made[i].defined() ? made[i].data_ptr() : nullptr;
+    }
+    const size_t bytes = lib.norm_workspace(in.rows, in.D, in.gate_rows);
+    const at::Tensor ws = room(bytes, made[0]);
+    return results(launch([&](void *s) {
+      return lib.norm_backward(&in, dn.p, dn.ld, dro.p, dro.ld, p[0], in.D, p[1], in.D, p[2], in.D, f32(p[3]), f32(p[4]), f32(p[5]), f32(p[6]),
+                               f32(p[7]), ws.data_ptr(), bytes, s);
+    }), made);
+  });
+}
+
 float *saved_of(const at::Tensor *t, int64_t T, int64_t F) {
   if (!t) return nullptr;
   if (!t->is_cuda() || t->scalar_type() != kFloat || t->dim() != 3 || t->size(0) != 2 || t->size(1) != T || t->size(2) != F || !t->is_contiguous())
@@ -485,6 +536,28 @@ PyObject *gated_ff_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {  // 
   });
 }
 
+PyObject *gated_ff_gradients(PyObject *, PyObject *const *a, Py_ssize_t n) {  // x, wg, wu, saved, dh -> dx, dwg, dwu
+  return guarded(a, n, 5, [](Args &v) {
+    const at::Tensor &tx = v.tensor(), &tg = v.tensor(), &tu = v.tensor();
+    const at::ScalarType type = tx.scalar_type();
+    const Matrix x = matrix(tx, type), wg = matrix(tg, type);
+    if (wg.cols != x.cols) throw Other();
+    const int64_t T = x.rows, D = x.cols, F = wg.rows;
+    const Matrix wu = matrix(tu, type, F, D);
+    const float *const saved = saved_of(&v.tensor(), T, F);
+    const Matrix dh = matrix(v.tensor(), type, T, F);
+    const int code = float_type(type);
+    const at::Tensor made[3] = {like(tx), like(tg), like(tu)};
+    const size_t bytes = lib.gated_workspace(T, D, F);
+    const at::Tensor ws = room(bytes, tx);
+    void *const p[3] = {made[0].data_ptr(), made[1].data_ptr(), made[2].data_ptr()};
+    return results(launch([&](void *s) {
+      return lib.gated_backward(x.p, x.ld, wg.p, wg.ld, wu.p, wu.ld, code, T, D, F, saved, dh.p, dh.ld, p[0], D, p[1], D, p[2], D,
+                                ws.data_ptr(), bytes, s);
+    }), made);
+  });
+}
+
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
   constexpr Py_ssize_t want = sizeof(Library) / sizeof(void *);
   static_assert(want == sizeof(names) / sizeof(names[0]), "an address for every name");
@@ -508,8 +581,8 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyMethodDef methods[] = {BNN_METHOD(bind), BNN_METHOD(gemm), BNN_METHOD(epilogue), BNN_METHOD(encode), BNN_METHOD(conv2d),
                          BNN_METHOD(conv2d_packed), BNN_METHOD(im2col), BNN_METHOD(f32_sign), BNN_METHOD(conv2d_f32),
                          BNN_METHOD(maxpool), BNN_METHOD(fc), BNN_METHOD(quant_rows), BNN_METHOD(linear_i8),
-                         BNN_METHOD(norm_gate), BNN_METHOD(norm_gate_backward), BNN_METHOD(gated_ff), BNN_METHOD(gated_ff_i8),
-                         BNN_METHOD(gated_ff_backward), {nullptr, nullptr, 0, nullptr}};
+                         BNN_METHOD(norm_gate), BNN_METHOD(norm_gate_backward), BNN_METHOD(norm_gate_gradients), BNN_METHOD(gated_ff), BNN_METHOD(gated_ff_i8),
+                         BNN_METHOD(gated_ff_backward), BNN_METHOD(gated_ff_gradients), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensorcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -572,3 +572,24 @@ def test_refusals_of_the_binding():
             (B.BnnError, lambda: B.bnn_norm_gate(x, x, q_out=q))):
         with pytest.raises(error):
             call()
+
+
+@pytest.mark.parametrize("post,pre,gate,vectors,dtype,rtype", NORM_KINDS)
+def test_gradients_made_by_the_call_itself(post, pre, gate, vectors, dtype, rtype, monkeypatch):
+    """The same tensors as where the binding makes room for them."""
+    g = gen(post, pre)
+    b, r, s = norm_inputs(g, 37, 200, dtype, rtype, post, pre, gate, vectors)
+    dn = None if pre == "none" else strided(normal(g, 37, 200).to(dtype), 8)
+    dr_out = strided(normal(g, 37, 200).to(rtype), 3)
+    x, wg, wu, dh = gated_inputs(20, 72, 40, BF16)
+    saved = B.gated_ff_saved(20, 40, DEV)
+    B.bnn_gated_ff(strided(x, 8), wg, strided(wu, 16), saved=saved)
+    norm = lambda: B.bnn_norm_gate_backward(b, r, dn, dr_out, **s)
+    gated = lambda: dict(enumerate(B.bnn_gated_ff_backward(strided(x, 8), wg, strided(wu, 16), saved, dh)))
+    got = norm(), gated()
+    for name in ("norm_gate_gradients", "gated_ff_gradients"):
+        monkeypatch.setattr(B._t(), name, lambda *args: None)
+    for a, c in zip(got, (norm(), gated())):
+        assert list(a) == list(c)
+        for k in a:
+            assert a[k].dtype == c[k].dtype and a[k].stride() == c[k].stride() and torch.equal(a[k], c[k]), k
