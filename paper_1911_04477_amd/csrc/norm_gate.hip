@@ -438,10 +438,11 @@ constexpr int NORM_MAX_D = 16384;
 struct NormPlan {
   int workers, per, segments;
 };
-// About as many teams as the card has room for; each takes contiguous rows, of one group where a gate is shared by more rows
-// than that, else of whole groups.
-inline NormPlan norm_plan(int64_t rows, int D, int64_t gate_rows) {
-  const int64_t waves = (D + 511) / 512, room = 256 * std::max<int64_t>(1, 12 / waves);  // three waves a SIMD have room
+// As many teams as run at once, about; each takes contiguous rows, of one group where a gate is shared by more rows than
+// that, else of whole groups.  at_once: waves of the kernel that a compute unit has registers for.
+constexpr int NORM_WAVES = 12, NORM_WAVES_CENTRED = 8;
+inline NormPlan norm_plan(int64_t rows, int D, int64_t gate_rows, int at_once) {
+  const int64_t waves = (D + 511) / 512, room = 256 * std::max<int64_t>(1, at_once / waves);
   int64_t per = (rows - 1) / room + 1;
   if (gate_rows > rows) gate_rows = rows;
   if (gate_rows > per) {
@@ -534,7 +535,7 @@ extern "C" bnn_status bnn_norm_gate(const bnn_norm_gate_in *in, void *r_out, int
 extern "C" size_t bnn_norm_gate_backward_workspace_bytes(int64_t rows, int D, int64_t gate_rows) {
   using namespace bnn;
   if (rows <= 0 || D <= 0 || D > NORM_MAX_D || rows > INT32_MAX || gate_rows < 0) return 0;
-  return sizeof(float) * 6 * (size_t)norm_plan(rows, D, gate_rows).workers * (size_t)D;
+  return sizeof(float) * 6 * (size_t)norm_plan(rows, D, gate_rows, NORM_WAVES).workers * (size_t)D;  // no other plan has more
 }
 
 extern "C" bnn_status bnn_norm_gate_backward(const bnn_norm_gate_in *in, const void *dn, int64_t dn_ld, const void *dr_out,
@@ -559,7 +560,9 @@ extern "C" bnn_status bnn_norm_gate_backward(const bnn_norm_gate_in *in, const v
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (p.rows > 0) {
     if (!p.r || !dr || (p.b && !db)) return BNN_ERR_NULL;
-    const NormPlan plan = norm_plan(p.rows, p.D, p.gate ? p.gate_rows : 0);
+    const bool centred = has_means(p);
+    const RowEdge edge = row_edge(p.D);
+    const NormPlan plan = norm_plan(p.rows, p.D, p.gate ? p.gate_rows : 0, centred || edge != EDGE_WHOLE ? NORM_WAVES_CENTRED : NORM_WAVES);
     q.dn = dn, q.dr_out = dr_out, q.dn_ld = dn_ld, q.dr_out_ld = dr_out_ld;
     q.dr = dr, q.db = db, q.dgate = dgate, q.dr_ld = dr_ld, q.db_ld = db_ld, q.dgate_ld = dgate_ld;
     q.workers = plan.workers, q.per = plan.per, q.segments = plan.segments;
@@ -571,8 +574,6 @@ extern "C" bnn_status bnn_norm_gate_backward(const bnn_norm_gate_in *in, const v
     q.part = static_cast<float *>(workspace);
     const bnn_norm_gate_in in_groups = cut_groups(p);
     ProfScope ps(KID_NORM_GATE_BACKWARD, s);
-    const bool centred = has_means(p);
-    const RowEdge edge = row_edge(p.D);
     with_norm(p, [&](auto e, auto r) {
       using E = decltype(e);
       using R = decltype(r);
