@@ -92,6 +92,8 @@ struct GatedEpilogue {
         o[i] = activation<false>(act, g[i], none) * u[i];
       }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm("" : "+v"(o[i]));  // h rounds the fp32 product in every form: no product and conversion in one
     store4(h + m * ldh, n, N, o);
   }
   template <class F>

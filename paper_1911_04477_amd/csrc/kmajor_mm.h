@@ -249,14 +249,18 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
   if constexpr (IN_PLACE)
 #pragma unroll
     for (int i = 0; i < TM; ++i) mm_settle(acc[i]);
-  const int m = m0 + wm * (BM / WGM) + (lane & 15), n = n0 + wn * (BN / WGN) + (lane >> 4) * 4;
+  const int m = m0 + wm * (BM / WGM) + (lane & 7), n = n0 + wn * (BN / WGN) + (lane & 8) * 2 + (lane >> 4) * 4;
+  static_assert(TN % 2 == 0, "");
 #pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    if (n + j * 16 >= p.N) continue;
+  for (int j = 0; j < TN; j += 2)
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
-      if (m + i * 16 < p.M) epi(m + i * 16, n + j * 16, p.N, split, acc[i][j]);
-  }
+    for (int i = 0; i < TM; ++i) {
+      Acc x[2] = {acc[i][j], acc[i][j + 1]};
+      mm_longer(x);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (n + j * 16 < p.N && m + i * 16 + h * 8 < p.M) epi(m + i * 16 + h * 8, n + j * 16, p.N, split, x[h]);
+    }
 }
 
 template <int TY, int BM, int BN, int WGM, int WGN, int STAGES, bool A_ROWS, class Epilogue>

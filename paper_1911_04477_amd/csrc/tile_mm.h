@@ -89,6 +89,27 @@ __device__ __forceinline__ void mm_weave(const Half &has, Acc (&acc)[8][8], cons
   }
 }
 
+// Two neighbouring tiles of 16 x 16 sums, four columns of row l % 16 a lane, as rows 0 to 7 and 8 to 15 of 16 x 32, row l % 8
+// a lane: lanes 8 to 15 of a row of sixteen trade their first tile's sums for the second's of the lanes eight below.  A store
+// then covers twice as much of each row: 32 columns of fp32 are a whole cache line (8192 x 4096 to 8192 gated with what its
+// backward pass needs 944 -> 861 us, 7039 x 256 to 14336 483 -> 356).
+__device__ __forceinline__ void mm_longer(int &a, int &b) {
+  const int low = a;
+  a = __builtin_amdgcn_update_dpp(a, b, 0x128, 0xf, 0xc, false);  // turned by eight lanes, written in the upper eight
+  b = __builtin_amdgcn_update_dpp(b, low, 0x128, 0xf, 0x3, false);  // in the lower eight
+}
+template <class Acc>
+__device__ __forceinline__ void mm_longer(Acc (&x)[2]) {
+  if constexpr (sizeof(Acc) % sizeof(int) == 0) {
+    constexpr int N = sizeof(Acc) / sizeof(int);
+    int a[N], b[N];
+    __builtin_memcpy(a, &x[0], sizeof(Acc)), __builtin_memcpy(b, &x[1], sizeof(Acc));
+#pragma unroll
+    for (int i = 0; i < N; ++i) mm_longer(a[i], b[i]);
+    __builtin_memcpy(&x[0], a, sizeof(Acc)), __builtin_memcpy(&x[1], b, sizeof(Acc));
+  }  // else of no constants
+}
+
 // Tiles in an order in which the workgroups that run at the same time on one XCD (ids go round the eight of them) read few
 // different rows: each XCD has a contiguous share of the tiles, and goes through it in bands of 8 tile rows.
 __device__ __forceinline__ void mm_tile(int id, int tilesM, int tilesN, int &tm, int &tn) {
@@ -190,7 +211,7 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
       multiply(f);
     }
   };
-  // Reads of LDS and requests between matrix instructions, not all in front of them (8192^3 bf16 841 -> 818 us).
+  // Reads of LDS and requests between matrix instructions, not all in front of them (8192^3 bf16 on eight waves 841 -> 818 us).
   constexpr int PER = TM * TN / (TM + TN) ? TM * TN / (TM + TN) : 1;
   const auto interleave = [&](auto loads) {
     constexpr int N = decltype(loads)::value;
@@ -342,19 +363,52 @@ __device__ __forceinline__ void mm_tile_product(const MmOperands &p, const Epilo
   if constexpr (IN_PLACE)
 #pragma unroll
     for (int i = 0; i < TM; ++i) mm_settle(acc[i]);
-  const int m = m0 + wm * (BM / WGM) + (lane & 15), n = n0 + wn * (NB / WGN) + (lane >> 4) * 4;
-  typename Epilogue::Row rows[TM];  // what the epilogue needs to know of them, all requested at once
+  constexpr int JT = DUAL ? TN / 2 : TN;
+  if constexpr (JT % 2 == 0) {
+    const int m = m0 + wm * (BM / WGM) + (lane & 7), n = n0 + wn * (NB / WGN) + (lane & 8) * 2 + (lane >> 4) * 4;
+    typename Epilogue::Row rows[TM];  // what the epilogue needs to know of them, all requested at once
 #pragma unroll
-  for (int i = 0; i < TM; ++i) rows[i] = epi.row(min(m + i * 16, p.M - 1));
+    for (int i = 0; i < TM; ++i) rows[i] = epi.row(min(m + (lane & 8) + i * 16, p.M - 1));
 #pragma unroll
-  for (int j = 0; j < (DUAL ? TN / 2 : TN); ++j) {
-    if (n + j * 16 >= p.N) continue;
-    const auto columns = epi.columns(n + j * 16, p.N);
+    for (int j = 0; j < JT; j += 2) {
+      const int nj = n + j * 16;
+      const bool inside = nj < p.N;
+      const auto columns = epi.columns(inside ? nj : 0, p.N);
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      if (m + i * 16 >= p.M) continue;
-      if constexpr (DUAL) epi(m + i * 16, n + j * 16, p.N, rows[i], columns, acc[i][j], acc[i][TN / 2 + j]);
-      else epi(m + i * 16, n + j * 16, p.N, rows[i], columns, acc[i][j]);
+      for (int i = 0; i < TM; ++i) {
+        Acc x[2] = {acc[i][j], acc[i][j + 1]}, y[2];
+        typename Epilogue::Row of[2] = {rows[i], rows[i]};
+        mm_longer(x);
+        mm_longer(of);
+        if constexpr (DUAL) {
+          y[0] = acc[i][JT + j], y[1] = acc[i][JT + j + 1];
+          mm_longer(y);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int mi = m + i * 16 + h * 8;
+          if (!inside || mi >= p.M) continue;
+          if constexpr (DUAL) epi(mi, nj, p.N, of[h], columns, x[h], y[h]);
+          else epi(mi, nj, p.N, of[h], columns, x[h]);
+        }
+        if constexpr (IN_PLACE) __builtin_amdgcn_sched_barrier(0);  // one pair's registers at a time
+      }
+    }
+  } else {
+    const int m = m0 + wm * (BM / WGM) + (lane & 15), n = n0 + wn * (NB / WGN) + (lane >> 4) * 4;
+    typename Epilogue::Row rows[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) rows[i] = epi.row(min(m + i * 16, p.M - 1));
+#pragma unroll
+    for (int j = 0; j < JT; ++j) {
+      if (n + j * 16 >= p.N) continue;
+      const auto columns = epi.columns(n + j * 16, p.N);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        if (m + i * 16 >= p.M) continue;
+        if constexpr (DUAL) epi(m + i * 16, n + j * 16, p.N, rows[i], columns, acc[i][j], acc[i][JT + j]);
+        else epi(m + i * 16, n + j * 16, p.N, rows[i], columns, acc[i][j]);
+      }
     }
   }
 }
