@@ -10,7 +10,7 @@
 namespace bnn {
 
 // The normal distribution's function: erfc by Abramowitz and Stegun 7.1.26 (absolute error of at most 1.5e-7, so of a GELU
-// of z 0.75e-7 |z|), with the density exp(-z^2 / 2) that it contains.  (erfcf: 1000 x 1024 to 2321 24.8 us instead of 21.)
+// of z 0.75e-7 |z|), with the density exp(-z^2 / 2) that it contains.  (With erfcf 1000 x 1024 to 2321 takes 3.8 us more.)
 __device__ __forceinline__ float normal_function(float z, float &density) {
   constexpr float LOG2E = 1.44269504088896341f;
   const float x = fabsf(z) * 0.70710678118654752f;
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256) void product_sums_kernel(ProductEpilogue<E> ep
 }
 
 // Gradients of the projections, dG = dh * saved[0] and dU = dh * saved[1], side by side in rows of 2 Fp (zeros beside F):
-// eight values a thread.  Bound by memory (14 B a value).
+// eight values a thread.  Bound by memory (14 B a value; 8192 x 8192 168 us, 5.6 TB/s).
 template <class E>
 __global__ __launch_bounds__(256) void gated_gradient_kernel(const E *dh, int64_t ldh, const float *saved, int64_t plane, int64_t groups,
                                                              int F, int Fp, E *out) {

@@ -1,6 +1,7 @@
 // Matrix-core product of 16-bit operands whose k axis runs down the rows of memory, out[m][n] = sum over k of
 // A(k, m) * B[k][n] with A in rows of k (the gradient of an input from a weight) or k-major as B is (the gradient of a
 // weight from an input): no transposed copy is made, the transposing read of LDS turns rows of k into fragments.
+// bf16, 8192 x 4096 by k 16384 and 16384 x 4096 by k 8192: 790 to 800 us, 1370 to 1390 TFLOP/s, matrix units busy 71 and 69 %.
 #pragma once
 #include "tile_mm.h"
 
@@ -25,7 +26,7 @@ __device__ __forceinline__ int km_turn(int k) {
 }
 
 // 16 bytes a lane from base + at straight to LDS at `to`, lane after lane.  Written out: for the builtin the compiler lets
-// every transposing read wait for all loads in flight (8192 x 4096 by k 16384: 1008 -> 828 us without).  It has no result
+// every transposing read wait for all loads in flight (8192 x 4096 by k 16384, eight waves: 1008 -> 828 us without).  It has no result
 // register, and mm_sync, not the compiler, waits for it; m0 takes a wait state before the load reads it.  Nothing else in
 // these kernels uses m0 (no builtin load to LDS, no indexed register), so it is not kept.
 __device__ __forceinline__ void km_load(const char *base, int at, uint32_t to) {

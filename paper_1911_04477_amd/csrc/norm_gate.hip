@@ -99,7 +99,7 @@ __device__ __forceinline__ int64_t norm_group(const bnn_norm_gate_in &p, int64_t
 
 // A team (a wave, or with BLOCK a workgroup) takes a row at a time, NV pieces of eight values a thread; all that a row needs
 // is requested before its first sum.  CENTRED: a norm with a mean or a bias takes part.  Bound by memory (8192 x 4096 bf16
-// with a gate a token 74 us, 4.5 TB/s), a few rows by the chain of request, sum, sum.
+// with a gate a token 68 us, 4.9 TB/s), a few rows by the chain of request, sum, sum.
 template <class E, class R, bool BLOCK, int MAXT, int NV, bool CENTRED, int EDGE>
 __global__ __launch_bounds__(MAXT) void norm_gate_kernel(bnn_norm_gate_in p, NormOut o, int teams) {
   __shared__ uint32_t lds[2 * 5 * 16];
@@ -178,7 +178,8 @@ __global__ __launch_bounds__(MAXT) void norm_gate_kernel(bnn_norm_gate_in p, Nor
 // Teams walk through contiguous rows and keep the sums over rows in registers; the sums of all teams meet in
 // norm_gate_sums_kernel, in the same order at every call.  A row's loads are in flight while the row before is worked on,
 // and its first sum is taken along with that row's last: between rms norms a row meets twice (8192 x 4096 bf16, a workgroup
-// a unit: 214 us without either, 173 with the loads ahead).  The vectors are in LDS, where there is room.  CENTRED: a norm
+// a unit: 214 us without either, 173 with the loads ahead; with all of it 125, and 5 for the sums, 4.1 TB/s).  The vectors are
+// in LDS, where there is room.  Values a thread: 8, since with 16 the sums and two rows no longer fit the registers (142 us).  CENTRED: a norm
 // with a mean or a bias takes part.
 template <class E, class R, bool BLOCK, int MAXT, int NV, bool CENTRED, int EDGE>
 __global__ __launch_bounds__(MAXT, NV > 1 || CENTRED ? 2 : 3) void norm_gate_backward_kernel(bnn_norm_gate_in p, NormGrad q) {
