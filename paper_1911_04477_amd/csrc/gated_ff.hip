@@ -210,7 +210,7 @@ constexpr int64_t MAX_DIM = (1 << 22) - 64;  // in bytes and doubled, 32 bits
 
 // Which kernel takes a k-major product, and into how many shares its k is split: the cheapest by microseconds a step and a
 // round of tiles, what a round costs beside its steps, and the shares' way through memory.  Measured in bf16: 256 x 256
-// tiles 8192 x 4096 by k 16384 799 us, 16384 x 4096 by k 256 93; 128 x 128 with one tile a unit 256 x 4096 by k 16384 in
+// tiles 8192 x 4096 by k 16384 799 us, 16384 x 4096 by k 256 72; 128 x 128 with one tile a unit 256 x 4096 by k 16384 in
 // four shares 39, 1000 x 1024 by k 4642 in four 18; two a unit 1040 and 62; 64 x 64 one a unit 30 (1000 x 1024), two 101.
 struct KmPlan {
   int form, shares;
@@ -219,11 +219,11 @@ inline KmPlan km_plan(int64_t M, int64_t N, int64_t steps) {
   constexpr struct {
     int tile, slots;
     double step, round;
-  } forms[] = {{256, 256, 1.5, 17.0}, {128, 256, 0.6, 4.0}, {128, 512, 1.016, 3.6}, {64, 256, 0.4, 1.5}, {64, 512, 0.55, 1.5}};
+  } forms[] = {{256, 256, 1.5, 11.5}, {128, 256, 0.6, 4.0}, {128, 512, 1.016, 3.6}, {64, 256, 0.4, 1.5}, {64, 512, 0.55, 1.5}};
   KmPlan best = {0, 1};
   double least = 1e300;
   for (int f = 0; f < 5; ++f)
-    for (int shares = 1; shares <= 32 && (shares == 1 || shares * 4 <= steps); shares *= 2) {
+    for (int shares = 1; shares <= 32 && (shares == 1 || shares * 4 <= steps); ++shares) {
       const double tiles = (double)((M - 1) / forms[f].tile + 1) * (double)((N - 1) / forms[f].tile + 1) * shares;
       if (f % 2 && tiles > forms[f].slots) continue;  // one tile a unit
       const double rounds = std::ceil(tiles / forms[f].slots);
