@@ -149,6 +149,14 @@ BNN_API int bnn_testing_conv_image(int N, int C, int H, int W, int D, int kH, in
  * waves; -1 for invalid arguments.  Host only, launches nothing. */
 BNN_API int bnn_testing_first_sign(int N, int H, int W, int D, int sH, int sW, int pH, int pW, int units);
 
+/* How bnn_gated_ff_backward takes a problem.  values receives
+ *   0 the kernel of the product that gives dx: 0 256 x 256 tiles, 1, 2 128 x 128 with one or two tiles a compute unit, 3, 4 64 x 64 the same
+ *   1 into how many shares its k is split   2, 3 the same of the products that give dwg and dwu
+ *   4 the largest offset, in bytes from a tile's first row, at which the first product reads the projections' gradients.
+ * 0, or -1 for sizes that are refused or empty.  Host only, launches nothing. */
+#define BNN_TESTING_GATED_PLAN_VALUES 5
+BNN_API int bnn_testing_gated_backward_plan(int64_t T, int64_t D, int64_t F, int64_t *values);
+
 #ifdef __cplusplus
 }
 #endif

@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "bnn_testing.h"
 #include "few_mm.h"
 #include "kmajor_mm.h"
 #include "rows.h"
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(E *y, int64_t ld, int64_
 inline bool half_type(int t) { return t == BNN_BF16 || t == BNN_F16; }
 inline bool act_known(int a) { return a >= BNN_ACT_SILU && a <= BNN_ACT_RELU; }
 inline int64_t pad(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
-constexpr int64_t MAX_DIM = (1 << 22) - 64;  // in bytes and doubled, 32 bits
+constexpr int64_t MAX_DIM = (1 << 22) - 64;  // km_at: 255 rows of two projections' gradients within 32 bits
 
 // Which kernel takes a k-major product, and into how many shares its k is split: the cheapest by microseconds a step and a
 // round of tiles, what a round costs beside its steps, and the shares' way through memory.  Measured in bf16: 256 x 256
@@ -393,4 +394,15 @@ extern "C" bnn_status bnn_gated_ff_backward(const void *x, int64_t x_ld, const v
   const auto run = type == BNN_BF16 ? gated_backward<MM_BF16> : gated_backward<MM_F16>;
   return run(static_cast<const char *>(x), x_ld, static_cast<const char *>(wg), wg_ld, static_cast<const char *>(wu), wu_ld, saved,
              dh, dh_ld, (int)T, (int)D, (int)F, dx, dx_ld, dwg, dwg_ld, dwu, dwu_ld, static_cast<char *>(workspace), s);
+}
+
+extern "C" int bnn_testing_gated_backward_plan(int64_t T, int64_t D, int64_t F, int64_t *values) {
+  using namespace bnn;
+  if (T <= 0 || D <= 0 || F <= 0 || T > MAX_DIM || D > MAX_DIM || F > MAX_DIM || !values) return -1;
+  const GatedSpace g = gated_space(T, D, F);
+  const KmPlan x = km_plan(T, g.Dp, 2 * (F / KM_STEP)), w = km_plan(2 * g.Fp, g.Dp, T / KM_STEP);
+  constexpr int tile[] = {256, 128, 128, 64, 64};
+  values[0] = x.form, values[1] = x.shares, values[2] = w.form, values[3] = w.shares;
+  values[4] = km_at(std::min<int64_t>(tile[x.form], T) - 1, 4 * g.Fp, 7 * 16);
+  return 0;
 }

@@ -18,6 +18,10 @@ struct KmOperands {
 
 constexpr int KM_STEP = 64;  // values of k a step: 128 bytes of a row of k, or 64 rows
 
+// Where a lane's piece of a row lies, in bytes from a tile's (or a step's) first row.  No sign: 255 rows of 2^24 - 256 bytes, the
+// longest that there are (gradients of two projections of 2^22 - 64 values side by side), end 2^24 below 2^32.
+__host__ __device__ inline uint32_t km_at(int64_t row, int64_t ld, int64_t within) { return (uint32_t)(row * ld + within); }
+
 // LDS, k-major operand of X columns: rows of 2 X bytes, 16-byte piece c of row k in slot c ^ km_turn(k).  The transposing
 // read takes four rows by 16 columns for every 16 lanes; the turns put the eight rows that 32 lanes read on all banks.
 template <int X>
@@ -29,7 +33,7 @@ __device__ __forceinline__ int km_turn(int k) {
 // every transposing read wait for all loads in flight (8192 x 4096 by k 16384, eight waves: 1008 -> 828 us without).  It has no result
 // register, and mm_sync, not the compiler, waits for it; m0 takes a wait state before the load reads it.  Nothing else in
 // these kernels uses m0 (no builtin load to LDS, no indexed register), so it is not kept.
-__device__ __forceinline__ void km_load(const char *base, int at, uint32_t to) {
+__device__ __forceinline__ void km_load(const char *base, uint32_t at, uint32_t to) {
   const uint64_t b = reinterpret_cast<uint64_t>(base);
   const v4i res = {(int)(uint32_t)b, (int)((uint32_t)(b >> 32) & 0xffffu), -1, 0x00020000};
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(res));
@@ -59,13 +63,13 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
   using XA = std::integral_constant<int, BM>;
   using XB = std::integral_constant<int, BN>;
   const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
-  int atA[LOADS_A], atB[LOADS_B];
+  uint32_t atA[LOADS_A], atB[LOADS_B];
 #pragma unroll
   for (int i = 0; i < LOADS_A; ++i)
-    atA[i] = A_ROWS ? (int)(min((i * WAVES + wave) * 8 + (lane >> 3), p.M - 1 - m0) * p.lda) + piece
-                    : (int)(row_k(i, XA()) * p.lda) + columns(i, XA(), m0, p.M);
+    atA[i] = A_ROWS ? km_at(min((i * WAVES + wave) * 8 + (lane >> 3), p.M - 1 - m0), p.lda, piece)
+                    : km_at(row_k(i, XA()), p.lda, columns(i, XA(), m0, p.M));
 #pragma unroll
-  for (int i = 0; i < LOADS_B; ++i) atB[i] = (int)(row_k(i, XB()) * p.ldb) + columns(i, XB(), n0, p.N);
+  for (int i = 0; i < LOADS_B; ++i) atB[i] = km_at(row_k(i, XB()), p.ldb, columns(i, XB(), n0, p.N));
 
   const char *const baseA = A_ROWS ? p.A + (int64_t)m0 * p.lda : p.A;
   const int whole = p.K / KM_STEP;  // steps of a stretch
@@ -165,7 +169,7 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
     const u32x4 none = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int l = 0; l < LOADS_A; ++l) {
-      if constexpr (A_ROWS) r.a[l] = bytes16<E>(a + atA[l] - piece, piece, 2 * left);
+      if constexpr (A_ROWS) r.a[l] = bytes16<E>(a + (atA[l] - piece), piece, 2 * left);
       else r.a[l] = row_k(l, XA()) < left ? *reinterpret_cast<const u32x4 *>(a + atA[l]) : none;
     }
 #pragma unroll

@@ -1,0 +1,39 @@
+"""How the gated layers' products are dealt out, and how far their addresses reach: answers of the library without a GPU."""
+import ctypes
+
+import pytest
+
+from paper_1911_04477_amd import binding as B
+
+LIMIT = (1 << 22) - 64  # the largest T, D and F
+
+
+def backward_plan(T, D, F):
+    out = (ctypes.c_int64 * 5)()
+    assert B.lib().bnn_testing_gated_backward_plan(T, D, F, out) == 0
+    return tuple(out)
+
+
+@pytest.mark.parametrize("T,D,F", [(1, 8, 64), (200, 64, 1000), (8192, 4096, 8192), (512, 1024, 2105377), (256, 2048, 2200001), (4096, 4096, 2200001),
+                                   (512, 1024, LIMIT - 1), (8192, 4096, LIMIT)])
+def test_offsets_of_a_tile_of_gradients(T, D, F):
+    """A tile's last row of gradients begins (rows - 1) * 4 * F bytes after its first, F rounded up to 64, and its last piece 112 bytes
+    further on; the reads take such an offset as 32 bits without a sign, and 16 bytes from there on stay below 2^32."""
+    form, _, _, _, largest = backward_plan(T, D, F)
+    rows = min(T, (256, 128, 128, 64, 64)[form])
+    assert largest == (rows - 1) * 4 * (-(-F // 64) * 64) + 112
+    assert 0 <= largest <= 2 ** 32 - 1 - 16
+
+
+def test_the_longest_rows_are_taken_by_the_largest_tiles():
+    """The sizes above that pass 2^31 do so in 256-row tiles with a remainder of k."""
+    for T, D, F in ((512, 1024, 2105377), (256, 2048, 2200001), (512, 1024, LIMIT - 1)):
+        form, _, _, _, largest = backward_plan(T, D, F)
+        assert form == 0 and F % 64 and largest > 2 ** 31
+
+
+def test_plans_of_refused_sizes():
+    out = (ctypes.c_int64 * 5)()
+    for sizes in ((0, 8, 8), (8, 0, 8), (8, 8, 0), (LIMIT + 1, 8, 8), (8, LIMIT + 1, 8), (8, 8, LIMIT + 1)):
+        assert B.lib().bnn_testing_gated_backward_plan(*sizes, out) == -1
+    assert B.lib().bnn_testing_gated_backward_plan(8, 8, 8, None) == -1
