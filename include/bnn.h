@@ -368,8 +368,9 @@ BNN_API bnn_status bnn_norm_gate(const bnn_norm_gate_in *in, void *r_out, int64_
  * bnn_norm_gate_backward -- gradients of bnn_norm_gate from its inputs (`in` as in the forward call; r is the stream that
  * went in, not r') and the gradients dn of n and dr_out of r' (either may be NULL: zero).
  *   dr [rows, D] of r_type, db [rows, D] of `type` (iff b), dgate [groups, D] of `type`, and fp32 [D] sums over the rows:
- *   dres_scale, dw_post, dbias_post, dw_pre, dbias_pre; each of these six may be NULL (not wanted).  Sums are in fp32, in
- *   an order that depends on the sizes alone.  rows 0: the sums are 0.
+ *   dres_scale, dw_post, dbias_post, dw_pre, dbias_pre; each of these six may be NULL (not wanted), and may be asked for
+ *   where the vector is absent: its gradient at 1, or for a bias at 0 (dgate needs a gate, the first three b, the last two a norm).
+ *   Sums are in fp32, in an order that depends on the call's sizes and pointers' presence alone.  rows 0: the sums are 0.
  *   workspace at least bnn_norm_gate_backward_workspace_bytes(rows, D, gate ? gate_rows : 0) bytes, needed where a
  *   sum or dgate is wanted.
  */

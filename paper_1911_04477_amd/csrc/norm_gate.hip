@@ -180,7 +180,7 @@ __global__ __launch_bounds__(MAXT) void norm_gate_kernel(bnn_norm_gate_in p, Nor
 // and its first sum is taken along with that row's last: between rms norms a row meets twice (8192 x 4096 bf16, a workgroup
 // a unit: 214 us without either, 173 with the loads ahead; with all of it 125, and 5 for the sums, 4.1 TB/s).  The vectors are
 // in LDS, where there is room.  Values a thread: 8, since with 16 the sums and two rows no longer fit the registers (142 us).  CENTRED: a norm
-// with a mean or a bias takes part.
+// with a mean, a bias or the gradient of a bias takes part.
 template <class E, class R, bool BLOCK, int MAXT, int NV, bool CENTRED, int EDGE>
 __global__ __launch_bounds__(MAXT, NV > 1 || CENTRED ? 2 : 3) void norm_gate_backward_kernel(bnn_norm_gate_in p, NormGrad q) {
   constexpr int WIDTH = (BLOCK ? MAXT : 64) * NV * 8;
@@ -561,7 +561,7 @@ extern "C" bnn_status bnn_norm_gate_backward(const bnn_norm_gate_in *in, const v
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (p.rows > 0) {
     if (!p.r || !dr || (p.b && !db)) return BNN_ERR_NULL;
-    const bool centred = has_means(p);
+    const bool centred = has_means(p) || dbias_post || dbias_pre;  // the gradient of a bias is one where the bias is absent, too
     const RowEdge edge = row_edge(p.D);
     const NormPlan plan = norm_plan(p.rows, p.D, p.gate ? p.gate_rows : 0, centred || edge != EDGE_WHOLE ? NORM_WAVES_CENTRED : NORM_WAVES);
     q.dn = dn, q.dr_out = dr_out, q.dn_ld = dn_ld, q.dr_out_ld = dr_out_ld;
