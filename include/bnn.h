@@ -392,7 +392,8 @@ BNN_API size_t bnn_norm_gate_backward_workspace_bytes(int64_t rows, int D, int64
  * bnn_gated_ff_i8: the same from 8-bit operands with scales (bnn_quant_rows_i8), g = x_scale[t] * wg_scale[f] * (exact
  *   int32 sum), u likewise; h of any `type`.  D at most 131071.
  * bnn_gated_ff_backward: from dh [T, F] the gradients dx [T, D], dwg, dwu [F, D], all of `type`.  The gradients of g and u
- *   are rounded to `type` as operands of the products, sums are fp32.  T or F 0: zeros.
+ *   are rounded to `type` as operands of the products, sums are fp32.  In fp16 they are rounded times a power of two, the same
+ *   for all, that the sums are divided by again: they may be larger or smaller than fp16 holds.  T or F 0: zeros.
  *   workspace at least bnn_gated_ff_backward_workspace_bytes(T, D, F) bytes.
  * T, D and F below 2^22 - 64 (BNN_ERR_UNSUPPORTED beyond; bnn_gated_ff_i8: D as above).
  */

@@ -52,6 +52,7 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
   int tm, tn;
   mm_tile(blockIdx.x, p.tilesM, p.tilesN, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
+  const float factor = epi.factor();  // requested here: at the end every workgroup would wait for it
 
   // Offsets of this lane's loads from a step's first value of k.  Rows and columns beyond the operands repeat their last
   // ones, their outputs are not stored; columns come eight at a time (M, if k-major, and N are multiples of eight).
@@ -264,7 +265,7 @@ __device__ __forceinline__ void km_tile_product(const KmOperands &p, const Epilo
       mm_longer(x);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        if (n + j * 16 < p.N && m + i * 16 + h * 8 < p.M) epi(m + i * 16 + h * 8, n + j * 16, p.N, split, x[h]);
+        if (n + j * 16 < p.N && m + i * 16 + h * 8 < p.M) epi(m + i * 16 + h * 8, n + j * 16, p.N, split, factor, x[h]);
     }
 }
 
