@@ -386,6 +386,8 @@ BNN_API size_t bnn_norm_gate_backward_workspace_bytes(int64_t rows, int D, int64
  *   h[t,f] = act(g) * u,  g = sum_k x[t,k] * wg[f,k],  u = sum_k x[t,k] * wu[f,k]   (fp32, rounded once)
  *   act: BNN_ACT_SILU z / (1 + exp(-z)); BNN_ACT_GELU z * (1 + erf(z / sqrt 2)) / 2; BNN_ACT_GELU_TANH
  *   z * (1 + tanh(sqrt(2 / pi) * (z + 0.044715 z^3))) / 2; BNN_ACT_RELU max(z, 0).
+ *   In fp32 GELU and its slope's terms are within 2^-20 of themselves where |z| <= 12; beyond, and in the other activations, the
+ *   exponential's argument is rounded: 2^-24 of it, relative to a value below zero.
  *   x [T, D], wg, wu [F, D], h [T, F] of `type`, BNN_BF16 or BNN_F16 (BNN_ERR_UNSUPPORTED for BNN_F32).
  *   saved  NULL, or bnn_gated_ff_saved_bytes(T, F) bytes that the backward pass reads: [2, T, F] fp32, act'(g) * u and
  *          act(g).

@@ -10,15 +10,29 @@
 
 namespace bnn {
 
-// The normal distribution's function: erfc by Abramowitz and Stegun 7.1.26 (absolute error of at most 1.5e-7, so of a GELU
-// of z 0.75e-7 |z|), with the density exp(-z^2 / 2) that it contains.  (With erfcf 1000 x 1024 to 2321 takes 3.8 us more.)
+// The normal distribution's function, and exp(-z^2 / 2).  Of a = |z| the tail is exp(-a^2 / 2) t P(t), t = 1 / (1 + 0.345 a): P is fitted
+// to exp(a^2 / 2) (1 - erf(a / sqrt 2)) / 2 on 0 .. 14, least squares with weights moved to where the relative error is largest, 2e-8 at
+// the end.  With what the squares and the exponent lose put back, a value below zero is off by 6 * 2^-24 of itself, as far as fp32's
+// normal numbers reach (1 + erf there loses all of its digits).  Beyond 16 it is 0.  (fp16, 1000 x 1024 to 2321: 19.2 us, 18.7 with a
+// formula good to 1.5e-7 of 1 and not of the value, 22.5 with erfcf.)
 __device__ __forceinline__ float normal_function(float z, float &density) {
-  constexpr float LOG2E = 1.44269504088896341f;
-  const float x = fabsf(z) * 0.70710678118654752f;
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
-  density = __builtin_amdgcn_exp2f(x * x * -LOG2E);
-  const float tail = 0.5f * density * t *
-                     fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  constexpr float C = -0.72134752044448170f, C_REST = (float)(-0.72134752044448170368 - (double)C), LN2 = 0.69314718055994531f;
+  const float a = fminf(fabsf(z), 16.0f);
+  const float square = a * a, power = square * C;
+  const float rest = fmaf(fmaf(a, a, -square), C, fmaf(square, C_REST, fmaf(square, C, -power)));
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.345f, a, 1.0f));
+  density = __builtin_amdgcn_exp2f(power);
+  density = fmaf(density, rest * LN2, density);
+  float p = -0.028381976f;
+  p = fmaf(p, t, 0.145282045f);
+  p = fmaf(p, t, -0.271173209f);
+  p = fmaf(p, t, 0.187196776f);
+  p = fmaf(p, t, -0.0376017168f);
+  p = fmaf(p, t, 0.111799605f);
+  p = fmaf(p, t, 0.117238283f);
+  p = fmaf(p, t, 0.138020888f);
+  p = fmaf(p, t, 0.137619287f);
+  const float tail = density * (t * p);
   return z < 0.0f ? tail : 1.0f - tail;
 }
 
