@@ -5,33 +5,29 @@
 
 namespace bnn {
 
-// A workgroup owns 16 columns and up to 16 * MT rows; its waves deal the k axis out in runs of RUN * 64 bytes, straight from
+// A workgroup owns 16 columns and up to 16 rows; its waves deal the k axis out in runs of RUN * 64 bytes, straight from
 // memory into matrix operands (any order of k is right as long as both operands have it), and their sums meet in LDS.  The
 // next run is requested before the products of the present one.
-template <int TY, int MT, int WAVES, int RUN, bool DUAL, class Epilogue>
+template <int TY, int WAVES, int RUN, bool DUAL, class Epilogue>
 __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void mm_few_kernel(MmOperands p, Epilogue epi) {
   using T = MmTraits<TY>;
   using E = typename T::elem;
   using Acc = typename T::acc;
   constexpr int NB = DUAL ? 2 : 1, BYTES = RUN * 64;
-  __shared__ Acc sums[WAVES][MT][NB][64];
+  __shared__ Acc sums[WAVES][NB][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT;
+  const int n0 = (p.first + blockIdx.x) * 16;
   const int row = lane & 15, piece = (lane >> 4) * 16;
   const int n = min(n0 + row, p.N - 1);
-  const char *b[NB], *a[MT];
+  const char *b[NB], *const a = p.A + (int64_t)min(row, p.M - 1) * p.lda;
   b[0] = p.B0 + n * p.ldb0;
   if constexpr (DUAL) b[1] = p.B1 + n * p.ldb1;
-#pragma unroll
-  for (int i = 0; i < MT; ++i) a[i] = p.A + (int64_t)min(m0 + i * 16 + row, p.M - 1) * p.lda;
 
-  Acc acc[MT][NB];
+  Acc acc[NB];
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int d = 0; d < NB; ++d) acc[i][d] = Acc{0, 0, 0, 0};
+  for (int d = 0; d < NB; ++d) acc[d] = Acc{0, 0, 0, 0};
   struct Run {
-    u32x4 b[RUN][NB], a[RUN][MT];
+    u32x4 b[RUN][NB], a[RUN];
   };
   const int K = p.kbytes;
   const auto request = [&](Run &v, int k) {
@@ -40,17 +36,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void mm_few_kernel(MmOperand
 #pragma unroll
       for (int d = 0; d < NB; ++d) v.b[r][d] = *reinterpret_cast<const u32x4_any *>(b[d] + k + r * 64 + piece);
 #pragma unroll
-    for (int r = 0; r < RUN; ++r)
-#pragma unroll
-      for (int i = 0; i < MT; ++i) v.a[r][i] = *reinterpret_cast<const u32x4_any *>(a[i] + k + r * 64 + piece);
+    for (int r = 0; r < RUN; ++r) v.a[r] = *reinterpret_cast<const u32x4_any *>(a + k + r * 64 + piece);
   };
   const auto multiply = [&](const Run &v) {
 #pragma unroll
     for (int r = 0; r < RUN; ++r)
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int d = 0; d < NB; ++d) acc[i][d] = T::mfma(v.b[r][d], v.a[r][i], acc[i][d]);
+      for (int d = 0; d < NB; ++d) acc[d] = T::mfma(v.b[r][d], v.a[r], acc[d]);
   };
   constexpr int STRIDE = WAVES * BYTES;
   int k = wave * BYTES;
@@ -69,42 +61,38 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void mm_few_kernel(MmOperand
     }
   }
   for (const int end = min(K, k + BYTES); k < end; k += 64) {  // the last run, cut short
-    u32x4 vb[NB], va[MT];
+    u32x4 vb[NB];
 #pragma unroll
     for (int d = 0; d < NB; ++d) vb[d] = bytes16<E>(b[d], k + piece, K);
+    const u32x4 va = bytes16<E>(a, k + piece, K);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) va[i] = bytes16<E>(a[i], k + piece, K);
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int d = 0; d < NB; ++d) acc[i][d] = T::mfma(vb[d], va[i], acc[i][d]);
+    for (int d = 0; d < NB; ++d) acc[d] = T::mfma(vb[d], va, acc[d]);
   }
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int d = 0; d < NB; ++d) sums[wave][i][d][lane] = acc[i][d];
+  for (int d = 0; d < NB; ++d) sums[wave][d][lane] = acc[d];
   __syncthreads();
-  for (int i = wave; i < MT; i += WAVES) {
-    Acc t[NB];
+  if (wave) return;
+  Acc t[NB];
 #pragma unroll
-    for (int d = 0; d < NB; ++d) {
-      t[d] = sums[0][i][d][lane];
+  for (int d = 0; d < NB; ++d) {
+    t[d] = sums[0][d][lane];
 #pragma unroll
-      for (int w = 1; w < WAVES; ++w) t[d] += sums[w][i][d][lane];
-    }
-    const int m = m0 + i * 16 + (lane & 15), nn = n0 + (lane >> 4) * 4;
-    if (m < p.M && nn < p.N) {
-      if constexpr (DUAL) epi(m, nn, p.N, epi.row(m), epi.columns(nn, p.N), t[0], t[1]);
-      else epi(m, nn, p.N, epi.row(m), epi.columns(nn, p.N), t[0]);
-    }
+    for (int w = 1; w < WAVES; ++w) t[d] += sums[w][d][lane];
+  }
+  const int m = lane & 15, nn = n0 + (lane >> 4) * 4;
+  if (m < p.M && nn < p.N) {
+    if constexpr (DUAL) epi(m, nn, p.N, epi.row(m), epi.columns(nn, p.N), t[0], t[1]);
+    else epi(m, nn, p.N, epi.row(m), epi.columns(nn, p.N), t[0]);
   }
 }
 
-template <int TY, int MT, int WAVES, int RUN, bool DUAL, class Epilogue>
-bnn_status launch_mm_few(const MmOperands &p, const Epilogue &epi, int kid, hipStream_t s) {
-  const dim3 grid((uint32_t)((p.N - 1) / 16 + 1), (uint32_t)((p.M - 1) / (16 * MT) + 1));
+template <int TY, int WAVES, int RUN, bool DUAL, class Epilogue>
+bnn_status launch_mm_few(MmOperands p, const Epilogue &epi, int kid, hipStream_t s) {
   ProfScope ps(kid, s);
-  mm_few_kernel<TY, MT, WAVES, RUN, DUAL, Epilogue><<<grid, 64 * WAVES, 0, s>>>(p, epi);
+  wide_launches((p.N - 1) / 16 + 1, [&](int64_t first, uint32_t n) {
+    p.first = (int)first;
+    mm_few_kernel<TY, WAVES, RUN, DUAL, Epilogue><<<n, 64 * WAVES, 0, s>>>(p, epi);
+  });
   return launch_status();
 }
 
@@ -140,7 +128,7 @@ inline int mm_form(int M, int N, bool dual, bool dma) {
 
 template <int TY, bool DUAL, class Epilogue>
 bnn_status run_product(const MmOperands &p, const Epilogue &epi, int kid_few, int kid, hipStream_t s) {
-  if (p.M <= 16) return launch_mm_few<TY, 1, 8, 4, DUAL>(p, epi, kid_few, s);
+  if (p.M <= 16) return launch_mm_few<TY, 8, 4, DUAL>(p, epi, kid_few, s);
   const int form = mm_form(p.M, p.N, DUAL, p.dma);
   if (!p.dma) {  // through registers
     if (form == MM_256_128) return launch_mm_tile<TY, 256, 128, 4, 2, 2, DUAL, false>(p, epi, kid, s);

@@ -7,6 +7,19 @@ namespace bnn {
 inline bool float_type(int t) { return t == BNN_F32 || t == BNN_BF16 || t == BNN_F16; }
 inline int float_size(int t) { return t == BNN_F32 ? 4 : 2; }
 
+// n workgroups of at most 1024 threads.  A launch counts the threads of a dimension in 32 bits, and drops what is above them without an
+// error; so from 2^20 workgroups on they lie in two dimensions, and some of the last row have nothing to do (wide_grid).  Kernels
+// that would wait for their arguments to know that are launched again instead (wide_launches).
+constexpr int64_t WIDE_ROW = 1 << 20;
+inline dim3 wide_grid(int64_t n) {
+  return n <= WIDE_ROW ? dim3((uint32_t)n) : dim3((uint32_t)WIDE_ROW, (uint32_t)((n - 1) / WIDE_ROW + 1));
+}
+__device__ __forceinline__ int64_t wide_block() { return blockIdx.y * WIDE_ROW + blockIdx.x; }
+template <class F>
+void wide_launches(int64_t n, const F &launch) {  // launch(first, workgroups)
+  for (int64_t first = 0; first < n; first += WIDE_ROW) launch(first, (uint32_t)(n - first < WIDE_ROW ? n - first : WIDE_ROW));
+}
+
 template <int DT>
 struct Float;
 template <>

@@ -177,7 +177,7 @@ struct ProductEpilogue {
 
 template <class E>
 __global__ __launch_bounds__(256) void product_sums_kernel(ProductEpilogue<E> epi, int M, int shares) {
-  const int64_t quads = epi.part_ld / 4, i = blockIdx.x * 256ll + threadIdx.x;
+  const int64_t quads = epi.part_ld / 4, i = wide_block() * 256 + threadIdx.x;
   if (i >= M * quads) return;
   const int m = (int)(i / quads), n = (int)(i - m * quads) * 4;
   v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -224,7 +224,7 @@ struct GradientOf {
 };
 template <class E>
 __global__ __launch_bounds__(256) void gated_gradient_kernel(GradientOf<E> q) {
-  const int64_t i = blockIdx.x * 256ll + threadIdx.x;
+  const int64_t i = wide_block() * 256 + threadIdx.x;
   if (i < q.groups) q.write(i, 1.0f);
 }
 
@@ -242,12 +242,12 @@ __device__ __forceinline__ float range_scale(uint32_t top) {
 }
 __global__ __launch_bounds__(GRADIENT_THREADS) void gated_gradient_top_kernel(GradientOf<_Float16> q, uint32_t *tops) {
   __shared__ uint32_t lds[16];
-  const int64_t i = blockIdx.x * (int64_t)GRADIENT_THREADS + threadIdx.x;
+  const int64_t i = wide_block() * GRADIENT_THREADS + threadIdx.x;
   uint32_t top = i < q.groups ? q.write(i, 1.0f) : 0u;
   top = wave_reduce(top, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
   __syncthreads();
-  if (threadIdx.x == 0) tops[blockIdx.x] = max(max(lds[0], lds[1]), max(lds[2], lds[3]));
+  if (threadIdx.x == 0 && i < q.groups) tops[wide_block()] = max(max(lds[0], lds[1]), max(lds[2], lds[3]));
 }
 // Every workgroup takes the largest of all (8192 x 8192: 128 KB of them), and its share of the groups where they are written again.
 __global__ __launch_bounds__(SCALE_THREADS) void gated_gradient_scale_kernel(GradientOf<_Float16> q, const uint32_t *tops, int64_t n, float *factor) {
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(SCALE_THREADS) void gated_gradient_scale_kernel(Gra
 // Rows of D values as rows of Dp that start on 16 bytes, zeros behind them.
 template <class E>
 __global__ __launch_bounds__(256) void realign_kernel(const E *in, int64_t ld, int64_t groups, int D, int Dp, E *out) {
-  const int64_t i = blockIdx.x * 256ll + threadIdx.x;
+  const int64_t i = wide_block() * 256 + threadIdx.x;
   if (i >= groups) return;
   const int per = Dp / 8;
   const int64_t r = i / per;
@@ -341,7 +341,7 @@ bnn_status km_product(KmOperands p, ProductEpilogue<E> epi, float *part, hipStre
   }
   if (st || plan.shares == 1) return st;
   ProfScope ps(KID_PRODUCT_SUMS, s);
-  product_sums_kernel<E><<<(uint32_t)(((int64_t)p.M * p.N / 4 + 255) / 256), 256, 0, s>>>(epi, p.M, plan.shares);
+  product_sums_kernel<E><<<wide_grid(((int64_t)p.M * p.N / 4 + 255) / 256), 256, 0, s>>>(epi, p.M, plan.shares);
   return launch_status();
 }
 
@@ -355,21 +355,21 @@ bnn_status gated_backward(const char *x, int64_t x_ld, const char *wg, int64_t w
   E *const grad = reinterpret_cast<E *>(workspace);
   float *const part = reinterpret_cast<float *>(workspace + g.part);
   float *const factor = reinterpret_cast<float *>(workspace + g.range);
-  const auto blocks = [](int64_t n) { return (uint32_t)((n + 255) / 256); };
+  const auto blocks = [](int64_t n) { return (n + 255) / 256; };
   {
     const GradientOf<E> q = {static_cast<const E *>(dh), dh_ld, saved, (int64_t)T * F, (int64_t)T * Fp / 8, F, Fp, grad};
     if constexpr (TY == MM_F16) {
       uint32_t *const tops = reinterpret_cast<uint32_t *>(workspace + g.range + 256);
-      const uint32_t grid = blocks(q.groups);
+      const int64_t grid = blocks(q.groups);
       {
         ProfScope ps(KID_GATED_GRADIENT, s);
-        gated_gradient_top_kernel<<<grid, GRADIENT_THREADS, 0, s>>>(q, tops);
+        gated_gradient_top_kernel<<<wide_grid(grid), GRADIENT_THREADS, 0, s>>>(q, tops);
       }
       ProfScope ps(KID_GATED_GRADIENT, s);
-      gated_gradient_scale_kernel<<<std::min<uint32_t>(grid, SCALE_BLOCKS), SCALE_THREADS, 0, s>>>(q, tops, grid, factor);
+      gated_gradient_scale_kernel<<<(uint32_t)std::min<int64_t>(grid, SCALE_BLOCKS), SCALE_THREADS, 0, s>>>(q, tops, grid, factor);
     } else {
       ProfScope ps(KID_GATED_GRADIENT, s);
-      gated_gradient_kernel<E><<<blocks(q.groups), 256, 0, s>>>(q);
+      gated_gradient_kernel<E><<<wide_grid(blocks(q.groups)), 256, 0, s>>>(q);
     }
   }
   // the products take columns eight at a time, from rows that start on 16 bytes
@@ -377,7 +377,7 @@ bnn_status gated_backward(const char *x, int64_t x_ld, const char *wg, int64_t w
   const auto realign = [&](const char *&m, int64_t &ld, int64_t rows, int64_t at) {
     const int64_t n = rows * Dp / 8;
     ProfScope ps(KID_REALIGN, s);
-    realign_kernel<E><<<blocks(n), 256, 0, s>>>(reinterpret_cast<const E *>(m), ld, n, D, Dp, reinterpret_cast<E *>(workspace + at));
+    realign_kernel<E><<<wide_grid(blocks(n)), 256, 0, s>>>(reinterpret_cast<const E *>(m), ld, n, D, Dp, reinterpret_cast<E *>(workspace + at));
     m = workspace + at, ld = Dp;
   };
   const bool as_they_are = fits(wg, wg_ld) && fits(wu, wu_ld) && wg_ld == wu_ld;  // one row stride for both

@@ -280,7 +280,7 @@ bnn_status launch_km_tile(KmOperands p, const Epilogue &epi, int kid, hipStream_
   p.tilesM = (p.M - 1) / BM + 1;
   p.tilesN = (p.N - 1) / BN + 1;
   const int64_t tiles = (int64_t)p.tilesM * p.tilesN;
-  if (tiles > 0x7fffffff) return BNN_ERR_UNSUPPORTED;
+  if (tiles * 64 * WGM * WGN > 0xffffffffll) return BNN_ERR_UNSUPPORTED;  // threads of a launch
   ProfScope ps(kid, s);
   km_tile_kernel<TY, BM, BN, WGM, WGN, STAGES, A_ROWS, Epilogue><<<dim3((uint32_t)tiles, p.splits), 64 * WGM * WGN, 0, s>>>(p, epi);
   return launch_status();

@@ -20,8 +20,8 @@ __global__ __launch_bounds__(MAXT) void quant_rows_kernel(QuantParams p) {
   __shared__ uint32_t lds[16];
   if constexpr (BLOCK) clear_words(lds);
   const int T = BLOCK ? blockDim.x : 64, t = BLOCK ? threadIdx.x : threadIdx.x & 63;
-  const int64_t row = BLOCK ? blockIdx.x : blockIdx.x * 4ll + (threadIdx.x >> 6);
-  if (row >= p.rows) return;  // whole waves, of workgroups without barriers
+  const int64_t row = BLOCK ? wide_block() : wide_block() * 4 + (threadIdx.x >> 6);
+  if (row >= p.rows) return;  // whole workgroups, or whole waves of those without barriers
   const E *x = static_cast<const E *>(p.x) + row * p.x_ld;
   int8_t *q = p.q + row * p.q_ld;
   uint32_t top = 0u;
@@ -74,16 +74,15 @@ extern "C" bnn_status bnn_quant_rows_i8(const void *x, int type, int64_t rows, i
   ProfScope ps(KID_QUANT_ROWS, s);
   with_float(type, [&](auto tag) {
     using E = typename decltype(tag)::type;
-    const uint32_t n = (uint32_t)rows;
     const auto run = [&](auto whole, auto ragged, int block, int teams) {
-      (row_edge(K) == EDGE_WHOLE ? whole : ragged)<<<(n - 1) / teams + 1, block, 0, s>>>(p);
+      (row_edge(K) == EDGE_WHOLE ? whole : ragged)<<<wide_grid((rows - 1) / teams + 1), block, 0, s>>>(p);
     };
 #define BNN_FORMS(...) quant_rows_kernel<E, __VA_ARGS__, EDGE_WHOLE>, quant_rows_kernel<E, __VA_ARGS__, EDGE_RAGGED>
-    if (K < 8) quant_rows_kernel<E, false, 256, 1, EDGE_SMALL><<<(n - 1) / 4 + 1, 256, 0, s>>>(p);
+    if (K < 8) quant_rows_kernel<E, false, 256, 1, EDGE_SMALL><<<wide_grid((rows - 1) / 4 + 1), 256, 0, s>>>(p);
     else if (K <= 512) run(BNN_FORMS(false, 256, 1), 256, 4);
     else if (K <= 4096) run(BNN_FORMS(true, 512, 1), row_threads(K, 1), 1);
     else if (K <= 32768) run(BNN_FORMS(true, 1024, 4), row_threads(K, 4), 1);
-    else quant_rows_kernel<E, true, 1024, 0, EDGE_RAGGED><<<n, 1024, 0, s>>>(p);
+    else quant_rows_kernel<E, true, 1024, 0, EDGE_RAGGED><<<wide_grid(rows), 1024, 0, s>>>(p);
 #undef BNN_FORMS
   });
   return launch_status();

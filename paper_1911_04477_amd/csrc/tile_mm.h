@@ -65,6 +65,7 @@ struct MmOperands {
   int M, N, kbytes;
   int dma;                  // rows and strides are multiples of 16 bytes (mm_dma)
   int tilesM, tilesN;
+  int first;                // tile, or group of columns, of this launch's first workgroup: a multiple of eight, or 0
 };
 
 // Whether an operand's tiles can go straight to LDS: 16-byte pieces that start on 16 bytes, 32-bit offsets in a tile.
@@ -421,7 +422,7 @@ template <int TY, int BM, int BN, int WGM, int WGN, int STAGES, bool DUAL, bool 
 __global__ __launch_bounds__(64 * WGM *WGN, WGM *WGN < 4 ? 1 : WGM *WGN / 4) void mm_tile_kernel(MmOperands p, Epilogue epi) {
   __shared__ __attribute__((aligned(16))) char lds[STAGES * (BM + BN) * MM_STEP];
   int tm, tn;
-  mm_tile(blockIdx.x, p.tilesM, p.tilesN, tm, tn);
+  mm_tile(p.first + blockIdx.x, p.tilesM, p.tilesN, tm, tn);
   mm_tile_product<TY, BM, BN, WGM, WGN, STAGES, DUAL, DMA>(p, epi, tm, tn, lds);
 }
 
@@ -432,7 +433,10 @@ bnn_status launch_mm_tile(MmOperands p, const Epilogue &epi, int kid, hipStream_
   const int64_t tiles = (int64_t)p.tilesM * p.tilesN;
   if (tiles > 0x7fffffff) return BNN_ERR_UNSUPPORTED;
   ProfScope ps(kid, s);
-  mm_tile_kernel<TY, BM, BN, WGM, WGN, STAGES, DUAL, DMA, Epilogue><<<(uint32_t)tiles, 64 * WGM * WGN, 0, s>>>(p, epi);
+  wide_launches(tiles, [&](int64_t first, uint32_t n) {
+    p.first = (int)first;
+    mm_tile_kernel<TY, BM, BN, WGM, WGN, STAGES, DUAL, DMA, Epilogue><<<n, 64 * WGM * WGN, 0, s>>>(p, epi);
+  });
   return launch_status();
 }
 
