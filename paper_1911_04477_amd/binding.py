@@ -719,6 +719,15 @@ def _vector(t: Optional[torch.Tensor], name: str, n: int) -> Optional[int]:
     return t.data_ptr()
 
 
+def _workspace(t: torch.Tensor) -> int:
+    """Bytes of a workspace that a caller brings; kernels write all through it."""
+    if not t.is_cuda:
+        raise TypeError("workspace must be a GPU tensor")
+    if not t.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor expected")
+    return t.numel() * t.element_size()
+
+
 def _one_of(table, key, name: str) -> int:
     if key not in table:
         raise ValueError(f"{name}: one of {', '.join(table)}")
@@ -842,6 +851,8 @@ def bnn_norm_gate_backward(b: Optional[torch.Tensor], r: torch.Tensor, dn: Optio
             if type(made) is int:
                 _check(made, "bnn_norm_gate_backward")
             return {name: t for name, t in zip(NORM_GRADIENTS, made) if t is not None}
+    if workspace is not None:
+        _workspace(workspace)
     if r.dim() != 2:
         raise ValueError("r: a matrix expected")
     rows, D = r.shape
@@ -871,8 +882,8 @@ def bnn_norm_gate_backward(b: Optional[torch.Tensor], r: torch.Tensor, dn: Optio
         args += [_ptr(t), 0 if t is None else _rows(t, name, n, D)]
     for name in ("dres_scale", "dw_post", "dbias_post", "dw_pre", "dbias_pre"):
         args.append(_vector(got.get(name), name, D))
-    _check(_c().bnn_norm_gate_backward(ctypes.addressof(p), *args, _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                        _stream()), "bnn_norm_gate_backward")
+    _check(_c().bnn_norm_gate_backward(ctypes.addressof(p), *args, _ptr(workspace), _workspace(workspace), _stream()),
+           "bnn_norm_gate_backward")
     return got
 
 
@@ -951,6 +962,8 @@ def bnn_gated_ff_backward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, s
             if type(made) is int:
                 _check(made, "bnn_gated_ff_backward")
             return made
+    if workspace is not None:
+        _workspace(workspace)
     if x.dim() != 2 or wg.dim() != 2:
         raise ValueError("x, wg: matrices expected")
     dx, dwg, dwu = (torch.empty(of.shape, dtype=x.dtype, device=x.device) if t is None else t
@@ -967,8 +980,8 @@ def bnn_gated_ff_backward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, s
         _dev(t, x.dtype, name)
     _check(_c().bnn_gated_ff_backward(_ptr(x), x_ld, _ptr(wg), g_ld, _ptr(wu), u_ld, kind, T, D, F, _saved(saved, T, F), _ptr(dh),
                                        _rows(dh, "dh", T, F), _ptr(dx), _rows(dx, "dx", T, D), _ptr(dwg), _rows(dwg, "dwg", F, D),
-                                       _ptr(dwu), _rows(dwu, "dwu", F, D), _ptr(workspace),
-                                       workspace.numel() * workspace.element_size(), _stream()), "bnn_gated_ff_backward")
+                                       _ptr(dwu), _rows(dwu, "dwu", F, D), _ptr(workspace), _workspace(workspace),
+                                       _stream()), "bnn_gated_ff_backward")
     return dx, dwg, dwu
 
 

@@ -340,6 +340,11 @@ float *vector(const at::Tensor *t, int64_t n) {
   if (!t->is_cuda() || t->scalar_type() != kFloat || t->dim() != 1 || t->size(0) != n || (n > 1 && t->stride(0) != 1)) throw Other();
   return f32(t->data_ptr());
 }
+void *workspace(const at::Tensor &t, size_t &bytes) {
+  if (!t.is_cuda() || !t.is_contiguous()) throw Other();
+  bytes = (size_t)t.numel() * t.element_size();
+  return t.data_ptr();
+}
 int float_type(at::ScalarType t) {
   if (t == kFloat) return BNN_F32;
   if (t == at::kBFloat16) return BNN_BF16;
@@ -417,9 +422,8 @@ PyObject *norm_gate_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
                  dg = matrix(v.tensor_or_none(), type, in.gate ? (in.rows - 1) / in.gate_rows + 1 : 0, in.D);
     float *sums[5];
     for (float *&p : sums) p = vector(v.tensor_or_none(), in.D);
-    const at::Tensor &ws = v.tensor();
-    void *const pws = ws.data_ptr();
-    const size_t nws = (size_t)ws.numel() * ws.element_size();
+    size_t nws;
+    void *const pws = workspace(v.tensor(), nws);
     return launch([&](void *s) {
       return lib.norm_backward(&in, dn.p, dn.ld, dro.p, dro.ld, dr.p, dr.ld, db.p, db.ld, dg.p, dg.ld, sums[0], sums[1], sums[2], sums[3],
                                sums[4], pws, nws, s);
@@ -525,9 +529,8 @@ PyObject *gated_ff_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {  // 
     const float *const saved = saved_of(&v.tensor(), T, F);
     const Matrix dh = matrix(v.tensor(), type, T, F), dx = matrix(v.tensor(), type, T, D), dwg = matrix(v.tensor(), type, F, D),
                  dwu = matrix(v.tensor(), type, F, D);
-    const at::Tensor &ws = v.tensor();
-    void *const pws = ws.data_ptr();
-    const size_t nws = (size_t)ws.numel() * ws.element_size();
+    size_t nws;
+    void *const pws = workspace(v.tensor(), nws);
     const int code = float_type(type);
     return launch([&](void *s) {
       return lib.gated_backward(x.p, x.ld, wg.p, wg.ld, wu.p, wu.ld, code, T, D, F, saved, dh.p, dh.ld, dx.p, dx.ld, dwg.p, dwg.ld, dwu.p,

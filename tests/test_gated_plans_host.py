@@ -37,3 +37,14 @@ def test_plans_of_refused_sizes():
     for sizes in ((0, 8, 8), (8, 0, 8), (8, 8, 0), (LIMIT + 1, 8, 8), (8, LIMIT + 1, 8), (8, 8, LIMIT + 1)):
         assert B.lib().bnn_testing_gated_backward_plan(*sizes, out) == -1
     assert B.lib().bnn_testing_gated_backward_plan(8, 8, 8, None) == -1
+
+
+def test_workspaces_of_other_memory_are_refused():
+    """Before anything else, so that no kernel gets an address of the host's memory."""
+    import torch
+    x = torch.zeros(4, 8, dtype=torch.bfloat16)
+    saved, dh, ws = torch.zeros(2, 4, 4), torch.zeros(4, 4, dtype=torch.bfloat16), torch.zeros(1 << 16, dtype=torch.uint8)
+    with pytest.raises(TypeError, match="workspace"):
+        B.bnn_gated_ff_backward(x, x, x, saved, dh, workspace=ws)
+    with pytest.raises(TypeError, match="workspace"):
+        B.bnn_norm_gate_backward(x, x, x, x, workspace=ws)
