@@ -149,6 +149,12 @@ BNN_API int bnn_testing_conv_image(int N, int C, int H, int W, int D, int kH, in
  * waves; -1 for invalid arguments.  Host only, launches nothing. */
 BNN_API int bnn_testing_first_sign(int N, int H, int W, int D, int sH, int sW, int pH, int pW, int units);
 
+/* The kernel that takes the forward products of the 8-bit and gated layers, M rows by N columns of one weight (bnn_linear_i8) or
+ * two, on a device of `units` compute units; aligned: rows of all operands start on 16 bytes.  0 256 x 256 tiles, 1 256 x 128, 2 128 x 128
+ * with two tiles a unit, 3 128 x 64, 4 64 x 64, 5 64 x 32, 6 32 x 32, 7 128 x 128 with one, 8 few rows; through registers where not aligned:
+ * 1, 2, 4, and 8 of any rows.  -1 for sizes that are refused or empty.  Host only, launches nothing. */
+BNN_API int bnn_testing_product_form(int64_t M, int64_t N, int weights, int aligned, int units);
+
 /* How bnn_gated_ff_backward takes a problem.  values receives
  *   0 the kernel of the product that gives dx: 0 256 x 256 tiles, 1, 2 128 x 128 with one or two tiles a compute unit, 3, 4 64 x 64 the same
  *   1 into how many shares its k is split   2, 3 the same of the products that give dwg and dwu

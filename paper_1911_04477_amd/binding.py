@@ -98,6 +98,7 @@ TESTING_SIGNATURES = {
     "bnn_testing_conv_region": (_i32, [_i32] * 12 + [ctypes.POINTER(_i64)]),
     "bnn_testing_nontemporal_maps": (_i32, [_i32, _i32, _i32, _i64, _i64]),
     "bnn_testing_xnor_gemm_mfma_fp4_expanded": (_i32, [_p, _i64, _p, _i64, _p, _i64, _i64, _i64, _i64, _i32, _p]),
+    "bnn_testing_product_form": (_i32, [_i64, _i64, _i32, _i32, _i32]),
     "bnn_testing_gated_backward_plan": (_i32, [_i64, _i64, _i64, ctypes.POINTER(_i64)]),
     "bnn_prof_enable": (_i32, [_i32]),
     "bnn_prof_reset": (_i32, []),

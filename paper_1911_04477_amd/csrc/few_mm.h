@@ -96,7 +96,7 @@ bnn_status launch_mm_few(MmOperands p, const Epilogue &epi, int kid, hipStream_t
   return launch_status();
 }
 
-// Which kernel takes a product of more than 16 rows: the cheapest by the rounds of tiles that the compute units go through,
+// Which kernel takes a product: that of few rows up to 16, else the cheapest by the rounds of tiles that the compute units go through,
 // in hundredths of a round of 256 x 256 tiles.  `one`: every unit has one tile at most; `two`: a round of two tiles a unit
 // (256 x 256 and 256 x 128: one at a time).  What the small tiles wait for is their operands' way into LDS, so that times
 // measured in 8 bits at k 4096 hold for 16 bits at k 2048.  In 8 bits, k 4096, by 4096, us:
@@ -109,11 +109,11 @@ bnn_status launch_mm_few(MmOperands p, const Epilogue &epi, int kid, hipStream_t
 struct MmForm {
   int bm, bn, one, two;
 };
-enum : int { MM_256, MM_256_128, MM_128, MM_128_64, MM_64, MM_64_32, MM_32, MM_FORM_COUNT };
+enum : int { MM_256, MM_256_128, MM_128, MM_128_64, MM_64, MM_64_32, MM_32, MM_FORM_COUNT, MM_128_DEEP = MM_FORM_COUNT, MM_FEW };
 constexpr MmForm MM_FORMS[MM_FORM_COUNT] = {{256, 256, 100, 200}, {256, 128, 70, 140}, {128, 128, 45, 74}, {128, 64, 28, 46},
                                             {64, 64, 22, 32},     {64, 32, 19, 28},    {32, 32, 17, 24}};
-inline int mm_form(int M, int N, bool dual, bool dma) {
-  const int64_t units = device_cu_count();
+inline int mm_form(int M, int N, bool dual, bool dma, int64_t units) {
+  if (M <= 16) return MM_FEW;
   int best = MM_64;
   int64_t least = INT64_MAX;
   for (int f = 0; f < MM_FORM_COUNT; ++f) {
@@ -123,13 +123,14 @@ inline int mm_form(int M, int N, bool dual, bool dma) {
     const int64_t cost = t.bm == 256 ? (tiles + units - 1) / units * t.one : tiles <= units ? t.one : (tiles + 2 * units - 1) / (2 * units) * t.two;
     if (cost <= least) least = cost, best = f;
   }
+  if (best == MM_128 && dma && (int64_t)((M - 1) / 128 + 1) * ((N - 1) / (dual ? 64 : 128) + 1) <= units) return MM_128_DEEP;
   return best;
 }
 
 template <int TY, bool DUAL, class Epilogue>
 bnn_status run_product(const MmOperands &p, const Epilogue &epi, int kid_few, int kid, hipStream_t s) {
-  if (p.M <= 16) return launch_mm_few<TY, 8, 4, DUAL>(p, epi, kid_few, s);
-  const int form = mm_form(p.M, p.N, DUAL, p.dma);
+  const int form = mm_form(p.M, p.N, DUAL, p.dma, device_cu_count());
+  if (form == MM_FEW) return launch_mm_few<TY, 8, 4, DUAL>(p, epi, kid_few, s);
   if (!p.dma) {  // through registers
     if (form == MM_256_128) return launch_mm_tile<TY, 256, 128, 4, 2, 2, DUAL, false>(p, epi, kid, s);
     if (form == MM_128) return launch_mm_tile<TY, 128, 128, 4, 2, 2, DUAL, false>(p, epi, kid, s);
@@ -139,13 +140,10 @@ bnn_status run_product(const MmOperands &p, const Epilogue &epi, int kid_few, in
     case MM_256:  // 128 outputs a thread: what the epilogue does is compiled for the call
       return epi.fixed([&](const auto &known) { return launch_mm_tile<TY, 256, 256, 2, 2, 2, DUAL, true>(p, known, kid, s); });
     case MM_256_128: return launch_mm_tile<TY, 256, 128, 4, 2, 3, DUAL, true>(p, epi, kid, s);
-    case MM_128: {
-      const int64_t tiles = (int64_t)((p.M - 1) / 128 + 1) * ((p.N - 1) / (DUAL ? 64 : 128) + 1);
-      // one tile a unit: four steps ahead (1024 x 4096 by k 1024 in 8 bits 8.9 us, with two 9.6); else two tiles a unit
-      // (2048 x 4096 by 4096 35 us, 41 with four steps)
-      if (tiles <= device_cu_count()) return launch_mm_tile<TY, 128, 128, 2, 4, 4, DUAL, true>(p, epi, kid, s);
-      return launch_mm_tile<TY, 128, 128, 4, 2, 2, DUAL, true>(p, epi, kid, s);
-    }
+    // one tile a unit: four steps ahead (1024 x 4096 by k 1024 in 8 bits 8.9 us, with two 9.6); else two tiles a unit
+    // (2048 x 4096 by 4096 35 us, 41 with four steps)
+    case MM_128_DEEP: return launch_mm_tile<TY, 128, 128, 2, 4, 4, DUAL, true>(p, epi, kid, s);
+    case MM_128: return launch_mm_tile<TY, 128, 128, 4, 2, 2, DUAL, true>(p, epi, kid, s);
     // eight waves a tile where its columns allow: 256 x 4096 by 4096 in 8 bits takes 9.8 us on 64 x 64, with four waves 11.8
     case MM_128_64: return launch_mm_tile<TY, 128, 64, 4, 2, 3, DUAL, true>(p, epi, kid, s);
     case MM_64: return launch_mm_tile<TY, 64, 64, 4, 2, 4, DUAL, true>(p, epi, kid, s);

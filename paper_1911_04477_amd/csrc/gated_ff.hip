@@ -484,6 +484,11 @@ extern "C" bnn_status bnn_gated_ff_backward(const void *x, int64_t x_ld, const v
              dh, dh_ld, (int)T, (int)D, (int)F, dx, dx_ld, dwg, dwg_ld, dwu, dwu_ld, static_cast<char *>(workspace), s);
 }
 
+extern "C" int bnn_testing_product_form(int64_t M, int64_t N, int weights, int aligned, int units) {
+  if (M <= 0 || N <= 0 || M > INT32_MAX - 256 || N > INT32_MAX - 256 || weights < 1 || weights > 2 || units < 1) return -1;
+  return bnn::mm_form((int)M, (int)N, weights == 2, aligned != 0, units);
+}
+
 extern "C" int bnn_testing_gated_backward_plan(int64_t T, int64_t D, int64_t F, int64_t *values) {
   using namespace bnn;
   if (T <= 0 || D <= 0 || F <= 0 || T > MAX_DIM || D > MAX_DIM || F > MAX_DIM || !values) return -1;
