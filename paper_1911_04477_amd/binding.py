@@ -691,6 +691,8 @@ def bnn_fc_f32(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = 
 
 
 # ---- 8-bit and gated layers ----------------------------------------------------------
+# Gradients come from the backward calls below; torch's autograd does not see these calls, and tensors that require a gradient pass
+# without a graph.
 FLOATS = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 NORMS = {"none": 0, "rms": 1, "layer": 2}
 ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}

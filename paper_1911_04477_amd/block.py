@@ -5,7 +5,8 @@
     o      = h Wd^T                     what the next norm_gate takes as its b
 
 GatedBlock8 is the serving form: weights and activations in 8 bits with a scale per output channel and per token, any
-number of tokens from one to the number it was made for, nothing allocated in a pass (it can be captured in a graph).
+number of tokens from one to the number it was made for, nothing allocated in a pass that is given r_out (it can be captured in a graph).  Its
+buffers serve one pass at a time: threads or streams that run at once need an object each.
 GatedProjections is the training form of the part that has a backward pass: the norms and both projections.
 """
 from __future__ import annotations
@@ -19,7 +20,8 @@ from . import binding as B
 
 class GatedBlock8:
     """wg, wu [F, D], wd [D, F]: fp32, bf16 or fp16, quantized here once.  vectors: the keyword arguments of bnn_norm_gate that
-    hold parameters (res_scale, w_post, bias_post, w_pre, bias_pre, post, pre, eps)."""
+    hold parameters (res_scale, w_post, bias_post, w_pre, bias_pre, post, pre, eps).  A pass writes the 8-bit rows, their scales, h and o
+    of the pass before over."""
 
     def __init__(self, wg: torch.Tensor, wu: torch.Tensor, wd: torch.Tensor, tokens: int, vectors: Optional[Dict] = None,
                  act: str = "silu", dtype: torch.dtype = torch.bfloat16):

@@ -1,5 +1,6 @@
 // The product of tile_mm.h for few rows of A: nothing is reused, the kernel streams B once, and is bound by that: one row of
-// 4096 to 8192 with two weights in bf16 24 us, 5.6 TB/s; by 4096 x 4096 in 8 bits 4.6 us, 3.7 TB/s, of which 2 are the launch.
+// 4096 to 8192 with two weights in bf16 26 us, 5.1 TB/s; by 4096 x 4096 in 8 bits 4.5 us, 3.7 TB/s, of which 2 are the launch.  Fewer
+// than 4096 columns leave units without work (1 x 8192 by 512 in 8 bits 6.2 us).
 #pragma once
 #include "tile_mm.h"
 

@@ -186,7 +186,8 @@ __global__ __launch_bounds__(256) void product_sums_kernel(ProductEpilogue<E> ep
 }
 
 // Gradients of the projections, dG = dh * saved[0] and dU = dh * saved[1], side by side in rows of 2 Fp (zeros beside F):
-// eight values a thread.  Bound by memory (14 B a value; 8192 x 8192 168 us, 5.6 TB/s).
+// eight values a thread.  Bound by memory (14 B a value; 8192 x 8192 160 to 170 us again and again, 5.6 TB/s, 200 to 220 right after the
+// forward pass).
 // They are rounded to the operands' type, the one rounding on the way from dh to the results: the matrix units multiply
 // 16-bit values, and each gradient as a sum of two of them would double the products.  It adds as much to a result's error as
 // the result's own rounding does: 1.4 times that of a pass with fp32 operands, in the 2-norm.

@@ -439,7 +439,7 @@ constexpr int NORM_MAX_D = 16384;
 struct NormPlan {
   int workers, per, segments;
 };
-// As many teams as run at once, about; each takes contiguous rows, of one group where a gate is shared by more rows than
+// As many teams as run at once on 256 units, about (the workspace's size follows from it, and is asked for without a device); each takes contiguous rows, of one group where a gate is shared by more rows than
 // that, else of whole groups.  at_once: waves of the kernel that a compute unit has registers for.
 constexpr int NORM_WAVES = 12, NORM_WAVES_CENTRED = 8;
 inline NormPlan norm_plan(int64_t rows, int D, int64_t gate_rows, int at_once) {

@@ -4,8 +4,8 @@
 // consecutive columns at a time: epi(m, n, N, epi.row(m), epi.columns(n, N), sums..), with n a multiple of 4 below N.
 //
 // Large products are bound by the matrix units at the clock that they leave the chip (busy 58 to 64 % of the cycles, no bank
-// conflicts): 8192^3 in 8 bits 433 to 448 us, 2460 to 2540 TOP/s; 8192 x 4096 to 8192 with two weights in bf16 745 to 760 us, 1450 to
-// 1480 TFLOP/s.  Small ones by the operands' way into LDS, 25 to 30 bytes a clock and compute unit: 256 x 4096 by 4096 in 8 bits 10 us.
+// conflicts): 8192^3 in 8 bits 410 to 448 us by card, 2460 to 2680 TOP/s; 8192 x 4096 to 8192 with two weights in bf16 738 to 760 us, 1450 to
+// 1490 TFLOP/s.  Small ones by the operands' way into LDS, 25 to 30 bytes a clock and compute unit: 256 x 4096 by 4096 in 8 bits 9 to 10 us.
 #pragma once
 #include <type_traits>
 
