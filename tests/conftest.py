@@ -1,5 +1,6 @@
 import os
 import sys
+import zlib
 
 import pytest
 
@@ -15,3 +16,20 @@ def pytest_configure(config):
 @pytest.fixture(scope="session")
 def golden_dir():
     return os.path.join(ROOT, "tests", "golden")
+
+
+@pytest.fixture(autouse=True)
+def seeds_that_repeat(request, monkeypatch):
+    """test_gated_layers_gpu.py makes its inputs from hash(key), which Python salts for every process where a key holds a string: a
+    failure could not be run again.  Such keys get a digest of themselves here; keys of numbers have the seeds they had."""
+    if request.module.__name__.split(".")[-1] != "test_gated_layers_gpu":
+        return
+    import torch
+
+    def gen(*key):
+        g = torch.Generator(device="cuda:0")
+        numbers = all(isinstance(k, int) for k in key)
+        g.manual_seed(hash(key) % (1 << 31) if numbers else zlib.crc32(repr(key).encode()))
+        return g
+
+    monkeypatch.setattr(request.module, "gen", gen)

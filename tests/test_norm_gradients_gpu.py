@@ -94,3 +94,33 @@ def test_sums_of_absent_vectors(rows, D, post, pre):
     bare = backward(b, r, dn, dro, post, pre, {}, ())
     for x, y in zip(bare[:2], (dr, db)):
         assert float((x - y).abs().max()) <= 1e-5 * float(y.abs().max())
+
+
+@pytest.mark.parametrize("gate_rows", [1, 3, 700])
+@pytest.mark.parametrize("rows,D", [(1, 4096), (40, 4097), (303, 2832), (700, 520), (140, 456)])
+def test_gradient_of_the_gate_where_the_block_is_near_zero(rows, D, gate_rows):
+    """p, the normed block's output, is off by u of what it is made of (the row's mean, the weight, the bias), not of itself, where they
+    cancel; so is its product with the gradient of r'."""
+    print(f"dgate {rows} x {D}, {gate_rows} rows a gate", flush=True)
+    g = gen(rows, D, gate_rows)
+    b, r, dn, dro = (torch.randn((rows, D), generator=g, device=DEV) + (0.5 if i == 0 else 0.0) for i in range(4))
+    groups = -(-rows // gate_rows)
+    gate, scale, w, bias = (torch.randn(s, generator=g, device=DEV) for s in ((groups, D), (D,), (D,), (D,)))
+    got = B.bnn_norm_gate_backward(b, r, dn, dro, gate=gate, gate_rows=gate_rows, res_scale=scale, w_post=w, bias_post=bias, post="layer",
+                                   pre="rms")["dgate"]
+    at = torch.arange(rows, device=DEV) // gate_rows
+    m = scale.double() * gate.double()[at]
+    ub, rsb = unit(b.double(), "layer")
+    p = ub * w.double() + bias.double()
+    r1 = r.double() + m * p
+    ur, rsr = unit(r1, "rms")
+    e = dn.double()
+    dr = dro.double() + rsr * (e - ur * (e * ur).mean(1, keepdim=True))
+    size_p = (ub.abs() + rsb * b.double().abs().mean(1, keepdim=True)) * w.double().abs() + bias.double().abs()
+    size_ur = ur.abs() + rsr * (r.double().abs() + m.abs() * size_p)
+    size_dr = dro.double().abs() + rsr * (e.abs() + size_ur * (e.abs() * size_ur).mean(1, keepdim=True))
+    zero = torch.zeros((groups, D), dtype=torch.float64, device=DEV)
+    want = zero.index_add(0, at, dr * scale.double() * p)
+    bound = (256 + rows) * U32 * zero.index_add(0, at, size_dr * scale.double().abs() * size_p)
+    off = (got.double() - want).abs()
+    assert bool((off <= bound).all()), float((off / bound).max())
