@@ -412,6 +412,117 @@ BNN_API bnn_status bnn_gated_ff_backward(const void *x, int64_t x_ld, const void
                                          const void *dh, int64_t dh_ld, void *dx, int64_t dx_ld, void *dwg, int64_t dwg_ld,
                                          void *dwu, int64_t dwu_ld, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- 8-bit floating point and experts ----------------------------------------------------------
+ *
+ * Linear layers on e4m3 values (the largest is 448) with a scale for each block of 128 of them, the layers of experts that tokens
+ * are sent to, and what is around them, each with its gradient.
+ *
+ * A matrix in this form, [rows, K]: rows of bnn_f8_row_bytes(K) bytes, whole blocks, zeros behind the K values, row strides `ld`
+ *   multiples of 16 bytes; scales [rows, ceil(K / 128)] of one byte, p + 127 for 2^p (E8M0), rows of bnn_f8_scale_bytes(K) readable
+ *   bytes, strides multiples of 4.  Operands of products: ld below 2^22.  All base pointers are on 16 bytes.
+ *   Values that are not numbers are NaN in e4m3 too, infinities become NaN; neither counts for a block's scale.
+ */
+typedef enum { BNN_SCALE_E8M0 = 0, BNN_SCALE_F32 = 1 } bnn_scale_type;
+BNN_API int64_t bnn_f8_row_bytes(int64_t K);   /* K up to a multiple of 128; 0 for K <= 0 */
+BNN_API int64_t bnn_f8_scale_bytes(int64_t K); /* ceil(K / 128) up to a multiple of 4; 0 for K <= 0 */
+
+/*
+ * bnn_quant_blocks_f8 -- rows in this form: of each block of 128 values with a = max |x| the least p >= -100 with a <= 448 * 2^p,
+ *   and q = x / 2^p rounded to nearest, ties to even (2^p changes no digit of x).
+ *   x [T, K] of `type` (bnn_float).  rows NULL: S = T rows as they are.  Else rows [S] int32 from bnn_expert_sort, slots of
+ *   T * k: position s is x[rows[s] / k]; -1: zeros; any other value outside [0, T * k): left as it was.
+ * bnn_quant_columns_f8 -- the same with x turned: q [D, S], blocks along the positions (the operands of a weight's gradient).
+ *   x [T, D]; positions without a slot are zeros, and so is the rest of the last block.  S at most 2^22 - 128; T > 0 where S > 0.
+ * bnn_quant_weight_f8 -- weights w [experts, N, K] (expert_ld elements between experts) in blocks of 128 x 128: `out` as they lie, q [N,
+ *   K] and scales [ceil(N / 128), ceil(K / 128)], `turned` q [K, N] and scales [ceil(K / 128), ceil(N / 128)]; either may be NULL.  The
+ *   structs are HOST structs; ld and expert_ld in bytes, scale_ld and scale_expert_ld too.  N and K at most 2^22.
+ */
+typedef struct {
+  uint8_t *q;
+  int64_t ld, expert_ld;
+  uint8_t *scale;
+  int64_t scale_ld, scale_expert_ld;
+} bnn_f8_weight;
+BNN_API bnn_status bnn_quant_blocks_f8(const void *x, int type, int64_t T, int64_t x_ld, const int32_t *rows, int64_t k,
+                                       int64_t S, int64_t K, uint8_t *q, int64_t q_ld, uint8_t *scale, int64_t scale_ld,
+                                       void *stream);
+BNN_API bnn_status bnn_quant_columns_f8(const void *x, int type, int64_t T, int64_t x_ld, const int32_t *rows, int64_t k,
+                                        int64_t S, int64_t D, uint8_t *q, int64_t q_ld, uint8_t *scale, int64_t scale_ld,
+                                        void *stream);
+BNN_API bnn_status bnn_quant_weight_f8(const void *w, int type, int64_t experts, int64_t expert_ld, int64_t N, int64_t K,
+                                       int64_t w_ld, const bnn_f8_weight *out, const bnn_f8_weight *turned, void *stream);
+
+/*
+ * bnn_linear_f8 -- y[m,n] = sum_b a_scale[m,b] * b_scale[n,b] * (sum over block b of a[m,k] * b[n,k]) (+ bias[n]), fp32, rounded
+ *   once to `type`.
+ *   a [M, K] with its scales.  b [N, K]; b_scale_rows rows of it share a row of scales: 1, or 128 (bnn_quant_weight_f8).
+ *   b_scale_type BNN_SCALE_E8M0, or BNN_SCALE_F32: fp32 scales, any value, b_scale_rows 128, rows of ceil(K / 128).  bias fp32 or NULL.
+ *   A training step: y from x and w; dx from bnn_quant_blocks_f8 of dy and `turned` of w; dw from bnn_quant_columns_f8 of dy and x.
+ * bnn_expert_linear_f8 -- the same for rows sorted by expert: rows offsets[e] .. offsets[e + 1] - 1 of a [S, K] times b[e], of
+ *   [experts, N, K] (b_expert_ld bytes, b_scale_expert_ld scales between experts).  offsets [experts + 1] int32, ascending, as
+ *   bnn_expert_sort gives them (what is outside [0, S] counts as its end).  Rows behind the last group are left as they were.
+ * bnn_expert_linear_f8_dw -- the gradients of those weights, dw[e] [N, K] = sum over the expert's positions s of a[n,s] * b[k,s], a [N,
+ *   S] and b [K, S] from bnn_quant_columns_f8 of the gradient and of the rows; offsets multiples of 128 (bnn_expert_sort with
+ *   align 128).  Experts without rows get zeros.
+ * M, S, N below 2^31 - 256, K at most 2^22, at most 65535 experts (BNN_ERR_UNSUPPORTED beyond).
+ */
+BNN_API bnn_status bnn_linear_f8(const uint8_t *a, int64_t lda, const uint8_t *a_scale, int64_t a_scale_ld, const uint8_t *b,
+                                 int64_t ldb, const void *b_scale, int b_scale_type, int64_t b_scale_ld, int b_scale_rows,
+                                 const float *bias, int64_t M, int64_t N, int64_t K, void *y, int type, int64_t ldy,
+                                 void *stream);
+BNN_API bnn_status bnn_expert_linear_f8(const uint8_t *a, int64_t lda, const uint8_t *a_scale, int64_t a_scale_ld,
+                                        const int32_t *offsets, int64_t experts, const uint8_t *b, int64_t ldb, int64_t b_expert_ld,
+                                        const void *b_scale, int b_scale_type, int64_t b_scale_ld, int64_t b_scale_expert_ld,
+                                        int b_scale_rows, int64_t S, int64_t N, int64_t K, void *y, int type, int64_t ldy,
+                                        void *stream);
+BNN_API bnn_status bnn_expert_linear_f8_dw(const uint8_t *a, int64_t lda, const uint8_t *a_scale, int64_t a_scale_ld,
+                                           const uint8_t *b, int64_t ldb, const uint8_t *b_scale, int64_t b_scale_ld,
+                                           const int32_t *offsets, int64_t experts, int64_t N, int64_t K, int64_t S, void *dw,
+                                           int type, int64_t dw_ld, int64_t dw_expert_ld, void *stream);
+
+/*
+ * bnn_expert_sort -- where each token's rows go among those of its experts.  experts [T, k] (index_bytes 4 or 8: int32 or int64):
+ *   slot t * k + j is token t's j-th choice; what is outside [0, E) is no expert (the slot is dropped).
+ *   offsets [E + 1]: expert e has positions offsets[e] .. offsets[e + 1] - 1, its number of slots up to a multiple of `align`;
+ *   rows [S]: the slot at a position, slots of an expert in their order; -1 between an expert's last slot and the next one's first
+ *   position, -2 behind the last expert's;  places [T, k]: the position of a slot, -1 for a dropped one.  All int32.
+ *   S at least bnn_expert_rows(T, k, E, align), which is enough for any choices; T * k at most 2^30, E at most 1024, align at most 4096.
+ *   workspace at least bnn_expert_sort_workspace_bytes(T, k, E) bytes (0 for few slots).
+ * bnn_expert_gather -- xs[s] = x[rows[s] / k], zeros for -1; positions with another value are left as they were.  x [T, D], xs [S, D].
+ * bnn_expert_combine -- out[t] = sum over j of weights[t,j] * ys[places[t,j]] in fp32, rounded once; places outside [0, S) add nothing
+ *   and are not read.  ys [S, D], weights [T, k] fp32 or NULL: 1 (which is the gradient of bnn_expert_gather: dx from dxs).
+ * bnn_expert_combine_backward -- dys[s] = weights[slot] * dout[slot / k], zeros at positions of -1 (rows), others left as they were;
+ *   dweights[t,j] = sum over columns of ys[places[t,j]] * dout[t], 0 for a dropped slot.  dys or dweights may be NULL (not wanted).
+ *   D at most 32768.
+ * Everything of `type` (bnn_float) but weights, dweights.  A slot's place and its row have to belong together, as the sort gives them.
+ */
+BNN_API int64_t bnn_expert_rows(int64_t T, int64_t k, int64_t experts, int64_t align);
+BNN_API size_t bnn_expert_sort_workspace_bytes(int64_t T, int64_t k, int64_t experts);
+BNN_API bnn_status bnn_expert_sort(const void *experts, int index_bytes, int64_t T, int64_t k, int64_t E, int64_t align, int64_t S,
+                                   int32_t *offsets, int32_t *rows, int32_t *places, void *workspace, size_t workspace_bytes,
+                                   void *stream);
+BNN_API bnn_status bnn_expert_gather(const void *x, int type, int64_t T, int64_t x_ld, const int32_t *rows, int64_t k, int64_t S,
+                                     int64_t D, void *xs, int64_t xs_ld, void *stream);
+BNN_API bnn_status bnn_expert_combine(const void *ys, int type, int64_t S, int64_t ys_ld, const int32_t *places, const float *weights,
+                                      int64_t T, int64_t k, int64_t D, void *out, int64_t out_ld, void *stream);
+BNN_API bnn_status bnn_expert_combine_backward(const void *ys, int type, int64_t S, int64_t ys_ld, const int32_t *rows,
+                                               const int32_t *places, const float *weights, const void *dout, int64_t dout_ld,
+                                               int64_t T, int64_t k, int64_t D, void *dys, int64_t dys_ld, float *dweights,
+                                               void *stream);
+
+/*
+ * bnn_gated_act -- h = act(g) * u of projections that lie side by side, gu [S, 2 F] = [g | u] (bnn_act, and its accuracy, as in
+ *   bnn_gated_ff); bnn_gated_act_f8: as e4m3 rows, h's fp32 values as by bnn_quant_blocks_f8.
+ * bnn_gated_act_backward -- dgu = [dh * u * act'(g) | dh * act(g)], beside gu and dh.
+ *   live  NULL, or one int32 on the device: rows from *live on are left alone (offsets + E of bnn_expert_sort).
+ */
+BNN_API bnn_status bnn_gated_act(const void *gu, int type, int64_t S, int64_t gu_ld, int64_t F, int act, const int32_t *live, void *h,
+                                 int64_t h_ld, void *stream);
+BNN_API bnn_status bnn_gated_act_f8(const void *gu, int type, int64_t S, int64_t gu_ld, int64_t F, int act, const int32_t *live,
+                                    uint8_t *q, int64_t q_ld, uint8_t *scale, int64_t scale_ld, void *stream);
+BNN_API bnn_status bnn_gated_act_backward(const void *gu, int type, int64_t S, int64_t gu_ld, int64_t F, int act, const int32_t *live,
+                                          const void *dh, int64_t dh_ld, void *dgu, int64_t dgu_ld, void *stream);
+
 /* ---- ablation --------------------------------------------------------------------------- */
 
 /*

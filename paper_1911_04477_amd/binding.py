@@ -37,6 +37,11 @@ class NormGateIn(ctypes.Structure):
                 ("gate_rows", _i64), ("res_scale", _p), ("w_post", _p), ("bias_post", _p), ("w_pre", _p), ("bias_pre", _p)]
 
 
+class F8Weight(ctypes.Structure):
+    """bnn_f8_weight"""
+    _fields_ = [("q", _p), ("ld", _i64), ("expert_ld", _i64), ("scale", _p), ("scale_ld", _i64), ("scale_expert_ld", _i64)]
+
+
 # name -> (restype, argtypes); the list mirrors include/bnn.h one to one.
 SIGNATURES = {
     "bnn_status_str": (ctypes.c_char_p, [_i32]),
@@ -82,6 +87,24 @@ SIGNATURES = {
     "bnn_gated_ff_backward_workspace_bytes": (_sz, [_i64, _i64, _i64]),
     "bnn_gated_ff_backward": (_i32, [_p, _i64, _p, _i64, _p, _i64, _i32, _i64, _i64, _i64, _p, _p, _i64, _p, _i64, _p, _i64,
                                      _p, _i64, _p, _sz, _p]),
+    "bnn_f8_row_bytes": (_i64, [_i64]),
+    "bnn_f8_scale_bytes": (_i64, [_i64]),
+    "bnn_quant_blocks_f8": (_i32, [_p, _i32, _i64, _i64, _p, _i64, _i64, _i64, _p, _i64, _p, _i64, _p]),
+    "bnn_quant_columns_f8": (_i32, [_p, _i32, _i64, _i64, _p, _i64, _i64, _i64, _p, _i64, _p, _i64, _p]),
+    "bnn_quant_weight_f8": (_i32, [_p, _i32, _i64, _i64, _i64, _i64, _i64, ctypes.POINTER(F8Weight), ctypes.POINTER(F8Weight), _p]),
+    "bnn_linear_f8": (_i32, [_p, _i64, _p, _i64, _p, _i64, _p, _i32, _i64, _i32, _p, _i64, _i64, _i64, _p, _i32, _i64, _p]),
+    "bnn_expert_linear_f8": (_i32, [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _i64, _p, _i32, _i64, _i64, _i32, _i64, _i64, _i64, _p,
+                                    _i32, _i64, _p]),
+    "bnn_expert_linear_f8_dw": (_i32, [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _i64, _i64, _i64, _p, _i32, _i64, _i64, _p]),
+    "bnn_expert_rows": (_i64, [_i64, _i64, _i64, _i64]),
+    "bnn_expert_sort_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "bnn_expert_sort": (_i32, [_p, _i32, _i64, _i64, _i64, _i64, _i64, _p, _p, _p, _p, _sz, _p]),
+    "bnn_expert_gather": (_i32, [_p, _i32, _i64, _i64, _p, _i64, _i64, _i64, _p, _i64, _p]),
+    "bnn_expert_combine": (_i32, [_p, _i32, _i64, _i64, _p, _p, _i64, _i64, _i64, _p, _i64, _p]),
+    "bnn_expert_combine_backward": (_i32, [_p, _i32, _i64, _i64, _p, _p, _p, _p, _i64, _i64, _i64, _i64, _p, _i64, _p, _p]),
+    "bnn_gated_act": (_i32, [_p, _i32, _i64, _i64, _i64, _i32, _p, _p, _i64, _p]),
+    "bnn_gated_act_f8": (_i32, [_p, _i32, _i64, _i64, _i64, _i32, _p, _p, _i64, _p, _i64, _p]),
+    "bnn_gated_act_backward": (_i32, [_p, _i32, _i64, _i64, _i64, _i32, _p, _p, _i64, _p, _i64, _p]),
 }
 
 # include/bnn_testing.h: the same calls with the kernel variant chosen by the caller, the
@@ -986,6 +1009,333 @@ def bnn_gated_ff_backward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, s
                                        _ptr(dwu), _rows(dwu, "dwu", F, D), _ptr(workspace), _workspace(workspace),
                                        _stream()), "bnn_gated_ff_backward")
     return dx, dwg, dwu
+
+
+# ---- 8-bit floating point and experts ------------------------------------------------
+F8, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+F8_BLOCK = 128
+
+
+def _present(t: torch.Tensor, name: str, *dtypes: torch.dtype) -> torch.Tensor:
+    """A tensor on the current device, whose stream the call goes to."""
+    if not t.is_cuda or (dtypes and t.dtype not in dtypes):
+        raise TypeError(f"{name} must be a GPU tensor" + (f" of dtype {', '.join(map(str, dtypes))}" if dtypes else ""))
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on another device than the current one")
+    return t
+
+
+def _float_rows(t: torch.Tensor, name: str, rows: Optional[int] = None, cols: Optional[int] = None) -> Tuple[int, int]:
+    """(type, row stride) of a floating-point matrix."""
+    _present(t, name, *FLOATS)
+    return FLOATS[t.dtype], _rows(t, name, rows, cols)
+
+
+def _whole(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, *shape: int) -> Optional[int]:
+    """A contiguous tensor of this shape, or None."""
+    if t is None:
+        return None
+    _present(t, name, dtype)
+    if tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {list(shape)} expected, got {list(t.shape)}")
+    return t.data_ptr()
+
+
+def _padded(t: torch.Tensor, name: str, shape: Tuple[int, ...], row: int, quantum: int) -> Tuple[int, int, int]:
+    """(pointer, row stride, stride between experts) of [.., rows, cols] whose rows have `row` elements of room each."""
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: {list(shape)} expected, got {list(t.shape)}")
+    if shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the values of a row have to be consecutive")
+    rows = shape[-2]
+    ld = t.stride(-2) if rows > 1 else max((row + quantum - 1) // quantum * quantum, t.stride(-2) // quantum * quantum)
+    experts, between = (1, 0) if len(shape) == 2 else (shape[0], t.stride(0))
+    if experts == 1:
+        between = rows * ld
+    if ld < row:
+        raise ValueError(f"{name}: rows need room for {row} elements each (rows_f8, scales_f8)")
+    if t.numel():
+        size = t.element_size()
+        last = t.storage_offset() + (experts - 1) * between + (rows - 1) * ld + row
+        if t.untyped_storage().nbytes() < last * size:
+            raise ValueError(f"{name}: the last row needs room for {row} elements too (rows_f8, scales_f8)")
+    return t.data_ptr(), ld, between
+
+
+def _blocks(K: int) -> int:
+    return (K + F8_BLOCK - 1) // F8_BLOCK
+
+
+def _f8(q: torch.Tensor, scale: torch.Tensor, name: str, shape: Tuple[int, ...]) -> Tuple[int, int, int, int]:
+    """Pointers and row strides of rows in e4m3 and of their scales."""
+    _present(q, name, F8)
+    _present(scale, name + "_scale", E8M0)
+    blocks = _blocks(shape[-1])
+    pq, ld, _ = _padded(q, name, shape, blocks * F8_BLOCK, 16)
+    ps, s_ld, _ = _padded(scale, name + "_scale", (*shape[:-1], blocks), (blocks + 3) // 4 * 4, 4)
+    return pq, ld, ps, s_ld
+
+
+def _f8_weight(b: torch.Tensor, scale: torch.Tensor, name: str, shape: Tuple[int, ...]):
+    """((pointer, row stride, stride between experts) of a weight [.., N, K], the same of its scales, their type, rows that share them)."""
+    _present(b, name, F8)
+    _present(scale, name + "_scale", E8M0, torch.float32)
+    N, K = shape[-2:]
+    blocks, wide = _blocks(K), scale.dtype == torch.float32
+    if scale.dim() != len(shape):
+        raise ValueError(f"{name}_scale: {len(shape)} dimensions expected")
+    per = 1 if scale.shape[-2] == N and not wide and N > 1 else F8_BLOCK
+    room, quantum = (blocks, 1) if wide else ((blocks + 3) // 4 * 4, 4)
+    return (_padded(b, name, shape, blocks * F8_BLOCK, 16),
+            _padded(scale, name + "_scale", (*shape[:-2], N if per == 1 else _blocks(N), blocks), room, quantum), int(wide), per)
+
+
+def rows_f8(rows: int, K: int, device="cuda:0", experts: Optional[int] = None) -> torch.Tensor:
+    """Room for e4m3 [rows, K] (or [experts, rows, K]) in rows of whole blocks of 128."""
+    lead = (rows,) if experts is None else (experts, rows)
+    return torch.empty((*lead, _blocks(K) * F8_BLOCK), dtype=torch.uint8, device=device).view(F8)[..., :K]
+
+
+def scales_f8(rows: int, K: int, device="cuda:0", experts: Optional[int] = None) -> torch.Tensor:
+    """Room for the scales of such rows, one a block: [rows, ceil(K / 128)] (or [experts, rows, ..])."""
+    lead = (rows,) if experts is None else (experts, rows)
+    return torch.empty((*lead, (_blocks(K) + 3) // 4 * 4), dtype=torch.uint8, device=device).view(E8M0)[..., :_blocks(K)]
+
+
+def _positions(rows: Optional[torch.Tensor], T: int) -> Tuple[Optional[int], int]:
+    if rows is None:
+        return None, T
+    if rows.dim() != 1:
+        raise ValueError("rows: a vector expected")
+    return _whole(rows, "rows", torch.int32, rows.shape[0]), rows.shape[0]
+
+
+def bnn_quant_blocks_f8(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                        rows: Optional[torch.Tensor] = None, k: int = 1) -> Tuple[torch.Tensor, torch.Tensor]:
+    """x [T, K] fp32, bf16 or fp16 -> (q e4m3 [S, K], scale [S, ceil(K / 128)]), powers of two.  rows (bnn_expert_sort): position s is
+    x[rows[s] // k], zeros for -1, left as it was for -2; without rows S = T."""
+    kind, ld = _float_rows(x, "x")
+    T, K = x.shape
+    p_rows, S = _positions(rows, T)
+    q = rows_f8(S, K, x.device) if q is None else q
+    scale = scales_f8(S, K, x.device) if scale is None else scale
+    pq, q_ld, ps, s_ld = _f8(q, scale, "q", (S, K))
+    _check(_c().bnn_quant_blocks_f8(_ptr(x), kind, T, ld, p_rows, k, S, K, pq, q_ld, ps, s_ld, _stream()), "bnn_quant_blocks_f8")
+    return q, scale
+
+
+def bnn_quant_columns_f8(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                         rows: Optional[torch.Tensor] = None, k: int = 1) -> Tuple[torch.Tensor, torch.Tensor]:
+    """x [T, D] -> (q e4m3 [D, S], scale [D, ceil(S / 128)]): x, or the rows of it that `rows` names, turned, in blocks along the
+    positions; positions without a row are zeros."""
+    kind, ld = _float_rows(x, "x")
+    T, D = x.shape
+    p_rows, S = _positions(rows, T)
+    q = rows_f8(D, S, x.device) if q is None else q
+    scale = scales_f8(D, S, x.device) if scale is None else scale
+    pq, q_ld, ps, s_ld = _f8(q, scale, "q", (D, S))
+    _check(_c().bnn_quant_columns_f8(_ptr(x), kind, T, ld, p_rows, k, S, D, pq, q_ld, ps, s_ld, _stream()), "bnn_quant_columns_f8")
+    return q, scale
+
+
+def bnn_quant_weight_f8(w: torch.Tensor, plain: bool = True, turned: bool = True):
+    """w [N, K] or [experts, N, K] -> ((q [.., N, K], scale [.., ceil(N / 128), ceil(K / 128)]), the same of w turned), in blocks of 128 x
+    128; None for a form that is not wanted."""
+    _present(w, "w", *FLOATS)
+    if w.dim() not in (2, 3):
+        raise ValueError("w: a matrix, or one for each expert")
+    if w.shape[-1] > 1 and w.stride(-1) != 1:
+        raise ValueError("w: the values of a row have to be consecutive")
+    E, (N, K) = None if w.dim() == 2 else w.shape[0], w.shape[-2:]
+    made, args = [], []
+    for wanted, r, c in ((plain, N, K), (turned, K, N)):
+        made.append((rows_f8(r, c, w.device, E), scales_f8(_blocks(r), c, w.device, E)) if wanted else None)
+        if wanted:
+            q, s = made[-1]
+            args.append(F8Weight(_ptr(q), q.stride(-2), 0 if E is None else q.stride(0), _ptr(s), s.stride(-2), 0 if E is None else s.stride(0)))
+        else:
+            args.append(None)
+    ld = w.stride(-2) if N > 1 else max(K, w.stride(-2))
+    _check(_c().bnn_quant_weight_f8(_ptr(w), FLOATS[w.dtype], 1 if E is None else E, 0 if E is None else w.stride(0), N, K, ld,
+                                     *[None if a is None else ctypes.addressof(a) for a in args], _stream()), "bnn_quant_weight_f8")
+    return tuple(made)
+
+
+def bnn_linear_f8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor,
+                  bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                  dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """a e4m3 [M, K] and its scales, b e4m3 [N, K] and its scales, a row of them for each of its rows or for 128 (these also
+    fp32) -> [M, N] of out's type, or of dtype."""
+    if a.dim() != 2 or b.dim() != 2:
+        raise ValueError("a, b: matrices expected")
+    (M, K), N = a.shape, b.shape[0]
+    pa, lda, psa, sa_ld = _f8(a, a_scale, "a", (M, K))
+    (pb, ldb, _), (psb, sb_ld, _), wide, per = _f8_weight(b, b_scale, "b", (N, K))
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype, device=a.device)
+    kind, ldy = _float_rows(out, "out", M, N)
+    if bias is not None:
+        _present(bias, "bias")
+    _check(_c().bnn_linear_f8(pa, lda, psa, sa_ld, pb, ldb, psb, wide, sb_ld, per, _vector(bias, "bias", N), M, N, K, _ptr(out),
+                               kind, ldy, _stream()), "bnn_linear_f8")
+    return out
+
+
+def _offsets(offsets: torch.Tensor, E: int) -> int:
+    return _whole(offsets, "offsets", torch.int32, E + 1)
+
+
+def bnn_expert_linear_f8(a: torch.Tensor, a_scale: torch.Tensor, offsets: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor,
+                         out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """Rows sorted by expert (bnn_expert_sort), a e4m3 [S, K], times their experts' weights, b e4m3 [E, N, K], scales as in
+    bnn_linear_f8 -> [S, N]; rows behind the last expert's are left as they were."""
+    if a.dim() != 2 or b.dim() != 3:
+        raise ValueError("a [S, K], b [experts, N, K] expected")
+    (S, K), (E, N) = a.shape, b.shape[:2]
+    pa, lda, psa, sa_ld = _f8(a, a_scale, "a", (S, K))
+    (pb, ldb, b_es), (psb, sb_ld, sb_es), wide, per = _f8_weight(b, b_scale, "b", (E, N, K))
+    if out is None:
+        out = torch.empty((S, N), dtype=dtype, device=a.device)
+    kind, ldy = _float_rows(out, "out", S, N)
+    _check(_c().bnn_expert_linear_f8(pa, lda, psa, sa_ld, _offsets(offsets, E), E, pb, ldb, b_es, psb, wide, sb_ld, sb_es, per, S, N, K,
+                                      _ptr(out), kind, ldy, _stream()), "bnn_expert_linear_f8")
+    return out
+
+
+def bnn_expert_linear_f8_dw(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, offsets: torch.Tensor,
+                            out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """The experts' weights' gradients [E, N, K] from those of the rows, a e4m3 [N, S], and the rows, b e4m3 [K, S], both as
+    bnn_quant_columns_f8 gives them; offsets multiples of 128 (bnn_expert_sort with align 128)."""
+    if a.dim() != 2 or b.dim() != 2 or offsets.dim() != 1 or offsets.shape[0] < 1:
+        raise ValueError("a [N, S], b [K, S], offsets [experts + 1] expected")
+    (N, S), K, E = a.shape, b.shape[0], offsets.shape[0] - 1
+    pa, lda, psa, sa_ld = _f8(a, a_scale, "a", (N, S))
+    pb, ldb, psb, sb_ld = _f8(b, b_scale, "b", (K, S))
+    if out is None:
+        out = torch.empty((E, N, K), dtype=dtype, device=a.device)
+    _present(out, "out", *FLOATS)
+    p_out, ld, es = _padded(out, "out", (E, N, K), K, 1)
+    _check(_c().bnn_expert_linear_f8_dw(pa, lda, psa, sa_ld, pb, ldb, psb, sb_ld, _offsets(offsets, E), E, N, K, S, p_out,
+                                         FLOATS[out.dtype], ld, es, _stream()), "bnn_expert_linear_f8_dw")
+    return out
+
+
+def expert_rows(T: int, k: int, experts: int, align: int = 1) -> int:
+    """Positions that the sorted rows of any choices fit into."""
+    return int(_c().bnn_expert_rows(T, k, experts, align))
+
+
+def expert_sort_workspace_bytes(T: int, k: int, experts: int) -> int:
+    return int(_c().bnn_expert_sort_workspace_bytes(T, k, experts))
+
+
+def bnn_expert_sort(experts: torch.Tensor, E: int, align: int = 1, offsets: Optional[torch.Tensor] = None,
+                    rows: Optional[torch.Tensor] = None, places: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """experts [T, k] int32 or int64 (outside 0 .. E - 1: none) -> (offsets [E + 1], rows [S], places [T, k]), all int32: where each
+    expert's rows begin (multiples of align), the slot token * k + choice at a position, the position of a slot."""
+    _present(experts, "experts", torch.int32, torch.int64)
+    if experts.dim() != 2 or not experts.is_contiguous():
+        raise ValueError("experts: contiguous [tokens, choices] expected")
+    T, k = experts.shape
+    make = dict(dtype=torch.int32, device=experts.device)
+    offsets = torch.empty((max(E, 0) + 1,), **make) if offsets is None else offsets
+    rows = torch.empty((expert_rows(T, k, E, align),), **make) if rows is None else rows
+    places = torch.empty((T, k), **make) if places is None else places
+    if workspace is None:
+        workspace = torch.empty((expert_sort_workspace_bytes(T, k, E),), dtype=torch.uint8, device=experts.device)
+    p_rows, S = _positions(rows, 0)
+    _check(_c().bnn_expert_sort(_ptr(experts), experts.element_size(), T, k, E, align, S, _offsets(offsets, E), p_rows,
+                                 _whole(places, "places", torch.int32, T, k), _ptr(_present(workspace, "workspace")),
+                                 _workspace(workspace), _stream()), "bnn_expert_sort")
+    return offsets, rows, places
+
+
+def bnn_expert_gather(x: torch.Tensor, rows: torch.Tensor, k: int, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [T, D] -> [S, D]: position s is x[rows[s] // k], zeros for -1, left as it was for -2."""
+    kind, ld = _float_rows(x, "x")
+    T, D = x.shape
+    p_rows, S = _positions(rows, T)
+    out = torch.empty((S, D), dtype=x.dtype, device=x.device) if out is None else out
+    _present(out, "out", x.dtype)
+    _check(_c().bnn_expert_gather(_ptr(x), kind, T, ld, p_rows, k, S, D, _ptr(out), _rows(out, "out", S, D), _stream()), "bnn_expert_gather")
+    return out
+
+
+def bnn_expert_combine(ys: torch.Tensor, places: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """ys [S, D] -> [T, D], out[t] = sum over j of weights[t, j] * ys[places[t, j]]; dropped slots (-1) add nothing.  Without weights:
+    the gradient of bnn_expert_gather."""
+    kind, ld = _float_rows(ys, "ys")
+    (S, D), (T, k) = ys.shape, places.shape
+    out = torch.empty((T, D), dtype=ys.dtype, device=ys.device) if out is None else out
+    _present(out, "out", ys.dtype)
+    _check(_c().bnn_expert_combine(_ptr(ys), kind, S, ld, _whole(places, "places", torch.int32, T, k),
+                                    _whole(weights, "weights", torch.float32, T, k), T, k, D, _ptr(out), _rows(out, "out", T, D),
+                                    _stream()), "bnn_expert_combine")
+    return out
+
+
+def bnn_expert_combine_backward(ys: torch.Tensor, rows: torch.Tensor, places: torch.Tensor, weights: Optional[torch.Tensor],
+                                dout: torch.Tensor, dys: Optional[torch.Tensor] = None,
+                                dweights: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(dys [S, D], dweights [T, k]) of bnn_expert_combine from dout [T, D]; positions of no slot between the experts' rows get zeros,
+    those behind the last are left as they were."""
+    kind, ld = _float_rows(ys, "ys")
+    (S, D), (T, k) = ys.shape, places.shape
+    p_rows, _ = _positions(rows, S)
+    if rows.shape[0] != S:
+        raise ValueError(f"rows: {S} positions expected")
+    dys = torch.empty((S, D), dtype=ys.dtype, device=ys.device) if dys is None else dys
+    dweights = torch.empty((T, k), dtype=torch.float32, device=ys.device) if dweights is None else dweights
+    for t, name in ((dout, "dout"), (dys, "dys")):
+        _present(t, name, ys.dtype)
+    _check(_c().bnn_expert_combine_backward(_ptr(ys), kind, S, ld, p_rows, _whole(places, "places", torch.int32, T, k),
+                                             _whole(weights, "weights", torch.float32, T, k), _ptr(dout), _rows(dout, "dout", T, D), T, k,
+                                             D, _ptr(dys), _rows(dys, "dys", S, D), _whole(dweights, "dweights", torch.float32, T, k),
+                                             _stream()), "bnn_expert_combine_backward")
+    return dys, dweights
+
+
+def _gated(gu: torch.Tensor, act: str, live: Optional[torch.Tensor]):
+    kind, ld = _float_rows(gu, "gu")
+    if gu.shape[1] % 2:
+        raise ValueError("gu: [S, 2 F] expected")
+    return gu.shape[0], gu.shape[1] // 2, kind, ld, _one_of(ACTS, act, "act"), _whole(live, "live", torch.int32, 1)
+
+
+def bnn_gated_act(gu: torch.Tensor, act: str = "silu", out: Optional[torch.Tensor] = None,
+                  live: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """gu [S, 2 F] = [g | u] -> h [S, F] = act(g) * u.  live (one int32, as offsets[-1:] of bnn_expert_sort): rows from there on are
+    left as they were."""
+    S, F, kind, ld, a, p_live = _gated(gu, act, live)
+    out = torch.empty((S, F), dtype=gu.dtype, device=gu.device) if out is None else out
+    _present(out, "out", gu.dtype)
+    _check(_c().bnn_gated_act(_ptr(gu), kind, S, ld, F, a, p_live, _ptr(out), _rows(out, "out", S, F), _stream()), "bnn_gated_act")
+    return out
+
+
+def bnn_gated_act_f8(gu: torch.Tensor, act: str = "silu", q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                     live: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The same as e4m3 rows with their scales, from h in fp32."""
+    S, F, kind, ld, a, p_live = _gated(gu, act, live)
+    q = rows_f8(S, F, gu.device) if q is None else q
+    scale = scales_f8(S, F, gu.device) if scale is None else scale
+    pq, q_ld, ps, s_ld = _f8(q, scale, "q", (S, F))
+    _check(_c().bnn_gated_act_f8(_ptr(gu), kind, S, ld, F, a, p_live, pq, q_ld, ps, s_ld, _stream()), "bnn_gated_act_f8")
+    return q, scale
+
+
+def bnn_gated_act_backward(gu: torch.Tensor, dh: torch.Tensor, act: str = "silu", out: Optional[torch.Tensor] = None,
+                           live: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dgu [S, 2 F] of bnn_gated_act from dh [S, F]."""
+    S, F, kind, ld, a, p_live = _gated(gu, act, live)
+    out = torch.empty((S, 2 * F), dtype=gu.dtype, device=gu.device) if out is None else out
+    for t, name in ((dh, "dh"), (out, "out")):
+        _present(t, name, gu.dtype)
+    _check(_c().bnn_gated_act_backward(_ptr(gu), kind, S, ld, F, a, p_live, _ptr(dh), _rows(dh, "dh", S, F), _ptr(out),
+                                        _rows(out, "out", S, 2 * F), _stream()), "bnn_gated_act_backward")
+    return out
 
 
 # ---- measurement helpers (include/bnn_testing.h) -----------------------------------

@@ -8,6 +8,12 @@ GatedBlock8 is the serving form: weights and activations in 8 bits with a scale 
 number of tokens from one to the number it was made for, nothing allocated in a pass that is given r_out (it can be captured in a graph).  Its
 buffers serve one pass at a time: threads or streams that run at once need an object each.
 GatedProjections is the training form of the part that has a backward pass: the norms and both projections.
+
+The same with experts, in 8-bit floating point: each token's rows go to the experts chosen for it and come back weighted.
+
+    xs = rows of x sorted by expert,  gu = xs W1_e^T,  h = act(g) * u,  ys = h W2_e^T,  out[t] = sum over its experts of weight * ys
+
+ExpertBlock8 serves it (weights quantised once, buffers made once), ExpertLayer trains it.
 """
 from __future__ import annotations
 
@@ -78,3 +84,75 @@ class GatedProjections:
         (b, r, n, saved, given), self.kept = self.kept, None
         dn, dwg, dwu = B.bnn_gated_ff_backward(n, self.wg, self.wu, saved, dh)
         return {"dwg": dwg, "dwu": dwu, **B.bnn_norm_gate_backward(b, r, dn, dr_out, **given)}
+
+
+class ExpertBlock8:
+    """w1 [E, 2 F, D] (gate and up projections one below the other), w2 [E, D, F]: fp32, bf16 or fp16, quantised here once to e4m3
+    in blocks of 128 x 128.  Any number of tokens from one to `tokens`, `choices` experts each; a pass allocates nothing where it is
+    given out (it can be captured in a graph), and writes the buffers of the pass before over: threads or streams that run at once need
+    an object each."""
+
+    def __init__(self, w1: torch.Tensor, w2: torch.Tensor, tokens: int, choices: int, act: str = "silu",
+                 dtype: torch.dtype = torch.bfloat16):
+        (self.E, self.D, self.F), self.act, self.tokens, self.choices = w2.shape, act, tokens, choices
+        if w1.shape != (self.E, 2 * self.F, self.D):
+            raise ValueError(f"w1: [{self.E}, {2 * self.F}, {self.D}] expected")
+        (self.w1, _), (self.w2, _) = (B.bnn_quant_weight_f8(w, turned=False) for w in (w1, w2))
+        dev, S = w1.device, tokens * choices
+        self.offsets = torch.empty((self.E + 1,), dtype=torch.int32, device=dev)
+        self.rows, self.places = (torch.empty((S,), dtype=torch.int32, device=dev) for _ in range(2))
+        self.workspace = torch.empty((B.expert_sort_workspace_bytes(tokens, choices, self.E),), dtype=torch.uint8, device=dev)
+        self.x8, self.x_scale = B.rows_f8(S, self.D, dev), B.scales_f8(S, self.D, dev)
+        self.h8, self.h_scale = B.rows_f8(S, self.F, dev), B.scales_f8(S, self.F, dev)
+        self.gu, self.ys = (torch.empty((S, n), dtype=dtype, device=dev) for n in (2 * self.F, self.D))
+
+    def forward(self, x: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x [T, D], experts [T, choices] int32 or int64 (outside 0 .. E - 1: none), weights [T, choices] fp32 -> [T, D]."""
+        T, k = experts.shape
+        if T > self.tokens or k != self.choices:
+            raise ValueError(f"made for {self.tokens} tokens of {self.choices} choices")
+        S = T * k
+        x8, x_scale, h8, h_scale, gu, ys = (t[:S] for t in (self.x8, self.x_scale, self.h8, self.h_scale, self.gu, self.ys))
+        offsets, rows, places = B.bnn_expert_sort(experts, self.E, offsets=self.offsets, rows=self.rows[:S],
+                                                  places=self.places[:S].view(T, k), workspace=self.workspace)
+        B.bnn_quant_blocks_f8(x, x8, x_scale, rows=rows, k=k)
+        B.bnn_expert_linear_f8(x8, x_scale, offsets, *self.w1, out=gu)
+        B.bnn_gated_act_f8(gu, act=self.act, q=h8, scale=h_scale)
+        B.bnn_expert_linear_f8(h8, h_scale, offsets, *self.w2, out=ys)
+        return B.bnn_expert_combine(ys, places, weights, out=out)
+
+
+class ExpertLayer:
+    """w1 [E, 2 F, D], w2 [E, D, F]; products in e4m3 with block scales, everything between them in the tensors' type.  Weights are
+    quantised anew in each forward pass, which keeps what backward needs, for one pass at a time."""
+
+    def __init__(self, w1: torch.Tensor, w2: torch.Tensor, act: str = "silu"):
+        self.w1, self.w2, self.act = w1, w2, act
+        self.kept: Optional[Tuple] = None
+
+    def forward(self, x: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor) -> torch.Tensor:
+        """x [T, D], experts [T, k], weights [T, k] fp32 -> [T, D]."""
+        k = experts.shape[1]
+        offsets, rows, places = B.bnn_expert_sort(experts, self.w2.shape[0], align=B.F8_BLOCK)
+        (w1, w1t), (w2, w2t) = B.bnn_quant_weight_f8(self.w1), B.bnn_quant_weight_f8(self.w2)
+        gu = B.bnn_expert_linear_f8(*B.bnn_quant_blocks_f8(x, rows=rows, k=k), offsets, *w1, dtype=x.dtype)
+        h8 = B.bnn_gated_act_f8(gu, act=self.act, live=offsets[-1:])
+        ys = B.bnn_expert_linear_f8(*h8, offsets, *w2, dtype=x.dtype)
+        self.kept = (x, k, offsets, rows, places, weights, w1t, w2t, gu, ys)
+        return B.bnn_expert_combine(ys, places, weights)
+
+    def backward(self, dout: torch.Tensor) -> Dict[str, torch.Tensor]:
+        """Gradients of the last forward pass from that of its output: dx, dweights [T, k], dw1 and dw2 (fp32)."""
+        if self.kept is None:
+            raise RuntimeError("backward comes after a forward pass of its own")
+        (x, k, offsets, rows, places, weights, w1t, w2t, gu, ys), self.kept = self.kept, None
+        live = offsets[-1:]
+        dys, dweights = B.bnn_expert_combine_backward(ys, rows, places, weights, dout)
+        dh = B.bnn_expert_linear_f8(*B.bnn_quant_blocks_f8(dys), offsets, *w2t, dtype=x.dtype)
+        h = B.bnn_gated_act(gu, act=self.act, live=live)
+        dw2 = B.bnn_expert_linear_f8_dw(*B.bnn_quant_columns_f8(dys), *B.bnn_quant_columns_f8(h), offsets)
+        dgu = B.bnn_gated_act_backward(gu, dh, act=self.act, live=live)
+        dw1 = B.bnn_expert_linear_f8_dw(*B.bnn_quant_columns_f8(dgu), *B.bnn_quant_columns_f8(x, rows=rows, k=k), offsets)
+        dxs = B.bnn_expert_linear_f8(*B.bnn_quant_blocks_f8(dgu), offsets, *w1t, dtype=x.dtype)
+        return {"dx": B.bnn_expert_combine(dxs, places), "dweights": dweights, "dw1": dw1, "dw2": dw2}

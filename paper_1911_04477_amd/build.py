@@ -18,7 +18,8 @@ FASTCALL = os.path.join(HERE, "_fastcall.so")
 TENSORCALL = os.path.join(HERE, "_tensorcall.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "encode.hip", "im2col.hip", "gemm.hip", "gemm_lowk.hip", "gemm_fewrows.hip", "gemm_fp4.hip", "gemm_fp4_split.hip", "conv.hip", "conv_first_sign.hip", "conv_chain.hip", "conv_pointwise.hip", "conv_word.hip", "glue.hip", "mfma.hip", "control.hip",
-           "quant_rows.hip", "linear_i8.hip", "norm_gate.hip", "gated_ff.hip"]
+           "quant_rows.hip", "linear_i8.hip", "norm_gate.hip", "gated_ff.hip",
+           "quant_f8.hip", "linear_f8.hip", "experts.hip", "gated_act.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # Packed-FP32 VALU forms are disabled for all device code of this library.

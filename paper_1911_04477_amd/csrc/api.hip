@@ -140,6 +140,17 @@ extern "C" const char *bnn_kernel_name(int kernel_id) {
     case bnn::KID_REALIGN: return "realign";
     case bnn::KID_PRODUCT_SUMS: return "product_sums";
     case bnn::KID_GATED_FF_BACKWARD: return "gated_ff_backward";
+    case bnn::KID_QUANT_F8: return "quant_blocks_f8";
+    case bnn::KID_QUANT_F8_COLUMNS: return "quant_columns_f8";
+    case bnn::KID_QUANT_F8_WEIGHT: return "quant_weight_f8";
+    case bnn::KID_LINEAR_F8: return "linear_f8";
+    case bnn::KID_LINEAR_F8_FEW: return "linear_f8_few";
+    case bnn::KID_EXPERT_SORT: return "expert_sort";
+    case bnn::KID_EXPERT_GATHER: return "expert_gather";
+    case bnn::KID_EXPERT_COMBINE: return "expert_combine";
+    case bnn::KID_EXPERT_COMBINE_BACKWARD: return "expert_combine_backward";
+    case bnn::KID_GATED_ACT: return "gated_act";
+    case bnn::KID_GATED_ACT_BACKWARD: return "gated_act_backward";
     case bnn::KID_VALU_PROBE: return "valu_probe";
     case bnn::KID_COPY_PROBE: return "copy_probe";
   }

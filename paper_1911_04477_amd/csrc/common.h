@@ -45,7 +45,18 @@ enum KernelId : int {
   KID_REALIGN = 34,
   KID_GATED_FF_BACKWARD = 35,
   KID_PRODUCT_SUMS = 36,
-  KID_COUNT = 37
+  KID_QUANT_F8 = 37,
+  KID_QUANT_F8_COLUMNS = 38,
+  KID_QUANT_F8_WEIGHT = 39,
+  KID_LINEAR_F8 = 40,
+  KID_LINEAR_F8_FEW = 41,
+  KID_EXPERT_SORT = 42,
+  KID_EXPERT_GATHER = 43,
+  KID_EXPERT_COMBINE = 44,
+  KID_EXPERT_COMBINE_BACKWARD = 45,
+  KID_GATED_ACT = 46,
+  KID_GATED_ACT_BACKWARD = 47,
+  KID_COUNT = 48
 };
 
 // Timing hook: records an event pair around a launch when profiling is on.
