@@ -3,6 +3,13 @@
 // fp32 sums.  A step of 128 bytes of k is one block.  Scales that are powers of two go into the matrix instruction as bytes;
 // fp32 scales of B, one for 128 rows and a block, multiply a block's sums on the vector unit (the rows' scale is
 // in them by then), which fits into the shadow of the matrix instructions: 16 multiply-adds for two of them.
+//
+// The 8-bit matrix instruction is exact in single products and adds up groups of them in fp32, but within a group of eight it keeps no bits
+// below 2^-13 of the largest: measured on normal values, 1.5e-5 of the result in the 2-norm, whatever the length (at worst 2^-10 of the sum of
+// magnitudes).  That is a hundredth of what rounding the result to bf16 costs (a fourteenth in fp16), and far below the 2^-4 of the operands'
+// own rounding, so results in 16 bits of many rows take it, at twice the rate.  fp32 results, and the kernel of few rows, which memory bounds, are
+// EXACT: values go to bf16 on their way into the 16-bit instruction, times their scales; no digit is lost, and sums are fp32's.
+//
 // The same kernels take the experts' products: rows of A in groups with a weight each, or groups along k with a result each.
 #pragma once
 #include "f8.h"
@@ -126,12 +133,27 @@ __device__ __forceinline__ void f8_store(const F8Operands &p, const F8Part &t, i
   else store8(reinterpret_cast<float *>(t.y) + m * p.ldy, n, t.N, v);
 }
 
+// Four e4m3 values times 2^p as bf16, both exactly.
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void f8_widen(int four, float scale, v8bf &to, int at) {
+  const v2bf lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, scale, true);
+  to[at] = lo[0], to[at + 1] = lo[1], to[at + 2] = hi[0], to[at + 3] = hi[1];
+}
+struct F8Wide {
+  v8bf v[4];
+  __device__ __forceinline__ F8Wide(const v8i &q, uint32_t scale) {  // the scale in the lowest byte
+    const float s = __uint_as_float((scale & 0xffu) << 23);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f8_widen(q[i], s, v[i / 2], i % 2 * 4);
+  }
+};
+
 __device__ __forceinline__ v16f f8_mfma(const v8i &a, const v8i &b, const v16f &c, uint32_t sa, uint32_t sb) {
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, (int)sa, 0, (int)sb);
 }
 
 // LDS as in tile_mm.h: rows of 128 bytes, 16-byte piece c of row r in slot c ^ (r % 8).  WGM x WGN waves of 32 x 32 blocks.
-template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE>  // WIDE: fp32 scales of B
+template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE, bool EXACT>  // WIDE: fp32 scales of B
 __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) {
   constexpr int WAVES = WGM * WGN, ROWS = BM + BN, LOADS = ROWS / 8 / WAVES, LOADS_A = BM / 8 / WAVES;
   static_assert(ROWS % (8 * WAVES) == 0 && BM % (8 * WAVES) == 0 && BM % (32 * WGM) == 0 && BN % (32 * WGN) == 0, "");
@@ -219,6 +241,35 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) 
     Half f[2];
     fetch(f[0], now, 0);
     fetch(f[1], now, 1);
+    if constexpr (EXACT) {
+      v16f part[TM][TN];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int a = 0; a < TM; ++a) {
+          const F8Wide wa(f[h].a[a], sa[a]);
+#pragma unroll
+          for (int b = 0; b < TN; ++b) {
+            const F8Wide wb(f[h].b[b], sb[b]);
+            v16f sum = !WIDE ? acc[a][b] : h ? part[a][b] : v16f{};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb.v[c], wa.v[c], sum, 0, 0, 0);
+            (WIDE ? part : acc)[a][b] = sum;
+          }
+        }
+      }
+      if constexpr (WIDE) {
+#pragma unroll
+        for (int a = 0; a < TM; ++a)
+#pragma unroll
+          for (int b = 0; b < TN; ++b) {
+            const float s = wide[b][i];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[a][b][r] = fmaf(part[a][b][r], s, acc[a][b][r]);
+          }
+      }
+    }
+    if constexpr (!EXACT)
 #pragma unroll
     for (int a = 0; a < TM; ++a)
 #pragma unroll
@@ -270,14 +321,14 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) 
     }
 }
 
-template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE>
+template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE, bool EXACT>
 __global__ __launch_bounds__(64 * WGM *WGN, WGM *WGN < 4 ? 1 : WGM *WGN / 4) void f8_tile_kernel(F8Operands p) {
   __shared__ __attribute__((aligned(16))) char lds[STAGES * (BM + BN) * MM_STEP];
-  f8_tile_product<BM, BN, WGM, WGN, STAGES, WIDE>(p, lds);
+  f8_tile_product<BM, BN, WGM, WGN, STAGES, WIDE, EXACT>(p, lds);
 }
 
 // At most 16 rows of A (of a group): nothing is reused, B is streamed once and bounds the kernel.  A workgroup owns 16
-// columns; its waves deal k out in runs of four blocks, straight from memory into matrix operands, sums meet in LDS.
+// columns; its waves deal k out in runs of four blocks, straight from memory into registers, and sums meet in LDS.
 template <int WAVES, bool WIDE>
 __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void f8_few_kernel(F8Operands p) {
   __shared__ v4f sums[WAVES][64];
@@ -312,16 +363,23 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void f8_few_kernel(F8Operand
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       if (kb + r >= t.blocks) break;
-      const v8i va = __builtin_shufflevector(v.a[r][0], v.a[r][1], 0, 1, 2, 3, 4, 5, 6, 7);
-      const v8i vb = __builtin_shufflevector(v.b[r][0], v.b[r][1], 0, 1, 2, 3, 4, 5, 6, 7);
-      const int sa = (int)(v.sa >> (8 * r)), sb = (int)(v.sb >> (8 * r));
+      const float fa = __uint_as_float((v.sa >> (8 * r) & 0xffu) << 23), fb = __uint_as_float((v.sb >> (8 * r) & 0xffu) << 23);
+      v4f sum = WIDE ? v4f{} : acc;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          v8bf wa, wb;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) f8_widen(v.a[r][h][c * 2 + i], fa, wa, i * 4), f8_widen(v.b[r][h][c * 2 + i], fb, wb, i * 4);
+          sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, wa, sum, 0, 0, 0);
+        }
       if constexpr (WIDE) {
-        const v4f part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb, va, v4f{}, 0, 0, 0, sb, 0, sa);
         const float s = wide[kb + r];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = fmaf(part[i], s, acc[i]);
+        for (int i = 0; i < 4; ++i) acc[i] = fmaf(sum[i], s, acc[i]);
       } else {
-        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb, va, acc, 0, 0, 0, sb, 0, sa);
+        acc = sum;
       }
     }
   };

@@ -11,11 +11,11 @@ namespace bnn {
 // Which kernel takes a product, by rounds of tiles as in few_mm.h.  rows: of a group, on average, and groups: how many.
 enum : int { F8_256, F8_128, F8_64, F8_32, F8_FORM_COUNT, F8_FEW = 8 };
 constexpr MmForm F8_FORMS[F8_FORM_COUNT] = {{256, 256, 100, 200}, {128, 128, 45, 74}, {64, 64, 22, 32}, {32, 64, 17, 24}};
-inline int f8_form(int64_t rows, int64_t groups, int64_t N, bool wide, int64_t units) {
+inline int f8_form(int64_t rows, int64_t groups, int64_t N, bool small, int64_t units) {
   if (rows <= 16) return F8_FEW;
   int best = F8_64;
   int64_t least = INT64_MAX;
-  for (int f = wide ? F8_128 : F8_256; f < F8_FORM_COUNT; ++f) {
+  for (int f = small ? F8_128 : F8_256; f < F8_FORM_COUNT; ++f) {
     const MmForm &t = F8_FORMS[f];
     const int64_t tiles = groups * ((rows - 1) / t.bm + 1) * ((N - 1) / t.bn + 1);
     const int64_t cost = t.bm == 256 ? (tiles + units - 1) / units * t.one : tiles <= units ? t.one : (tiles + 2 * units - 1) / (2 * units) * t.two;
@@ -24,7 +24,7 @@ inline int f8_form(int64_t rows, int64_t groups, int64_t N, bool wide, int64_t u
   return best;
 }
 
-template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE>
+template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE, bool EXACT>
 bnn_status launch_f8_tile(F8Operands p, hipStream_t s) {
   p.tilesN = (p.N - 1) / BN + 1;
   // groups of rows: each has a part of a tile more than its rows fill at most
@@ -34,7 +34,7 @@ bnn_status launch_f8_tile(F8Operands p, hipStream_t s) {
   ProfScope ps(KID_LINEAR_F8, s);
   wide_launches(tiles, [&](int64_t first, uint32_t n) {
     p.first = first;
-    f8_tile_kernel<BM, BN, WGM, WGN, STAGES, WIDE><<<n, 64 * WGM * WGN, 0, s>>>(p);
+    f8_tile_kernel<BM, BN, WGM, WGN, STAGES, WIDE, EXACT><<<n, 64 * WGM * WGN, 0, s>>>(p);
   });
   return launch_status();
 }
@@ -52,19 +52,23 @@ bnn_status launch_f8_few(F8Operands p, hipStream_t s) {
   return launch_status();
 }
 
-template <bool WIDE>
-bnn_status run_f8(const F8Operands &p, hipStream_t s) {
+template <bool WIDE, bool EXACT>
+bnn_status run_f8_as(const F8Operands &p, hipStream_t s) {
   int64_t rows = p.M, groups = 1;
   if (p.groups == F8_GROUP_ROWS) groups = std::min(p.E, p.M), rows = (p.M - 1) / groups + 1;
   if (p.groups == F8_GROUP_K) groups = p.E;
-  switch (f8_form(rows, groups, p.N, WIDE, device_cu_count())) {
+  switch (f8_form(rows, groups, p.N, WIDE || EXACT, device_cu_count())) {
     case F8_256:
-      if constexpr (!WIDE) return launch_f8_tile<256, 256, 2, 2, 2, false>(p, s);
-    case F8_128: return launch_f8_tile<128, 128, 2, 2, 2, WIDE>(p, s);
-    case F8_64: return launch_f8_tile<64, 64, 2, 2, 3, WIDE>(p, s);
-    case F8_32: return launch_f8_tile<32, 64, 1, 2, 4, WIDE>(p, s);
+      if constexpr (!WIDE && !EXACT) return launch_f8_tile<256, 256, 2, 2, 2, false, false>(p, s);
+    case F8_128: return launch_f8_tile<128, 128, 2, 2, 2, WIDE, EXACT>(p, s);
+    case F8_64: return launch_f8_tile<64, 64, 2, 2, 3, WIDE, EXACT>(p, s);
+    case F8_32: return launch_f8_tile<32, 64, 1, 2, 4, WIDE, EXACT>(p, s);
     default: return launch_f8_few<WIDE>(p, s);
   }
+}
+template <bool WIDE>
+bnn_status run_f8(const F8Operands &p, hipStream_t s) {
+  return p.type == BNN_F32 ? run_f8_as<WIDE, true>(p, s) : run_f8_as<WIDE, false>(p, s);
 }
 
 // B's scales, checked: N rows of K values, of which `per` share a row of scales.
