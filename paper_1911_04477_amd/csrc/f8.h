@@ -61,7 +61,7 @@ __device__ __forceinline__ void f8_store_block(const float (&v)[8], uint8_t *q, 
 inline bnn_status f8_check(const void *q, int64_t ld, const void *scale, int64_t scale_ld, int64_t K, bool products = true) {
   if (ld < f8_row_bytes(K) || scale_ld < f8_scale_bytes(K)) return BNN_ERR_STRIDE;
   if (ld % 16 || scale_ld % 4) return BNN_ERR_STRIDE;
-  if (products && ld >= (1 << 22)) return BNN_ERR_UNSUPPORTED;
+  if (products && (ld >= (1 << 22) || scale_ld >= (1 << 22))) return BNN_ERR_UNSUPPORTED;
   if (!q || !scale) return BNN_ERR_NULL;
   if (!aligned16(q) || !aligned16(scale)) return BNN_ERR_ALIGN;
   return BNN_OK;

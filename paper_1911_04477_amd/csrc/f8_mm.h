@@ -48,6 +48,7 @@ struct F8Part {
   const char *A, *B;
   const uint8_t *sa, *sb;
   int readable;        // bytes of a row of scales
+  int first;           // block of k
   char *y;
   int m0, n0, M, N;    // first row and column; the ends
   int blocks;
@@ -100,7 +101,7 @@ __device__ __forceinline__ bool f8_part(const F8Operands &p, int64_t id, F8Part 
     if (id >= (int64_t)tilesM * p.tilesN) return false;
     mm_tile((int)id, tilesM, p.tilesN, tm, tn);
     f8_row_tiles<BM>(p, tm, g, tile);
-    t = {p.A, p.B + g.e * p.b_es, p.sa, static_cast<const uint8_t *>(p.sb) + g.e * p.sb_es, readable, static_cast<char *>(p.y),
+    t = {p.A, p.B + g.e * p.b_es, p.sa, static_cast<const uint8_t *>(p.sb) + g.e * p.sb_es, readable, 0, static_cast<char *>(p.y),
          g.lo + tile * BM, tn * BN, g.hi, p.N, p.blocks};
     return true;
   }
@@ -110,13 +111,12 @@ __device__ __forceinline__ bool f8_part(const F8Operands &p, int64_t id, F8Part 
     if (e >= p.E) return false;
     mm_tile((int)(id - e * of), p.tilesM, p.tilesN, tm, tn);
     const int end = p.blocks * F8_BLOCK, lo = f8_clamped(p.offsets, e, end) / F8_BLOCK, hi = max(f8_clamped(p.offsets, e + 1, end) / F8_BLOCK, lo);
-    t = {p.A + (int64_t)lo * F8_BLOCK, p.B + (int64_t)lo * F8_BLOCK, p.sa + lo, static_cast<const uint8_t *>(p.sb) + lo,
-         readable - lo, static_cast<char *>(p.y) + e * p.y_es * size, tm * BM, tn * BN, p.M, p.N, hi - lo};
+    t = {p.A + (int64_t)lo * F8_BLOCK, p.B + (int64_t)lo * F8_BLOCK, p.sa, static_cast<const uint8_t *>(p.sb), readable, lo, static_cast<char *>(p.y) + e * p.y_es * size, tm * BM, tn * BN, p.M, p.N, hi - lo};
     return true;
   }
   if (id >= of) return false;
   mm_tile((int)id, p.tilesM, p.tilesN, tm, tn);
-  t = {p.A, p.B, p.sa, static_cast<const uint8_t *>(p.sb), readable, static_cast<char *>(p.y), tm * BM, tn * BN, p.M, p.N, p.blocks};
+  t = {p.A, p.B, p.sa, static_cast<const uint8_t *>(p.sb), readable, 0, static_cast<char *>(p.y), tm * BM, tn * BN, p.M, p.N, p.blocks};
   return true;
 }
 
@@ -127,12 +127,6 @@ __device__ __forceinline__ uint32_t f8_scales(const uint8_t *row, int kb, int en
   return *reinterpret_cast<const u32_any *>(row + at) >> (8 * (kb - at));
 }
 
-__device__ __forceinline__ void f8_store(const F8Operands &p, const F8Part &t, int m, int n, const float (&v)[8]) {
-  if (p.type == BNN_BF16) store8(reinterpret_cast<__bf16 *>(t.y) + m * p.ldy, n, t.N, v);
-  else if (p.type == BNN_F16) store8(reinterpret_cast<_Float16 *>(t.y) + m * p.ldy, n, t.N, v);
-  else store8(reinterpret_cast<float *>(t.y) + m * p.ldy, n, t.N, v);
-}
-
 // Four e4m3 values times 2^p as bf16, both exactly.
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void f8_widen(int four, float scale, v8bf &to, int at) {
@@ -141,8 +135,8 @@ __device__ __forceinline__ void f8_widen(int four, float scale, v8bf &to, int at
 }
 struct F8Wide {
   v8bf v[4];
-  __device__ __forceinline__ F8Wide(const v8i &q, uint32_t scale) {  // the scale in the lowest byte
-    const float s = __uint_as_float((scale & 0xffu) << 23);
+  __device__ __forceinline__ void set(const v8i &q, uint32_t scale) {  // scale: p + 127
+    const float s = __uint_as_float(scale << 23);
 #pragma unroll
     for (int i = 0; i < 8; ++i) f8_widen(q[i], s, v[i / 2], i % 2 * 4);
   }
@@ -152,178 +146,276 @@ __device__ __forceinline__ v16f f8_mfma(const v8i &a, const v8i &b, const v16f &
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, (int)sa, 0, (int)sb);
 }
 
-// LDS as in tile_mm.h: rows of 128 bytes, 16-byte piece c of row r in slot c ^ (r % 8).  WGM x WGN waves of 32 x 32 blocks.
+// A wave's 16 accumulators of a 256 x 256 tile fill the accumulation registers (mm_settle in tile_mm.h): products written out, each in place.
+__device__ __forceinline__ void f8_mfma_in_place(const v8i &a, const v8i &b, v16f &c, uint32_t sa, uint32_t sb) {
+  asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]" : "+a"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+}
+__device__ __forceinline__ void f8_settle(v16f (&c)[4]) {  // a matrix instruction of 16 passes: 19 wait states
+  asm volatile("s_nop 15\n\ts_nop 7" : "+a"(c[0]), "+a"(c[1]), "+a"(c[2]), "+a"(c[3]));
+}
+
+// LDS: a step's rows of 128 bytes as in tile_mm.h (16-byte piece c of row r in slot c ^ (r % 8)), behind them for each row the
+// four bytes of scales that hold the step's.  WGM x WGN waves of 32 x 32 blocks.
+template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE>
+struct F8Tile {
+  static constexpr int WAVES = WGM * WGN, ROWS = BM + BN, SCALED = WIDE ? BM : ROWS, LOADS_A = BM / 8 / WAVES, LOADS_ROWS = ROWS / 8 / WAVES,
+                       LOADS_SCALES = (SCALED / 64 + WAVES - 1) / WAVES, LOADS = LOADS_ROWS + (LOADS_SCALES ? LOADS_SCALES : 1),
+                       STAGE = ROWS * MM_STEP + (SCALED + 63) / 64 * 256, TM = BM / WGM / 32, TN = BN / WGN / 32;
+  static_assert(ROWS % (8 * WAVES) == 0 && BM % (8 * WAVES) == 0 && BM % (32 * WGM) == 0 && BN % (32 * WGN) == 0, "");
+};
 template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE, bool EXACT>  // WIDE: fp32 scales of B
 __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) {
-  constexpr int WAVES = WGM * WGN, ROWS = BM + BN, LOADS = ROWS / 8 / WAVES, LOADS_A = BM / 8 / WAVES;
-  static_assert(ROWS % (8 * WAVES) == 0 && BM % (8 * WAVES) == 0 && BM % (32 * WGM) == 0 && BN % (32 * WGN) == 0, "");
-  constexpr int TM = BM / WGM / 32, TN = BN / WGN / 32, STAGE = ROWS * MM_STEP;
+  using L = F8Tile<BM, BN, WGM, WGN, STAGES, WIDE>;
+  constexpr int WAVES = L::WAVES, LOADS = L::LOADS, STAGE = L::STAGE, TM = L::TM, TN = L::TN;
+  constexpr bool IN_PLACE = TM * TN == 16;
   F8Part t;
   if (!f8_part<BM, BN>(p, p.first + blockIdx.x, t)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WGN, wn = wave % WGN;
   const int piece = ((lane & 7) ^ (lane >> 3)) * 16;  // of the 128 bytes of a step, that this lane's loads bring
-  const char *baseA = t.A + (int64_t)t.m0 * p.lda, *baseB = t.B + (int64_t)t.n0 * p.ldb;
-  const auto resA = __builtin_amdgcn_make_buffer_rsrc((void *)baseA, 0, 0xffffffffu, 0x00020000);
-  const auto resB = __builtin_amdgcn_make_buffer_rsrc((void *)baseB, 0, 0xffffffffu, 0x00020000);
+  const auto resA = __builtin_amdgcn_make_buffer_rsrc((void *)(t.A + (int64_t)t.m0 * p.lda), 0, 0xffffffffu, 0x00020000);
+  const auto resB = __builtin_amdgcn_make_buffer_rsrc((void *)(t.B + (int64_t)t.n0 * p.ldb), 0, 0xffffffffu, 0x00020000);
+  const auto resSA = __builtin_amdgcn_make_buffer_rsrc((void *)(t.sa + (int64_t)t.m0 * p.sa_ld), 0, 0xffffffffu, 0x00020000);
+  const auto resSB = __builtin_amdgcn_make_buffer_rsrc((void *)(t.sb + (WIDE ? 0 : (int64_t)(t.n0 >> p.sb_shift) * p.sb_ld)), 0, 0xffffffffu, 0x00020000);
   uint32_t at[LOADS];  // rows beyond the operands repeat the last one, their outputs are not stored
+  const auto is_scale = [](int i) { return i >= L::LOADS_ROWS; };
+  const auto scale_row = [&](int i) { return min((i - L::LOADS_ROWS) * WAVES + wave, (L::SCALED + 63) / 64 - 1) * 64; };  // first of a load
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) {
-    const int row = (i * WAVES + wave) * 8 + (lane >> 3);
-    at[i] = i < LOADS_A ? (uint32_t)min(row, t.M - 1 - t.m0) * (uint32_t)p.lda + piece
-                        : (uint32_t)min(row - BM, t.N - 1 - t.n0) * (uint32_t)p.ldb + piece;
+    if (!is_scale(i)) {
+      const int row = (i * WAVES + wave) * 8 + (lane >> 3);
+      at[i] = i < L::LOADS_A ? (uint32_t)min(row, t.M - 1 - t.m0) * (uint32_t)p.lda + piece
+                             : (uint32_t)min(row - BM, t.N - 1 - t.n0) * (uint32_t)p.ldb + piece;
+    } else {
+      const int row = min(scale_row(i) + lane, L::SCALED - 1);
+      at[i] = row < BM ? (uint32_t)min(row, t.M - 1 - t.m0) * (uint32_t)p.sa_ld
+                       : (uint32_t)((min(t.n0 + row - BM, t.N - 1) >> p.sb_shift) - (t.n0 >> p.sb_shift)) * (uint32_t)p.sb_ld;
+    }
   }
-  const auto request = [&](int step, char *lds) {
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const auto to = (__attribute__((address_space(3))) void *)(lds + (i * WAVES + wave) * 8 * MM_STEP);
-      if (i < LOADS_A) __builtin_amdgcn_raw_ptr_buffer_load_lds(resA, to, 16, at[i], step * MM_STEP, 0, 0);
+  static_assert(BM % 64 == 0 || WIDE || BM + BN <= 128, "a load of scales is of one operand, or lanes choose");
+  const auto request_one = [&](int i, int step, char *lds) {
+    using To = __attribute__((address_space(3))) void *;
+    if (is_scale(i)) {
+      const int row = scale_row(i), k = (t.first + step) & ~3;
+      const To to = (To)(lds + L::ROWS * MM_STEP + row * 4);
+      if constexpr (BM % 64 == 0 || WIDE) {
+        if (row < BM) __builtin_amdgcn_raw_ptr_buffer_load_lds(resSA, to, 4, at[i], k, 0, 0);
+        else __builtin_amdgcn_raw_ptr_buffer_load_lds(resSB, to, 4, at[i], k, 0, 0);
+      } else {  // 32 rows of each operand
+        if (lane < BM - row) __builtin_amdgcn_raw_ptr_buffer_load_lds(resSA, to, 4, at[i], k, 0, 0);
+        else __builtin_amdgcn_raw_ptr_buffer_load_lds(resSB, to, 4, at[i], k, 0, 0);
+      }
+    } else {
+      const To to = (To)(lds + (i * WAVES + wave) * 8 * MM_STEP);
+      if (i < L::LOADS_A) __builtin_amdgcn_raw_ptr_buffer_load_lds(resA, to, 16, at[i], step * MM_STEP, 0, 0);
       else __builtin_amdgcn_raw_ptr_buffer_load_lds(resB, to, 16, at[i], step * MM_STEP, 0, 0);
     }
+  };
+  const auto request = [&](int step, char *lds) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) request_one(i, step, lds);
   };
   const int steps = t.blocks;
   for (int i = 0; i < min(steps, STAGES); ++i) request(i, lds + i * STAGE);
 
-  // Scales: four blocks' bytes of a row at once, the present block's in the lowest.
-  const int row_a = t.m0 + wm * (BM / WGM) + (lane & 31), row_b = t.n0 + wn * (BN / WGN) + (lane & 31);
-  const uint8_t *rowsA[TM], *rowsB[WIDE ? 1 : TN];
-  uint32_t sa[TM], sb[TN], next_sa[TM], next_sb[TN];
   const float *wide[TN];
 #pragma unroll
-  for (int i = 0; i < TM; ++i) rowsA[i] = t.sa + (int64_t)min(row_a + i * 32, t.M - 1) * p.sa_ld, sa[i] = next_sa[i] = 0u;
-#pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    const int n = min(t.n0 + wn * (BN / WGN) + j * 32, t.N - 1);  // of the first of 32 columns, which share an fp32 scale
-    if constexpr (WIDE) wide[j] = reinterpret_cast<const float *>(t.sb) + (int64_t)__builtin_amdgcn_readfirstlane(n >> 7) * p.sb_ld;
-    else rowsB[j] = t.sb + (int64_t)(min(row_b + j * 32, t.N - 1) >> p.sb_shift) * p.sb_ld;
-    sb[j] = WIDE ? 127u : 0u, next_sb[j] = sb[j];
+  for (int j = 0; j < TN; ++j) {  // the first of 32 columns, which share an fp32 scale
+    const int n = min(t.n0 + wn * (BN / WGN) + j * 32, t.N - 1);
+    wide[j] = WIDE ? reinterpret_cast<const float *>(t.sb) + (int64_t)__builtin_amdgcn_readfirstlane(n >> 7) * p.sb_ld : nullptr;
   }
-  const auto request_scales = [&](int kb) {
-#pragma unroll
-    for (int i = 0; i < TM; ++i) next_sa[i] = f8_scales(rowsA[i], kb, t.readable);
-    if constexpr (!WIDE)
-#pragma unroll
-      for (int j = 0; j < TN; ++j) next_sb[j] = f8_scales(rowsB[j], kb, t.readable);
-  };
-  if (steps) request_scales(0);
-
   v16f acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = v16f{};
+  if (p.bias) {  // sums start from it
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float v = p.bias[min(t.n0 + wn * (BN / WGN) + j * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4, t.N - 1)];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) acc[i][j][r] = v;
+      }
+  }
+  if constexpr (IN_PLACE && !EXACT)
+#pragma unroll
+    for (int i = 0; i < TM; ++i) f8_settle(acc[i]);
   // Lanes 0 to 31 have pieces 0, 1 of a half step's four, the others 2, 3.
   const int slot = (((lane >> 5) * 2) ^ (lane & 7)) * 16;
-  const int fragA = (wm * (BM / WGM) + (lane & 31)) * MM_STEP + slot, fragB = (BM + wn * (BN / WGN) + (lane & 31)) * MM_STEP + slot;
-  struct Half {
-    v8i a[TM], b[TN];
+  const int rowA = wm * (BM / WGM) + (lane & 31), rowB = BM + wn * (BN / WGN) + (lane & 31);
+  const int fragA = rowA * MM_STEP + slot, fragB = rowB * MM_STEP + slot;
+  struct Half {  // fragments of 64 bytes of k
+    v4i a[TM][2], b[TN][2];
   };
-  const auto read = [&](const char *at) {
-    return __builtin_shufflevector(*reinterpret_cast<const v4i *>(at), *reinterpret_cast<const v4i *>(lds + ((at - lds) ^ 16)), 0, 1, 2, 3, 4, 5, 6, 7);
+  struct Scales {
+    uint32_t a[TM], b[TN];
   };
-  const auto fetch = [&](Half &f, int stage, int half) {
-#pragma unroll
-    for (int j = 0; j < TN; ++j) f.b[j] = read(lds + stage * STAGE + ((fragB + j * 32 * MM_STEP) ^ (half * 64)));
-#pragma unroll
-    for (int i = 0; i < TM; ++i) f.a[i] = read(lds + stage * STAGE + ((fragA + i * 32 * MM_STEP) ^ (half * 64)));
-  };
-  int now = 0;
-  for (int i = 0; i < steps; ++i) {
-    // (this wave's loads of step i; the rest may be under way)
-    if (i + STAGES - 1 < steps) mm_sync<(STAGES - 1) * LOADS>();
-    else mm_sync<0>();
-    if ((i & 3) == 0) {
-#pragma unroll
-      for (int k = 0; k < TM; ++k) sa[k] = next_sa[k];
-#pragma unroll
-      for (int k = 0; k < TN; ++k) sb[k] = next_sb[k];
+  // The k-th read of a half step: B's pieces, A's, then with the first half the step's scales.
+  constexpr int PIECES = 2 * (TM + TN), READS = PIECES + TM + (WIDE ? 0 : TN);
+  const auto fetch_one = [&](Half &f, Scales &s, const char *lds, int step, int half, int k) {
+    if (k < 2 * TN) f.b[k / 2][k % 2] = *reinterpret_cast<const v4i *>(lds + (fragB ^ (half * 64 + k % 2 * 16)) + k / 2 * 32 * MM_STEP);
+    else if (k < PIECES) f.a[k / 2 - TN][k % 2] = *reinterpret_cast<const v4i *>(lds + (fragA ^ (half * 64 + k % 2 * 16)) + (k / 2 - TN) * 32 * MM_STEP);
+    else {
+      const uint8_t *scales = reinterpret_cast<const uint8_t *>(lds + L::ROWS * MM_STEP) + ((t.first + step) & 3);
+      if (k < PIECES + TM) s.a[k - PIECES] = scales[(rowA + (k - PIECES) * 32) * 4];
+      else s.b[k - PIECES - TM] = scales[(rowB + (k - PIECES - TM) * 32) * 4];
     }
-    Half f[2];
-    fetch(f[0], now, 0);
-    fetch(f[1], now, 1);
+  };
+  const auto fetch = [&](Half &f, Scales &s, const char *lds, int step, int half) {
+#pragma unroll
+    for (int k = 0; k < (half ? PIECES : READS); ++k) fetch_one(f, s, lds, step, half, k);
+  };
+  const auto whole = [](const v4i (&v)[2]) { return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7); };
+  v16f part[TM][TN];  // WIDE: a block's sums
+  const auto multiply = [&](const Half &f, const Scales &s, int half) {
     if constexpr (EXACT) {
-      v16f part[TM][TN];
+      const auto start = [&](int i, int j) { return !WIDE ? acc[i][j] : half ? part[i][j] : v16f{}; };
+      F8Wide b[TN];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int a = 0; a < TM; ++a) {
-          const F8Wide wa(f[h].a[a], sa[a]);
-#pragma unroll
-          for (int b = 0; b < TN; ++b) {
-            const F8Wide wb(f[h].b[b], sb[b]);
-            v16f sum = !WIDE ? acc[a][b] : h ? part[a][b] : v16f{};
-#pragma unroll
-            for (int c = 0; c < 4; ++c) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb.v[c], wa.v[c], sum, 0, 0, 0);
-            (WIDE ? part : acc)[a][b] = sum;
-          }
-        }
-      }
-      if constexpr (WIDE) {
-#pragma unroll
-        for (int a = 0; a < TM; ++a)
-#pragma unroll
-          for (int b = 0; b < TN; ++b) {
-            const float s = wide[b][i];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[a][b][r] = fmaf(part[a][b][r], s, acc[a][b][r]);
-          }
-      }
-    }
-    if constexpr (!EXACT)
-#pragma unroll
-    for (int a = 0; a < TM; ++a)
-#pragma unroll
-      for (int b = 0; b < TN; ++b) {
-        if constexpr (WIDE) {
-          v16f part = f8_mfma(f[0].b[b], f[0].a[a], v16f{}, sb[b], sa[a]);
-          part = f8_mfma(f[1].b[b], f[1].a[a], part, sb[b], sa[a]);
-          const float s = wide[b][i];
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[a][b][r] = fmaf(part[r], s, acc[a][b][r]);
-        } else {
-          acc[a][b] = f8_mfma(f[0].b[b], f[0].a[a], acc[a][b], sb[b], sa[a]);  // rows of the result: n
-          acc[a][b] = f8_mfma(f[1].b[b], f[1].a[a], acc[a][b], sb[b], sa[a]);
-        }
-      }
-#pragma unroll
-    for (int k = 0; k < TM; ++k) sa[k] >>= 8;
-    if constexpr (!WIDE)
-#pragma unroll
-      for (int k = 0; k < TN; ++k) sb[k] >>= 8;
-    if (i + STAGES < steps) {
-      mm_meet();
-      request(i + STAGES, lds + now * STAGE);
-    }
-    if ((i & 3) == 0 && i + 4 < steps) request_scales(i + 4);
-    now = now + 1 == STAGES ? 0 : now + 1;
-  }
-
-  // A lane has column m = lane % 32 of the blocks and four times four consecutive n, those of lanes 32 above in between: these trade,
-  // so that a lane has eight consecutive ones.
-  const int m = t.m0 + wm * (BM / WGM) + (lane & 31);
-#pragma unroll
-  for (int j = 0; j < TN; ++j)
-#pragma unroll
-    for (int q = 0; q < 4; q += 2) {
-      const int n = t.n0 + wn * (BN / WGN) + j * 32 + q * 8 + (lane >> 5) * 8;
-      float bias[8] = {};
-      if (p.bias && n < t.N) load8(bias, p.bias, n, t.N);
+      for (int j = 0; j < TN; ++j) b[j].set(whole(f.b[j]), WIDE ? 127u : s.b[j]);
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
-        float v[8];
+        F8Wide a;
+        a.set(whole(f.a[i]), s.a[i]);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][q * 4 + r]), __float_as_uint(acc[i][j][q * 4 + 4 + r]), false, false);
-          v[r] = __uint_as_float(two[0]) + bias[r], v[4 + r] = __uint_as_float(two[1]) + bias[4 + r];
+        for (int j = 0; j < TN; ++j) {
+          v16f sum = start(i, j);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j].v[c], a.v[c], sum, 0, 0, 0);
+          (WIDE ? part : acc)[i][j] = sum;
         }
-        if (m + i * 32 < t.M && n < t.N) f8_store(p, t, m + i * 32, n, v);
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {  // rows of the result: n
+          if constexpr (WIDE) part[i][j] = f8_mfma(whole(f.b[j]), whole(f.a[i]), half ? part[i][j] : v16f{}, 127u, s.a[i]);
+          else acc[i][j] = f8_mfma(whole(f.b[j]), whole(f.a[i]), acc[i][j], s.b[j], s.a[i]);
+        }
     }
+  };
+  const auto scale_parts = [&](int step) {
+    if constexpr (WIDE)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const float w = wide[j][step];
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = fmaf(part[i][j][r], w, acc[i][j][r]);
+      }
+  };
+
+  // As in tile_mm.h: the workgroup meets in the middle of a step, when both halves of its fragments are in registers; from there on
+  // its place in LDS takes the step STAGES ahead, and the next step's first half is read under the products of the second.
+  if (steps) {
+    Half first, second;
+    Scales scales[2];
+    if (steps >= STAGES) mm_sync<(STAGES - 1) * LOADS>();
+    else mm_sync<0>();
+    fetch(first, scales[0], lds, 0, 0);
+    int now = 0;
+    const auto turn = [&](int i, Scales &mine, Scales &other, auto inside) {  // inside: known to be neither last nor among the last STAGES
+      const int next = now + 1 == STAGES ? 0 : now + 1;
+      const bool more = decltype(inside)::value || i + STAGES < steps, last = !decltype(inside)::value && i + 1 == steps;
+      if constexpr (IN_PLACE && !EXACT) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          fetch_one(second, mine, lds + now * STAGE, i, 1, q);
+          f8_mfma_in_place(whole(first.b[q % 4]), whole(first.a[q / 4]), acc[q / 4][q % 4], mine.b[q % 4], mine.a[q / 4]);
+        }
+        if (decltype(inside)::value || i + STAGES - 1 < steps) mm_sync<(STAGES - 2) * LOADS>();
+        else mm_sync<0>();
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          if (!last) {
+            fetch_one(first, other, lds + next * STAGE, i + 1, 0, q);
+            if (q % 2 == 0) fetch_one(first, other, lds + next * STAGE, i + 1, 0, 16 + q / 2);
+          }
+          f8_mfma_in_place(whole(second.b[q % 4]), whole(second.a[q / 4]), acc[q / 4][q % 4], mine.b[q % 4], mine.a[q / 4]);
+          if (more) {
+            request_one(q, i + STAGES, lds + now * STAGE);
+            if (q < LOADS - 16) request_one(16 + q, i + STAGES, lds + now * STAGE);
+          }
+        }
+      } else {
+        fetch(second, mine, lds + now * STAGE, i, 1);
+        multiply(first, mine, 0);
+        if (decltype(inside)::value || i + STAGES - 1 < steps) mm_sync<(STAGES - 2) * LOADS>();
+        else mm_sync<0>();
+        if (more) request(i + STAGES, lds + now * STAGE);
+        if (!last) fetch(first, other, lds + next * STAGE, i + 1, 0);
+        multiply(second, mine, 1);
+        scale_parts(i);
+      }
+      now = next;
+    };
+    int i = 0;
+    for (; i + 1 + STAGES < steps; i += 2) {
+      turn(i, scales[0], scales[1], std::true_type());
+      turn(i + 1, scales[1], scales[0], std::true_type());
+    }
+    for (; i < steps; i += 2) {
+      turn(i, scales[0], scales[1], std::false_type());
+      if (i + 1 < steps) turn(i + 1, scales[1], scales[0], std::false_type());
+    }
+  }
+  if constexpr (IN_PLACE && !EXACT)
+#pragma unroll
+    for (int i = 0; i < TM; ++i) f8_settle(acc[i]);
+
+  // Results leave through LDS, 32 rows of a wave's columns at a time, so that a store covers whole lines of a row.
+  mm_meet();
+  const auto finish = [&](auto tag) {
+    using E = decltype(tag);
+    constexpr int SIZE = sizeof(E), PITCH = TN * 32 * SIZE + 16, PIECES = TN * 32 * SIZE / 16, PER = 16 / SIZE;
+    static_assert(WAVES * 32 * PITCH <= STAGES * STAGE, "");
+    char *const mine = lds + wave * 32 * PITCH;
+    const int n0 = t.n0 + wn * (BN / WGN);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int m0 = t.m0 + wm * (BM / WGM) + i * 32;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+          // A lane has column m = lane % 32 of a block and four times four consecutive n, those of the lane 32 above in between: these
+          // trade, so that a lane has eight consecutive ones.
+          const int n = j * 32 + q * 8 + (lane >> 5) * 8;
+          float v[8];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][q * 4 + r]), __float_as_uint(acc[i][j][q * 4 + 4 + r]), false, false);
+            v[r] = __uint_as_float(two[0]), v[4 + r] = __uint_as_float(two[1]);
+          }
+          store8(reinterpret_cast<E *>(mine + (lane & 31) * PITCH), n, TN * 32, v);
+        }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int k = 0; k < PIECES / 2; ++k) {
+        const int at = k * 64 + lane, row = at / PIECES, n = n0 + at % PIECES * PER, m = m0 + row;
+        const char *from = mine + row * PITCH + at % PIECES * 16;
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(from);
+        if (m >= t.M || n >= t.N) continue;
+        E *to = reinterpret_cast<E *>(t.y) + m * p.ldy + n;
+        if (n + PER <= t.N) *reinterpret_cast<u32x4_any *>(to) = v;
+        else
+          for (int r = 0; r < t.N - n; ++r) to[r] = reinterpret_cast<const E *>(from)[r];
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+  };
+  if constexpr (EXACT) finish(0.0f);
+  else if (p.type == BNN_BF16) finish((__bf16)0.0f);
+  else finish((_Float16)0.0f);
 }
 
 template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE, bool EXACT>
 __global__ __launch_bounds__(64 * WGM *WGN, WGM *WGN < 4 ? 1 : WGM *WGN / 4) void f8_tile_kernel(F8Operands p) {
-  __shared__ __attribute__((aligned(16))) char lds[STAGES * (BM + BN) * MM_STEP];
+  __shared__ __attribute__((aligned(16))) char lds[STAGES * F8Tile<BM, BN, WGM, WGN, STAGES, WIDE>::STAGE];
   f8_tile_product<BM, BN, WGM, WGN, STAGES, WIDE, EXACT>(p, lds);
 }
 
@@ -356,8 +448,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void f8_few_kernel(F8Operand
       const int64_t k = (int64_t)min(kb + r, t.blocks - 1) * F8_BLOCK;
       v.a[r][0] = *reinterpret_cast<const v4i *>(a + k), v.a[r][1] = *reinterpret_cast<const v4i *>(a + k + 16);
     }
-    v.sa = f8_scales(sa_row, kb, t.readable);
-    v.sb = WIDE ? 0x7f7f7f7fu : f8_scales(sb_row, kb, t.readable);
+    v.sa = f8_scales(sa_row, t.first + kb, t.readable);
+    v.sb = WIDE ? 0x7f7f7f7fu : f8_scales(sb_row, t.first + kb, t.readable);
   };
   const auto multiply = [&](const Run &v, int kb) {
 #pragma unroll
