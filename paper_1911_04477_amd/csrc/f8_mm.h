@@ -154,6 +154,21 @@ __device__ __forceinline__ void f8_settle(v16f (&c)[4]) {  // a matrix instructi
   asm volatile("s_nop 15\n\ts_nop 7" : "+a"(c[0]), "+a"(c[1]), "+a"(c[2]), "+a"(c[3]));
 }
 
+// Reads of LDS, requests and what the vector unit does between MATRIX matrix instructions, not all in front of them.
+template <int Q, int MATRIX, int READS, int LOADS, bool WIDENS>
+__device__ __forceinline__ void f8_interleave() {
+  if constexpr (Q == MATRIX) {
+    __builtin_amdgcn_sched_barrier(0);
+  } else {
+    constexpr int R = READS * (Q + 1) / MATRIX - READS * Q / MATRIX, N = LOADS * (Q + 1) / MATRIX - LOADS * Q / MATRIX;
+    if constexpr (WIDENS) __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+    if constexpr (R > 0) __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+    if constexpr (N > 0) __builtin_amdgcn_sched_group_barrier(0x010, N, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    f8_interleave<Q + 1, MATRIX, READS, LOADS, WIDENS>();
+  }
+}
+
 // LDS: a step's rows of 128 bytes as in tile_mm.h (16-byte piece c of row r in slot c ^ (r % 8)), behind them for each row the
 // four bytes of scales that hold the step's.  WGM x WGN waves of 32 x 32 blocks.
 template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE>
@@ -309,6 +324,10 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) 
       }
   };
 
+  const auto interleave = [&](auto reads, auto loads) {
+    constexpr int MATRIX = TM * TN * (EXACT ? 4 : 1);
+    if constexpr (MATRIX >= 16) f8_interleave<0, MATRIX, decltype(reads)::value, decltype(loads)::value, EXACT>();
+  };
   // As in tile_mm.h: the workgroup meets in the middle of a step, when both halves of its fragments are in registers; from there on
   // its place in LDS takes the step STAGES ahead, and the next step's first half is read under the products of the second.
   if (steps) {
@@ -318,6 +337,30 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) 
     else mm_sync<0>();
     fetch(first, scales[0], lds, 0, 0);
     int now = 0;
+    // EXACT, 256 x 256: eight bytes of every fragment at a time are widened for 16 products, two instructions behind each product of
+    // the 16 before.
+    constexpr bool WOVEN = EXACT && IN_PLACE;
+    struct Chunk {
+      v8bf a[TM], b[TN];
+    };
+    Chunk chunk[2];
+    float factors[2][TM + TN];
+    const auto factor = [&](const Scales &s, float (&to)[TM + TN]) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) to[i] = __uint_as_float(s.a[i] << 23);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) to[TM + j] = __uint_as_float(s.b[j] << 23);
+    };
+    const auto widen = [&](Chunk &to, const Half &f, const float (&by)[TM + TN], int c, int u) {  // the u-th of 2 * (TM + TN) parts; B first
+      const int k = u / 2, w = c % 2 * 2 + u % 2;
+      if (k < TN) f8_widen(f.b[k][c / 2][w], by[TM + k], to.b[k], u % 2 * 4);
+      else f8_widen(f.a[k - TN][c / 2][w], by[k - TN], to.a[k - TN], u % 2 * 4);
+    };
+    if constexpr (WOVEN) {
+      factor(scales[0], factors[0]);
+#pragma unroll
+      for (int u = 0; u < 16; ++u) widen(chunk[0], first, factors[0], 0, u);
+    }
     const auto turn = [&](int i, Scales &mine, Scales &other, auto inside) {  // inside: known to be neither last nor among the last STAGES
       const int next = now + 1 == STAGES ? 0 : now + 1;
       const bool more = decltype(inside)::value || i + STAGES < steps, last = !decltype(inside)::value && i + 1 == steps;
@@ -341,14 +384,41 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) 
             if (q < LOADS - 16) request_one(16 + q, i + STAGES, lds + now * STAGE);
           }
         }
-      } else {
-        fetch(second, mine, lds + now * STAGE, i, 1);
-        multiply(first, mine, 0);
+      } else if constexpr (WOVEN) {
+        const int which = &mine == &scales[0] ? 0 : 1;
+        const auto phase = [&](const Half &of, const Half &then, const float (&by)[TM + TN], const float (&then_by)[TM + TN], const auto &between) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+              between(c * 16 + q);
+              widen(chunk[(c + 1) % 2], c < 3 ? of : then, c < 3 ? by : then_by, (c + 1) % 4, q);
+              acc[q / 4][q % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(chunk[c % 2].b[q % 4], chunk[c % 2].a[q / 4], acc[q / 4][q % 4], 0, 0, 0);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        phase(first, second, factors[which], factors[which], [&](int q) {
+          if (q % 2 == 0 && q / 2 < PIECES) fetch_one(second, mine, lds + now * STAGE, i, 1, q / 2);
+        });
         if (decltype(inside)::value || i + STAGES - 1 < steps) mm_sync<(STAGES - 2) * LOADS>();
         else mm_sync<0>();
+        phase(second, first, factors[which], factors[which ^ 1], [&](int q) {
+          if (q % 2 == 0 && q / 2 < READS && !last) fetch_one(first, other, lds + next * STAGE, i + 1, 0, q / 2);
+          if (q % 2 == 1 && q / 2 < LOADS && more) request_one(q / 2, i + STAGES, lds + now * STAGE);
+          if (q == 48) factor(other, factors[which ^ 1]);
+        });
+      } else {
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(second, mine, lds + now * STAGE, i, 1);
+        multiply(first, mine, 0);
+        interleave(std::integral_constant<int, PIECES>(), std::integral_constant<int, 0>());
+        if (decltype(inside)::value || i + STAGES - 1 < steps) mm_sync<(STAGES - 2) * LOADS>();
+        else mm_sync<0>();
+        __builtin_amdgcn_sched_barrier(0);
         if (more) request(i + STAGES, lds + now * STAGE);
         if (!last) fetch(first, other, lds + next * STAGE, i + 1, 0);
         multiply(second, mine, 1);
+        if constexpr (decltype(inside)::value) interleave(std::integral_constant<int, READS>(), std::integral_constant<int, LOADS>());
         scale_parts(i);
       }
       now = next;

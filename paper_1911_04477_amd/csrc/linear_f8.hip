@@ -57,9 +57,9 @@ bnn_status run_f8_as(const F8Operands &p, hipStream_t s) {
   int64_t rows = p.M, groups = 1;
   if (p.groups == F8_GROUP_ROWS) groups = std::min(p.E, p.M), rows = (p.M - 1) / groups + 1;
   if (p.groups == F8_GROUP_K) groups = p.E;
-  switch (f8_form(rows, groups, p.N, WIDE || EXACT, device_cu_count())) {
+  switch (f8_form(rows, groups, p.N, WIDE, device_cu_count())) {
     case F8_256:
-      if constexpr (!WIDE && !EXACT) return launch_f8_tile<256, 256, 2, 2, 2, false, false>(p, s);
+      if constexpr (!WIDE) return launch_f8_tile<256, 256, 2, 2, 2, false, EXACT>(p, s);
     case F8_128: return launch_f8_tile<128, 128, 2, 2, 2, WIDE, EXACT>(p, s);
     case F8_64: return launch_f8_tile<64, 64, 2, 2, 3, WIDE, EXACT>(p, s);
     case F8_32: return launch_f8_tile<32, 64, 1, 2, 4, WIDE, EXACT>(p, s);
