@@ -54,55 +54,81 @@ struct F8Part {
   int blocks;
 };
 
-// Tiles of rows by group: the tiles before each group from a scan over the experts' counts (64 at a time; a launch has
-// workgroups for as many as there can be, those beyond end).  Returns the number of tiles of rows; finds tile tm's group where
-// tm is among them: expert, its first and last row.
+// Tiles of rows by group: those before each group from a scan over the experts' counts, 64 at a time.  A launch has workgroups for as
+// many tiles as there can be; those beyond end.
 struct F8Group {
-  int e, lo, hi;
+  int e, lo, hi, tile;  // expert, its first row and its end, the tile among its own
 };
 __device__ __forceinline__ int f8_clamped(const int32_t *offsets, int e, int S) { return min(max(offsets[e], 0), S); }
-template <int BM>
-__device__ __forceinline__ int f8_row_tiles(const F8Operands &p, int wanted, F8Group &g, int &tile) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int e0 = 0; e0 < p.E; e0 += 64) {
-    const int e = e0 + lane;
-    const int lo = e < p.E ? f8_clamped(p.offsets, e, p.M) : 0, hi = e < p.E ? max(f8_clamped(p.offsets, e + 1, p.M), lo) : 0;
-    int sum = (hi - lo + BM - 1) / BM;
+struct F8Scan {
+  int lo, hi, sum;  // of this lane's expert; tiles up to and with its own
+  template <int BM>
+  __device__ __forceinline__ void run(const F8Operands &p, int e0) {
+    const int lane = threadIdx.x & 63, e = e0 + lane;
+    lo = e < p.E ? f8_clamped(p.offsets, e, p.M) : 0;
+    hi = e < p.E ? max(f8_clamped(p.offsets, e + 1, p.M), lo) : 0;
+    sum = (hi - lo + BM - 1) / BM;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
       const int other = __shfl_up(sum, d);
       if (lane >= d) sum += other;
     }
-    if (wanted >= 0) {
-      const uint64_t past = __ballot(before + sum > wanted);
-      if (past) {
-        const int l = __builtin_ctzll(past);
-        const int start = l ? __shfl(sum, l - 1) : 0;
-        g.e = __builtin_amdgcn_readfirstlane(e0 + l);
-        g.lo = __builtin_amdgcn_readfirstlane(__shfl(lo, l)), g.hi = __builtin_amdgcn_readfirstlane(__shfl(hi, l));
-        tile = __builtin_amdgcn_readfirstlane(wanted - before - start);
-        return -1;
-      }
-    }
-    before += __builtin_amdgcn_readfirstlane(__shfl(sum, 63));
   }
-  return before;
+  __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(sum, 63); }
+  __device__ __forceinline__ bool find(int wanted, int e0, F8Group &g) const {
+    const uint64_t past = __ballot(sum > wanted);
+    if (!past) return false;
+    const int l = __builtin_ctzll(past);
+    g = {e0 + l, __builtin_amdgcn_readlane(lo, l), __builtin_amdgcn_readlane(hi, l), wanted - (l ? __builtin_amdgcn_readlane(sum, l - 1) : 0)};
+    return true;
+  }
+};
+template <int BM>
+__device__ __forceinline__ int f8_row_tiles(const F8Operands &p) {
+  int all = 0;
+  for (int e0 = 0; e0 < p.E; e0 += 64) {
+    F8Scan scan;
+    scan.run<BM>(p, e0);
+    all += scan.total();
+  }
+  return all;
+}
+template <int BM>
+__device__ __forceinline__ bool f8_row_group(const F8Operands &p, int wanted, F8Group &g) {
+  for (int e0 = 0; e0 < p.E; e0 += 64) {
+    F8Scan scan;
+    scan.run<BM>(p, e0);
+    if (scan.find(wanted, e0, g)) return true;
+    wanted -= scan.total();
+  }
+  return false;
 }
 
-// The tile of a workgroup; false: none is left for it.  BM x BN outputs.
-template <int BM, int BN>
+// The tile of a workgroup; false: none is left for it.  BM x BN outputs.  STREAMED: B is read once, so tiles of a group follow each other.
+template <int BM, int BN, bool STREAMED = false>
 __device__ __forceinline__ bool f8_part(const F8Operands &p, int64_t id, F8Part &t) {
-  int tm, tn, tile;
+  int tm, tn;
   const int size = p.type == BNN_F32 ? 4 : 2, readable = (p.blocks + 3) & ~3;
   if (p.groups == F8_GROUP_ROWS) {
-    F8Group g = {0, 0, 0};
-    const int tilesM = f8_row_tiles<BM>(p, -1, g, tile);
-    if (id >= (int64_t)tilesM * p.tilesN) return false;
-    mm_tile((int)id, tilesM, p.tilesN, tm, tn);
-    f8_row_tiles<BM>(p, tm, g, tile);
+    F8Group g;
+    if (STREAMED) {
+      tm = (int)(id / p.tilesN), tn = (int)(id - (int64_t)tm * p.tilesN);
+      if (!f8_row_group<BM>(p, tm, g)) return false;
+    } else if (p.E <= 64) {
+      F8Scan scan;
+      scan.run<BM>(p, 0);
+      const int tilesM = scan.total();
+      if (id >= (int64_t)tilesM * p.tilesN) return false;
+      mm_tile((int)id, tilesM, p.tilesN, tm, tn);
+      scan.find(tm, 0, g);
+    } else {
+      const int tilesM = f8_row_tiles<BM>(p);
+      if (id >= (int64_t)tilesM * p.tilesN) return false;
+      mm_tile((int)id, tilesM, p.tilesN, tm, tn);
+      f8_row_group<BM>(p, tm, g);
+    }
     t = {p.A, p.B + g.e * p.b_es, p.sa, static_cast<const uint8_t *>(p.sb) + g.e * p.sb_es, readable, 0, static_cast<char *>(p.y),
-         g.lo + tile * BM, tn * BN, g.hi, p.N, p.blocks};
+         g.lo + g.tile * BM, tn * BN, g.hi, p.N, p.blocks};
     return true;
   }
   const int64_t of = (int64_t)p.tilesM * p.tilesN;
@@ -111,7 +137,8 @@ __device__ __forceinline__ bool f8_part(const F8Operands &p, int64_t id, F8Part 
     if (e >= p.E) return false;
     mm_tile((int)(id - e * of), p.tilesM, p.tilesN, tm, tn);
     const int end = p.blocks * F8_BLOCK, lo = f8_clamped(p.offsets, e, end) / F8_BLOCK, hi = max(f8_clamped(p.offsets, e + 1, end) / F8_BLOCK, lo);
-    t = {p.A + (int64_t)lo * F8_BLOCK, p.B + (int64_t)lo * F8_BLOCK, p.sa, static_cast<const uint8_t *>(p.sb), readable, lo, static_cast<char *>(p.y) + e * p.y_es * size, tm * BM, tn * BN, p.M, p.N, hi - lo};
+    t = {p.A + (int64_t)lo * F8_BLOCK, p.B + (int64_t)lo * F8_BLOCK, p.sa, static_cast<const uint8_t *>(p.sb), readable, lo,
+         static_cast<char *>(p.y) + e * p.y_es * size, tm * BM, tn * BN, p.M, p.N, hi - lo};
     return true;
   }
   if (id >= of) return false;
@@ -170,23 +197,26 @@ __device__ __forceinline__ void f8_interleave() {
 }
 
 // LDS: a step's rows of 128 bytes as in tile_mm.h (16-byte piece c of row r in slot c ^ (r % 8)), behind them for each row the
-// four bytes of scales that hold the step's.  WGM x WGN waves of 32 x 32 blocks.
-template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE>
+// four bytes of scales that hold the step's.  WGM x WGN waves of 32 x 32 blocks; KG such groups of waves take the blocks of k in turn, KG
+// of them a step, and their sums meet in the end: small tiles, one a compute unit, are bound by what a step does one after the other
+// (64 x 4096 by 4096 on 64 x 32 tiles 9.9 us with one group, 8.6 with four).
+template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE>
 struct F8Tile {
   static constexpr int WAVES = WGM * WGN, ROWS = BM + BN, SCALED = WIDE ? BM : ROWS, LOADS_A = BM / 8 / WAVES, LOADS_ROWS = ROWS / 8 / WAVES,
                        LOADS_SCALES = (SCALED / 64 + WAVES - 1) / WAVES, LOADS = LOADS_ROWS + (LOADS_SCALES ? LOADS_SCALES : 1),
-                       STAGE = ROWS * MM_STEP + (SCALED + 63) / 64 * 256, TM = BM / WGM / 32, TN = BN / WGN / 32;
+                       PART = ROWS * MM_STEP + (SCALED + 63) / 64 * 256, STAGE = KG * PART, TM = BM / WGM / 32, TN = BN / WGN / 32;
   static_assert(ROWS % (8 * WAVES) == 0 && BM % (8 * WAVES) == 0 && BM % (32 * WGM) == 0 && BN % (32 * WGN) == 0, "");
 };
-template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE, bool EXACT>  // WIDE: fp32 scales of B
-__device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) {
-  using L = F8Tile<BM, BN, WGM, WGN, STAGES, WIDE>;
+template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, bool EXACT>  // WIDE: fp32 scales of B
+__device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *const whole_lds) {
+  using L = F8Tile<BM, BN, WGM, WGN, KG, STAGES, WIDE>;
   constexpr int WAVES = L::WAVES, LOADS = L::LOADS, STAGE = L::STAGE, TM = L::TM, TN = L::TN;
   constexpr bool IN_PLACE = TM * TN == 16;
   F8Part t;
   if (!f8_part<BM, BN>(p, p.first + blockIdx.x, t)) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = id / WAVES, wave = id % WAVES;
   const int wm = wave / WGN, wn = wave % WGN;
+  char *const lds = whole_lds + group * L::PART;
   const int piece = ((lane & 7) ^ (lane >> 3)) * 16;  // of the 128 bytes of a step, that this lane's loads bring
   const auto resA = __builtin_amdgcn_make_buffer_rsrc((void *)(t.A + (int64_t)t.m0 * p.lda), 0, 0xffffffffu, 0x00020000);
   const auto resB = __builtin_amdgcn_make_buffer_rsrc((void *)(t.B + (int64_t)t.n0 * p.ldb), 0, 0xffffffffu, 0x00020000);
@@ -226,11 +256,12 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) 
       else __builtin_amdgcn_raw_ptr_buffer_load_lds(resB, to, 16, at[i], step * MM_STEP, 0, 0);
     }
   };
+  const auto block_of = [&](int step) { return KG == 1 ? step : min(step * KG + group, t.blocks - 1); };  // past the end: not used
   const auto request = [&](int step, char *lds) {
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) request_one(i, step, lds);
+    for (int i = 0; i < LOADS; ++i) request_one(i, block_of(step), lds);
   };
-  const int steps = t.blocks;
+  const int steps = (t.blocks + KG - 1) / KG;
   for (int i = 0; i < min(steps, STAGES); ++i) request(i, lds + i * STAGE);
 
   const float *wide[TN];
@@ -244,7 +275,7 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) 
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = v16f{};
-  if (p.bias) {  // sums start from it
+  if (p.bias && group == 0) {  // sums start from it
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -269,18 +300,18 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) 
   };
   // The k-th read of a half step: B's pieces, A's, then with the first half the step's scales.
   constexpr int PIECES = 2 * (TM + TN), READS = PIECES + TM + (WIDE ? 0 : TN);
-  const auto fetch_one = [&](Half &f, Scales &s, const char *lds, int step, int half, int k) {
+  const auto fetch_one = [&](Half &f, Scales &s, const char *lds, int block, int half, int k) {
     if (k < 2 * TN) f.b[k / 2][k % 2] = *reinterpret_cast<const v4i *>(lds + (fragB ^ (half * 64 + k % 2 * 16)) + k / 2 * 32 * MM_STEP);
     else if (k < PIECES) f.a[k / 2 - TN][k % 2] = *reinterpret_cast<const v4i *>(lds + (fragA ^ (half * 64 + k % 2 * 16)) + (k / 2 - TN) * 32 * MM_STEP);
     else {
-      const uint8_t *scales = reinterpret_cast<const uint8_t *>(lds + L::ROWS * MM_STEP) + ((t.first + step) & 3);
+      const uint8_t *scales = reinterpret_cast<const uint8_t *>(lds + L::ROWS * MM_STEP) + ((t.first + block) & 3);
       if (k < PIECES + TM) s.a[k - PIECES] = scales[(rowA + (k - PIECES) * 32) * 4];
       else s.b[k - PIECES - TM] = scales[(rowB + (k - PIECES - TM) * 32) * 4];
     }
   };
   const auto fetch = [&](Half &f, Scales &s, const char *lds, int step, int half) {
 #pragma unroll
-    for (int k = 0; k < (half ? PIECES : READS); ++k) fetch_one(f, s, lds, step, half, k);
+    for (int k = 0; k < (half ? PIECES : READS); ++k) fetch_one(f, s, lds, block_of(step), half, k);
   };
   const auto whole = [](const v4i (&v)[2]) { return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7); };
   v16f part[TM][TN];  // WIDE: a block's sums
@@ -316,7 +347,7 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) 
     if constexpr (WIDE)
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        const float w = wide[j][step];
+        const float w = wide[j][block_of(step)];
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -409,17 +440,20 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) 
         });
       } else {
         __builtin_amdgcn_sched_barrier(0);
+        const bool any = decltype(inside)::value || i * KG + group < t.blocks;  // a block for this group
         fetch(second, mine, lds + now * STAGE, i, 1);
-        multiply(first, mine, 0);
-        interleave(std::integral_constant<int, PIECES>(), std::integral_constant<int, 0>());
+        if (any) multiply(first, mine, 0);
+        if constexpr (decltype(inside)::value) interleave(std::integral_constant<int, PIECES>(), std::integral_constant<int, 0>());
         if (decltype(inside)::value || i + STAGES - 1 < steps) mm_sync<(STAGES - 2) * LOADS>();
         else mm_sync<0>();
         __builtin_amdgcn_sched_barrier(0);
         if (more) request(i + STAGES, lds + now * STAGE);
         if (!last) fetch(first, other, lds + next * STAGE, i + 1, 0);
-        multiply(second, mine, 1);
-        if constexpr (decltype(inside)::value) interleave(std::integral_constant<int, READS>(), std::integral_constant<int, LOADS>());
-        scale_parts(i);
+        if (any) {
+          multiply(second, mine, 1);
+          if constexpr (decltype(inside)::value) interleave(std::integral_constant<int, READS>(), std::integral_constant<int, LOADS>());
+          scale_parts(i);
+        }
       }
       now = next;
     };
@@ -437,13 +471,45 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) 
 #pragma unroll
     for (int i = 0; i < TM; ++i) f8_settle(acc[i]);
 
+  if constexpr (KG > 1) {  // the groups' sums, in their order
+    constexpr int SUMS = TM * TN * 16 * 64;  // a wave's
+    static_assert((KG - 1) * WAVES * SUMS * 4 <= STAGES * STAGE, "");
+    float *const sums = reinterpret_cast<float *>(whole_lds) + wave * (KG - 1) * SUMS + lane * 4;
+    mm_meet();
+    if (group) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<v4f *>(sums + (group - 1) * SUMS + ((i * TN + j) * 4 + q) * 256) =
+                v4f{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+    }
+    mm_meet();
+    if (group) return;
+#pragma unroll
+    for (int g = 1; g < KG; ++g)
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const v4f v = *reinterpret_cast<const v4f *>(sums + (g - 1) * SUMS + ((i * TN + j) * 4 + q) * 256);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][j][q * 4 + r] += v[r];
+          }
+  }
+
   // Results leave through LDS, 32 rows of a wave's columns at a time, so that a store covers whole lines of a row.
-  mm_meet();
+  if constexpr (KG == 1) mm_meet();
+  else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // a wave's own part of what it has just read
   const auto finish = [&](auto tag) {
     using E = decltype(tag);
     constexpr int SIZE = sizeof(E), PITCH = TN * 32 * SIZE + 16, PIECES = TN * 32 * SIZE / 16, PER = 16 / SIZE;
-    static_assert(WAVES * 32 * PITCH <= STAGES * STAGE, "");
-    char *const mine = lds + wave * 32 * PITCH;
+    static_assert(WAVES * 32 * PITCH <= STAGES * STAGE && (KG == 1 || 32 * PITCH <= (KG - 1) * TM * TN * 16 * 64 * 4), "");
+    char *const mine = KG == 1 ? lds + wave * 32 * PITCH : whole_lds + wave * (KG - 1) * (TM * TN * 16 * 64 * 4);  // where only this wave reads
     const int n0 = t.n0 + wn * (BN / WGN);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -483,38 +549,41 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *lds) 
   else finish((_Float16)0.0f);
 }
 
-template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE, bool EXACT>
-__global__ __launch_bounds__(64 * WGM *WGN, WGM *WGN < 4 ? 1 : WGM *WGN / 4) void f8_tile_kernel(F8Operands p) {
-  __shared__ __attribute__((aligned(16))) char lds[STAGES * F8Tile<BM, BN, WGM, WGN, STAGES, WIDE>::STAGE];
-  f8_tile_product<BM, BN, WGM, WGN, STAGES, WIDE, EXACT>(p, lds);
+template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, bool EXACT>
+__global__ __launch_bounds__(64 * WGM *WGN *KG, WGM *WGN *KG < 4 ? 1 : WGM *WGN *KG / 4) void f8_tile_kernel(F8Operands p) {
+  __shared__ __attribute__((aligned(16))) char lds[STAGES * F8Tile<BM, BN, WGM, WGN, KG, STAGES, WIDE>::STAGE];
+  f8_tile_product<BM, BN, WGM, WGN, KG, STAGES, WIDE, EXACT>(p, lds);
 }
 
-// At most 16 rows of A (of a group): nothing is reused, B is streamed once and bounds the kernel.  A workgroup owns 16
-// columns; its waves deal k out in runs of four blocks, straight from memory into registers, and sums meet in LDS.
-template <int WAVES, bool WIDE>
-__global__ __launch_bounds__(64 * WAVES, WAVES / 4) void f8_few_kernel(F8Operands p) {
-  __shared__ v4f sums[WAVES][64];
+// At most 16 rows of A (of a group): nothing is reused, B is streamed once and bounds the kernel.  A wave owns 16 columns and deals with
+// every SPLIT-th run of two blocks of k, straight from memory into registers, the next run requested before the products of the present one; the
+// SPLIT waves of a column's sums meet in LDS.  Short-lived workgroups wait for their first loads most of their time, so k is split no
+// further than it takes to give every unit waves (32 rows of eight experts, 8192 x 4096 each: split eight ways 73 us, two ways 57, 4.7 TB/s).
+template <int SPLIT, bool WIDE>
+__device__ __forceinline__ void f8_few_product(const F8Operands &p, v4f (*sums)[64]) {
+  constexpr int WAVES = 8, COLUMNS = WAVES / SPLIT * 16;
   F8Part t;
-  if (!f8_part<16, 16>(p, p.first + blockIdx.x, t)) return;
+  if (!f8_part<16, COLUMNS, true>(p, p.first + blockIdx.x, t)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = lane & 15, piece = (lane >> 4) * 32;
-  const int n = min(t.n0 + row, t.N - 1), mr = min(t.m0 + row, t.M - 1);
+  const int n0 = t.n0 + wave / SPLIT * 16, row = lane & 15, piece = (lane >> 4) * 32;
+  const int n = min(n0 + row, t.N - 1), mr = min(t.m0 + row, t.M - 1);
   const char *a = t.A + (int64_t)mr * p.lda + piece, *b = t.B + (int64_t)n * p.ldb + piece;
   const uint8_t *sa_row = t.sa + (int64_t)mr * p.sa_ld, *sb_row = WIDE ? nullptr : t.sb + (int64_t)(n >> p.sb_shift) * p.sb_ld;
-  const float *wide = WIDE ? reinterpret_cast<const float *>(t.sb) + (int64_t)__builtin_amdgcn_readfirstlane(t.n0 >> 7) * p.sb_ld : nullptr;
+  const float *wide = WIDE ? reinterpret_cast<const float *>(t.sb) + (int64_t)__builtin_amdgcn_readfirstlane(min(n0, t.N - 1) >> 7) * p.sb_ld : nullptr;
   v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  constexpr int RUN = 2;
   struct Run {
-    v4i a[4][2], b[4][2];
+    v4i a[RUN][2], b[RUN][2];
     uint32_t sa, sb;
   };
   const auto request = [&](Run &v, int kb) {  // blocks past the end: the last one, not used
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < RUN; ++r) {
       const int64_t k = (int64_t)min(kb + r, t.blocks - 1) * F8_BLOCK;
       v.b[r][0] = *reinterpret_cast<const v4i *>(b + k), v.b[r][1] = *reinterpret_cast<const v4i *>(b + k + 16);
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < RUN; ++r) {
       const int64_t k = (int64_t)min(kb + r, t.blocks - 1) * F8_BLOCK;
       v.a[r][0] = *reinterpret_cast<const v4i *>(a + k), v.a[r][1] = *reinterpret_cast<const v4i *>(a + k + 16);
     }
@@ -523,7 +592,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void f8_few_kernel(F8Operand
   };
   const auto multiply = [&](const Run &v, int kb) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < RUN; ++r) {
       if (kb + r >= t.blocks) break;
       const float fa = __uint_as_float((v.sa >> (8 * r) & 0xffu) << 23), fb = __uint_as_float((v.sb >> (8 * r) & 0xffu) << 23);
       v4f sum = WIDE ? v4f{} : acc;
@@ -545,8 +614,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void f8_few_kernel(F8Operand
       }
     }
   };
-  constexpr int STRIDE = WAVES * 4;
-  int kb = wave * 4;
+  constexpr int STRIDE = SPLIT * RUN;
+  int kb = wave % SPLIT * RUN;
   if (kb < t.blocks) {
     Run v[2];
     request(v[0], kb);
@@ -561,12 +630,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void f8_few_kernel(F8Operand
       if (kb >= t.blocks) break;
     }
   }
-  sums[wave][lane] = acc;
-  __syncthreads();
-  if (wave) return;
+  if constexpr (SPLIT > 1) {
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (wave % SPLIT) return;
 #pragma unroll
-  for (int w = 1; w < WAVES; ++w) acc += sums[w][lane];
-  const int m = t.m0 + (lane & 15), nn = t.n0 + (lane >> 4) * 4;
+    for (int w = 1; w < SPLIT; ++w) acc += sums[wave + w][lane];
+  }
+  const int m = t.m0 + (lane & 15), nn = n0 + (lane >> 4) * 4;
   if (m >= t.M || nn >= t.N) return;
   float v[4];
 #pragma unroll
@@ -574,6 +645,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void f8_few_kernel(F8Operand
   if (p.type == BNN_BF16) store4(reinterpret_cast<__bf16 *>(t.y) + m * p.ldy, nn, t.N, v);
   else if (p.type == BNN_F16) store4(reinterpret_cast<_Float16 *>(t.y) + m * p.ldy, nn, t.N, v);
   else store4(reinterpret_cast<float *>(t.y) + m * p.ldy, nn, t.N, v);
+}
+template <int SPLIT, bool WIDE>
+__global__ __launch_bounds__(512, 4) void f8_few_kernel(F8Operands p) {
+  __shared__ v4f sums[8][64];
+  f8_few_product<SPLIT, WIDE>(p, sums);
 }
 
 }  // namespace bnn

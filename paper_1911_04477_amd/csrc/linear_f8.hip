@@ -8,23 +8,55 @@
 
 namespace bnn {
 
-// Which kernel takes a product, by rounds of tiles as in few_mm.h.  rows: of a group, on average, and groups: how many.
-enum : int { F8_256, F8_128, F8_64, F8_32, F8_FORM_COUNT, F8_FEW = 8 };
-constexpr MmForm F8_FORMS[F8_FORM_COUNT] = {{256, 256, 100, 200}, {128, 128, 45, 74}, {64, 64, 22, 32}, {32, 64, 17, 24}};
-inline int f8_form(int64_t rows, int64_t groups, int64_t N, bool small, int64_t units) {
-  if (rows <= 16) return F8_FEW;
+// Which kernel takes a product: that of few rows, or the tiles with the least time by what a round of them was measured to take, in us, with
+// k of b blocks: start + block * b.  one: a compute unit has one tile at a time; two: it has two, and rounds count in parts (there a unit
+// that is done takes the next tile, and rounds overlap).  Measured in bf16, scales powers of two (fp32 results in brackets), us:
+//   rows x columns x k     256x256    256x128    128x128    128x128, 8 waves    128x64    64x64    64x32
+//   64 x 4096 x 4096          40         28         25         20                 13        12       8.6
+//   256 x 4096 x 4096         46         29         27         21                 15        12      15.7
+//   512 x 4096 x 4096         46         29         27         22                 15        19      29.5
+//   1000 x 3001 x 2321        33         20       17.6 (24)    15 (24)            20 (25)   18 (25)  32
+//   2048 x 4096 x 4096        50 (81)    36 (61)    38 (63)    50 (80)            60        67
+//   8192 x 8192 x 2048       146        184        184        248                246       294
+//   8192 x 4096 x 512         35 (62)    35 (63)    33 (58)    44 (87)            39 (66)   60
+enum : int { F8_256, F8_256_128, F8_128, F8_128_EIGHT, F8_128_64, F8_64, F8_64_32, F8_FORM_COUNT, F8_FEW };
+struct F8Cost {
+  float start, block, start2, block2;  // of one tile a unit, of two (0: one at a time)
+};
+struct F8Form {
+  int bm, bn;
+  F8Cost bits16, f32, bits16_wide, f32_wide;
+};
+constexpr F8Cost F8_NEVER = {1e9f, 0.0f, 0.0f, 0.0f};
+constexpr F8Form F8_FORMS[F8_FORM_COUNT] = {
+    {256, 256, {12, 1.5f, 0, 0}, {18, 3.0f, 0, 0}, F8_NEVER, F8_NEVER},
+    {256, 128, {5, 1.0f, 0, 0}, {8, 1.65f, 0, 0}, {6, 1.28f, 0, 0}, {9, 2.1f, 0, 0}},
+    {128, 128, {3.5f, 0.73f, 4.5f, 1.07f}, {6, 0.95f, 8, 1.7f}, {3.5f, 0.85f, 4.5f, 2.2f}, {6, 1.25f, 8, 2.1f}},
+    {128, 128, {3.5f, 0.58f, 0, 0}, {5, 1.0f, 0, 0}, {3.5f, 0.8f, 0, 0}, {5, 1.05f, 0, 0}},
+    {128, 64, {3, 0.37f, 0, 0}, {4, 0.6f, 0, 0}, {3.5f, 0.5f, 0, 0}, {4, 0.8f, 0, 0}},
+    {64, 64, {2.5f, 0.3f, 2.5f, 0.5f}, {3, 0.4f, 3, 0.65f}, {2.5f, 0.4f, 2.5f, 0.6f}, {3, 0.5f, 3, 0.8f}},
+    {64, 32, {2.2f, 0.2f, 0, 0}, {2.5f, 0.25f, 0, 0}, {2.5f, 0.25f, 0, 0}, {2.5f, 0.3f, 0, 0}}};
+// rows: of all groups, or where these are along k (`same`) of each; blocks: of k a group.
+inline int f8_form(int64_t rows, int64_t groups, bool same, int64_t N, int64_t blocks, bool wide, bool exact, int64_t units) {
+  // Few rows: sixteen of A cost what sixteen of B do, so more than a few want tiles where there is enough to stream (16 rows of two
+  // experts, 8192 x 4096 each: 18 us, on 64 x 64 tiles 14), and fewer columns than units can keep busy want k split (one row, 4096 x 4096: 6.0, 11).
+  const int64_t each = same ? rows : (rows - 1) / groups + 1, columns = groups * ((N - 1) / 16 + 1);
+  if (each <= 4 || (each <= 16 && columns <= 2 * units)) return F8_FEW;
   int best = F8_64;
-  int64_t least = INT64_MAX;
-  for (int f = small ? F8_128 : F8_256; f < F8_FORM_COUNT; ++f) {
-    const MmForm &t = F8_FORMS[f];
-    const int64_t tiles = groups * ((rows - 1) / t.bm + 1) * ((N - 1) / t.bn + 1);
-    const int64_t cost = t.bm == 256 ? (tiles + units - 1) / units * t.one : tiles <= units ? t.one : (tiles + 2 * units - 1) / (2 * units) * t.two;
-    if (cost <= least) least = cost, best = f;
+  double least = 1e30;
+  for (int f = 0; f < F8_FORM_COUNT; ++f) {
+    const F8Form &t = F8_FORMS[f];
+    const F8Cost &c = wide ? (exact ? t.f32_wide : t.bits16_wide) : exact ? t.f32 : t.bits16;
+    const int64_t row_tiles = groups == 1 || same ? groups * ((rows - 1) / t.bm + 1) : std::max(groups, rows / t.bm + groups / 2);  // groups end inside tiles
+    const int64_t tiles = row_tiles * ((N - 1) / t.bn + 1);
+    const double one = (double)((tiles + units - 1) / units) * (c.start + c.block * blocks);
+    const double two = tiles > units && c.block2 > 0 ? std::max(1.0, (double)tiles / (2.0 * units)) * (c.start2 + c.block2 * blocks) : 1e30;
+    if (std::min(one, two) < least) least = std::min(one, two), best = f;
   }
   return best;
 }
 
-template <int BM, int BN, int WGM, int WGN, int STAGES, bool WIDE, bool EXACT>
+template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, bool EXACT>
 bnn_status launch_f8_tile(F8Operands p, hipStream_t s) {
   p.tilesN = (p.N - 1) / BN + 1;
   // groups of rows: each has a part of a tile more than its rows fill at most
@@ -34,35 +66,45 @@ bnn_status launch_f8_tile(F8Operands p, hipStream_t s) {
   ProfScope ps(KID_LINEAR_F8, s);
   wide_launches(tiles, [&](int64_t first, uint32_t n) {
     p.first = first;
-    f8_tile_kernel<BM, BN, WGM, WGN, STAGES, WIDE, EXACT><<<n, 64 * WGM * WGN, 0, s>>>(p);
+    f8_tile_kernel<BM, BN, WGM, WGN, KG, STAGES, WIDE, EXACT><<<n, 64 * WGM * WGN * KG, 0, s>>>(p);
   });
   return launch_status();
 }
 
-template <bool WIDE>
-bnn_status launch_f8_few(F8Operands p, hipStream_t s) {
-  p.tilesN = (p.N - 1) / 16 + 1;
-  p.tilesM = p.groups == F8_GROUP_ROWS ? p.M / 16 + std::min(p.E, p.M) : (p.M - 1) / 16 + 1;
-  if ((int64_t)p.tilesM * p.tilesN > INT32_MAX) return BNN_ERR_UNSUPPORTED;
+template <int SPLIT, bool WIDE>
+bnn_status launch_f8_few_split(F8Operands p, int64_t row_tiles, hipStream_t s) {
+  p.tilesN = (p.N - 1) / (128 / SPLIT) + 1;
+  p.tilesM = (int)row_tiles;
+  if (row_tiles * p.tilesN > INT32_MAX) return BNN_ERR_UNSUPPORTED;
   ProfScope ps(KID_LINEAR_F8_FEW, s);
-  wide_launches((int64_t)p.tilesM * p.tilesN * (p.groups == F8_GROUP_K ? p.E : 1), [&](int64_t first, uint32_t n) {
+  wide_launches(row_tiles * p.tilesN * (p.groups == F8_GROUP_K ? p.E : 1), [&](int64_t first, uint32_t n) {
     p.first = first;
-    f8_few_kernel<8, WIDE><<<n, 512, 0, s>>>(p);
+    f8_few_kernel<SPLIT, WIDE><<<n, 512, 0, s>>>(p);
   });
   return launch_status();
+}
+template <bool WIDE>
+bnn_status launch_f8_few(const F8Operands &p, hipStream_t s) {
+  const int64_t row_tiles = p.groups == F8_GROUP_ROWS ? p.M / 16 + std::min(p.E, p.M) : (p.M - 1) / 16 + 1;
+  const int64_t columns = (row_tiles * (p.groups == F8_GROUP_K ? p.E : 1) * ((p.N - 1) / 16 + 1)), units = device_cu_count();
+  if (columns >= 4 * units) return launch_f8_few_split<2, WIDE>(p, row_tiles, s);
+  if (columns >= 2 * units) return launch_f8_few_split<4, WIDE>(p, row_tiles, s);
+  return launch_f8_few_split<8, WIDE>(p, row_tiles, s);
 }
 
 template <bool WIDE, bool EXACT>
 bnn_status run_f8_as(const F8Operands &p, hipStream_t s) {
-  int64_t rows = p.M, groups = 1;
-  if (p.groups == F8_GROUP_ROWS) groups = std::min(p.E, p.M), rows = (p.M - 1) / groups + 1;
-  if (p.groups == F8_GROUP_K) groups = p.E;
-  switch (f8_form(rows, groups, p.N, WIDE, device_cu_count())) {
+  const bool along_k = p.groups == F8_GROUP_K;
+  const int64_t groups = p.groups == F8_PLAIN ? 1 : along_k ? p.E : std::min(p.E, p.M);
+  switch (f8_form(p.M, groups, along_k, p.N, along_k ? p.blocks / p.E + 1 : p.blocks, WIDE, EXACT, device_cu_count())) {
     case F8_256:
-      if constexpr (!WIDE) return launch_f8_tile<256, 256, 2, 2, 2, false, EXACT>(p, s);
-    case F8_128: return launch_f8_tile<128, 128, 2, 2, 2, WIDE, EXACT>(p, s);
-    case F8_64: return launch_f8_tile<64, 64, 2, 2, 3, WIDE, EXACT>(p, s);
-    case F8_32: return launch_f8_tile<32, 64, 1, 2, 4, WIDE, EXACT>(p, s);
+      if constexpr (!WIDE) return launch_f8_tile<256, 256, 2, 2, 1, 2, false, EXACT>(p, s);
+    case F8_256_128: return launch_f8_tile<256, 128, 4, 2, 1, 3, WIDE, EXACT>(p, s);
+    case F8_128: return launch_f8_tile<128, 128, 2, 2, 1, 2, WIDE, EXACT>(p, s);
+    case F8_128_EIGHT: return launch_f8_tile<128, 128, 4, 2, 1, 4, WIDE, EXACT>(p, s);
+    case F8_128_64: return launch_f8_tile<128, 64, 2, 2, 2, 3, WIDE, EXACT>(p, s);
+    case F8_64: return launch_f8_tile<64, 64, 2, 2, 1, 4, WIDE, EXACT>(p, s);
+    case F8_64_32: return launch_f8_tile<64, 32, 2, 1, 4, 3, WIDE, EXACT>(p, s);
     default: return launch_f8_few<WIDE>(p, s);
   }
 }
