@@ -188,7 +188,8 @@ class _Tensors:
 
     FUNCTIONS = ("gemm", "epilogue", "encode", "conv2d", "conv2d_packed", "im2col", "f32_sign", "conv2d_f32", "maxpool", "fc",
                  "quant_rows", "linear_i8", "norm_gate", "norm_gate_backward", "norm_gate_gradients", "gated_ff", "gated_ff_i8",
-                 "gated_ff_backward", "gated_ff_gradients")
+                 "gated_ff_backward", "gated_ff_gradients", "quant_f8", "linear_f8", "expert_linear_f8", "expert_linear_f8_dw", "expert_sort",
+                 "expert_gather", "expert_combine", "expert_combine_backward", "gated_act", "gated_act_f8", "gated_act_backward")
 
     def __init__(self, L: ctypes.CDLL, path: str):
         module = None
@@ -1090,16 +1091,23 @@ def _f8_weight(b: torch.Tensor, scale: torch.Tensor, name: str, shape: Tuple[int
             _padded(scale, name + "_scale", (*shape[:-2], N if per == 1 else _blocks(N), blocks), room, quantum), int(wide), per)
 
 
+def _made(made, where: str):
+    """What a call from the tensors themselves gave, where it was one: its results, or the error of its status."""
+    if type(made) is int:
+        _check(made, where)
+    return made
+
+
 def rows_f8(rows: int, K: int, device="cuda:0", experts: Optional[int] = None) -> torch.Tensor:
     """Room for e4m3 [rows, K] (or [experts, rows, K]) in rows of whole blocks of 128."""
     lead = (rows,) if experts is None else (experts, rows)
-    return torch.empty((*lead, _blocks(K) * F8_BLOCK), dtype=torch.uint8, device=device).view(F8)[..., :K]
+    return torch.empty((*lead, _blocks(K) * F8_BLOCK), dtype=F8, device=device)[..., :K]
 
 
 def scales_f8(rows: int, K: int, device="cuda:0", experts: Optional[int] = None) -> torch.Tensor:
     """Room for the scales of such rows, one a block: [rows, ceil(K / 128)] (or [experts, rows, ..])."""
     lead = (rows,) if experts is None else (experts, rows)
-    return torch.empty((*lead, (_blocks(K) + 3) // 4 * 4), dtype=torch.uint8, device=device).view(E8M0)[..., :_blocks(K)]
+    return torch.empty((*lead, (_blocks(K) + 3) // 4 * 4), dtype=E8M0, device=device)[..., :_blocks(K)]
 
 
 def _positions(rows: Optional[torch.Tensor], T: int) -> Tuple[Optional[int], int]:
@@ -1114,6 +1122,9 @@ def bnn_quant_blocks_f8(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale
                         rows: Optional[torch.Tensor] = None, k: int = 1) -> Tuple[torch.Tensor, torch.Tensor]:
     """x [T, K] fp32, bf16 or fp16 -> (q e4m3 [S, K], scale [S, ceil(K / 128)]), powers of two.  rows (bnn_expert_sort): position s is
     x[rows[s] // k], zeros for -1, left as it was for -2; without rows S = T."""
+    made = _made(_t().quant_f8(x, q, scale, rows, k, 0), "bnn_quant_blocks_f8")
+    if made is not None:
+        return made
     kind, ld = _float_rows(x, "x")
     T, K = x.shape
     p_rows, S = _positions(rows, T)
@@ -1128,6 +1139,9 @@ def bnn_quant_columns_f8(x: torch.Tensor, q: Optional[torch.Tensor] = None, scal
                          rows: Optional[torch.Tensor] = None, k: int = 1) -> Tuple[torch.Tensor, torch.Tensor]:
     """x [T, D] -> (q e4m3 [D, S], scale [D, ceil(S / 128)]): x, or the rows of it that `rows` names, turned, in blocks along the
     positions; positions without a row are zeros."""
+    made = _made(_t().quant_f8(x, q, scale, rows, k, 1), "bnn_quant_columns_f8")
+    if made is not None:
+        return made
     kind, ld = _float_rows(x, "x")
     T, D = x.shape
     p_rows, S = _positions(rows, T)
@@ -1166,13 +1180,15 @@ def bnn_linear_f8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_sca
                   dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """a e4m3 [M, K] and its scales, b e4m3 [N, K] and its scales, a row of them for each of its rows or for 128 (these also
     fp32) -> [M, N] of out's type, or of dtype."""
+    if out is None and a.dim() == 2 and b.dim() == 2:
+        out = torch.empty((a.shape[0], b.shape[0]), dtype=dtype, device=a.device)
+    if _made(_t().linear_f8(a, a_scale, b, b_scale, bias, out), "bnn_linear_f8") is not None:
+        return out
     if a.dim() != 2 or b.dim() != 2:
         raise ValueError("a, b: matrices expected")
     (M, K), N = a.shape, b.shape[0]
     pa, lda, psa, sa_ld = _f8(a, a_scale, "a", (M, K))
     (pb, ldb, _), (psb, sb_ld, _), wide, per = _f8_weight(b, b_scale, "b", (N, K))
-    if out is None:
-        out = torch.empty((M, N), dtype=dtype, device=a.device)
     kind, ldy = _float_rows(out, "out", M, N)
     if bias is not None:
         _present(bias, "bias")
@@ -1189,13 +1205,15 @@ def bnn_expert_linear_f8(a: torch.Tensor, a_scale: torch.Tensor, offsets: torch.
                          out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """Rows sorted by expert (bnn_expert_sort), a e4m3 [S, K], times their experts' weights, b e4m3 [E, N, K], scales as in
     bnn_linear_f8 -> [S, N]; rows behind the last expert's are left as they were."""
+    if out is None and a.dim() == 2 and b.dim() == 3:
+        out = torch.empty((a.shape[0], b.shape[1]), dtype=dtype, device=a.device)
+    if _made(_t().expert_linear_f8(a, a_scale, offsets, b, b_scale, out), "bnn_expert_linear_f8") is not None:
+        return out
     if a.dim() != 2 or b.dim() != 3:
         raise ValueError("a [S, K], b [experts, N, K] expected")
     (S, K), (E, N) = a.shape, b.shape[:2]
     pa, lda, psa, sa_ld = _f8(a, a_scale, "a", (S, K))
     (pb, ldb, b_es), (psb, sb_ld, sb_es), wide, per = _f8_weight(b, b_scale, "b", (E, N, K))
-    if out is None:
-        out = torch.empty((S, N), dtype=dtype, device=a.device)
     kind, ldy = _float_rows(out, "out", S, N)
     _check(_c().bnn_expert_linear_f8(pa, lda, psa, sa_ld, _offsets(offsets, E), E, pb, ldb, b_es, psb, wide, sb_ld, sb_es, per, S, N, K,
                                       _ptr(out), kind, ldy, _stream()), "bnn_expert_linear_f8")
@@ -1206,13 +1224,15 @@ def bnn_expert_linear_f8_dw(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Ten
                             out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
     """The experts' weights' gradients [E, N, K] from those of the rows, a e4m3 [N, S], and the rows, b e4m3 [K, S], both as
     bnn_quant_columns_f8 gives them; offsets multiples of 128 (bnn_expert_sort with align 128)."""
+    if out is None and a.dim() == 2 and b.dim() == 2 and offsets.dim() == 1 and offsets.shape[0] > 0:
+        out = torch.empty((offsets.shape[0] - 1, a.shape[0], b.shape[0]), dtype=dtype, device=a.device)
+    if _made(_t().expert_linear_f8_dw(a, a_scale, b, b_scale, offsets, out), "bnn_expert_linear_f8_dw") is not None:
+        return out
     if a.dim() != 2 or b.dim() != 2 or offsets.dim() != 1 or offsets.shape[0] < 1:
         raise ValueError("a [N, S], b [K, S], offsets [experts + 1] expected")
     (N, S), K, E = a.shape, b.shape[0], offsets.shape[0] - 1
     pa, lda, psa, sa_ld = _f8(a, a_scale, "a", (N, S))
     pb, ldb, psb, sb_ld = _f8(b, b_scale, "b", (K, S))
-    if out is None:
-        out = torch.empty((E, N, K), dtype=dtype, device=a.device)
     _present(out, "out", *FLOATS)
     p_out, ld, es = _padded(out, "out", (E, N, K), K, 1)
     _check(_c().bnn_expert_linear_f8_dw(pa, lda, psa, sa_ld, pb, ldb, psb, sb_ld, _offsets(offsets, E), E, N, K, S, p_out,
@@ -1234,6 +1254,9 @@ def bnn_expert_sort(experts: torch.Tensor, E: int, align: int = 1, offsets: Opti
                     workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """experts [T, k] int32 or int64 (outside 0 .. E - 1: none) -> (offsets [E + 1], rows [S], places [T, k]), all int32: where each
     expert's rows begin (multiples of align), the slot token * k + choice at a position, the position of a slot."""
+    made = _made(_t().expert_sort(experts, E, align, offsets, rows, places, workspace), "bnn_expert_sort")
+    if made is not None:
+        return made
     _present(experts, "experts", torch.int32, torch.int64)
     if experts.dim() != 2 or not experts.is_contiguous():
         raise ValueError("experts: contiguous [tokens, choices] expected")
@@ -1253,6 +1276,9 @@ def bnn_expert_sort(experts: torch.Tensor, E: int, align: int = 1, offsets: Opti
 
 def bnn_expert_gather(x: torch.Tensor, rows: torch.Tensor, k: int, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [T, D] -> [S, D]: position s is x[rows[s] // k], zeros for -1, left as it was for -2."""
+    made = _made(_t().expert_gather(x, rows, k, out), "bnn_expert_gather")
+    if made is not None:
+        return made
     kind, ld = _float_rows(x, "x")
     T, D = x.shape
     p_rows, S = _positions(rows, T)
@@ -1266,6 +1292,9 @@ def bnn_expert_combine(ys: torch.Tensor, places: torch.Tensor, weights: Optional
                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """ys [S, D] -> [T, D], out[t] = sum over j of weights[t, j] * ys[places[t, j]]; dropped slots (-1) add nothing.  Without weights:
     the gradient of bnn_expert_gather."""
+    made = _made(_t().expert_combine(ys, places, weights, out), "bnn_expert_combine")
+    if made is not None:
+        return made
     kind, ld = _float_rows(ys, "ys")
     (S, D), (T, k) = ys.shape, places.shape
     out = torch.empty((T, D), dtype=ys.dtype, device=ys.device) if out is None else out
@@ -1281,6 +1310,9 @@ def bnn_expert_combine_backward(ys: torch.Tensor, rows: torch.Tensor, places: to
                                 dweights: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(dys [S, D], dweights [T, k]) of bnn_expert_combine from dout [T, D]; positions of no slot between the experts' rows get zeros,
     those behind the last are left as they were."""
+    made = _made(_t().expert_combine_backward(ys, rows, places, weights, dout, dys, dweights), "bnn_expert_combine_backward")
+    if made is not None:
+        return made
     kind, ld = _float_rows(ys, "ys")
     (S, D), (T, k) = ys.shape, places.shape
     p_rows, _ = _positions(rows, S)
@@ -1308,6 +1340,9 @@ def bnn_gated_act(gu: torch.Tensor, act: str = "silu", out: Optional[torch.Tenso
                   live: Optional[torch.Tensor] = None) -> torch.Tensor:
     """gu [S, 2 F] = [g | u] -> h [S, F] = act(g) * u.  live (one int32, as offsets[-1:] of bnn_expert_sort): rows from there on are
     left as they were."""
+    made = _made(_t().gated_act(gu, ACTS.get(act), out, live), "bnn_gated_act")
+    if made is not None:
+        return made
     S, F, kind, ld, a, p_live = _gated(gu, act, live)
     out = torch.empty((S, F), dtype=gu.dtype, device=gu.device) if out is None else out
     _present(out, "out", gu.dtype)
@@ -1318,6 +1353,9 @@ def bnn_gated_act(gu: torch.Tensor, act: str = "silu", out: Optional[torch.Tenso
 def bnn_gated_act_f8(gu: torch.Tensor, act: str = "silu", q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
                      live: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The same as e4m3 rows with their scales, from h in fp32."""
+    made = _made(_t().gated_act_f8(gu, ACTS.get(act), q, scale, live), "bnn_gated_act_f8")
+    if made is not None:
+        return made
     S, F, kind, ld, a, p_live = _gated(gu, act, live)
     q = rows_f8(S, F, gu.device) if q is None else q
     scale = scales_f8(S, F, gu.device) if scale is None else scale
@@ -1329,6 +1367,9 @@ def bnn_gated_act_f8(gu: torch.Tensor, act: str = "silu", q: Optional[torch.Tens
 def bnn_gated_act_backward(gu: torch.Tensor, dh: torch.Tensor, act: str = "silu", out: Optional[torch.Tensor] = None,
                            live: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dgu [S, 2 F] of bnn_gated_act from dh [S, F]."""
+    made = _made(_t().gated_act_backward(gu, dh, ACTS.get(act), out, live), "bnn_gated_act_backward")
+    if made is not None:
+        return made
     S, F, kind, ld, a, p_live = _gated(gu, act, live)
     out = torch.empty((S, 2 * F), dtype=gu.dtype, device=gu.device) if out is None else out
     for t, name in ((dh, "dh"), (out, "out")):

@@ -40,11 +40,28 @@ struct Library {
   decltype(&bnn_gated_ff_backward) gated_backward;
   decltype(&bnn_norm_gate_backward_workspace_bytes) norm_workspace;
   decltype(&bnn_gated_ff_backward_workspace_bytes) gated_workspace;
+  decltype(&bnn_quant_blocks_f8) quant_blocks;
+  decltype(&bnn_quant_columns_f8) quant_columns;
+  decltype(&bnn_linear_f8) linear_f8;
+  decltype(&bnn_expert_linear_f8) expert_linear;
+  decltype(&bnn_expert_linear_f8_dw) expert_linear_dw;
+  decltype(&bnn_expert_rows) expert_rows;
+  decltype(&bnn_expert_sort_workspace_bytes) sort_workspace;
+  decltype(&bnn_expert_sort) sort;
+  decltype(&bnn_expert_gather) gather;
+  decltype(&bnn_expert_combine) combine;
+  decltype(&bnn_expert_combine_backward) combine_backward;
+  decltype(&bnn_gated_act) gated_act;
+  decltype(&bnn_gated_act_f8) gated_act_f8;
+  decltype(&bnn_gated_act_backward) gated_act_backward;
 };
 constexpr const char *names[] = {"bnn_xnor_gemm", "bnn_xnor_gemm_epilogue", "bnn_encode", "bnn_conv2d", "bnn_conv2d_packed",
                                  "bnn_im2col_packed", "bnn_conv2d_f32_sign", "bnn_conv2d_f32", "bnn_maxpool2x2", "bnn_fc_f32", "bnn_quant_rows_i8", "bnn_linear_i8",
                                  "bnn_norm_gate", "bnn_norm_gate_backward", "bnn_gated_ff", "bnn_gated_ff_i8", "bnn_gated_ff_backward",
-                                 "bnn_norm_gate_backward_workspace_bytes", "bnn_gated_ff_backward_workspace_bytes"};
+                                 "bnn_norm_gate_backward_workspace_bytes", "bnn_gated_ff_backward_workspace_bytes",
+                                 "bnn_quant_blocks_f8", "bnn_quant_columns_f8", "bnn_linear_f8", "bnn_expert_linear_f8", "bnn_expert_linear_f8_dw",
+                                 "bnn_expert_rows", "bnn_expert_sort_workspace_bytes", "bnn_expert_sort", "bnn_expert_gather", "bnn_expert_combine",
+                                 "bnn_expert_combine_backward", "bnn_gated_act", "bnn_gated_act_f8", "bnn_gated_act_backward"};
 Library lib = {};
 
 struct Other {};  // not the plain case
@@ -561,6 +578,278 @@ PyObject *gated_ff_gradients(PyObject *, PyObject *const *a, Py_ssize_t n) {  //
   });
 }
 
+// ---- 8-bit floating point and experts: outputs are made here where they are not given (None); what comes back are the tensors ----
+const at::Tensor &present(const at::Tensor &t, at::ScalarType type) {  // on the device whose stream the call goes to
+  if (!t.is_cuda() || t.scalar_type() != type || t.get_device() != c10::hip::getCurrentHIPStream().device_index()) throw Other();
+  return t;
+}
+Matrix present_matrix(const at::Tensor &t, at::ScalarType type) { return matrix(present(t, type), type); }
+Matrix present_matrix(const at::Tensor &t, at::ScalarType type, int64_t rows, int64_t cols) {
+  return matrix(present(t, type), type, rows, cols);
+}
+template <class T>
+T *whole(const at::Tensor *t, at::ScalarType type, std::initializer_list<int64_t> shape) {
+  if (!t) return nullptr;
+  if (present(*t, type).sizes() != at::IntArrayRef(shape) || !t->is_contiguous()) throw Other();
+  return static_cast<T *>(t->data_ptr());
+}
+// Rows with `row` elements of room each, [rows, cols] or for experts [experts, rows, cols], as the binding checks them.
+struct Padded {
+  uint8_t *p;
+  int64_t ld, between;
+};
+Padded padded(const at::Tensor &t, int64_t experts, int64_t rows, int64_t cols, int64_t row, int64_t quantum) {
+  const int64_t d = t.dim();
+  if (d != (experts < 0 ? 2 : 3) || t.size(d - 2) != rows || t.size(d - 1) != cols || (experts >= 0 && t.size(0) != experts)) throw Other();
+  if (cols > 1 && t.stride(d - 1) != 1) throw Other();
+  Padded m;
+  m.ld = rows > 1 ? t.stride(d - 2) : std::max((row + quantum - 1) / quantum * quantum, t.stride(d - 2) / quantum * quantum);
+  m.between = experts > 1 ? t.stride(0) : rows * m.ld;
+  if (m.ld < row) throw Other();
+  if (t.numel() > 0) {
+    const double last = (double)t.storage_offset() + (double)(std::max<int64_t>(experts, 1) - 1) * m.between + (double)(rows - 1) * m.ld + row;
+    if (last * t.element_size() > (double)t.storage().nbytes()) throw Other();
+  }
+  m.p = static_cast<uint8_t *>(t.data_ptr());
+  return m;
+}
+int64_t blocks_of(int64_t K) { return (K + 127) / 128; }
+constexpr at::ScalarType kF8 = at::kFloat8_e4m3fn, kE8 = at::kFloat8_e8m0fnu;
+Padded f8_values(const at::Tensor &t, int64_t experts, int64_t rows, int64_t K) {
+  return padded(present(t, kF8), experts, rows, K, blocks_of(K) * 128, 16);
+}
+Padded f8_scales(const at::Tensor &t, int64_t experts, int64_t rows, int64_t K) {
+  return padded(present(t, kE8), experts, rows, blocks_of(K), (blocks_of(K) + 3) / 4 * 4, 4);
+}
+struct Weight {
+  Padded q, s;
+  int wide, per;
+};
+Weight f8_weight(const at::Tensor &q, const at::Tensor &s, int64_t experts, int64_t N, int64_t K) {
+  Weight w;
+  w.q = f8_values(q, experts, N, K);
+  w.wide = s.scalar_type() == kFloat;
+  if (s.dim() != q.dim()) throw Other();
+  w.per = s.size(s.dim() - 2) == N && !w.wide && N > 1 ? 1 : 128;
+  const int64_t rows = w.per == 1 ? N : blocks_of(N);
+  w.s = w.wide ? padded(present(s, kFloat), experts, rows, blocks_of(K), blocks_of(K), 1) : f8_scales(s, experts, rows, K);
+  return w;
+}
+at::Tensor made_f8(const at::Tensor *t, int64_t rows, int64_t K, const at::Tensor &on) {
+  return t ? *t : at::empty({rows, blocks_of(K) * 128}, on.options().dtype(kF8)).narrow(1, 0, K);
+}
+at::Tensor made_scales(const at::Tensor *t, int64_t rows, int64_t K, const at::Tensor &on) {
+  return t ? *t : at::empty({rows, (blocks_of(K) + 3) / 4 * 4}, on.options().dtype(kE8)).narrow(1, 0, blocks_of(K));
+}
+at::Tensor made(const at::Tensor *t, at::IntArrayRef sizes, at::ScalarType type, const at::Tensor &on) {
+  return t ? *t : at::empty(sizes, on.options().dtype(type));
+}
+PyObject *result(PyObject *status, const at::Tensor &t) {
+  if (!status || PyLong_AsLong(status) != BNN_OK) return status;
+  Py_DECREF(status);
+  return THPVariable_Wrap(t);
+}
+
+// x, q, scale, rows, k, columns -> q, scale
+PyObject *quant_f8(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 6, [](Args &v) {
+    const at::Tensor &t = v.tensor(), *const gq = v.tensor_or_none(), *const gs = v.tensor_or_none(), *const gr = v.tensor_or_none();
+    const int64_t k = v.integer();
+    const bool columns = v.integer() != 0;
+    const int type = float_type(t.scalar_type());
+    const Matrix x = present_matrix(t, t.scalar_type());
+    if (gr && gr->dim() != 1) throw Other();
+    const int64_t S = gr ? gr->size(0) : x.rows, out_rows = columns ? x.cols : S, K = columns ? S : x.cols;
+    const int32_t *const rows = gr ? whole<int32_t>(gr, kInt, {S}) : nullptr;
+    const at::Tensor out[2] = {made_f8(gq, out_rows, K, t), made_scales(gs, out_rows, K, t)};
+    const Padded q = f8_values(out[0], -1, out_rows, K), s = f8_scales(out[1], -1, out_rows, K);
+    return results(launch([&](void *stream) {
+      return (columns ? lib.quant_columns : lib.quant_blocks)(x.p, type, x.rows, x.ld, rows, k, S, x.cols, q.p, q.ld, s.p, s.ld, stream);
+    }), out);
+  });
+}
+
+PyObject *linear_f8(PyObject *, PyObject *const *args, Py_ssize_t n) {  // a, a_scale, b, b_scale, bias, out -> status
+  return guarded(args, n, 6, [](Args &v) {
+    const at::Tensor &ta = v.tensor(), &tsa = v.tensor(), &tb = v.tensor(), &tsb = v.tensor();
+    if (ta.dim() != 2 || tb.dim() != 2) throw Other();
+    const int64_t M = ta.size(0), K = ta.size(1), N = tb.size(0);
+    const Padded a = f8_values(ta, -1, M, K), sa = f8_scales(tsa, -1, M, K);
+    const Weight b = f8_weight(tb, tsb, -1, N, K);
+    const at::Tensor *const tbias = v.tensor_or_none();
+    if (tbias) present(*tbias, kFloat);
+    const float *const bias = vector(tbias, N);
+    const at::Tensor &out = v.tensor();
+    const int code = float_type(out.scalar_type());
+    const Matrix y = present_matrix(out, out.scalar_type(), M, N);
+    return launch([&](void *s) {
+      return lib.linear_f8(a.p, a.ld, sa.p, sa.ld, b.q.p, b.q.ld, b.s.p, b.wide, b.s.ld, b.per, bias, M, N, K, y.p, code, y.ld, s);
+    });
+  });
+}
+
+PyObject *expert_linear_f8(PyObject *, PyObject *const *args, Py_ssize_t n) {  // a, a_scale, offsets, b, b_scale, out -> status
+  return guarded(args, n, 6, [](Args &v) {
+    const at::Tensor &ta = v.tensor(), &tsa = v.tensor(), &to = v.tensor(), &tb = v.tensor(), &tsb = v.tensor(), &out = v.tensor();
+    if (ta.dim() != 2 || tb.dim() != 3) throw Other();
+    const int64_t S = ta.size(0), K = ta.size(1), E = tb.size(0), N = tb.size(1);
+    const Padded a = f8_values(ta, -1, S, K), sa = f8_scales(tsa, -1, S, K);
+    const Weight b = f8_weight(tb, tsb, E, N, K);
+    const int32_t *const offsets = whole<int32_t>(&to, kInt, {E + 1});
+    const int code = float_type(out.scalar_type());
+    const Matrix y = present_matrix(out, out.scalar_type(), S, N);
+    return launch([&](void *s) {
+      return lib.expert_linear(a.p, a.ld, sa.p, sa.ld, offsets, E, b.q.p, b.q.ld, b.q.between, b.s.p, b.wide, b.s.ld, b.s.between, b.per, S, N,
+                               K, y.p, code, y.ld, s);
+    });
+  });
+}
+
+PyObject *expert_linear_f8_dw(PyObject *, PyObject *const *args, Py_ssize_t n) {  // a, a_scale, b, b_scale, offsets, out -> status
+  return guarded(args, n, 6, [](Args &v) {
+    const at::Tensor &ta = v.tensor(), &tsa = v.tensor(), &tb = v.tensor(), &tsb = v.tensor(), &to = v.tensor(), &out = v.tensor();
+    if (ta.dim() != 2 || tb.dim() != 2 || to.dim() != 1 || to.size(0) < 1) throw Other();
+    const int64_t N = ta.size(0), S = ta.size(1), K = tb.size(0), E = to.size(0) - 1;
+    const Padded a = f8_values(ta, -1, N, S), sa = f8_scales(tsa, -1, N, S), b = f8_values(tb, -1, K, S), sb = f8_scales(tsb, -1, K, S);
+    const int32_t *const offsets = whole<int32_t>(&to, kInt, {E + 1});
+    const int code = float_type(out.scalar_type());
+    const Padded dw = padded(present(out, out.scalar_type()), E, N, K, K, 1);
+    return launch([&](void *s) {
+      return lib.expert_linear_dw(a.p, a.ld, sa.p, sa.ld, b.p, b.ld, sb.p, sb.ld, offsets, E, N, K, S, dw.p, code, dw.ld, dw.between, s);
+    });
+  });
+}
+
+// experts, E, align, offsets, rows, places, workspace -> offsets, rows, places
+PyObject *expert_sort(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 7, [](Args &v) {
+    const at::Tensor &t = v.tensor();
+    const int64_t E = v.integer(), align = v.integer();
+    const at::Tensor *const go = v.tensor_or_none(), *const gr = v.tensor_or_none(), *const gp = v.tensor_or_none(), *const gw = v.tensor_or_none();
+    if ((t.scalar_type() != kInt && t.scalar_type() != kLong) || t.dim() != 2 || !t.is_contiguous() || E < 1) throw Other();
+    present(t, t.scalar_type());
+    const int64_t T = t.size(0), k = t.size(1);
+    const at::Tensor out[3] = {made(go, {E + 1}, kInt, t), made(gr, {gr ? 0 : lib.expert_rows(T, k, E, align)}, kInt, t), made(gp, {T, k}, kInt, t)};
+    if (out[1].dim() != 1) throw Other();
+    const int64_t S = out[1].size(0);
+    int32_t *const offsets = whole<int32_t>(&out[0], kInt, {E + 1}), *const rows = whole<int32_t>(&out[1], kInt, {S}),
+            *const places = whole<int32_t>(&out[2], kInt, {T, k});
+    size_t bytes = lib.sort_workspace(T, k, E);
+    at::Tensor room_for;
+    void *ws = nullptr;
+    if (gw) ws = workspace(present(*gw, gw->scalar_type()), bytes);
+    else if (bytes) room_for = room(bytes, t), ws = room_for.data_ptr();
+    return results(launch([&](void *s) {
+      return lib.sort(t.data_ptr(), t.scalar_type() == kLong ? 8 : 4, T, k, E, align, S, offsets, rows, places, ws, bytes, s);
+    }), out);
+  });
+}
+
+PyObject *expert_gather(PyObject *, PyObject *const *a, Py_ssize_t n) {  // x, rows, k, out -> out
+  return guarded(a, n, 4, [](Args &v) {
+    const at::Tensor &t = v.tensor(), &tr = v.tensor();
+    const int64_t k = v.integer();
+    const at::ScalarType type = t.scalar_type();
+    const Matrix x = present_matrix(t, type);
+    if (tr.dim() != 1) throw Other();
+    const int64_t S = tr.size(0);
+    const int32_t *const rows = whole<int32_t>(&tr, kInt, {S});
+    const int code = float_type(type);
+    const at::Tensor out = made(v.tensor_or_none(), {S, x.cols}, type, t);
+    const Matrix y = present_matrix(out, type, S, x.cols);
+    return result(launch([&](void *s) { return lib.gather(x.p, code, x.rows, x.ld, rows, k, S, x.cols, y.p, y.ld, s); }), out);
+  });
+}
+
+PyObject *expert_combine(PyObject *, PyObject *const *a, Py_ssize_t n) {  // ys, places, weights, out -> out
+  return guarded(a, n, 4, [](Args &v) {
+    const at::Tensor &t = v.tensor(), &tp = v.tensor(), *const tw = v.tensor_or_none();
+    const at::ScalarType type = t.scalar_type();
+    const Matrix ys = present_matrix(t, type);
+    if (tp.dim() != 2) throw Other();
+    const int64_t T = tp.size(0), k = tp.size(1);
+    const int32_t *const places = whole<int32_t>(&tp, kInt, {T, k});
+    const float *const weights = whole<float>(tw, kFloat, {T, k});
+    const int code = float_type(type);
+    const at::Tensor out = made(v.tensor_or_none(), {T, ys.cols}, type, t);
+    const Matrix y = present_matrix(out, type, T, ys.cols);
+    return result(launch([&](void *s) { return lib.combine(ys.p, code, ys.rows, ys.ld, places, weights, T, k, ys.cols, y.p, y.ld, s); }), out);
+  });
+}
+
+// ys, rows, places, weights, dout, dys, dweights -> dys, dweights
+PyObject *expert_combine_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 7, [](Args &v) {
+    const at::Tensor &t = v.tensor(), &tr = v.tensor(), &tp = v.tensor(), *const tw = v.tensor_or_none(), &td = v.tensor();
+    const at::ScalarType type = t.scalar_type();
+    const Matrix ys = present_matrix(t, type);
+    if (tp.dim() != 2) throw Other();
+    const int64_t T = tp.size(0), k = tp.size(1), S = ys.rows, D = ys.cols;
+    const int32_t *const rows = whole<int32_t>(&tr, kInt, {S}), *const places = whole<int32_t>(&tp, kInt, {T, k});
+    const float *const weights = whole<float>(tw, kFloat, {T, k});
+    const Matrix dout = present_matrix(td, type, T, D);
+    const int code = float_type(type);
+    const at::Tensor *const gy = v.tensor_or_none(), *const gw = v.tensor_or_none();
+    const at::Tensor out[2] = {made(gy, {S, D}, type, t), made(gw, {T, k}, kFloat, t)};
+    const Matrix dys = present_matrix(out[0], type, S, D);
+    float *const dweights = whole<float>(&out[1], kFloat, {T, k});
+    return results(launch([&](void *s) {
+      return lib.combine_backward(ys.p, code, S, ys.ld, rows, places, weights, dout.p, dout.ld, T, k, D, dys.p, dys.ld, dweights, s);
+    }), out);
+  });
+}
+
+struct Gated {
+  Matrix gu;
+  int64_t S, F;
+  int code;
+  at::ScalarType type;
+};
+Gated gated_of(const at::Tensor &t) {
+  Gated g;
+  g.type = t.scalar_type(), g.code = float_type(g.type), g.gu = present_matrix(t, g.type);
+  if (g.gu.cols % 2) throw Other();
+  g.S = g.gu.rows, g.F = g.gu.cols / 2;
+  return g;
+}
+PyObject *gated_act(PyObject *, PyObject *const *a, Py_ssize_t n) {  // gu, act, out, live -> out
+  return guarded(a, n, 4, [](Args &v) {
+    const at::Tensor &t = v.tensor();
+    const Gated g = gated_of(t);
+    const int act = v.small();
+    const at::Tensor out = made(v.tensor_or_none(), {g.S, g.F}, g.type, t);
+    const int32_t *const live = whole<int32_t>(v.tensor_or_none(), kInt, {1});
+    const Matrix h = present_matrix(out, g.type, g.S, g.F);
+    return result(launch([&](void *s) { return lib.gated_act(g.gu.p, g.code, g.S, g.gu.ld, g.F, act, live, h.p, h.ld, s); }), out);
+  });
+}
+PyObject *gated_act_f8(PyObject *, PyObject *const *a, Py_ssize_t n) {  // gu, act, q, scale, live -> q, scale
+  return guarded(a, n, 5, [](Args &v) {
+    const at::Tensor &t = v.tensor();
+    const Gated g = gated_of(t);
+    const int act = v.small();
+    const at::Tensor *const gq = v.tensor_or_none(), *const gs = v.tensor_or_none();
+    const int32_t *const live = whole<int32_t>(v.tensor_or_none(), kInt, {1});
+    const at::Tensor out[2] = {made_f8(gq, g.S, g.F, t), made_scales(gs, g.S, g.F, t)};
+    const Padded q = f8_values(out[0], -1, g.S, g.F), sc = f8_scales(out[1], -1, g.S, g.F);
+    return results(launch([&](void *s) { return lib.gated_act_f8(g.gu.p, g.code, g.S, g.gu.ld, g.F, act, live, q.p, q.ld, sc.p, sc.ld, s); }), out);
+  });
+}
+PyObject *gated_act_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {  // gu, dh, act, out, live -> out
+  return guarded(a, n, 5, [](Args &v) {
+    const at::Tensor &t = v.tensor(), &td = v.tensor();
+    const Gated g = gated_of(t);
+    const int act = v.small();
+    const Matrix dh = present_matrix(td, g.type, g.S, g.F);
+    const at::Tensor out = made(v.tensor_or_none(), {g.S, 2 * g.F}, g.type, t);
+    const int32_t *const live = whole<int32_t>(v.tensor_or_none(), kInt, {1});
+    const Matrix dgu = present_matrix(out, g.type, g.S, 2 * g.F);
+    return result(launch([&](void *s) {
+      return lib.gated_act_backward(g.gu.p, g.code, g.S, g.gu.ld, g.F, act, live, dh.p, dh.ld, dgu.p, dgu.ld, s);
+    }), out);
+  });
+}
+
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
   constexpr Py_ssize_t want = sizeof(Library) / sizeof(void *);
   static_assert(want == sizeof(names) / sizeof(names[0]), "an address for every name");
@@ -585,7 +874,10 @@ PyMethodDef methods[] = {BNN_METHOD(bind), BNN_METHOD(gemm), BNN_METHOD(epilogue
                          BNN_METHOD(conv2d_packed), BNN_METHOD(im2col), BNN_METHOD(f32_sign), BNN_METHOD(conv2d_f32),
                          BNN_METHOD(maxpool), BNN_METHOD(fc), BNN_METHOD(quant_rows), BNN_METHOD(linear_i8),
                          BNN_METHOD(norm_gate), BNN_METHOD(norm_gate_backward), BNN_METHOD(norm_gate_gradients), BNN_METHOD(gated_ff), BNN_METHOD(gated_ff_i8),
-                         BNN_METHOD(gated_ff_backward), BNN_METHOD(gated_ff_gradients), {nullptr, nullptr, 0, nullptr}};
+                         BNN_METHOD(gated_ff_backward), BNN_METHOD(gated_ff_gradients), BNN_METHOD(quant_f8), BNN_METHOD(linear_f8),
+                         BNN_METHOD(expert_linear_f8), BNN_METHOD(expert_linear_f8_dw), BNN_METHOD(expert_sort), BNN_METHOD(expert_gather),
+                         BNN_METHOD(expert_combine), BNN_METHOD(expert_combine_backward), BNN_METHOD(gated_act), BNN_METHOD(gated_act_f8),
+                         BNN_METHOD(gated_act_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensorcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -342,3 +342,52 @@ def test_calls_on_another_stream_and_repeated():
     stream.synchronize()
     for a, b, c in zip(first, second, third):
         assert torch.equal(a, b) and torch.equal(b, c)
+
+
+def test_calls_without_the_tensor_extension(monkeypatch):
+    """Each call checked and converted by the binding itself gives what the extension's gives, and refuses what that leaves to it."""
+    T, k, E, D = 70, 2, 6, 264
+    g = gen(51)
+    e, x, w = choices(g, T, k, E).to(DEV), torch.randn((T, D), generator=g).to(BF16).to(DEV), torch.rand((T, k), generator=g).to(DEV)
+    weight = torch.randn((E, 272, D), generator=g).to(DEV)
+
+    def step():
+        offsets, rows, places = B.bnn_expert_sort(e, E, 128)
+        wq, wt = B.bnn_quant_weight_f8(weight)
+        x8 = B.bnn_quant_blocks_f8(x, rows=rows, k=k)
+        gu = B.bnn_expert_linear_f8(*x8, offsets, *wq, out=torch.zeros((rows.shape[0], 272), dtype=BF16, device=DEV))
+        h = B.bnn_gated_act(gu, "gelu", live=offsets[-1:], out=torch.zeros((rows.shape[0], 136), dtype=BF16, device=DEV))
+        h8 = B.bnn_gated_act_f8(gu, "gelu")
+        dgu = B.bnn_gated_act_backward(gu, h, "gelu")
+        y = B.bnn_linear_f8(*B.bnn_quant_blocks_f8(h), *h8, dtype=F32)
+        out = B.bnn_expert_combine(gu, places, w)
+        dys, dw = B.bnn_expert_combine_backward(gu, rows, places, w, out, dys=torch.zeros_like(gu))
+        dwe = B.bnn_expert_linear_f8_dw(*B.bnn_quant_columns_f8(dgu), *B.bnn_quant_columns_f8(x, rows=rows, k=k), offsets)
+        xs = B.bnn_expert_gather(x, rows, k, out=torch.zeros((rows.shape[0], D), dtype=BF16, device=DEV))
+        return [t.contiguous().view(torch.uint8) for t in (offsets, rows, places, gu, h, h8[0], dgu, y, out, dys, dw, dwe, xs)]
+
+    with_extension = step()
+
+    class None_:
+        def __getattr__(self, name):
+            return lambda *args: None
+
+    monkeypatch.setattr(B, "_t", lambda: None_())
+    for a, b in zip(with_extension, step()):
+        assert torch.equal(a, b)
+    monkeypatch.undo()
+    q, s = B.bnn_quant_blocks_f8(x)
+    offsets, rows, places = B.bnn_expert_sort(e, E)
+    for call in (lambda: B.bnn_linear_f8(q[:, :200], s, q, s), lambda: B.bnn_linear_f8(q, s[:, :1], q, s), lambda: B.bnn_linear_f8(q.clone(), s, q, s),
+                 lambda: B.bnn_linear_f8(q, s, q, s, out=torch.empty((3, 3), device=DEV)), lambda: B.bnn_expert_gather(x, rows[::2], k),
+                 lambda: B.bnn_expert_combine(x, places, w[:5]), lambda: B.bnn_expert_sort(e.t(), E), lambda: B.bnn_gated_act(x[:, :7]),
+                 lambda: B.bnn_gated_act(x, act="tanh"), lambda: B.bnn_expert_linear_f8(q, s, offsets[:-1].clone(), *B.bnn_quant_weight_f8(weight)[0])):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: B.bnn_quant_blocks_f8(x.double()), lambda: B.bnn_quant_blocks_f8(x.cpu()), lambda: B.bnn_linear_f8(x, s, q, s),
+                 lambda: B.bnn_expert_sort(e.float(), E), lambda: B.bnn_expert_combine(x.cpu(), places)):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: B.bnn_expert_sort(e, 1025), lambda: B.bnn_expert_sort(e, E, align=0), lambda: B.bnn_quant_blocks_f8(x, rows=rows, k=0)):
+        with pytest.raises(B.BnnError):
+            call()
