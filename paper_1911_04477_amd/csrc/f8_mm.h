@@ -207,8 +207,9 @@ struct F8Tile {
                        PART = ROWS * MM_STEP + (SCALED + 63) / 64 * 256, STAGE = KG * PART, TM = BM / WGM / 32, TN = BN / WGN / 32;
   static_assert(ROWS % (8 * WAVES) == 0 && BM % (8 * WAVES) == 0 && BM % (32 * WGM) == 0 && BN % (32 * WGN) == 0, "");
 };
-template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, bool EXACT>  // WIDE: fp32 scales of B
+template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, class E>  // WIDE: fp32 scales of B; E: the results' type
 __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *const whole_lds) {
+  constexpr bool EXACT = sizeof(E) == 4;
   using L = F8Tile<BM, BN, WGM, WGN, KG, STAGES, WIDE>;
   constexpr int WAVES = L::WAVES, LOADS = L::LOADS, STAGE = L::STAGE, TM = L::TM, TN = L::TN;
   constexpr bool IN_PLACE = TM * TN == 16;
@@ -229,27 +230,22 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *const
   for (int i = 0; i < LOADS; ++i) {
     if (!is_scale(i)) {
       const int row = (i * WAVES + wave) * 8 + (lane >> 3);
-      at[i] = i < L::LOADS_A ? (uint32_t)min(row, t.M - 1 - t.m0) * (uint32_t)p.lda + piece
-                             : (uint32_t)min(row - BM, t.N - 1 - t.n0) * (uint32_t)p.ldb + piece;
+      at[i] = i < L::LOADS_A ? __umul24(min(row, t.M - 1 - t.m0), (uint32_t)p.lda) + piece  // strides are below 2^22
+                             : __umul24(min(row - BM, t.N - 1 - t.n0), (uint32_t)p.ldb) + piece;
     } else {
       const int row = min(scale_row(i) + lane, L::SCALED - 1);
-      at[i] = row < BM ? (uint32_t)min(row, t.M - 1 - t.m0) * (uint32_t)p.sa_ld
-                       : (uint32_t)((min(t.n0 + row - BM, t.N - 1) >> p.sb_shift) - (t.n0 >> p.sb_shift)) * (uint32_t)p.sb_ld;
+      at[i] = row < BM ? __umul24(min(row, t.M - 1 - t.m0), (uint32_t)p.sa_ld)
+                       : __umul24((min(t.n0 + row - BM, t.N - 1) >> p.sb_shift) - (t.n0 >> p.sb_shift), (uint32_t)p.sb_ld);
     }
   }
-  static_assert(BM % 64 == 0 || WIDE || BM + BN <= 128, "a load of scales is of one operand, or lanes choose");
+  static_assert(BM % 64 == 0, "a load of scales is of one operand");
   const auto request_one = [&](int i, int step, char *lds) {
     using To = __attribute__((address_space(3))) void *;
     if (is_scale(i)) {
       const int row = scale_row(i), k = (t.first + step) & ~3;
       const To to = (To)(lds + L::ROWS * MM_STEP + row * 4);
-      if constexpr (BM % 64 == 0 || WIDE) {
-        if (row < BM) __builtin_amdgcn_raw_ptr_buffer_load_lds(resSA, to, 4, at[i], k, 0, 0);
-        else __builtin_amdgcn_raw_ptr_buffer_load_lds(resSB, to, 4, at[i], k, 0, 0);
-      } else {  // 32 rows of each operand
-        if (lane < BM - row) __builtin_amdgcn_raw_ptr_buffer_load_lds(resSA, to, 4, at[i], k, 0, 0);
-        else __builtin_amdgcn_raw_ptr_buffer_load_lds(resSB, to, 4, at[i], k, 0, 0);
-      }
+      if (row < BM) __builtin_amdgcn_raw_ptr_buffer_load_lds(resSA, to, 4, at[i], k, 0, 0);
+      else __builtin_amdgcn_raw_ptr_buffer_load_lds(resSB, to, 4, at[i], k, 0, 0);
     } else {
       const To to = (To)(lds + (i * WAVES + wave) * 8 * MM_STEP);
       if (i < L::LOADS_A) __builtin_amdgcn_raw_ptr_buffer_load_lds(resA, to, 16, at[i], step * MM_STEP, 0, 0);
@@ -505,54 +501,48 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *const
   // Results leave through LDS, 32 rows of a wave's columns at a time, so that a store covers whole lines of a row.
   if constexpr (KG == 1) mm_meet();
   else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // a wave's own part of what it has just read
-  const auto finish = [&](auto tag) {
-    using E = decltype(tag);
-    constexpr int SIZE = sizeof(E), PITCH = TN * 32 * SIZE + 16, PIECES = TN * 32 * SIZE / 16, PER = 16 / SIZE;
-    static_assert(WAVES * 32 * PITCH <= STAGES * STAGE && (KG == 1 || 32 * PITCH <= (KG - 1) * TM * TN * 16 * 64 * 4), "");
-    char *const mine = KG == 1 ? lds + wave * 32 * PITCH : whole_lds + wave * (KG - 1) * (TM * TN * 16 * 64 * 4);  // where only this wave reads
-    const int n0 = t.n0 + wn * (BN / WGN);
+  constexpr int SIZE = sizeof(E), PITCH = TN * 32 * SIZE + 16, PARTS = TN * 32 * SIZE / 16, PER = 16 / SIZE;
+  static_assert(WAVES * 32 * PITCH <= STAGES * STAGE && (KG == 1 || 32 * PITCH <= (KG - 1) * TM * TN * 16 * 64 * 4), "");
+  char *const mine = KG == 1 ? lds + wave * 32 * PITCH : whole_lds + wave * (KG - 1) * (TM * TN * 16 * 64 * 4);  // where only this wave reads
+  const int n0 = t.n0 + wn * (BN / WGN);
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int m0 = t.m0 + wm * (BM / WGM) + i * 32;
+  for (int i = 0; i < TM; ++i) {
+    const int m0 = t.m0 + wm * (BM / WGM) + i * 32;
 #pragma unroll
-      for (int j = 0; j < TN; ++j)
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; q += 2) {
-          // A lane has column m = lane % 32 of a block and four times four consecutive n, those of the lane 32 above in between: these
-          // trade, so that a lane has eight consecutive ones.
-          const int n = j * 32 + q * 8 + (lane >> 5) * 8;
-          float v[8];
+      for (int q = 0; q < 4; q += 2) {
+        // A lane has column m = lane % 32 of a block and four times four consecutive n, those of the lane 32 above in between: these
+        // trade, so that a lane has eight consecutive ones.
+        const int n = j * 32 + q * 8 + (lane >> 5) * 8;
+        float v[8];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][q * 4 + r]), __float_as_uint(acc[i][j][q * 4 + 4 + r]), false, false);
-            v[r] = __uint_as_float(two[0]), v[4 + r] = __uint_as_float(two[1]);
-          }
-          store8(reinterpret_cast<E *>(mine + (lane & 31) * PITCH), n, TN * 32, v);
+        for (int r = 0; r < 4; ++r) {
+          const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][q * 4 + r]), __float_as_uint(acc[i][j][q * 4 + 4 + r]), false, false);
+          v[r] = __uint_as_float(two[0]), v[4 + r] = __uint_as_float(two[1]);
         }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-      for (int k = 0; k < PIECES / 2; ++k) {
-        const int at = k * 64 + lane, row = at / PIECES, n = n0 + at % PIECES * PER, m = m0 + row;
-        const char *from = mine + row * PITCH + at % PIECES * 16;
-        const u32x4 v = *reinterpret_cast<const u32x4 *>(from);
-        if (m >= t.M || n >= t.N) continue;
-        E *to = reinterpret_cast<E *>(t.y) + m * p.ldy + n;
-        if (n + PER <= t.N) *reinterpret_cast<u32x4_any *>(to) = v;
-        else
-          for (int r = 0; r < t.N - n; ++r) to[r] = reinterpret_cast<const E *>(from)[r];
+        store8(reinterpret_cast<E *>(mine + (lane & 31) * PITCH), n, TN * 32, v);
       }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < PARTS / 2; ++k) {
+      const int at = k * 64 + lane, row = at / PARTS, n = n0 + at % PARTS * PER, m = m0 + row;
+      const char *from = mine + row * PITCH + at % PARTS * 16;
+      const u32x4 v = *reinterpret_cast<const u32x4 *>(from);
+      if (m >= t.M || n >= t.N) continue;
+      E *to = reinterpret_cast<E *>(t.y) + m * p.ldy + n;
+      if (n + PER <= t.N) *reinterpret_cast<u32x4_any *>(to) = v;
+      else
+        for (int r = 0; r < t.N - n; ++r) to[r] = reinterpret_cast<const E *>(from)[r];
     }
-  };
-  if constexpr (EXACT) finish(0.0f);
-  else if (p.type == BNN_BF16) finish((__bf16)0.0f);
-  else finish((_Float16)0.0f);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
 }
 
-template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, bool EXACT>
+template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, class E>
 __global__ __launch_bounds__(64 * WGM *WGN *KG, WGM *WGN *KG < 4 ? 1 : WGM *WGN *KG / 4) void f8_tile_kernel(F8Operands p) {
   __shared__ __attribute__((aligned(16))) char lds[STAGES * F8Tile<BM, BN, WGM, WGN, KG, STAGES, WIDE>::STAGE];
-  f8_tile_product<BM, BN, WGM, WGN, KG, STAGES, WIDE, EXACT>(p, lds);
+  f8_tile_product<BM, BN, WGM, WGN, KG, STAGES, WIDE, E>(p, lds);
 }
 
 // At most 16 rows of A (of a group): nothing is reused, B is streamed once and bounds the kernel.  A wave owns 16 columns and deals with

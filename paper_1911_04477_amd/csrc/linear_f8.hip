@@ -56,7 +56,7 @@ inline int f8_form(int64_t rows, int64_t groups, bool same, int64_t N, int64_t b
   return best;
 }
 
-template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, bool EXACT>
+template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, class E>
 bnn_status launch_f8_tile(F8Operands p, hipStream_t s) {
   p.tilesN = (p.N - 1) / BN + 1;
   // groups of rows: each has a part of a tile more than its rows fill at most
@@ -66,7 +66,7 @@ bnn_status launch_f8_tile(F8Operands p, hipStream_t s) {
   ProfScope ps(KID_LINEAR_F8, s);
   wide_launches(tiles, [&](int64_t first, uint32_t n) {
     p.first = first;
-    f8_tile_kernel<BM, BN, WGM, WGN, KG, STAGES, WIDE, EXACT><<<n, 64 * WGM * WGN * KG, 0, s>>>(p);
+    f8_tile_kernel<BM, BN, WGM, WGN, KG, STAGES, WIDE, E><<<n, 64 * WGM * WGN * KG, 0, s>>>(p);
   });
   return launch_status();
 }
@@ -92,25 +92,25 @@ bnn_status launch_f8_few(const F8Operands &p, hipStream_t s) {
   return launch_f8_few_split<8, WIDE>(p, row_tiles, s);
 }
 
-template <bool WIDE, bool EXACT>
+template <bool WIDE, class E>
 bnn_status run_f8_as(const F8Operands &p, hipStream_t s) {
   const bool along_k = p.groups == F8_GROUP_K;
   const int64_t groups = p.groups == F8_PLAIN ? 1 : along_k ? p.E : std::min(p.E, p.M);
-  switch (f8_form(p.M, groups, along_k, p.N, along_k ? p.blocks / p.E + 1 : p.blocks, WIDE, EXACT, device_cu_count())) {
+  switch (f8_form(p.M, groups, along_k, p.N, along_k ? p.blocks / p.E + 1 : p.blocks, WIDE, sizeof(E) == 4, device_cu_count())) {
     case F8_256:
-      if constexpr (!WIDE) return launch_f8_tile<256, 256, 2, 2, 1, 2, false, EXACT>(p, s);
-    case F8_256_128: return launch_f8_tile<256, 128, 4, 2, 1, 3, WIDE, EXACT>(p, s);
-    case F8_128: return launch_f8_tile<128, 128, 2, 2, 1, 2, WIDE, EXACT>(p, s);
-    case F8_128_EIGHT: return launch_f8_tile<128, 128, 4, 2, 1, 4, WIDE, EXACT>(p, s);
-    case F8_128_64: return launch_f8_tile<128, 64, 2, 2, 2, 3, WIDE, EXACT>(p, s);
-    case F8_64: return launch_f8_tile<64, 64, 2, 2, 1, 4, WIDE, EXACT>(p, s);
-    case F8_64_32: return launch_f8_tile<64, 32, 2, 1, 4, 3, WIDE, EXACT>(p, s);
+      if constexpr (!WIDE) return launch_f8_tile<256, 256, 2, 2, 1, 2, false, E>(p, s);
+    case F8_256_128: return launch_f8_tile<256, 128, 4, 2, 1, 3, WIDE, E>(p, s);
+    case F8_128: return launch_f8_tile<128, 128, 2, 2, 1, 2, WIDE, E>(p, s);
+    case F8_128_EIGHT: return launch_f8_tile<128, 128, 4, 2, 1, 4, WIDE, E>(p, s);
+    case F8_128_64: return launch_f8_tile<128, 64, 2, 2, 2, 3, WIDE, E>(p, s);
+    case F8_64: return launch_f8_tile<64, 64, 2, 2, 1, 4, WIDE, E>(p, s);
+    case F8_64_32: return launch_f8_tile<64, 32, 2, 1, 4, 3, WIDE, E>(p, s);
     default: return launch_f8_few<WIDE>(p, s);
   }
 }
 template <bool WIDE>
 bnn_status run_f8(const F8Operands &p, hipStream_t s) {
-  return p.type == BNN_F32 ? run_f8_as<WIDE, true>(p, s) : run_f8_as<WIDE, false>(p, s);
+  return with_float(p.type, [&](auto tag) { return run_f8_as<WIDE, typename decltype(tag)::type>(p, s); });
 }
 
 // B's scales, checked: N rows of K values, of which `per` share a row of scales.
