@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256) void expert_gather_kernel(GatherParams p) {
   }
 #pragma unroll
   for (int i = 0; i < GATHER_PIECES; ++i)
-    if (start + i * 1024 < p.bytes) *reinterpret_cast<u32x4_any *>(y + at[i]) = v[i];
+    if (start + i * 1024 < p.bytes) __builtin_nontemporal_store(v[i], reinterpret_cast<u32x4_any *>(y + at[i]));
 }
 
 struct CombineParams {
@@ -201,19 +201,18 @@ struct CombineParams {
   int k, D;
 };
 
-// A wave takes 512 columns of a token; four experts' rows are requested at once.
-template <class E, int EDGE>
+// A wave takes 512 or 1024 columns of a token; four experts' rows are requested at once.
+template <class E, int EDGE, int NV>
 __global__ __launch_bounds__(256) void expert_combine_kernel(CombineParams p) {
   const int64_t id = wide_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t t = id / p.chunks;
   if (t >= p.T) return;
-  const int c = (int)(id - t * p.chunks) * 512 + (threadIdx.x & 63) * 8;
-  const Place8<EDGE> at(c, p.D);
+  const int c = (int)(id - t * p.chunks) * (512 * NV) + (threadIdx.x & 63) * 8;
   const int32_t *places = p.places + t * p.k;
   const float *weights = p.weights ? p.weights + t * p.k : nullptr;
-  float sum[8] = {};
+  float sum[NV][8] = {};
   for (int j0 = 0; j0 < p.k; j0 += 4) {
-    Piece8<E> v[4];
+    Piece8<E> v[4][NV];
     float w[4];
     bool has[4];
 #pragma unroll
@@ -221,17 +220,25 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(CombineParams p) {
       const int jj = min(j0 + j, p.k - 1), pos = places[jj];
       has[j] = j0 + j < p.k && pos >= 0 && pos < p.S;
       w[j] = weights ? weights[jj] : 1.0f;
-      if (has[j]) v[j].load(static_cast<const E *>(p.ys) + pos * p.ys_ld, at, p.D);
+      if (has[j])
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[j][i].load(static_cast<const E *>(p.ys) + pos * p.ys_ld, Place8<EDGE>(c + i * 512, p.D), p.D);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (!has[j]) continue;
-      if (at.shift) v[j].settle(at);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] = fmaf(w[j], (float)v[j].v[i], sum[i]);
+      for (int i = 0; i < NV; ++i) {
+        const Place8<EDGE> at(c + i * 512, p.D);
+        if (at.shift) v[j][i].settle(at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[i][e] = fmaf(w[j], (float)v[j][i].v[e], sum[i][e]);
+      }
     }
   }
-  if (c < p.D) store8(static_cast<E *>(p.out) + t * p.out_ld, c, p.D, sum);
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (c + i * 512 < p.D) store8(static_cast<E *>(p.out) + t * p.out_ld, c + i * 512, p.D, sum[i]);
 }
 
 struct CombineBackwardParams {
@@ -392,16 +399,17 @@ extern "C" bnn_status bnn_expert_combine(const void *ys, int type, int64_t S, in
   if (T == 0) return BNN_OK;
   if ((S > 0 && !ys) || !places || !out) return BNN_ERR_NULL;
   if (!aligned16(ys) || !aligned16(places) || !aligned16(weights) || !aligned16(out)) return BNN_ERR_ALIGN;
-  const CombineParams p = {ys, out, ys_ld, out_ld, places, weights, T, S, (D - 1) / 512 + 1, (int)k, (int)D};
+  const int pieces = D > 512 && T * ((D - 1) / 512 + 1) > 16384 ? 2 : 1;  // more of them only where there are waves enough
+  const CombineParams p = {ys, out, ys_ld, out_ld, places, weights, T, S, (D - 1) / (512 * pieces) + 1, (int)k, (int)D};
   hipStream_t s = static_cast<hipStream_t>(stream);
   ProfScope ps(KID_EXPERT_COMBINE, s);
   with_float(type, [&](auto tag) {
     using E = typename decltype(tag)::type;
     const dim3 grid = wide_grid((T * p.chunks - 1) / 4 + 1);
     switch (row_edge(D)) {
-      case EDGE_WHOLE: expert_combine_kernel<E, EDGE_WHOLE><<<grid, 256, 0, s>>>(p); break;
-      case EDGE_RAGGED: expert_combine_kernel<E, EDGE_RAGGED><<<grid, 256, 0, s>>>(p); break;
-      default: expert_combine_kernel<E, EDGE_SMALL><<<grid, 256, 0, s>>>(p);
+      case EDGE_WHOLE: (pieces == 2 ? expert_combine_kernel<E, EDGE_WHOLE, 2> : expert_combine_kernel<E, EDGE_WHOLE, 1>)<<<grid, 256, 0, s>>>(p); break;
+      case EDGE_RAGGED: (pieces == 2 ? expert_combine_kernel<E, EDGE_RAGGED, 2> : expert_combine_kernel<E, EDGE_RAGGED, 1>)<<<grid, 256, 0, s>>>(p); break;
+      default: expert_combine_kernel<E, EDGE_SMALL, 1><<<grid, 256, 0, s>>>(p);
     }
   });
   return launch_status();
