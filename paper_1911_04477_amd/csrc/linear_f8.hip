@@ -11,15 +11,17 @@ namespace bnn {
 // Which kernel takes a product: that of few rows, or the tiles with the least time by what a round of them was measured to take, in us, with
 // k of b blocks: start + block * b.  one: a compute unit has one tile at a time; two: it has two, and rounds count in parts (there a unit
 // that is done takes the next tile, and rounds overlap).  Measured in bf16, scales powers of two (fp32 results in brackets), us:
-//   rows x columns x k     256x256    256x128    128x128    128x128, 8 waves    128x64    64x64    64x32
-//   64 x 4096 x 4096          40         28         25         20                 13        12       8.6
-//   256 x 4096 x 4096         46         29         27         21                 15        12      15.7
-//   512 x 4096 x 4096         46         29         27         22                 15        19      29.5
-//   1000 x 3001 x 2321        33         20       17.6 (24)    15 (24)            20 (25)   18 (25)  32
-//   2048 x 4096 x 4096        50 (81)    36 (61)    38 (63)    50 (80)            60        67
-//   8192 x 8192 x 2048       146        184        184        248                246       294
-//   8192 x 4096 x 512         35 (62)    35 (63)    33 (58)    44 (87)            39 (66)   60
-enum : int { F8_256, F8_256_128, F8_128, F8_128_EIGHT, F8_128_64, F8_64, F8_64_32, F8_FORM_COUNT, F8_FEW };
+//   rows x columns x k     256x256    256x128    128x128    the same, short k    128x128, one    128x64    64x64    64x32
+//   64 x 4096 x 4096          40         28         25                             20              13        12       8.6
+//   256 x 4096 x 4096         46         29         27                             21              15        12      15.7
+//   512 x 4096 x 4096         46         29         27                             22              15        19      29.5
+//   1000 x 3001 x 2321        33         20       17.6 (31)     17.3 (26.5)        15 (24)         20 (25)   18 (25)  32
+//   2048 x 4096 x 4096        50 (81)    36 (61)    38 (63)       41 (85)          50 (80)         60        67
+//   8192 x 8192 x 2048       146        178        186 (267)     188 (277)        243             246       287
+//   8192 x 4096 x 512         38 (65)    35 (67)    33 (63)       29 (58)          42 (85)         39 (66)   59
+// 128 x 128 tiles come in three: two a unit of four waves each, two a unit of eight waves, whose starts and ends hide each other's better (short
+// k), and one a unit with four steps in LDS.
+enum : int { F8_256, F8_256_128, F8_128, F8_128_SHORT, F8_128_ONE, F8_128_64, F8_64, F8_64_32, F8_FORM_COUNT, F8_FEW };
 struct F8Cost {
   float start, block, start2, block2;  // of one tile a unit, of two (0: one at a time)
 };
@@ -31,7 +33,8 @@ constexpr F8Cost F8_NEVER = {1e9f, 0.0f, 0.0f, 0.0f};
 constexpr F8Form F8_FORMS[F8_FORM_COUNT] = {
     {256, 256, {12, 1.5f, 0, 0}, {18, 3.0f, 0, 0}, F8_NEVER, F8_NEVER},
     {256, 128, {5, 1.0f, 0, 0}, {8, 1.65f, 0, 0}, {6, 1.28f, 0, 0}, {9, 2.1f, 0, 0}},
-    {128, 128, {3.5f, 0.73f, 4.5f, 1.07f}, {6, 0.95f, 8, 1.7f}, {3.5f, 0.85f, 4.5f, 2.2f}, {6, 1.25f, 8, 2.1f}},
+    {128, 128, {3.5f, 0.73f, 4.5f, 1.07f}, {6, 0.95f, 8, 1.7f}, {3.5f, 0.85f, 4.5f, 1.65f}, {6, 1.4f, 11, 3.0f}},
+    {128, 128, {3.5f, 0.73f, 1.8f, 1.3f}, {5.5f, 1.1f, 8.2f, 1.55f}, {3.5f, 0.8f, 3.5f, 1.8f}, {5, 1.05f, 10.5f, 2.2f}},
     {128, 128, {3.5f, 0.58f, 0, 0}, {5, 1.0f, 0, 0}, {3.5f, 0.8f, 0, 0}, {5, 1.05f, 0, 0}},
     {128, 64, {3, 0.37f, 0, 0}, {4, 0.6f, 0, 0}, {3.5f, 0.5f, 0, 0}, {4, 0.8f, 0, 0}},
     {64, 64, {2.5f, 0.3f, 2.5f, 0.5f}, {3, 0.4f, 3, 0.65f}, {2.5f, 0.4f, 2.5f, 0.6f}, {3, 0.5f, 3, 0.8f}},
@@ -101,7 +104,8 @@ bnn_status run_f8_as(const F8Operands &p, hipStream_t s) {
       if constexpr (!WIDE) return launch_f8_tile<256, 256, 2, 2, 1, 2, false, E>(p, s);
     case F8_256_128: return launch_f8_tile<256, 128, 4, 2, 1, 3, WIDE, E>(p, s);
     case F8_128: return launch_f8_tile<128, 128, 2, 2, 1, 2, WIDE, E>(p, s);
-    case F8_128_EIGHT: return launch_f8_tile<128, 128, 4, 2, 1, 4, WIDE, E>(p, s);
+    case F8_128_SHORT: return launch_f8_tile<128, 128, 2, 4, 1, 2, WIDE, E>(p, s);
+    case F8_128_ONE: return launch_f8_tile<128, 128, 4, 2, 1, 4, WIDE, E>(p, s);
     case F8_128_64: return launch_f8_tile<128, 64, 2, 2, 2, 3, WIDE, E>(p, s);
     case F8_64: return launch_f8_tile<64, 64, 2, 2, 1, 4, WIDE, E>(p, s);
     case F8_64_32: return launch_f8_tile<64, 32, 2, 1, 4, 3, WIDE, E>(p, s);
