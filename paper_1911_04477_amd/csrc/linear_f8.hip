@@ -29,14 +29,14 @@ struct F8Form {
   int bm, bn;
   F8Cost bits16, f32, bits16_wide, f32_wide;
 };
-constexpr F8Cost F8_NEVER = {1e9f, 0.0f, 0.0f, 0.0f};
+constexpr F8Cost F8_NEVER = {1e9f, 0.0f, 0.0f, 0.0f};  // another is always faster
 constexpr F8Form F8_FORMS[F8_FORM_COUNT] = {
     {256, 256, {12, 1.5f, 0, 0}, {18, 3.0f, 0, 0}, F8_NEVER, F8_NEVER},
     {256, 128, {5, 1.0f, 0, 0}, {8, 1.65f, 0, 0}, {6, 1.28f, 0, 0}, {9, 2.1f, 0, 0}},
-    {128, 128, {3.5f, 0.73f, 4.5f, 1.07f}, {6, 0.95f, 8, 1.7f}, {3.5f, 0.85f, 4.5f, 1.65f}, {6, 1.4f, 11, 3.0f}},
+    {128, 128, {3.5f, 0.73f, 4.5f, 1.07f}, {6, 0.95f, 8, 1.7f}, {3.5f, 0.85f, 4.5f, 1.65f}, F8_NEVER},
     {128, 128, {3.5f, 0.73f, 1.8f, 1.3f}, {5.5f, 1.1f, 8.2f, 1.55f}, {3.5f, 0.8f, 3.5f, 1.8f}, {5, 1.05f, 10.5f, 2.2f}},
-    {128, 128, {3.5f, 0.58f, 0, 0}, {5, 1.0f, 0, 0}, {3.5f, 0.8f, 0, 0}, {5, 1.05f, 0, 0}},
-    {128, 64, {3, 0.37f, 0, 0}, {4, 0.6f, 0, 0}, {3.5f, 0.5f, 0, 0}, {4, 0.8f, 0, 0}},
+    {128, 128, {3.5f, 0.58f, 0, 0}, {5, 1.0f, 0, 0}, F8_NEVER, F8_NEVER},
+    {128, 64, {3, 0.37f, 0, 0}, {4, 0.6f, 0, 0}, {3.5f, 0.5f, 0, 0}, F8_NEVER},
     {64, 64, {2.5f, 0.3f, 2.5f, 0.5f}, {3, 0.4f, 3, 0.65f}, {2.5f, 0.4f, 2.5f, 0.6f}, {3, 0.5f, 3, 0.8f}},
     {64, 32, {2.2f, 0.2f, 0, 0}, {2.5f, 0.25f, 0, 0}, {2.5f, 0.25f, 0, 0}, {2.5f, 0.3f, 0, 0}}};
 // rows: of all groups, or where these are along k (`same`) of each; blocks: of k a group.
@@ -102,15 +102,23 @@ bnn_status run_f8_as(const F8Operands &p, hipStream_t s) {
   switch (f8_form(p.M, groups, along_k, p.N, along_k ? p.blocks / p.E + 1 : p.blocks, WIDE, sizeof(E) == 4, device_cu_count())) {
     case F8_256:
       if constexpr (!WIDE) return launch_f8_tile<256, 256, 2, 2, 1, 2, false, E>(p, s);
+      break;
     case F8_256_128: return launch_f8_tile<256, 128, 4, 2, 1, 3, WIDE, E>(p, s);
-    case F8_128: return launch_f8_tile<128, 128, 2, 2, 1, 2, WIDE, E>(p, s);
+    case F8_128:
+      if constexpr (!WIDE || sizeof(E) == 2) return launch_f8_tile<128, 128, 2, 2, 1, 2, WIDE, E>(p, s);
+      break;
     case F8_128_SHORT: return launch_f8_tile<128, 128, 2, 4, 1, 2, WIDE, E>(p, s);
-    case F8_128_ONE: return launch_f8_tile<128, 128, 4, 2, 1, 4, WIDE, E>(p, s);
-    case F8_128_64: return launch_f8_tile<128, 64, 2, 2, 2, 3, WIDE, E>(p, s);
+    case F8_128_ONE:
+      if constexpr (!WIDE) return launch_f8_tile<128, 128, 4, 2, 1, 4, false, E>(p, s);
+      break;
+    case F8_128_64:
+      if constexpr (!WIDE || sizeof(E) == 2) return launch_f8_tile<128, 64, 2, 2, 2, 3, WIDE, E>(p, s);
+      break;
     case F8_64: return launch_f8_tile<64, 64, 2, 2, 1, 4, WIDE, E>(p, s);
     case F8_64_32: return launch_f8_tile<64, 32, 2, 1, 4, 3, WIDE, E>(p, s);
     default: return launch_f8_few<WIDE>(p, s);
   }
+  return BNN_ERR_UNSUPPORTED;  // not reached: these forms are never the fastest (F8_NEVER)
 }
 template <bool WIDE>
 bnn_status run_f8(const F8Operands &p, hipStream_t s) {
@@ -208,4 +216,10 @@ extern "C" bnn_status bnn_expert_linear_f8_dw(const uint8_t *a, int64_t lda, con
   p.M = (int)N, p.N = (int)K, p.blocks = (int)f8_blocks(S), p.y = dw, p.type = type, p.ldy = dw_ld;
   p.groups = F8_GROUP_K, p.offsets = offsets, p.E = (int)experts, p.y_es = dw_expert_ld;
   return run_f8<false>(p, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int bnn_testing_f8_form(int64_t rows, int64_t groups, int along_k, int64_t N, int64_t K, int scale_type, int type, int units) {
+  using namespace bnn;
+  if (rows <= 0 || groups <= 0 || N <= 0 || K <= 0 || !float_type(type) || units <= 0) return -1;
+  return f8_form(rows, groups, along_k != 0, N, f8_blocks(K), scale_type == BNN_SCALE_F32, type == BNN_F32, units);
 }

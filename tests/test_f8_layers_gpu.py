@@ -328,3 +328,87 @@ def test_offsets_out_of_range_stay_inside():
     dw = B.bnn_expert_linear_f8_dw(*R.stored(a.T.contiguous(), torch.zeros((K, 1), dtype=torch.int64)), *R.stored(a.T.contiguous(), torch.zeros((K, 1), dtype=torch.int64)),
                                    (offsets * 128).to(DEV))
     assert dw.shape == (E, K, K)
+
+
+# ---- every kernel form ------------------------------------------------------------------------------------------------
+from tests import f8_forms as F  # noqa: E402
+
+
+def whole_on_gpu(g, rows, K, scale_rows=None):
+    """Whole numbers with scales 1, 2 and 4 for rows, or for 128 of them, made on the GPU: (stored q, stored scales, values in fp32)."""
+    blocks = R.up(K, 128) // 128
+    q = torch.randint(-4, 5, (rows, K), generator=g, device=DEV).float()
+    p = torch.randint(0, 3, (scale_rows or rows, blocks), generator=g, device=DEV)
+    stored = B.rows_f8(rows, K, DEV)
+    torch.as_strided(stored.view(torch.uint8), (rows, stored.stride(0)), (stored.stride(0), 1)).zero_()
+    stored.copy_(q.to(B.F8))
+    s = B.scales_f8(scale_rows or rows, K, DEV)
+    s.view(torch.uint8).copy_((p + 127).to(torch.uint8))
+    each = p if scale_rows is None else p.repeat_interleave(128, 0)[:rows]
+    return stored, s, q * torch.pow(2.0, each.float()).repeat_interleave(128, 1)[:, :K]
+
+
+def gpu_gen(*key):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(sum((i + 1) * 7919 * int(k) for i, k in enumerate(key)) % (1 << 31))
+    return g
+
+
+def units():
+    return torch.cuda.get_device_properties(0).multi_processor_count
+
+
+@pytest.mark.parametrize("wide,bits16,form,size", F.cases(F.PLAIN), ids=str)
+def test_every_form_plain(wide, bits16, form, size):
+    print(f"form {form} wide {wide} bits16 {bits16} {size}", flush=True)
+    assert units() == 256  # the sizes are for this many
+    _, M, N, K = size
+    g = gpu_gen(M, N, K)
+    qa, sa, a = whole_on_gpu(g, M, K)
+    qb, sb, b = whole_on_gpu(g, N, K, None if not wide else R.up(N, 128) // 128)
+    if wide:
+        sb = sb.float().contiguous()
+    want = a @ b.T
+    bias = torch.randint(-9, 10, (N,), generator=g, device=DEV).float()
+    for dtype in ((BF16, F16) if bits16 else (F32,)):
+        room = torch.full((M, N + 1), -7.0, dtype=dtype, device=DEV)
+        assert torch.equal(B.bnn_linear_f8(qa, sa, qb, sb, bias, out=room[:, :N]), (want + bias).to(dtype))
+        assert (room[:, N:] == -7).all()
+
+
+@pytest.mark.parametrize("wide,bits16,form,size", F.cases(F.ROWS), ids=str)
+def test_every_form_of_rows_by_expert(wide, bits16, form, size):
+    print(f"form {form} wide {wide} bits16 {bits16} {size}", flush=True)
+    E, S, N, K = size
+    g = gpu_gen(E, S, N, K)
+    cuts = torch.randint(0, S - 4, (E - 1,), generator=g, device=DEV).sort().values.tolist()
+    bounds = [0, *cuts, S - 5]  # five rows behind the last expert's
+    offsets = torch.tensor(bounds, dtype=torch.int32, device=DEV)
+    qa, sa, a = whole_on_gpu(g, S, K)
+    qb, sb, b = whole_on_gpu(g, E * R.up(N, 128), K, None if not wide else E * R.up(N, 128) // 128)
+    qb = torch.as_strided(qb, (E, N, K), (R.up(N, 128) * qb.stride(0), qb.stride(0), 1))
+    b = b.reshape(E, -1, K)[:, :N]
+    sb = sb.float().contiguous().reshape(E, -1, sb.shape[1]) if wide else torch.as_strided(sb, (E, N, sb.shape[1]), (R.up(N, 128) * sb.stride(0), sb.stride(0), 1))
+    dtype = BF16 if bits16 else F32
+    want = torch.full((S, N), -7.0, dtype=dtype, device=DEV)
+    for e in range(E):
+        want[bounds[e]: bounds[e + 1]] = (a[bounds[e]: bounds[e + 1]] @ b[e].T).to(dtype)
+    got = B.bnn_expert_linear_f8(qa, sa, offsets, qb, sb, out=torch.full((S, N), -7.0, dtype=dtype, device=DEV))
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("wide,bits16,form,size", F.cases(F.ALONG_K), ids=str)
+def test_every_form_of_weight_gradients(wide, bits16, form, size):
+    print(f"form {form} bits16 {bits16} {size}", flush=True)
+    E, N, K, k = size
+    blocks = E * (k // 128) - 1  # of all groups: the rule has k for their mean, rounded up
+    g = gpu_gen(E, N, K, k)
+    cuts = torch.randint(0, blocks + 1, (E - 1,), generator=g, device=DEV).sort().values.tolist()
+    bounds = [0, *[128 * c for c in cuts], 128 * blocks]
+    S = 128 * blocks
+    qa, sa, a = whole_on_gpu(g, N, S)
+    qb, sb, b = whole_on_gpu(g, K, S)
+    dtype = BF16 if bits16 else F32
+    got = B.bnn_expert_linear_f8_dw(qa, sa, qb, sb, torch.tensor(bounds, dtype=torch.int32, device=DEV), dtype=dtype)
+    for e in range(E):
+        assert torch.equal(got[e], (a[:, bounds[e]: bounds[e + 1]] @ b[:, bounds[e]: bounds[e + 1]].T).to(dtype)), e
