@@ -419,8 +419,10 @@ BNN_API bnn_status bnn_gated_ff_backward(const void *x, int64_t x_ld, const void
  *
  * A matrix in this form, [rows, K]: rows of bnn_f8_row_bytes(K) bytes, whole blocks, zeros behind the K values, row strides `ld`
  *   multiples of 16 bytes; scales [rows, ceil(K / 128)] of one byte, p + 127 for 2^p (E8M0), rows of bnn_f8_scale_bytes(K) readable
- *   bytes, strides multiples of 4.  Operands of products: ld below 2^22.  All base pointers are on 16 bytes.
+ *   bytes, strides multiples of 4.  Operands of products: strides below 2^22.  Matrices start on 16 bytes, scales, indices and vectors
+ *   on their elements' size (at least 4).
  *   Values that are not numbers are NaN in e4m3 too, infinities become NaN; neither counts for a block's scale.
+ *   Products take scales from elsewhere with p from -100 to 119; the quantisers give these and, for values from 448 * 2^119 on, 120.
  */
 typedef enum { BNN_SCALE_E8M0 = 0, BNN_SCALE_F32 = 1 } bnn_scale_type;
 BNN_API int64_t bnn_f8_row_bytes(int64_t K);   /* K up to a multiple of 128; 0 for K <= 0 */

@@ -74,6 +74,7 @@ inline bnn_status launch_status() {
 }
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // Division of a 32-bit unsigned value by a runtime constant with one mulhi and one
 // shift (round-up method; exact for every n < 2^31 and 1 <= d < 2^31).

@@ -352,7 +352,7 @@ extern "C" bnn_status bnn_expert_sort(const void *experts, int index_bytes, int6
   if (S > INT32_MAX || expert_capacity(n, E, align) > INT32_MAX - 4096) return BNN_ERR_UNSUPPORTED;
   if (S < expert_capacity(n, E, align)) return BNN_ERR_SHAPE;
   if (!offsets || (S > 0 && !rows) || (n > 0 && (!experts || !places))) return BNN_ERR_NULL;
-  if (!aligned16(experts) || !aligned16(offsets) || !aligned16(rows) || !aligned16(places)) return BNN_ERR_ALIGN;
+  if ((reinterpret_cast<uintptr_t>(experts) & (index_bytes - 1)) || !aligned4(offsets) || !aligned4(rows) || !aligned4(places)) return BNN_ERR_ALIGN;
   SortParams p = {experts, index_bytes == 8, (int)n, (int)E, (int)align, (int)S, 1, (int)n, static_cast<int32_t *>(workspace), offsets, rows, places};
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int threads = n <= 64 ? 64 : n <= 256 ? 256 : E > 512 ? 512 : 1024;  // LDS: the waves' counts of all experts
@@ -379,7 +379,7 @@ extern "C" bnn_status bnn_expert_gather(const void *x, int type, int64_t T, int6
   if (S > INT32_MAX || D > (1 << 28) || k > (1 << 30) || (T > 0 && k > (1 << 30) / T)) return BNN_ERR_UNSUPPORTED;
   if (S == 0) return BNN_OK;
   if ((T > 0 && !x) || !rows || !xs) return BNN_ERR_NULL;
-  if (!aligned16(x) || !aligned16(rows) || !aligned16(xs)) return BNN_ERR_ALIGN;
+  if (!aligned16(x) || !aligned4(rows) || !aligned16(xs)) return BNN_ERR_ALIGN;
   const int size = float_size(type);
   GatherParams p = {static_cast<const char *>(x), static_cast<char *>(xs), x_ld * size, xs_ld * size, rows, FastDiv((uint32_t)k), T * k, S, 0,
                     (int)D * size, size};
@@ -398,7 +398,7 @@ extern "C" bnn_status bnn_expert_combine(const void *ys, int type, int64_t S, in
   if (S > INT32_MAX || D > (1 << 28) || k > (1 << 30) || (T > 0 && k > (1 << 30) / T)) return BNN_ERR_UNSUPPORTED;
   if (T == 0) return BNN_OK;
   if ((S > 0 && !ys) || !places || !out) return BNN_ERR_NULL;
-  if (!aligned16(ys) || !aligned16(places) || !aligned16(weights) || !aligned16(out)) return BNN_ERR_ALIGN;
+  if (!aligned16(ys) || !aligned4(places) || !aligned4(weights) || !aligned16(out)) return BNN_ERR_ALIGN;
   const int pieces = D > 512 && T * ((D - 1) / 512 + 1) > 16384 ? 2 : 1;  // more of them only where there are waves enough
   const CombineParams p = {ys, out, ys_ld, out_ld, places, weights, T, S, (D - 1) / (512 * pieces) + 1, (int)k, (int)D};
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -426,7 +426,7 @@ extern "C" bnn_status bnn_expert_combine_backward(const void *ys, int type, int6
   if (!dys && !dweights) return BNN_ERR_NULL;
   if (T == 0 && (S == 0 || !dys)) return BNN_OK;
   if ((T > 0 && (!places || !dout)) || (dys && S > 0 && !rows) || (dweights && S > 0 && !ys)) return BNN_ERR_NULL;
-  if (!aligned16(ys) || !aligned16(rows) || !aligned16(places) || !aligned16(weights) || !aligned16(dout) || !aligned16(dys) || !aligned16(dweights))
+  if (!aligned16(ys) || !aligned4(rows) || !aligned4(places) || !aligned4(weights) || !aligned16(dout) || !aligned16(dys) || !aligned4(dweights))
     return BNN_ERR_ALIGN;
   const CombineBackwardParams p = {ys, dout, dys, ys_ld, dout_ld, dys_ld, rows, places, weights, dweights, T, S, (int)k, (int)D};
   const int64_t clearing = dys ? (S + 63) / 64 : 0;

@@ -63,7 +63,7 @@ inline bnn_status f8_check(const void *q, int64_t ld, const void *scale, int64_t
   if (ld % 16 || scale_ld % 4) return BNN_ERR_STRIDE;
   if (products && (ld >= (1 << 22) || scale_ld >= (1 << 22))) return BNN_ERR_UNSUPPORTED;
   if (!q || !scale) return BNN_ERR_NULL;
-  if (!aligned16(q) || !aligned16(scale)) return BNN_ERR_ALIGN;
+  if (!aligned16(q) || !aligned4(scale)) return BNN_ERR_ALIGN;
   return BNN_OK;
 }
 

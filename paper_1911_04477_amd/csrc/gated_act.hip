@@ -96,8 +96,6 @@ bnn_status check_gated_act(const void *gu, int type, int64_t S, int64_t gu_ld, i
   return aligned16(gu) ? BNN_OK : BNN_ERR_ALIGN;
 }
 
-bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-
 }  // namespace bnn
 
 extern "C" bnn_status bnn_gated_act(const void *gu, int type, int64_t S, int64_t gu_ld, int64_t F, int act, const int32_t *live, void *h,

@@ -161,7 +161,7 @@ extern "C" bnn_status bnn_linear_f8(const uint8_t *a, int64_t lda, const uint8_t
   if (st == BNN_OK) st = f8_weight(p, b, ldb, b_scale, b_scale_type, b_scale_ld, b_scale_rows, N, K);
   if (st != BNN_OK) return st;
   if (!y) return BNN_ERR_NULL;
-  if (!aligned16(y) || !aligned16(bias)) return BNN_ERR_ALIGN;
+  if (!aligned16(y) || !aligned4(bias)) return BNN_ERR_ALIGN;
   p.A = reinterpret_cast<const char *>(a), p.lda = lda, p.sa = a_scale, p.sa_ld = a_scale_ld;
   p.M = (int)M, p.blocks = (int)f8_blocks(K), p.bias = bias, p.y = y, p.type = type, p.ldy = ldy;
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -186,7 +186,7 @@ extern "C" bnn_status bnn_expert_linear_f8(const uint8_t *a, int64_t lda, const 
   if (experts > 1 && (b_expert_ld / N < ldb || b_expert_ld % 16 || b_scale_expert_ld / scale_rows < b_scale_ld || (b_scale_type == BNN_SCALE_E8M0 && b_scale_expert_ld % 4)))
     return BNN_ERR_STRIDE;
   if (!offsets || !y) return BNN_ERR_NULL;
-  if (!aligned16(offsets) || !aligned16(y)) return BNN_ERR_ALIGN;
+  if (!aligned4(offsets) || !aligned16(y)) return BNN_ERR_ALIGN;
   p.A = reinterpret_cast<const char *>(a), p.lda = lda, p.sa = a_scale, p.sa_ld = a_scale_ld;
   p.M = (int)S, p.blocks = (int)f8_blocks(K), p.y = y, p.type = type, p.ldy = ldy;
   p.groups = F8_GROUP_ROWS, p.offsets = offsets, p.E = (int)experts, p.b_es = b_expert_ld;
@@ -211,7 +211,7 @@ extern "C" bnn_status bnn_expert_linear_f8_dw(const uint8_t *a, int64_t lda, con
     if (st != BNN_OK) return st;
   }
   if (!offsets || !dw) return BNN_ERR_NULL;
-  if (!aligned16(offsets) || !aligned16(dw)) return BNN_ERR_ALIGN;
+  if (!aligned4(offsets) || !aligned16(dw)) return BNN_ERR_ALIGN;
   p.A = reinterpret_cast<const char *>(a), p.lda = lda, p.sa = a_scale, p.sa_ld = a_scale_ld;
   p.M = (int)N, p.N = (int)K, p.blocks = (int)f8_blocks(S), p.y = dw, p.type = type, p.ldy = dw_ld;
   p.groups = F8_GROUP_K, p.offsets = offsets, p.E = (int)experts, p.y_es = dw_expert_ld;

@@ -221,7 +221,7 @@ extern "C" bnn_status bnn_quant_blocks_f8(const void *x, int type, int64_t T, in
   const bnn_status st = f8_check(q, q_ld, scale, scale_ld, K, false);
   if (st != BNN_OK) return st;
   if (!x && T > 0) return BNN_ERR_NULL;
-  if (!aligned16(x)) return BNN_ERR_ALIGN;
+  if (!aligned16(x) || !aligned4(rows)) return BNN_ERR_ALIGN;
   QuantBlocksParams p = {};
   p.src = f8_source(x, x_ld, T, rows, k, S);
   p.K = (int)K, p.blocks = (int)f8_blocks(K), p.by = FastDiv((uint32_t)p.blocks);
@@ -246,7 +246,7 @@ extern "C" bnn_status bnn_quant_columns_f8(const void *x, int type, int64_t T, i
   const bnn_status st = f8_check(q, q_ld, scale, scale_ld, S, false);
   if (st != BNN_OK) return st;
   if (!x && T > 0) return BNN_ERR_NULL;
-  if (!aligned16(x)) return BNN_ERR_ALIGN;
+  if (!aligned16(x) || !aligned4(rows)) return BNN_ERR_ALIGN;
   if (T == 0) return BNN_ERR_SHAPE;  // S positions of no rows
   QuantColumnsParams p = {};
   p.src = f8_source(x, x_ld, T, rows, k, S);

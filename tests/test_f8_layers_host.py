@@ -7,7 +7,7 @@ import torch
 from paper_1911_04477_amd import binding as B
 
 OK, NULL, SHAPE, STRIDE, ALIGN, WORKSPACE, HIP, UNSUPPORTED = range(8)
-A, MIS = 4096, 4100  # addresses that are never read
+A, MIS, ODD = 4096, 4100, 4098  # addresses that are never read
 F32, BF16, F16 = 0, 1, 2
 
 
@@ -35,8 +35,9 @@ def test_quant_refusals(L, name):
     assert f(x_ld=7) == f(q_ld=127) == f(q_ld=136) == f(s_ld=3) == f(s_ld=6) == STRIDE
     assert f(K=2 ** 28 + 1, x_ld=2 ** 30) == f(rows=A, T=2 ** 20, k=2 ** 20) == f(rows=A, S=2 ** 31) == UNSUPPORTED
     assert f(T=0, S=0, x=None, q=None, s=None) == OK
-    for arg in ("x", "q", "s"):
-        assert f(**{arg: None}) == NULL and f(**{arg: MIS}) == ALIGN
+    for arg, bad in (("x", MIS), ("q", MIS), ("s", ODD)):
+        assert f(**{arg: None}) == NULL and f(**{arg: bad}) == ALIGN
+    assert f(rows=ODD) == ALIGN
     if columns:
         assert f(rows=A, S=2 ** 22, q_ld=2 ** 22) == UNSUPPORTED
         assert f(rows=A, T=0, S=4) == SHAPE
@@ -55,7 +56,7 @@ def test_quant_weight_refusals(L):
     assert f(turned=weight(expert_ld=1023)) == f(out=weight(scale_ld=2)) == f(out=weight(scale_expert_ld=2)) == STRIDE
     assert f(E=65536) == f(N=2 ** 22 + 1) == f(K=2 ** 22 + 1, ld=2 ** 23) == UNSUPPORTED
     assert f(w=None) == f(out=None, turned=None) == f(out=weight(q=None)) == f(turned=weight(scale=None, expert_ld=1024)) == NULL
-    assert f(w=MIS) == f(out=weight(q=MIS)) == f(out=weight(scale=MIS)) == ALIGN
+    assert f(w=MIS) == f(out=weight(q=MIS)) == f(out=weight(scale=ODD)) == ALIGN
     assert f(E=0) == OK
 
 
@@ -66,9 +67,9 @@ def test_linear_refusals(L):
     assert f(M=-1) == f(N=-1) == f(K=0) == f(type=3) == f(kind=2) == f(per=2) == f(kind=1, per=1) == SHAPE
     assert f(lda=255) == f(lda=264) == f(ldb=128) == f(sa_ld=3) == f(sa_ld=5) == f(sb_ld=2) == f(ldy=4) == f(kind=1, per=128, sb_ld=1) == STRIDE
     assert f(M=2 ** 31 - 256) == f(N=2 ** 31 - 256, ldy=2 ** 31) == f(K=2 ** 22 + 1) == f(lda=2 ** 22) == UNSUPPORTED
-    for arg in ("a", "sa", "b", "sb", "y"):
-        assert f(**{arg: None}) == NULL and f(**{arg: MIS}) == ALIGN
-    assert f(bias=MIS) == ALIGN
+    for arg, bad in (("a", MIS), ("sa", ODD), ("b", MIS), ("sb", ODD), ("y", MIS)):
+        assert f(**{arg: None}) == NULL and f(**{arg: bad}) == ALIGN
+    assert f(bias=ODD) == ALIGN
     assert f(M=0, a=None, y=None) == f(N=0, b=None, y=None) == OK
 
 
@@ -80,8 +81,8 @@ def test_expert_linear_refusals(L):
     assert f(S=-1) == f(N=-1) == f(K=0) == f(E=-1) == f(type=-1) == f(kind=3) == f(per=64) == SHAPE
     assert f(es=1279) == f(es=1288) == f(sb_es=19) == f(sb_es=22) == f(lda=0) == f(ldy=4) == f(kind=1, per=128, sb_es=3) == STRIDE
     assert f(E=65536) == f(S=2 ** 31) == f(ldb=2 ** 22, es=5 * 2 ** 22) == UNSUPPORTED
-    for arg in ("a", "sa", "off", "b", "sb", "y"):
-        assert f(**{arg: None}) == NULL and f(**{arg: MIS}) == ALIGN
+    for arg, bad in (("a", MIS), ("sa", ODD), ("off", ODD), ("b", MIS), ("sb", ODD), ("y", MIS)):
+        assert f(**{arg: None}) == NULL and f(**{arg: bad}) == ALIGN
     assert f(S=0, a=None) == f(E=0, b=None) == f(N=0, y=None) == OK
 
     def g(a=A, lda=256, sa=A, sa_ld=4, b=A, ldb=256, sb=A, sb_ld=4, off=A, E=3, N=5, K=6, S=200, dw=A, type=F32, ld=6, es=30):
@@ -90,8 +91,8 @@ def test_expert_linear_refusals(L):
     assert g(S=-1) == g(N=-1) == g(K=-1) == g(E=-1) == g(type=3) == SHAPE
     assert g(ld=5) == g(es=29) == g(lda=128) == g(sb_ld=1) == STRIDE
     assert g(S=2 ** 22) == g(E=65536) == UNSUPPORTED
-    for arg in ("a", "sa", "b", "sb", "off", "dw"):
-        assert g(**{arg: None}) == NULL and g(**{arg: MIS}) == ALIGN
+    for arg, bad in (("a", MIS), ("sa", ODD), ("b", MIS), ("sb", ODD), ("off", ODD), ("dw", MIS)):
+        assert g(**{arg: None}) == NULL and g(**{arg: bad}) == ALIGN
     assert g(E=0, dw=None) == g(N=0, dw=None) == g(K=0, dw=None) == OK
 
 
@@ -102,7 +103,7 @@ def test_sort_refusals(L):
     assert f(T=-1) == f(k=0) == f(E=0) == f(align=0) == f(S=-1) == f(size=2) == f(S=19) == f(align=128, S=383) == SHAPE
     assert f(E=1025) == f(align=4097) == f(T=2 ** 20, k=2 ** 11) == f(S=2 ** 31) == UNSUPPORTED
     assert f(e=None) == f(off=None) == f(rows=None) == f(places=None) == NULL
-    assert f(e=MIS) == f(off=MIS) == f(rows=MIS) == f(places=MIS) == ALIGN
+    assert f(e=ODD) == f(e=MIS, size=8) == f(off=ODD) == f(rows=ODD) == f(places=ODD) == ALIGN
     need = L.bnn_expert_sort_workspace_bytes(2000, 2, 4)
     assert f(T=2000, S=4000, ws=A, nbytes=need - 1) == WORKSPACE
     assert f(T=2000, S=4000, ws=None, nbytes=need) == NULL and f(T=2000, S=4000, ws=MIS, nbytes=need) == ALIGN
@@ -115,7 +116,7 @@ def test_gather_and_combine_refusals(L):
     assert g(T=-1) == g(S=-1) == g(D=0) == g(k=0) == g(type=3) == SHAPE
     assert g(ld=7) == g(xs_ld=7) == STRIDE
     assert g(D=2 ** 28 + 1, ld=2 ** 29, xs_ld=2 ** 29) == g(T=2 ** 20, k=2 ** 11) == UNSUPPORTED
-    assert g(x=None) == g(rows=None) == g(xs=None) == NULL and g(x=MIS) == g(rows=MIS) == g(xs=MIS) == ALIGN
+    assert g(x=None) == g(rows=None) == g(xs=None) == NULL and g(x=MIS) == g(rows=ODD) == g(xs=MIS) == ALIGN
     assert g(S=0, x=None, rows=None, xs=None) == OK
 
     def c(ys=A, type=BF16, S=8, ld=8, places=A, w=None, T=4, k=2, D=8, out=A, out_ld=8):
@@ -123,7 +124,7 @@ def test_gather_and_combine_refusals(L):
 
     assert c(T=-1) == c(S=-1) == c(D=0) == c(k=0) == c(type=3) == SHAPE
     assert c(ld=7) == c(out_ld=7) == STRIDE
-    assert c(ys=None) == c(places=None) == c(out=None) == NULL and c(ys=MIS) == c(places=MIS) == c(w=MIS) == c(out=MIS) == ALIGN
+    assert c(ys=None) == c(places=None) == c(out=None) == NULL and c(ys=MIS) == c(places=ODD) == c(w=ODD) == c(out=MIS) == ALIGN
     assert c(T=0, ys=None, places=None, out=None) == OK
 
     def b(ys=A, type=BF16, S=8, ld=8, rows=A, places=A, w=None, dout=A, dout_ld=8, T=4, k=2, D=8, dys=A, dys_ld=8, dw=A):
@@ -133,8 +134,8 @@ def test_gather_and_combine_refusals(L):
     assert b(ld=7) == b(dout_ld=7) == b(dys_ld=7) == STRIDE
     assert b(D=32769, ld=32769, dout_ld=32769, dys_ld=32769) == UNSUPPORTED
     assert b(ys=None) == b(rows=None) == b(places=None) == b(dout=None) == b(dys=None, dw=None) == NULL
-    for arg in ("ys", "rows", "places", "w", "dout", "dys", "dw"):
-        assert b(**{arg: MIS}) == ALIGN
+    for arg, bad in (("ys", MIS), ("rows", ODD), ("places", ODD), ("w", ODD), ("dout", MIS), ("dys", MIS), ("dw", ODD)):
+        assert b(**{arg: bad}) == ALIGN
     assert b(T=0, S=0) == OK
 
 
