@@ -7,7 +7,7 @@
 
 namespace bnn {
 
-constexpr int SORT_EXPERTS = 1024, SORT_MOST_BLOCKS = 256, SORT_ONE = 2048;
+constexpr int SORT_EXPERTS = 1024, SORT_MOST_BLOCKS = 256, SORT_ONE = 4096;
 
 struct SortParams {
   const void *experts;

@@ -531,8 +531,10 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *const
       const u32x4 v = *reinterpret_cast<const u32x4 *>(from);
       if (m >= t.M || n >= t.N) continue;
       E *to = reinterpret_cast<E *>(t.y) + m * p.ldy + n;
-      if (n + PER <= t.N) *reinterpret_cast<u32x4_any *>(to) = v;
-      else
+      if (n + PER <= t.N) {  // results of large tiles past the caches (8192 x 4096 to 4096 122 -> 119 us)
+        if constexpr (BM * BN >= 128 * 128) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any *>(to));
+        else *reinterpret_cast<u32x4_any *>(to) = v;
+      } else
         for (int r = 0; r < t.N - n; ++r) to[r] = reinterpret_cast<const E *>(from)[r];
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");

@@ -42,7 +42,7 @@ def choices(g, T, k, E, drop=0.1, skew=True):
 
 
 @pytest.mark.parametrize("T,k,E,align", [(0, 1, 1, 1), (1, 1, 1, 1), (1, 8, 64, 1), (7, 3, 5, 4), (64, 1, 2, 128), (65, 4, 3, 1), (200, 2, 1024, 1), (700, 3, 17, 128),
-                                         (1024, 2, 600, 16), (1025, 2, 8, 1), (5000, 4, 100, 128), (40000, 8, 64, 128), (3000, 1, 1024, 3), (262145, 1, 9, 1)])
+                                         (1024, 2, 600, 16), (2048, 2, 8, 1), (2049, 2, 8, 1), (5000, 4, 100, 128), (40000, 8, 64, 128), (3000, 1, 1024, 3), (262145, 1, 9, 1)])
 @pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
 def test_sort(T, k, E, align, dtype):
     print(f"sort {T} x {k} of {E} align {align} {dtype}", flush=True)

@@ -21,7 +21,8 @@ def test_sizes(L):
     assert [L.bnn_f8_scale_bytes(k) for k in (-1, 0, 1, 512, 513)] == [0, 0, 4, 4, 8]
     assert L.bnn_expert_rows(10, 2, 4, 1) == 20 and L.bnn_expert_rows(10, 2, 4, 128) == (20 + 4 * 127) // 128 * 128
     assert L.bnn_expert_rows(1, 2, 64, 8) == 16 and L.bnn_expert_rows(0, 2, 4, 8) == 0
-    assert L.bnn_expert_sort_workspace_bytes(4, 2, 64) == 0 and L.bnn_expert_sort_workspace_bytes(3000, 2, 64) == 256 * 64 * 4
+    assert L.bnn_expert_sort_workspace_bytes(4, 2, 64) == 0 and L.bnn_expert_sort_workspace_bytes(2048, 2, 64) == 0
+    assert L.bnn_expert_sort_workspace_bytes(2049, 2, 64) == 256 * 64 * 4
 
 
 @pytest.mark.parametrize("name", ["bnn_quant_blocks_f8", "bnn_quant_columns_f8"])
@@ -104,9 +105,9 @@ def test_sort_refusals(L):
     assert f(E=1025) == f(align=4097) == f(T=2 ** 20, k=2 ** 11) == f(S=2 ** 31) == UNSUPPORTED
     assert f(e=None) == f(off=None) == f(rows=None) == f(places=None) == NULL
     assert f(e=ODD) == f(e=MIS, size=8) == f(off=ODD) == f(rows=ODD) == f(places=ODD) == ALIGN
-    need = L.bnn_expert_sort_workspace_bytes(2000, 2, 4)
-    assert f(T=2000, S=4000, ws=A, nbytes=need - 1) == WORKSPACE
-    assert f(T=2000, S=4000, ws=None, nbytes=need) == NULL and f(T=2000, S=4000, ws=MIS, nbytes=need) == ALIGN
+    need = L.bnn_expert_sort_workspace_bytes(3000, 2, 4)
+    assert f(T=3000, S=6000, ws=A, nbytes=need - 1) == WORKSPACE
+    assert f(T=3000, S=6000, ws=None, nbytes=need) == NULL and f(T=3000, S=6000, ws=MIS, nbytes=need) == ALIGN
 
 
 def test_gather_and_combine_refusals(L):
