@@ -201,7 +201,7 @@ struct CombineParams {
   int k, D;
 };
 
-// A wave takes 512 or 1024 columns of a token; four experts' rows are requested at once.
+// A wave takes 512 columns of a token, eight experts' rows requested at once, or 1024 and four.
 template <class E, int EDGE, int NV>
 __global__ __launch_bounds__(256) void expert_combine_kernel(CombineParams p) {
   const int64_t id = wide_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -211,12 +211,13 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(CombineParams p) {
   const int32_t *places = p.places + t * p.k;
   const float *weights = p.weights ? p.weights + t * p.k : nullptr;
   float sum[NV][8] = {};
-  for (int j0 = 0; j0 < p.k; j0 += 4) {
-    Piece8<E> v[4][NV];
-    float w[4];
-    bool has[4];
+  constexpr int ROWS = NV == 1 ? 8 : 4;
+  for (int j0 = 0; j0 < p.k; j0 += ROWS) {
+    Piece8<E> v[ROWS][NV];
+    float w[ROWS];
+    bool has[ROWS];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < ROWS; ++j) {
       const int jj = min(j0 + j, p.k - 1), pos = places[jj];
       has[j] = j0 + j < p.k && pos >= 0 && pos < p.S;
       w[j] = weights ? weights[jj] : 1.0f;
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(CombineParams p) {
         for (int i = 0; i < NV; ++i) v[j][i].load(static_cast<const E *>(p.ys) + pos * p.ys_ld, Place8<EDGE>(c + i * 512, p.D), p.D);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < ROWS; ++j) {
       if (!has[j]) continue;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
