@@ -196,7 +196,8 @@ __device__ __forceinline__ void f8_interleave() {
   }
 }
 
-// LDS: a step's rows of 128 bytes as in tile_mm.h (16-byte piece c of row r in slot c ^ (r % 8)), behind them for each row the
+// LDS: a step's rows of 128 bytes, 16-byte piece c of row r in slot c ^ (r / 2 % 8), so that the 16 rows of a clock spread over
+// all 64 banks (with r % 8 a read takes twice as long); behind them for each row the
 // four bytes of scales that hold the step's.  WGM x WGN waves of 32 x 32 blocks; KG such groups of waves take the blocks of k in turn, KG
 // of them a step, and their sums meet in the end: small tiles, one a compute unit, are bound by what a step does one after the other
 // (64 x 4096 by 4096 on 64 x 32 tiles 9.9 us with one group, 8.6 with four).
@@ -218,7 +219,7 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *const
   const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = id / WAVES, wave = id % WAVES;
   const int wm = wave / WGN, wn = wave % WGN;
   char *const lds = whole_lds + group * L::PART;
-  const int piece = ((lane & 7) ^ (lane >> 3)) * 16;  // of the 128 bytes of a step, that this lane's loads bring
+  const auto piece = [&](int load) { return ((lane & 7) ^ (lane >> 4) ^ (load & 1) * 4) * 16; };  // of a step's 128 bytes, that this lane brings
   const auto resA = __builtin_amdgcn_make_buffer_rsrc((void *)(t.A + (int64_t)t.m0 * p.lda), 0, 0xffffffffu, 0x00020000);
   const auto resB = __builtin_amdgcn_make_buffer_rsrc((void *)(t.B + (int64_t)t.n0 * p.ldb), 0, 0xffffffffu, 0x00020000);
   const auto resSA = __builtin_amdgcn_make_buffer_rsrc((void *)(t.sa + (int64_t)t.m0 * p.sa_ld), 0, 0xffffffffu, 0x00020000);
@@ -229,9 +230,9 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *const
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) {
     if (!is_scale(i)) {
-      const int row = (i * WAVES + wave) * 8 + (lane >> 3);
-      at[i] = i < L::LOADS_A ? __umul24(min(row, t.M - 1 - t.m0), (uint32_t)p.lda) + piece  // strides are below 2^22
-                             : __umul24(min(row - BM, t.N - 1 - t.n0), (uint32_t)p.ldb) + piece;
+      const int load = i * WAVES + wave, row = load * 8 + (lane >> 3);
+      at[i] = i < L::LOADS_A ? __umul24(min(row, t.M - 1 - t.m0), (uint32_t)p.lda) + piece(load)  // strides are below 2^22
+                             : __umul24(min(row - BM, t.N - 1 - t.n0), (uint32_t)p.ldb) + piece(load);
     } else {
       const int row = min(scale_row(i) + lane, L::SCALED - 1);
       at[i] = row < BM ? __umul24(min(row, t.M - 1 - t.m0), (uint32_t)p.sa_ld)
@@ -285,7 +286,7 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *const
 #pragma unroll
     for (int i = 0; i < TM; ++i) f8_settle(acc[i]);
   // Lanes 0 to 31 have pieces 0, 1 of a half step's four, the others 2, 3.
-  const int slot = (((lane >> 5) * 2) ^ (lane & 7)) * 16;
+  const int slot = (((lane >> 5) * 2) ^ (lane >> 1 & 7)) * 16;
   const int rowA = wm * (BM / WGM) + (lane & 31), rowB = BM + wn * (BN / WGN) + (lane & 31);
   const int fragA = rowA * MM_STEP + slot, fragB = rowB * MM_STEP + slot;
   struct Half {  // fragments of 64 bytes of k
