@@ -422,6 +422,7 @@ BNN_API bnn_status bnn_gated_ff_backward(const void *x, int64_t x_ld, const void
  *   bytes, strides multiples of 4.  Operands of products: strides below 2^22.  Matrices start on 16 bytes, scales, indices and vectors
  *   on their elements' size (at least 4).
  *   Values that are not numbers are NaN in e4m3 too, infinities become NaN; neither counts for a block's scale.
+ *   No result of these calls shares memory with what the call reads, or with another of its results.
  *   Products take scales from elsewhere with p from -100 to 119; the quantisers give these and, for values from 448 * 2^119 on, 120.
  */
 typedef enum { BNN_SCALE_E8M0 = 0, BNN_SCALE_F32 = 1 } bnn_scale_type;
@@ -489,7 +490,7 @@ BNN_API bnn_status bnn_expert_linear_f8_dw(const uint8_t *a, int64_t lda, const 
  *   rows [S]: the slot at a position, slots of an expert in their order; -1 between an expert's last slot and the next one's first
  *   position, -2 behind the last expert's;  places [T, k]: the position of a slot, -1 for a dropped one.  All int32.
  *   S at least bnn_expert_rows(T, k, E, align), which is enough for any choices; T * k at most 2^30, E at most 1024, align at most 4096.
- *   workspace at least bnn_expert_sort_workspace_bytes(T, k, E) bytes (0 for few slots).
+ *   workspace at least bnn_expert_sort_workspace_bytes(T, k, E) bytes (0 for few slots, and for sizes that are refused).
  * bnn_expert_gather -- xs[s] = x[rows[s] / k], zeros for -1; positions with another value are left as they were.  x [T, D], xs [S, D].
  * bnn_expert_combine -- out[t] = sum over j of weights[t,j] * ys[places[t,j]] in fp32, rounded once; places outside [0, S) add nothing
  *   and are not read.  ys [S, D], weights [T, k] fp32 or NULL: 1 (which is the gradient of bnn_expert_gather: dx from dxs).

@@ -339,7 +339,7 @@ extern "C" int64_t bnn_expert_rows(int64_t T, int64_t k, int64_t experts, int64_
 }
 
 extern "C" size_t bnn_expert_sort_workspace_bytes(int64_t T, int64_t k, int64_t experts) {
-  if (T <= 0 || k <= 0 || experts <= 0 || T * k <= bnn::SORT_ONE) return 0;
+  if (T <= 0 || k <= 0 || experts <= 0 || experts > bnn::SORT_EXPERTS || k > (1 << 30) / T || T * k <= bnn::SORT_ONE) return 0;
   return (size_t)bnn::SORT_MOST_BLOCKS * (size_t)experts * 4;
 }
 

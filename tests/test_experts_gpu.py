@@ -391,3 +391,69 @@ def test_calls_without_the_tensor_extension(monkeypatch):
     for call in (lambda: B.bnn_expert_sort(e, 1025), lambda: B.bnn_expert_sort(e, E, align=0), lambda: B.bnn_quant_blocks_f8(x, rows=rows, k=0)):
         with pytest.raises(B.BnnError):
             call()
+
+
+def test_training_pass_captured_and_replayed():
+    """A whole pass of ExpertLayer, forward and backward, as a graph: replayed on other inputs that go to other experts it gives the bits
+    of the eager pass, with eager passes between the replays."""
+    from paper_1911_04477_amd import block
+
+    T, k, E, D, F = 1500, 3, 9, 264, 136  # slots enough that the sort takes two launches
+    g = gen(61)
+    w1, w2 = (torch.randn(s, generator=g).to(BF16).to(DEV) for s in ((E, 2 * F, D), (E, D, F)))
+
+    def inputs(seed):
+        g = gen(seed)
+        e = choices(g, T, k, E, drop=0.03)
+        e[e == seed % E] = (seed + 1) % E  # another expert without tokens each time
+        return torch.randn((T, D), generator=g).to(BF16), e, torch.rand((T, k), generator=g), torch.randn((T, D), generator=g).to(BF16)
+
+    x, e, w, dout = (t.to(DEV) for t in inputs(62))
+
+    def step():
+        layer = block.ExpertLayer(w1, w2)
+        return {"out": layer.forward(x, e, w), **layer.backward(dout)}
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for seed in (63, 64, 65):
+        for to, t in zip((x, e, w, dout), inputs(seed)):
+            to.copy_(t)
+        graph.replay()
+        got = {n: t.clone() for n, t in captured.items()}
+        torch.cuda.synchronize()
+        eager = step()
+        for n, t in eager.items():
+            assert torch.equal(got[n], t), (seed, n)
+        graph.replay()
+        torch.cuda.synchronize()
+        for n, t in eager.items():
+            assert torch.equal(captured[n], t), (seed, n)
+
+
+def test_two_blocks_at_once():
+    """Two ExpertBlock8 on streams of their own, their passes under way together, give what each gives alone."""
+    from paper_1911_04477_amd import block
+
+    T, k, E, D, F = 2200, 2, 8, 512, 256
+    g = gen(71)
+    layers, inputs = [], []
+    for _ in range(2):
+        w1, w2 = (torch.randn(s, generator=g).to(BF16).to(DEV) for s in ((E, 2 * F, D), (E, D, F)))
+        layers.append(block.ExpertBlock8(w1, w2, tokens=T, choices=k))
+        inputs.append((torch.randn((T, D), generator=g).to(BF16).to(DEV), choices(g, T, k, E).to(DEV), torch.rand((T, k), generator=g).to(DEV)))
+    alone = [layer.forward(*i).clone() for layer, i in zip(layers, inputs)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[], []]
+    for _ in range(8):
+        for n in range(2):
+            with torch.cuda.stream(streams[n]):
+                outs[n].append(layers[n].forward(*inputs[n]))
+    torch.cuda.synchronize()
+    for n in range(2):
+        for out in outs[n]:
+            assert torch.equal(out, alone[n])

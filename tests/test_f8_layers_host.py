@@ -110,6 +110,13 @@ def test_sort_refusals(L):
     assert f(T=3000, S=6000, ws=None, nbytes=need) == NULL and f(T=3000, S=6000, ws=MIS, nbytes=need) == ALIGN
 
 
+def test_sizes_of_refused_sorts(L):
+    """Products of sizes past 64 bits, and experts that the sort does not take, ask for nothing."""
+    for T, k, E in ((2 ** 40, 2 ** 40, 8), (2 ** 20, 2 ** 11, 8), (2 ** 62, 3, 1), (4096, 2, 1025), (-1, 2, 8)):
+        assert L.bnn_expert_sort_workspace_bytes(T, k, E) == L.bnn_expert_rows(T, k, E, 1) == 0
+    assert L.bnn_expert_sort_workspace_bytes(2 ** 20, 2 ** 10, 1024) > 0 and L.bnn_expert_rows(2 ** 20, 2 ** 10, 1024, 1) == 2 ** 30
+
+
 def test_gather_and_combine_refusals(L):
     def g(x=A, type=BF16, T=4, ld=8, rows=A, k=2, S=8, D=8, xs=A, xs_ld=8):
         return L.bnn_expert_gather(x, type, T, ld, rows, k, S, D, xs, xs_ld, None)
