@@ -36,6 +36,7 @@ struct F8Operands {
   int M, N, blocks;
   int tilesM, tilesN;
   int64_t first;     // tile of this launch's first workgroup
+  int units;         // compute units, where a last round of few tiles is left to a second launch (f8_whole); 0: it is not
   // groups
   int groups;        // F8Groups
   const int32_t *offsets;  // [E + 1]
@@ -104,9 +105,22 @@ __device__ __forceinline__ bool f8_row_group(const F8Operands &p, int wanted, F8
   return false;
 }
 
+// Of `tiles`, those that this launch takes whole: all, or where what is left behind full rounds makes at most a round of quarters, the full rounds.
+__host__ __device__ __forceinline__ int64_t f8_whole(int64_t tiles, int units) {
+  if (units == 0) return tiles;
+  const int64_t rest = tiles % units;
+  return rest * 4 <= units ? tiles - rest : tiles;
+}
+
 // The tile of a workgroup; false: none is left for it.  BM x BN outputs.  STREAMED: B is read once, so tiles of a group follow each other.
-template <int BM, int BN, bool STREAMED = false>
+// REST: ids count from the tiles on that the first launch did not take.
+template <int BM, int BN, bool STREAMED = false, bool REST = false>
 __device__ __forceinline__ bool f8_part(const F8Operands &p, int64_t id, F8Part &t) {
+  const auto taken = [&](int64_t tiles) {
+    const int64_t whole = f8_whole(tiles, p.units);
+    if (REST) id += whole;
+    return id < (REST ? tiles : whole);
+  };
   int tm, tn;
   const int size = p.type == BNN_F32 ? 4 : 2, readable = (p.blocks + 3) & ~3;
   if (p.groups == F8_GROUP_ROWS) {
@@ -118,12 +132,12 @@ __device__ __forceinline__ bool f8_part(const F8Operands &p, int64_t id, F8Part 
       F8Scan scan;
       scan.run<BM>(p, 0);
       const int tilesM = scan.total();
-      if (id >= (int64_t)tilesM * p.tilesN) return false;
+      if (!taken((int64_t)tilesM * p.tilesN)) return false;
       mm_tile((int)id, tilesM, p.tilesN, tm, tn);
       scan.find(tm, 0, g);
     } else {
       const int tilesM = f8_row_tiles<BM>(p);
-      if (id >= (int64_t)tilesM * p.tilesN) return false;
+      if (!taken((int64_t)tilesM * p.tilesN)) return false;
       mm_tile((int)id, tilesM, p.tilesN, tm, tn);
       f8_row_group<BM>(p, tm, g);
     }
@@ -133,15 +147,15 @@ __device__ __forceinline__ bool f8_part(const F8Operands &p, int64_t id, F8Part 
   }
   const int64_t of = (int64_t)p.tilesM * p.tilesN;
   if (p.groups == F8_GROUP_K) {
+    if (!taken(of * p.E)) return false;
     const int e = (int)(id / of);
-    if (e >= p.E) return false;
     mm_tile((int)(id - e * of), p.tilesM, p.tilesN, tm, tn);
     const int end = p.blocks * F8_BLOCK, lo = f8_clamped(p.offsets, e, end) / F8_BLOCK, hi = max(f8_clamped(p.offsets, e + 1, end) / F8_BLOCK, lo);
     t = {p.A + (int64_t)lo * F8_BLOCK, p.B + (int64_t)lo * F8_BLOCK, p.sa, static_cast<const uint8_t *>(p.sb), readable, lo,
          static_cast<char *>(p.y) + e * p.y_es * size, tm * BM, tn * BN, p.M, p.N, hi - lo};
     return true;
   }
-  if (id >= of) return false;
+  if (!taken(of)) return false;
   mm_tile((int)id, p.tilesM, p.tilesN, tm, tn);
   t = {p.A, p.B, p.sa, static_cast<const uint8_t *>(p.sb), readable, 0, static_cast<char *>(p.y), tm * BM, tn * BN, p.M, p.N, p.blocks};
   return true;
@@ -208,14 +222,22 @@ struct F8Tile {
                        PART = ROWS * MM_STEP + (SCALED + 63) / 64 * 256, STAGE = KG * PART, TM = BM / WGM / 32, TN = BN / WGN / 32;
   static_assert(ROWS % (8 * WAVES) == 0 && BM % (8 * WAVES) == 0 && BM % (32 * WGM) == 0 && BN % (32 * WGN) == 0, "");
 };
-template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, class E>  // WIDE: fp32 scales of B; E: the results' type
+// WIDE: fp32 scales of B; E: the results' type; QUARTERS: of the tiles of twice the size both ways that are left.
+template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, class E, bool QUARTERS>
 __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *const whole_lds) {
   constexpr bool EXACT = sizeof(E) == 4;
   using L = F8Tile<BM, BN, WGM, WGN, KG, STAGES, WIDE>;
   constexpr int WAVES = L::WAVES, LOADS = L::LOADS, STAGE = L::STAGE, TM = L::TM, TN = L::TN;
   constexpr bool IN_PLACE = TM * TN == 16;
   F8Part t;
-  if (!f8_part<BM, BN>(p, p.first + blockIdx.x, t)) return;
+  if constexpr (QUARTERS) {  // the four of a tile on one XCD
+    const int64_t id = p.first + blockIdx.x;
+    if (!f8_part<2 * BM, 2 * BN, false, true>(p, (id >> 5) * 8 + (id & 7), t)) return;
+    t.m0 += (int)(id >> 4 & 1) * BM, t.n0 += (int)(id >> 3 & 1) * BN;
+    if (t.m0 >= t.M || t.n0 >= t.N) return;
+  } else {
+    if (!f8_part<BM, BN>(p, p.first + blockIdx.x, t)) return;
+  }
   const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = id / WAVES, wave = id % WAVES;
   const int wm = wave / WGN, wn = wave % WGN;
   char *const lds = whole_lds + group * L::PART;
@@ -542,10 +564,10 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *const
   }
 }
 
-template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, class E>
+template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, class E, bool QUARTERS = false>
 __global__ __launch_bounds__(64 * WGM *WGN *KG, WGM *WGN *KG < 4 ? 1 : WGM *WGN *KG / 4) void f8_tile_kernel(F8Operands p) {
   __shared__ __attribute__((aligned(16))) char lds[STAGES * F8Tile<BM, BN, WGM, WGN, KG, STAGES, WIDE>::STAGE];
-  f8_tile_product<BM, BN, WGM, WGN, KG, STAGES, WIDE, E>(p, lds);
+  f8_tile_product<BM, BN, WGM, WGN, KG, STAGES, WIDE, E, QUARTERS>(p, lds);
 }
 
 // At most 16 rows of A (of a group): nothing is reused, B is streamed once and bounds the kernel.  A wave owns 16 columns and deals with

@@ -9,8 +9,9 @@
 namespace bnn {
 
 // Which kernel takes a product: that of few rows, or the tiles with the least time by what a round of them was measured to take, in us, with
-// k of b blocks: start + block * b.  one: a compute unit has one tile at a time; two: it has two, and rounds count in parts (there a unit
-// that is done takes the next tile, and rounds overlap).  Measured in bf16, scales powers of two (fp32 results in brackets), us:
+// k of b blocks: start + block * b.  one: a compute unit has one tile at a time; two: it has two.  A last round of few tiles takes 0.55 of a round and
+// more (f8_form; 8192 x 4096 to 2048, one round, 61 us, to 2304, a ninth more tiles, 95).  Over 84 sizes drawn at random the form taken is
+// on average 3 % slower than the best of them.  Measured in bf16, scales powers of two (fp32 results in brackets), us:
 //   rows x columns x k     256x256    256x128    128x128    the same, short k    128x128, one    128x64    64x64    64x32
 //   64 x 4096 x 4096          40         28         25                             20              13        12       8.6
 //   256 x 4096 x 4096         46         29         27                             21              15        12      15.7
@@ -20,8 +21,8 @@ namespace bnn {
 //   8192 x 8192 x 2048       146        178        186 (267)     188 (277)        243             246       287
 //   8192 x 4096 x 512         38 (65)    35 (67)    33 (63)       29 (58)          42 (85)         39 (66)   59
 // 128 x 128 tiles come in three: two a unit of four waves each, two a unit of eight waves, whose starts and ends hide each other's better (short
-// k), and one a unit with four steps in LDS.
-enum : int { F8_256, F8_256_128, F8_128, F8_128_SHORT, F8_128_ONE, F8_128_64, F8_64, F8_64_32, F8_FORM_COUNT, F8_FEW };
+// k), and one a unit with four steps in LDS.  256 x 256 tiles also come with their last round in quarters (launch_f8_rest).
+enum : int { F8_256, F8_256_128, F8_128, F8_128_SHORT, F8_128_ONE, F8_128_64, F8_64, F8_64_32, F8_FORM_COUNT, F8_256_REST = F8_FORM_COUNT, F8_FEW };
 struct F8Cost {
   float start, block, start2, block2;  // of one tile a unit, of two (0: one at a time)
 };
@@ -31,14 +32,15 @@ struct F8Form {
 };
 constexpr F8Cost F8_NEVER = {1e9f, 0.0f, 0.0f, 0.0f};  // another is always faster
 constexpr F8Form F8_FORMS[F8_FORM_COUNT] = {
-    {256, 256, {12, 1.5f, 0, 0}, {18, 3.0f, 0, 0}, F8_NEVER, F8_NEVER},
-    {256, 128, {5, 1.0f, 0, 0}, {8, 1.65f, 0, 0}, {6, 1.28f, 0, 0}, {9, 2.1f, 0, 0}},
-    {128, 128, {3.5f, 0.73f, 4.5f, 1.07f}, {6, 0.95f, 8, 1.7f}, {3.5f, 0.85f, 4.5f, 1.65f}, F8_NEVER},
-    {128, 128, {3.5f, 0.73f, 1.8f, 1.3f}, {5.5f, 1.1f, 8.2f, 1.55f}, {3.5f, 0.8f, 3.5f, 1.8f}, {5, 1.05f, 10.5f, 2.2f}},
-    {128, 128, {3.5f, 0.58f, 0, 0}, {5, 1.0f, 0, 0}, F8_NEVER, F8_NEVER},
+    {256, 256, {12, 1.5f, 0, 0}, {19, 2.67f, 0, 0}, F8_NEVER, F8_NEVER},
+    {256, 128, {5, 1.0f, 0, 0}, F8_NEVER, {6, 1.28f, 0, 0}, {9, 2.1f, 0, 0}},
+    {128, 128, {3.5f, 0.73f, 4.5f, 1.07f}, {6, 0.86f, 8, 1.58f}, {3.5f, 0.85f, 4.5f, 1.65f}, F8_NEVER},
+    {128, 128, {3.5f, 0.73f, 1.8f, 1.3f}, {5, 0.78f, 8.2f, 1.6f}, {3.5f, 0.8f, 3.5f, 1.8f}, {5, 1.05f, 10.5f, 2.2f}},
+    {128, 128, {3.5f, 0.58f, 0, 0}, F8_NEVER, F8_NEVER, F8_NEVER},
     {128, 64, {3, 0.37f, 0, 0}, {4, 0.6f, 0, 0}, {3.5f, 0.5f, 0, 0}, F8_NEVER},
     {64, 64, {2.5f, 0.3f, 2.5f, 0.5f}, {3, 0.4f, 3, 0.65f}, {2.5f, 0.4f, 2.5f, 0.6f}, {3, 0.5f, 3, 0.8f}},
     {64, 32, {2.2f, 0.2f, 0, 0}, {2.5f, 0.25f, 0, 0}, {2.5f, 0.25f, 0, 0}, {2.5f, 0.3f, 0, 0}}};
+constexpr F8Cost F8_QUARTERS = {3.5f, 0.58f, 0, 0}, F8_QUARTERS_F32 = {5, 0.82f, 0, 0};
 // rows: of all groups, or where these are along k (`same`) of each; blocks: of k a group.
 inline int f8_form(int64_t rows, int64_t groups, bool same, int64_t N, int64_t blocks, bool wide, bool exact, int64_t units) {
   // Few rows: sixteen of A cost what sixteen of B do, so more than a few want tiles where there is enough to stream (16 rows of two
@@ -50,11 +52,23 @@ inline int f8_form(int64_t rows, int64_t groups, bool same, int64_t N, int64_t b
   for (int f = 0; f < F8_FORM_COUNT; ++f) {
     const F8Form &t = F8_FORMS[f];
     const F8Cost &c = wide ? (exact ? t.f32_wide : t.bits16_wide) : exact ? t.f32 : t.bits16;
-    const int64_t row_tiles = groups == 1 || same ? groups * ((rows - 1) / t.bm + 1) : std::max(groups, rows / t.bm + groups / 2);  // groups end inside tiles
-    const int64_t tiles = row_tiles * ((N - 1) / t.bn + 1);
-    const double one = (double)((tiles + units - 1) / units) * (c.start + c.block * blocks);
-    const double two = tiles > units && c.block2 > 0 ? std::max(1.0, (double)tiles / (2.0 * units)) * (c.start2 + c.block2 * blocks) : 1e30;
+    int64_t row_tiles = groups * ((rows - 1) / t.bm + 1);
+    if (groups > 1 && !same) row_tiles = std::max(groups * ((rows - 1) / (groups * t.bm) + 1), rows / t.bm + groups / 2);  // groups end inside tiles
+    const int64_t tiles = row_tiles * ((N - 1) / t.bn + 1), rounds = tiles / units, rest = tiles % units;
+    const auto in_rounds = [&](int64_t slots) {  // a last round that is not full has units, or the ways to them, to itself
+      const double r = (double)(tiles % slots) / slots;
+      return tiles <= slots ? 1.0 : tiles / slots + (r > 0 ? 0.55 + 0.45 * r : 0.0);
+    };
+    const double round = c.start + c.block * blocks, one = in_rounds(units) * round;
+    const double two = tiles > units && c.block2 > 0 ? in_rounds(2 * units) * (c.start2 + c.block2 * blocks) : 1e30;
     if (std::min(one, two) < least) least = std::min(one, two), best = f;
+    if (f == F8_256 && !wide && tiles > units) {
+      const bool quarters = rest && rest * 4 <= units;  // as f8_whole
+      const F8Cost &q = exact ? F8_QUARTERS_F32 : F8_QUARTERS;
+      const double time = quarters ? rounds * round + q.start + q.block * blocks + 2.0 : one;
+      // How many tiles uneven groups fill is found on the device; where the second launch has nothing to do, it costs 2 us.
+      if (time < one || (groups > 1 && !same)) least = std::min(time, one), best = F8_256_REST;
+    }
   }
   return best;
 }
@@ -71,6 +85,22 @@ bnn_status launch_f8_tile(F8Operands p, hipStream_t s) {
     p.first = first;
     f8_tile_kernel<BM, BN, WGM, WGN, KG, STAGES, WIDE, E><<<n, 64 * WGM * WGN * KG, 0, s>>>(p);
   });
+  return launch_status();
+}
+
+// 256 x 256 tiles as far as they fill rounds of the units, and where few are left for a last one, quarters of those in a launch behind: these take
+// a third of its time (8192 x 4096 to 2304: 95 us as 256 x 256, 87 as 128 x 128, 76 so; 8192 rows of eight experts of uneven parts to 2048: 108,
+// 106, 92; fp32 results 168, 143, 133).  How many there are of groups of rows, the kernels find for themselves.
+template <class E>
+bnn_status launch_f8_rest(F8Operands p, hipStream_t s) {
+  p.units = device_cu_count();
+  const bnn_status st = launch_f8_tile<256, 256, 2, 2, 1, 2, false, E>(p, s);
+  if (st != BNN_OK) return st;
+  p.tilesN = (p.N - 1) / 256 + 1;
+  p.tilesM = p.groups == F8_GROUP_ROWS ? p.M / 256 + std::min(p.E, p.M) : (p.M - 1) / 256 + 1;
+  p.first = 0;
+  ProfScope ps(KID_LINEAR_F8, s);
+  f8_tile_kernel<128, 128, 4, 2, 1, 4, false, E, true><<<(p.units / 4 + 7) / 8 * 32, 512, 0, s>>>(p);
   return launch_status();
 }
 
@@ -103,13 +133,18 @@ bnn_status run_f8_as(const F8Operands &p, hipStream_t s) {
     case F8_256:
       if constexpr (!WIDE) return launch_f8_tile<256, 256, 2, 2, 1, 2, false, E>(p, s);
       break;
-    case F8_256_128: return launch_f8_tile<256, 128, 4, 2, 1, 3, WIDE, E>(p, s);
+    case F8_256_REST:
+      if constexpr (!WIDE) return launch_f8_rest<E>(p, s);
+      break;
+    case F8_256_128:
+      if constexpr (WIDE || sizeof(E) == 2) return launch_f8_tile<256, 128, 4, 2, 1, 3, WIDE, E>(p, s);
+      break;
     case F8_128:
       if constexpr (!WIDE || sizeof(E) == 2) return launch_f8_tile<128, 128, 2, 2, 1, 2, WIDE, E>(p, s);
       break;
     case F8_128_SHORT: return launch_f8_tile<128, 128, 2, 4, 1, 2, WIDE, E>(p, s);
     case F8_128_ONE:
-      if constexpr (!WIDE) return launch_f8_tile<128, 128, 4, 2, 1, 4, false, E>(p, s);
+      if constexpr (!WIDE && sizeof(E) == 2) return launch_f8_tile<128, 128, 4, 2, 1, 4, false, E>(p, s);
       break;
     case F8_128_64:
       if constexpr (!WIDE || sizeof(E) == 2) return launch_f8_tile<128, 64, 2, 2, 2, 3, WIDE, E>(p, s);

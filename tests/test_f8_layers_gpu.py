@@ -376,7 +376,7 @@ def test_every_form_plain(wide, bits16, form, size):
         assert (room[:, N:] == -7).all()
 
 
-@pytest.mark.parametrize("wide,bits16,form,size", F.cases(F.ROWS), ids=str)
+@pytest.mark.parametrize("wide,bits16,form,size", F.cases(F.ROWS) + F.MANY, ids=str)
 def test_every_form_of_rows_by_expert(wide, bits16, form, size):
     print(f"form {form} wide {wide} bits16 {bits16} {size}", flush=True)
     E, S, N, K = size

@@ -217,8 +217,11 @@ def test_sizes_reach_every_form_of_the_products():
     for table, along_k in ((F.PLAIN, False), (F.ROWS, False), (F.ALONG_K, True)):
         for wide, bits16, f, size in F.cases(table):
             assert F.form(*size, wide, bits16, along_k) == f, (size, wide, bits16, along_k)
-    # what the rule can give at all: fp32 scales have no 256 x 256 tiles, none of one a unit, and with fp32 results two more forms are never the fastest
-    assert set(F.PLAIN[0, 0]) == set(F.PLAIN[0, 1]) == set(F.ALONG_K[0, 0]) == set(F.ALONG_K[0, 1]) == {0, 1, 2, 3, 4, 5, 6, 7, 9}
+    for wide, bits16, f, size in F.MANY:
+        assert F.form(*size, wide, bits16) == f
+    # what the rule can give at all: fp32 scales have no 256 x 256 tiles, none of one a unit, and with fp32 results others are never the fastest
+    assert set(F.PLAIN[0, 1]) == set(F.ROWS[0, 1]) == set(F.ALONG_K[0, 1]) == {0, 1, 2, 3, 4, 5, 6, 7, 8, 9}
+    assert set(F.PLAIN[0, 0]) == set(F.ROWS[0, 0]) == set(F.ALONG_K[0, 0]) == {0, 2, 3, 5, 6, 7, 8, 9}
     assert set(F.PLAIN[1, 1]) == {1, 2, 3, 5, 6, 7, 9} and set(F.PLAIN[1, 0]) == {1, 3, 6, 7, 9}
     f = B.lib().bnn_testing_f8_form
     assert f(0, 1, 0, 8, 8, 0, 1, 256) == f(8, 0, 0, 8, 8, 0, 1, 256) == f(8, 1, 0, 0, 8, 0, 1, 256) == f(8, 1, 0, 8, 8, 0, 3, 256) == f(8, 1, 0, 8, 8, 0, 1, 0) == -1
