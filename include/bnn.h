@@ -426,6 +426,7 @@ BNN_API bnn_status bnn_gated_ff_backward(const void *x, int64_t x_ld, const void
  *   Products take scales from elsewhere with p from -100 to 119; the quantisers give these and, for values from 448 * 2^119 on, 120.
  */
 typedef enum { BNN_SCALE_E8M0 = 0, BNN_SCALE_F32 = 1 } bnn_scale_type;
+typedef enum { BNN_FAST_SUMS = 16 } bnn_sums; /* added to BNN_BF16: bnn_linear_f8 */
 BNN_API int64_t bnn_f8_row_bytes(int64_t K);   /* K up to a multiple of 128; 0 for K <= 0 */
 BNN_API int64_t bnn_f8_scale_bytes(int64_t K); /* ceil(K / 128) up to a multiple of 4; 0 for K <= 0 */
 
@@ -456,8 +457,12 @@ BNN_API bnn_status bnn_quant_weight_f8(const void *w, int type, int64_t experts,
                                        int64_t w_ld, const bnn_f8_weight *out, const bnn_f8_weight *turned, void *stream);
 
 /*
- * bnn_linear_f8 -- y[m,n] = sum_b a_scale[m,b] * b_scale[n,b] * (sum over block b of a[m,k] * b[n,k]) (+ bias[n]), fp32, rounded
- *   once to `type`.
+ * bnn_linear_f8 -- y[m,n] = sum_b a_scale[m,b] * b_scale[n,b] * (sum over block b of a[m,k] * b[n,k]) (+ bias[n]), a[m,k] * b[n,k]
+ *   exact, sums in fp32, rounded once to `type`.
+ *   type BNN_BF16 | BNN_FAST_SUMS, here and in the two calls below: bf16 results by the 8-bit matrix instruction, up to twice as fast, which
+ *   of the products of eight consecutive k drops what lies below 2^-13 of the largest.  A result is off by less than 2^-10 of the sum
+ *   of its products' magnitudes before it is rounded: for normal values by 1.5e-5 in the 2-norm, a hundredth of what bf16's rounding costs, but
+ *   by many of its steps where a sum cancels.  Calls of few rows take no part in it, so a row's bits depend on how many rows a call has.
  *   a [M, K] with its scales.  b [N, K]; b_scale_rows rows of it share a row of scales: 1, or 128 (bnn_quant_weight_f8).
  *   b_scale_type BNN_SCALE_E8M0, or BNN_SCALE_F32: fp32 scales, any value, b_scale_rows 128, rows of ceil(K / 128).  bias fp32 or NULL.
  *   A training step: y from x and w; dx from bnn_quant_blocks_f8 of dy and `turned` of w; dw from bnn_quant_columns_f8 of dy and x.

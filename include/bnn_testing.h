@@ -164,7 +164,7 @@ BNN_API int bnn_testing_product_form(int64_t M, int64_t N, int weights, int alig
 BNN_API int bnn_testing_gated_backward_plan(int64_t T, int64_t D, int64_t F, int64_t *values);
 
 /* The kernel that takes a product in 8-bit floating point on a device of `units` compute units: `rows` of all groups (plain: groups 1), or
- * with along_k the rows of each; K of one group.  0 256 x 256 tiles, 1 256 x 128, 2 128 x 128 with two tiles a unit, 3 the same for short k,
+ * with along_k the rows of each; K of one group; type BNN_BF16: fast sums, the others: exact ones.  0 256 x 256 tiles, 1 256 x 128, 2 128 x 128 with two tiles a unit, 3 the same for short k,
  * 4 128 x 128 with one, 5 128 x 64, 6 64 x 64, 7 64 x 32, 8 256 x 256 with the last round in
  * quarters, 9 few rows; -1 for invalid arguments.  Host only, launches nothing. */
 BNN_API int bnn_testing_f8_form(int64_t rows, int64_t groups, int along_k, int64_t N, int64_t K, int scale_type, int type, int units);

@@ -1176,14 +1176,18 @@ def bnn_quant_weight_f8(w: torch.Tensor, plain: bool = True, turned: bool = True
     return tuple(made)
 
 
+FAST_SUMS = 16  # bnn_sums
+
+
 def bnn_linear_f8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor,
                   bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
-                  dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+                  dtype: torch.dtype = torch.bfloat16, fast: bool = False) -> torch.Tensor:
     """a e4m3 [M, K] and its scales, b e4m3 [N, K] and its scales, a row of them for each of its rows or for 128 (these also
-    fp32) -> [M, N] of out's type, or of dtype."""
+    fp32) -> [M, N] of out's type, or of dtype.  fast, here and in the experts' products: bf16 results at up to twice the rate, from sums
+    that lose bits (BNN_FAST_SUMS in include/bnn.h)."""
     if out is None and a.dim() == 2 and b.dim() == 2:
         out = torch.empty((a.shape[0], b.shape[0]), dtype=dtype, device=a.device)
-    if _made(_t().linear_f8(a, a_scale, b, b_scale, bias, out), "bnn_linear_f8") is not None:
+    if _made(_t().linear_f8(a, a_scale, b, b_scale, bias, out, FAST_SUMS if fast else 0), "bnn_linear_f8") is not None:
         return out
     if a.dim() != 2 or b.dim() != 2:
         raise ValueError("a, b: matrices expected")
@@ -1194,7 +1198,7 @@ def bnn_linear_f8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_sca
     if bias is not None:
         _present(bias, "bias")
     _check(_c().bnn_linear_f8(pa, lda, psa, sa_ld, pb, ldb, psb, wide, sb_ld, per, _vector(bias, "bias", N), M, N, K, _ptr(out),
-                               kind, ldy, _stream()), "bnn_linear_f8")
+                               kind | (FAST_SUMS if fast else 0), ldy, _stream()), "bnn_linear_f8")
     return out
 
 
@@ -1203,12 +1207,12 @@ def _offsets(offsets: torch.Tensor, E: int) -> int:
 
 
 def bnn_expert_linear_f8(a: torch.Tensor, a_scale: torch.Tensor, offsets: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor,
-                         out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+                         out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16, fast: bool = False) -> torch.Tensor:
     """Rows sorted by expert (bnn_expert_sort), a e4m3 [S, K], times their experts' weights, b e4m3 [E, N, K], scales as in
     bnn_linear_f8 -> [S, N]; rows behind the last expert's are left as they were."""
     if out is None and a.dim() == 2 and b.dim() == 3:
         out = torch.empty((a.shape[0], b.shape[1]), dtype=dtype, device=a.device)
-    if _made(_t().expert_linear_f8(a, a_scale, offsets, b, b_scale, out), "bnn_expert_linear_f8") is not None:
+    if _made(_t().expert_linear_f8(a, a_scale, offsets, b, b_scale, out, FAST_SUMS if fast else 0), "bnn_expert_linear_f8") is not None:
         return out
     if a.dim() != 2 or b.dim() != 3:
         raise ValueError("a [S, K], b [experts, N, K] expected")
@@ -1217,17 +1221,17 @@ def bnn_expert_linear_f8(a: torch.Tensor, a_scale: torch.Tensor, offsets: torch.
     (pb, ldb, b_es), (psb, sb_ld, sb_es), wide, per = _f8_weight(b, b_scale, "b", (E, N, K))
     kind, ldy = _float_rows(out, "out", S, N)
     _check(_c().bnn_expert_linear_f8(pa, lda, psa, sa_ld, _offsets(offsets, E), E, pb, ldb, b_es, psb, wide, sb_ld, sb_es, per, S, N, K,
-                                      _ptr(out), kind, ldy, _stream()), "bnn_expert_linear_f8")
+                                      _ptr(out), kind | (FAST_SUMS if fast else 0), ldy, _stream()), "bnn_expert_linear_f8")
     return out
 
 
 def bnn_expert_linear_f8_dw(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, offsets: torch.Tensor,
-                            out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+                            out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float32, fast: bool = False) -> torch.Tensor:
     """The experts' weights' gradients [E, N, K] from those of the rows, a e4m3 [N, S], and the rows, b e4m3 [K, S], both as
     bnn_quant_columns_f8 gives them; offsets multiples of 128 (bnn_expert_sort with align 128)."""
     if out is None and a.dim() == 2 and b.dim() == 2 and offsets.dim() == 1 and offsets.shape[0] > 0:
         out = torch.empty((offsets.shape[0] - 1, a.shape[0], b.shape[0]), dtype=dtype, device=a.device)
-    if _made(_t().expert_linear_f8_dw(a, a_scale, b, b_scale, offsets, out), "bnn_expert_linear_f8_dw") is not None:
+    if _made(_t().expert_linear_f8_dw(a, a_scale, b, b_scale, offsets, out, FAST_SUMS if fast else 0), "bnn_expert_linear_f8_dw") is not None:
         return out
     if a.dim() != 2 or b.dim() != 2 or offsets.dim() != 1 or offsets.shape[0] < 1:
         raise ValueError("a [N, S], b [K, S], offsets [experts + 1] expected")
@@ -1237,7 +1241,7 @@ def bnn_expert_linear_f8_dw(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Ten
     _present(out, "out", *FLOATS)
     p_out, ld, es = _padded(out, "out", (E, N, K), K, 1)
     _check(_c().bnn_expert_linear_f8_dw(pa, lda, psa, sa_ld, pb, ldb, psb, sb_ld, _offsets(offsets, E), E, N, K, S, p_out,
-                                         FLOATS[out.dtype], ld, es, _stream()), "bnn_expert_linear_f8_dw")
+                                         FLOATS[out.dtype] | (FAST_SUMS if fast else 0), ld, es, _stream()), "bnn_expert_linear_f8_dw")
     return out
 
 

@@ -90,11 +90,11 @@ class ExpertBlock8:
     """w1 [E, 2 F, D] (gate and up projections one below the other), w2 [E, D, F]: fp32, bf16 or fp16, quantised here once to e4m3
     in blocks of 128 x 128.  Any number of tokens from one to `tokens`, `choices` experts each; a pass allocates nothing where it is
     given out (it can be captured in a graph), and writes the buffers of the pass before over: threads or streams that run at once need
-    an object each."""
+    an object each.  fast: products with fast sums, of bf16 only (B.bnn_linear_f8)."""
 
     def __init__(self, w1: torch.Tensor, w2: torch.Tensor, tokens: int, choices: int, act: str = "silu",
-                 dtype: torch.dtype = torch.bfloat16):
-        (self.E, self.D, self.F), self.act, self.tokens, self.choices = w2.shape, act, tokens, choices
+                 dtype: torch.dtype = torch.bfloat16, fast: bool = False):
+        (self.E, self.D, self.F), self.act, self.tokens, self.choices, self.fast = w2.shape, act, tokens, choices, fast
         if w1.shape != (self.E, 2 * self.F, self.D):
             raise ValueError(f"w1: [{self.E}, {2 * self.F}, {self.D}] expected")
         (self.w1, _), (self.w2, _) = (B.bnn_quant_weight_f8(w, turned=False) for w in (w1, w2))
@@ -117,18 +117,19 @@ class ExpertBlock8:
         offsets, rows, places = B.bnn_expert_sort(experts, self.E, offsets=self.offsets, rows=self.rows[:S],
                                                   places=self.places[:S].view(T, k), workspace=self.workspace)
         B.bnn_quant_blocks_f8(x, x8, x_scale, rows=rows, k=k)
-        B.bnn_expert_linear_f8(x8, x_scale, offsets, *self.w1, out=gu)
+        B.bnn_expert_linear_f8(x8, x_scale, offsets, *self.w1, out=gu, fast=self.fast)
         B.bnn_gated_act_f8(gu, act=self.act, q=h8, scale=h_scale)
-        B.bnn_expert_linear_f8(h8, h_scale, offsets, *self.w2, out=ys)
+        B.bnn_expert_linear_f8(h8, h_scale, offsets, *self.w2, out=ys, fast=self.fast)
         return B.bnn_expert_combine(ys, places, weights, out=out)
 
 
 class ExpertLayer:
     """w1 [E, 2 F, D], w2 [E, D, F]; products in e4m3 with block scales, everything between them in the tensors' type.  Weights are
-    quantised anew in each forward pass, which keeps what backward needs, for one pass at a time."""
+    quantised anew in each forward pass, which keeps what backward needs, for one pass at a time.  fast: products of rows with fast sums,
+    of bf16 only (B.bnn_linear_f8); the weights' gradients are fp32's always."""
 
-    def __init__(self, w1: torch.Tensor, w2: torch.Tensor, act: str = "silu"):
-        self.w1, self.w2, self.act = w1, w2, act
+    def __init__(self, w1: torch.Tensor, w2: torch.Tensor, act: str = "silu", fast: bool = False):
+        self.w1, self.w2, self.act, self.fast = w1, w2, act, fast
         self.kept: Optional[Tuple] = None
 
     def forward(self, x: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor) -> torch.Tensor:
@@ -136,9 +137,9 @@ class ExpertLayer:
         k = experts.shape[1]
         offsets, rows, places = B.bnn_expert_sort(experts, self.w2.shape[0], align=B.F8_BLOCK)
         (w1, w1t), (w2, w2t) = B.bnn_quant_weight_f8(self.w1), B.bnn_quant_weight_f8(self.w2)
-        gu = B.bnn_expert_linear_f8(*B.bnn_quant_blocks_f8(x, rows=rows, k=k), offsets, *w1, dtype=x.dtype)
+        gu = B.bnn_expert_linear_f8(*B.bnn_quant_blocks_f8(x, rows=rows, k=k), offsets, *w1, dtype=x.dtype, fast=self.fast)
         h8 = B.bnn_gated_act_f8(gu, act=self.act, live=offsets[-1:])
-        ys = B.bnn_expert_linear_f8(*h8, offsets, *w2, dtype=x.dtype)
+        ys = B.bnn_expert_linear_f8(*h8, offsets, *w2, dtype=x.dtype, fast=self.fast)
         self.kept = (x, k, offsets, rows, places, weights, w1t, w2t, gu, ys)
         return B.bnn_expert_combine(ys, places, weights)
 
@@ -149,10 +150,10 @@ class ExpertLayer:
         (x, k, offsets, rows, places, weights, w1t, w2t, gu, ys), self.kept = self.kept, None
         live = offsets[-1:]
         dys, dweights = B.bnn_expert_combine_backward(ys, rows, places, weights, dout)
-        dh = B.bnn_expert_linear_f8(*B.bnn_quant_blocks_f8(dys), offsets, *w2t, dtype=x.dtype)
+        dh = B.bnn_expert_linear_f8(*B.bnn_quant_blocks_f8(dys), offsets, *w2t, dtype=x.dtype, fast=self.fast)
         h = B.bnn_gated_act(gu, act=self.act, live=live)
         dw2 = B.bnn_expert_linear_f8_dw(*B.bnn_quant_columns_f8(dys), *B.bnn_quant_columns_f8(h), offsets)
         dgu = B.bnn_gated_act_backward(gu, dh, act=self.act, live=live)
         dw1 = B.bnn_expert_linear_f8_dw(*B.bnn_quant_columns_f8(dgu), *B.bnn_quant_columns_f8(x, rows=rows, k=k), offsets)
-        dxs = B.bnn_expert_linear_f8(*B.bnn_quant_blocks_f8(dgu), offsets, *w1t, dtype=x.dtype)
+        dxs = B.bnn_expert_linear_f8(*B.bnn_quant_blocks_f8(dgu), offsets, *w1t, dtype=x.dtype, fast=self.fast)
         return {"dx": B.bnn_expert_combine(dxs, places), "dweights": dweights, "dw1": dw1, "dw2": dw2}

@@ -4,11 +4,14 @@
 // fp32 scales of B, one for 128 rows and a block, multiply a block's sums on the vector unit (the rows' scale is
 // in them by then), which fits into the shadow of the matrix instructions: 16 multiply-adds for two of them.
 //
-// The 8-bit matrix instruction is exact in single products and adds up groups of them in fp32, but within a group of eight it keeps no bits
-// below 2^-13 of the largest: measured on normal values, 1.5e-5 of the result in the 2-norm, whatever the length (at worst 2^-10 of the sum of
-// magnitudes).  That is a hundredth of what rounding the result to bf16 costs (a fourteenth in fp16), and far below the 2^-4 of the operands'
-// own rounding, so results in 16 bits of many rows take it, at twice the rate.  fp32 results, and the kernel of few rows, which memory bounds, are
-// EXACT: values go to bf16 on their way into the 16-bit instruction, times their scales; no digit is lost, and sums are fp32's.
+// Sums are EXACT: values go to bf16 on their way into the 16-bit matrix instruction, times their scales; no digit is lost, and sums are fp32's.
+//
+// bf16 results may be asked for with FAST sums, at twice the rate (8192^3 433 to 478 us, EXACT 760): the 8-bit matrix instruction is exact in single
+// products and adds up groups of them in fp32, but of the products of eight consecutive k it keeps no bits below 2^-13 of the largest.  A
+// result is off by less than 2^-10 of the sum of its products' magnitudes, for normal values by 1.5e-5 of itself in the 2-norm, whatever the length:
+// a hundredth of what rounding it to bf16 costs, but more where terms cancel; and where a result is quantised again, values next to
+// a border go to the other side of it (a layer of experts in bf16 is off by 0.0028 for 0.0017).  So it is the caller's choice (BNN_FAST_SUMS).  The
+// kernel of few rows is bound by memory and always EXACT.
 //
 // The same kernels take the experts' products: rows of A in groups with a weight each, or groups along k with a result each.
 #pragma once
@@ -33,6 +36,7 @@ struct F8Operands {
   void *y;
   int64_t ldy;
   int type;
+  bool fast;  // sums
   int M, N, blocks;
   int tilesM, tilesN;
   int64_t first;     // tile of this launch's first workgroup
@@ -222,10 +226,9 @@ struct F8Tile {
                        PART = ROWS * MM_STEP + (SCALED + 63) / 64 * 256, STAGE = KG * PART, TM = BM / WGM / 32, TN = BN / WGN / 32;
   static_assert(ROWS % (8 * WAVES) == 0 && BM % (8 * WAVES) == 0 && BM % (32 * WGM) == 0 && BN % (32 * WGN) == 0, "");
 };
-// WIDE: fp32 scales of B; E: the results' type; QUARTERS: of the tiles of twice the size both ways that are left.
-template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, class E, bool QUARTERS>
+// WIDE: fp32 scales of B; E: the results' type; EXACT: see above; QUARTERS: of the tiles of twice the size both ways that are left.
+template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, class E, bool EXACT, bool QUARTERS>
 __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *const whole_lds) {
-  constexpr bool EXACT = sizeof(E) == 4;
   using L = F8Tile<BM, BN, WGM, WGN, KG, STAGES, WIDE>;
   constexpr int WAVES = L::WAVES, LOADS = L::LOADS, STAGE = L::STAGE, TM = L::TM, TN = L::TN;
   constexpr bool IN_PLACE = TM * TN == 16;
@@ -564,10 +567,10 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *const
   }
 }
 
-template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, class E, bool QUARTERS = false>
+template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, class E, bool EXACT, bool QUARTERS = false>
 __global__ __launch_bounds__(64 * WGM *WGN *KG, WGM *WGN *KG < 4 ? 1 : WGM *WGN *KG / 4) void f8_tile_kernel(F8Operands p) {
   __shared__ __attribute__((aligned(16))) char lds[STAGES * F8Tile<BM, BN, WGM, WGN, KG, STAGES, WIDE>::STAGE];
-  f8_tile_product<BM, BN, WGM, WGN, KG, STAGES, WIDE, E, QUARTERS>(p, lds);
+  f8_tile_product<BM, BN, WGM, WGN, KG, STAGES, WIDE, E, EXACT, QUARTERS>(p, lds);
 }
 
 // At most 16 rows of A (of a group): nothing is reused, B is streamed once and bounds the kernel.  A wave owns 16 columns and deals with

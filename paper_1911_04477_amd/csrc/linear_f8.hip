@@ -11,7 +11,7 @@ namespace bnn {
 // Which kernel takes a product: that of few rows, or the tiles with the least time by what a round of them was measured to take, in us, with
 // k of b blocks: start + block * b.  one: a compute unit has one tile at a time; two: it has two.  A last round of few tiles takes 0.55 of a round and
 // more (f8_form; 8192 x 4096 to 2048, one round, 61 us, to 2304, a ninth more tiles, 95).  Over 84 sizes drawn at random the form taken is
-// on average 3 % slower than the best of them.  Measured in bf16, scales powers of two (fp32 results in brackets), us:
+// on average 3 % slower than the best of them.  Measured with fast sums in bf16, scales powers of two (exact sums, fp32 results, in brackets), us:
 //   rows x columns x k     256x256    256x128    128x128    the same, short k    128x128, one    128x64    64x64    64x32
 //   64 x 4096 x 4096          40         28         25                             20              13        12       8.6
 //   256 x 4096 x 4096         46         29         27                             21              15        12      15.7
@@ -28,7 +28,7 @@ struct F8Cost {
 };
 struct F8Form {
   int bm, bn;
-  F8Cost bits16, f32, bits16_wide, f32_wide;
+  F8Cost fast, exact, fast_wide, exact_wide;
 };
 constexpr F8Cost F8_NEVER = {1e9f, 0.0f, 0.0f, 0.0f};  // another is always faster
 constexpr F8Form F8_FORMS[F8_FORM_COUNT] = {
@@ -40,7 +40,7 @@ constexpr F8Form F8_FORMS[F8_FORM_COUNT] = {
     {128, 64, {3, 0.37f, 0, 0}, {4, 0.6f, 0, 0}, {3.5f, 0.5f, 0, 0}, F8_NEVER},
     {64, 64, {2.5f, 0.3f, 2.5f, 0.5f}, {3, 0.4f, 3, 0.65f}, {2.5f, 0.4f, 2.5f, 0.6f}, {3, 0.5f, 3, 0.8f}},
     {64, 32, {2.2f, 0.2f, 0, 0}, {2.5f, 0.25f, 0, 0}, {2.5f, 0.25f, 0, 0}, {2.5f, 0.3f, 0, 0}}};
-constexpr F8Cost F8_QUARTERS = {3.5f, 0.58f, 0, 0}, F8_QUARTERS_F32 = {5, 0.82f, 0, 0};
+constexpr F8Cost F8_QUARTERS = {3.5f, 0.58f, 0, 0}, F8_QUARTERS_EXACT = {5, 0.82f, 0, 0};
 // rows: of all groups, or where these are along k (`same`) of each; blocks: of k a group.
 inline int f8_form(int64_t rows, int64_t groups, bool same, int64_t N, int64_t blocks, bool wide, bool exact, int64_t units) {
   // Few rows: sixteen of A cost what sixteen of B do, so more than a few want tiles where there is enough to stream (16 rows of two
@@ -51,7 +51,7 @@ inline int f8_form(int64_t rows, int64_t groups, bool same, int64_t N, int64_t b
   double least = 1e30;
   for (int f = 0; f < F8_FORM_COUNT; ++f) {
     const F8Form &t = F8_FORMS[f];
-    const F8Cost &c = wide ? (exact ? t.f32_wide : t.bits16_wide) : exact ? t.f32 : t.bits16;
+    const F8Cost &c = wide ? (exact ? t.exact_wide : t.fast_wide) : exact ? t.exact : t.fast;
     int64_t row_tiles = groups * ((rows - 1) / t.bm + 1);
     if (groups > 1 && !same) row_tiles = std::max(groups * ((rows - 1) / (groups * t.bm) + 1), rows / t.bm + groups / 2);  // groups end inside tiles
     const int64_t tiles = row_tiles * ((N - 1) / t.bn + 1), rounds = tiles / units, rest = tiles % units;
@@ -64,7 +64,7 @@ inline int f8_form(int64_t rows, int64_t groups, bool same, int64_t N, int64_t b
     if (std::min(one, two) < least) least = std::min(one, two), best = f;
     if (f == F8_256 && !wide && tiles > units) {
       const bool quarters = rest && rest * 4 <= units;  // as f8_whole
-      const F8Cost &q = exact ? F8_QUARTERS_F32 : F8_QUARTERS;
+      const F8Cost &q = exact ? F8_QUARTERS_EXACT : F8_QUARTERS;
       const double time = quarters ? rounds * round + q.start + q.block * blocks + 2.0 : one;
       // How many tiles uneven groups fill is found on the device; where the second launch has nothing to do, it costs 2 us.
       if (time < one || (groups > 1 && !same)) least = std::min(time, one), best = F8_256_REST;
@@ -73,7 +73,7 @@ inline int f8_form(int64_t rows, int64_t groups, bool same, int64_t N, int64_t b
   return best;
 }
 
-template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, class E>
+template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE, class E, bool EXACT>
 bnn_status launch_f8_tile(F8Operands p, hipStream_t s) {
   p.tilesN = (p.N - 1) / BN + 1;
   // groups of rows: each has a part of a tile more than its rows fill at most
@@ -83,7 +83,7 @@ bnn_status launch_f8_tile(F8Operands p, hipStream_t s) {
   ProfScope ps(KID_LINEAR_F8, s);
   wide_launches(tiles, [&](int64_t first, uint32_t n) {
     p.first = first;
-    f8_tile_kernel<BM, BN, WGM, WGN, KG, STAGES, WIDE, E><<<n, 64 * WGM * WGN * KG, 0, s>>>(p);
+    f8_tile_kernel<BM, BN, WGM, WGN, KG, STAGES, WIDE, E, EXACT><<<n, 64 * WGM * WGN * KG, 0, s>>>(p);
   });
   return launch_status();
 }
@@ -91,16 +91,16 @@ bnn_status launch_f8_tile(F8Operands p, hipStream_t s) {
 // 256 x 256 tiles as far as they fill rounds of the units, and where few are left for a last one, quarters of those in a launch behind: these take
 // a third of its time (8192 x 4096 to 2304: 95 us as 256 x 256, 87 as 128 x 128, 76 so; 8192 rows of eight experts of uneven parts to 2048: 108,
 // 106, 92; fp32 results 168, 143, 133).  How many there are of groups of rows, the kernels find for themselves.
-template <class E>
+template <class E, bool EXACT>
 bnn_status launch_f8_rest(F8Operands p, hipStream_t s) {
   p.units = device_cu_count();
-  const bnn_status st = launch_f8_tile<256, 256, 2, 2, 1, 2, false, E>(p, s);
+  const bnn_status st = launch_f8_tile<256, 256, 2, 2, 1, 2, false, E, EXACT>(p, s);
   if (st != BNN_OK) return st;
   p.tilesN = (p.N - 1) / 256 + 1;
   p.tilesM = p.groups == F8_GROUP_ROWS ? p.M / 256 + std::min(p.E, p.M) : (p.M - 1) / 256 + 1;
   p.first = 0;
   ProfScope ps(KID_LINEAR_F8, s);
-  f8_tile_kernel<128, 128, 4, 2, 1, 4, false, E, true><<<(p.units / 4 + 7) / 8 * 32, 512, 0, s>>>(p);
+  f8_tile_kernel<128, 128, 4, 2, 1, 4, false, E, EXACT, true><<<(p.units / 4 + 7) / 8 * 32, 512, 0, s>>>(p);
   return launch_status();
 }
 
@@ -125,39 +125,40 @@ bnn_status launch_f8_few(const F8Operands &p, hipStream_t s) {
   return launch_f8_few_split<8, WIDE>(p, row_tiles, s);
 }
 
-template <bool WIDE, class E>
+template <bool WIDE, class E, bool EXACT>
 bnn_status run_f8_as(const F8Operands &p, hipStream_t s) {
   const bool along_k = p.groups == F8_GROUP_K;
   const int64_t groups = p.groups == F8_PLAIN ? 1 : along_k ? p.E : std::min(p.E, p.M);
-  switch (f8_form(p.M, groups, along_k, p.N, along_k ? p.blocks / p.E + 1 : p.blocks, WIDE, sizeof(E) == 4, device_cu_count())) {
+  switch (f8_form(p.M, groups, along_k, p.N, along_k ? p.blocks / p.E + 1 : p.blocks, WIDE, EXACT, device_cu_count())) {
     case F8_256:
-      if constexpr (!WIDE) return launch_f8_tile<256, 256, 2, 2, 1, 2, false, E>(p, s);
+      if constexpr (!WIDE) return launch_f8_tile<256, 256, 2, 2, 1, 2, false, E, EXACT>(p, s);
       break;
     case F8_256_REST:
-      if constexpr (!WIDE) return launch_f8_rest<E>(p, s);
+      if constexpr (!WIDE) return launch_f8_rest<E, EXACT>(p, s);
       break;
     case F8_256_128:
-      if constexpr (WIDE || sizeof(E) == 2) return launch_f8_tile<256, 128, 4, 2, 1, 3, WIDE, E>(p, s);
+      if constexpr (WIDE || !EXACT) return launch_f8_tile<256, 128, 4, 2, 1, 3, WIDE, E, EXACT>(p, s);
       break;
     case F8_128:
-      if constexpr (!WIDE || sizeof(E) == 2) return launch_f8_tile<128, 128, 2, 2, 1, 2, WIDE, E>(p, s);
+      if constexpr (!WIDE || !EXACT) return launch_f8_tile<128, 128, 2, 2, 1, 2, WIDE, E, EXACT>(p, s);
       break;
-    case F8_128_SHORT: return launch_f8_tile<128, 128, 2, 4, 1, 2, WIDE, E>(p, s);
+    case F8_128_SHORT: return launch_f8_tile<128, 128, 2, 4, 1, 2, WIDE, E, EXACT>(p, s);
     case F8_128_ONE:
-      if constexpr (!WIDE && sizeof(E) == 2) return launch_f8_tile<128, 128, 4, 2, 1, 4, false, E>(p, s);
+      if constexpr (!WIDE && !EXACT) return launch_f8_tile<128, 128, 4, 2, 1, 4, false, E, EXACT>(p, s);
       break;
     case F8_128_64:
-      if constexpr (!WIDE || sizeof(E) == 2) return launch_f8_tile<128, 64, 2, 2, 2, 3, WIDE, E>(p, s);
+      if constexpr (!WIDE || !EXACT) return launch_f8_tile<128, 64, 2, 2, 2, 3, WIDE, E, EXACT>(p, s);
       break;
-    case F8_64: return launch_f8_tile<64, 64, 2, 2, 1, 4, WIDE, E>(p, s);
-    case F8_64_32: return launch_f8_tile<64, 32, 2, 1, 4, 3, WIDE, E>(p, s);
+    case F8_64: return launch_f8_tile<64, 64, 2, 2, 1, 4, WIDE, E, EXACT>(p, s);
+    case F8_64_32: return launch_f8_tile<64, 32, 2, 1, 4, 3, WIDE, E, EXACT>(p, s);
     default: return launch_f8_few<WIDE>(p, s);
   }
   return BNN_ERR_UNSUPPORTED;  // not reached: these forms are never the fastest (F8_NEVER)
 }
 template <bool WIDE>
 bnn_status run_f8(const F8Operands &p, hipStream_t s) {
-  return with_float(p.type, [&](auto tag) { return run_f8_as<WIDE, typename decltype(tag)::type>(p, s); });
+  if (p.fast) return run_f8_as<WIDE, __bf16, false>(p, s);
+  return with_float(p.type, [&](auto tag) { return run_f8_as<WIDE, typename decltype(tag)::type, true>(p, s); });
 }
 
 // B's scales, checked: N rows of K values, of which `per` share a row of scales.
@@ -180,6 +181,13 @@ bnn_status f8_weight(F8Operands &p, const uint8_t *b, int64_t ldb, const void *s
 
 constexpr int64_t F8_MOST = INT32_MAX - 256;
 
+// The type of results without the choice of their sums.
+bnn_status f8_type(F8Operands &p, int type) {
+  p.fast = type == (BNN_BF16 | BNN_FAST_SUMS);
+  p.type = p.fast ? BNN_BF16 : type;
+  return float_type(p.type) ? BNN_OK : BNN_ERR_SHAPE;
+}
+
 }  // namespace bnn
 
 extern "C" bnn_status bnn_linear_f8(const uint8_t *a, int64_t lda, const uint8_t *a_scale, int64_t a_scale_ld, const uint8_t *b,
@@ -187,18 +195,18 @@ extern "C" bnn_status bnn_linear_f8(const uint8_t *a, int64_t lda, const uint8_t
                                     const float *bias, int64_t M, int64_t N, int64_t K, void *y, int type, int64_t ldy,
                                     void *stream) {
   using namespace bnn;
-  if (M < 0 || N < 0 || K <= 0 || !float_type(type)) return BNN_ERR_SHAPE;
+  F8Operands p = {};
+  if (M < 0 || N < 0 || K <= 0 || f8_type(p, type) != BNN_OK) return BNN_ERR_SHAPE;
   if (ldy < N) return BNN_ERR_STRIDE;
   if (M > F8_MOST || N > F8_MOST || K > (1 << 22)) return BNN_ERR_UNSUPPORTED;
   if (M == 0 || N == 0) return BNN_OK;
-  F8Operands p = {};
   bnn_status st = f8_check(a, lda, a_scale, a_scale_ld, K);
   if (st == BNN_OK) st = f8_weight(p, b, ldb, b_scale, b_scale_type, b_scale_ld, b_scale_rows, N, K);
   if (st != BNN_OK) return st;
   if (!y) return BNN_ERR_NULL;
   if (!aligned16(y) || !aligned4(bias)) return BNN_ERR_ALIGN;
   p.A = reinterpret_cast<const char *>(a), p.lda = lda, p.sa = a_scale, p.sa_ld = a_scale_ld;
-  p.M = (int)M, p.blocks = (int)f8_blocks(K), p.bias = bias, p.y = y, p.type = type, p.ldy = ldy;
+  p.M = (int)M, p.blocks = (int)f8_blocks(K), p.bias = bias, p.y = y, p.ldy = ldy;
   hipStream_t s = static_cast<hipStream_t>(stream);
   return b_scale_type == BNN_SCALE_F32 ? run_f8<true>(p, s) : run_f8<false>(p, s);
 }
@@ -209,11 +217,11 @@ extern "C" bnn_status bnn_expert_linear_f8(const uint8_t *a, int64_t lda, const 
                                            int b_scale_rows, int64_t S, int64_t N, int64_t K, void *y, int type, int64_t ldy,
                                            void *stream) {
   using namespace bnn;
-  if (S < 0 || N < 0 || K <= 0 || experts < 0 || !float_type(type)) return BNN_ERR_SHAPE;
+  F8Operands p = {};
+  if (S < 0 || N < 0 || K <= 0 || experts < 0 || f8_type(p, type) != BNN_OK) return BNN_ERR_SHAPE;
   if (ldy < N) return BNN_ERR_STRIDE;
   if (S > F8_MOST || N > F8_MOST || K > (1 << 22) || experts > 65535) return BNN_ERR_UNSUPPORTED;
   if (S == 0 || N == 0 || experts == 0) return BNN_OK;
-  F8Operands p = {};
   bnn_status st = f8_check(a, lda, a_scale, a_scale_ld, K);
   if (st == BNN_OK) st = f8_weight(p, b, ldb, b_scale, b_scale_type, b_scale_ld, b_scale_rows, N, K);
   if (st != BNN_OK) return st;
@@ -223,7 +231,7 @@ extern "C" bnn_status bnn_expert_linear_f8(const uint8_t *a, int64_t lda, const 
   if (!offsets || !y) return BNN_ERR_NULL;
   if (!aligned4(offsets) || !aligned16(y)) return BNN_ERR_ALIGN;
   p.A = reinterpret_cast<const char *>(a), p.lda = lda, p.sa = a_scale, p.sa_ld = a_scale_ld;
-  p.M = (int)S, p.blocks = (int)f8_blocks(K), p.y = y, p.type = type, p.ldy = ldy;
+  p.M = (int)S, p.blocks = (int)f8_blocks(K), p.y = y, p.ldy = ldy;
   p.groups = F8_GROUP_ROWS, p.offsets = offsets, p.E = (int)experts, p.b_es = b_expert_ld;
   p.sb_es = b_scale_expert_ld * (b_scale_type == BNN_SCALE_F32 ? 4 : 1);
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -235,11 +243,11 @@ extern "C" bnn_status bnn_expert_linear_f8_dw(const uint8_t *a, int64_t lda, con
                                               const int32_t *offsets, int64_t experts, int64_t N, int64_t K, int64_t S, void *dw,
                                               int type, int64_t dw_ld, int64_t dw_expert_ld, void *stream) {
   using namespace bnn;
-  if (S < 0 || N < 0 || K < 0 || experts < 0 || !float_type(type)) return BNN_ERR_SHAPE;
+  F8Operands p = {};
+  if (S < 0 || N < 0 || K < 0 || experts < 0 || f8_type(p, type) != BNN_OK) return BNN_ERR_SHAPE;
   if (dw_ld < K || (experts > 1 && N > 0 && dw_expert_ld / N < dw_ld)) return BNN_ERR_STRIDE;
   if (S > (1 << 22) - F8_BLOCK || N > F8_MOST || K > F8_MOST || experts > 65535) return BNN_ERR_UNSUPPORTED;
   if (N == 0 || K == 0 || experts == 0) return BNN_OK;
-  F8Operands p = {};
   if (S > 0) {  // else every group is empty, and the result 0
     bnn_status st = f8_check(a, lda, a_scale, a_scale_ld, S);
     if (st == BNN_OK) st = f8_weight(p, b, ldb, b_scale, BNN_SCALE_E8M0, b_scale_ld, 1, K, S);
@@ -248,7 +256,7 @@ extern "C" bnn_status bnn_expert_linear_f8_dw(const uint8_t *a, int64_t lda, con
   if (!offsets || !dw) return BNN_ERR_NULL;
   if (!aligned4(offsets) || !aligned16(dw)) return BNN_ERR_ALIGN;
   p.A = reinterpret_cast<const char *>(a), p.lda = lda, p.sa = a_scale, p.sa_ld = a_scale_ld;
-  p.M = (int)N, p.N = (int)K, p.blocks = (int)f8_blocks(S), p.y = dw, p.type = type, p.ldy = dw_ld;
+  p.M = (int)N, p.N = (int)K, p.blocks = (int)f8_blocks(S), p.y = dw, p.ldy = dw_ld;
   p.groups = F8_GROUP_K, p.offsets = offsets, p.E = (int)experts, p.y_es = dw_expert_ld;
   return run_f8<false>(p, static_cast<hipStream_t>(stream));
 }
@@ -256,5 +264,5 @@ extern "C" bnn_status bnn_expert_linear_f8_dw(const uint8_t *a, int64_t lda, con
 extern "C" int bnn_testing_f8_form(int64_t rows, int64_t groups, int along_k, int64_t N, int64_t K, int scale_type, int type, int units) {
   using namespace bnn;
   if (rows <= 0 || groups <= 0 || N <= 0 || K <= 0 || !float_type(type) || units <= 0) return -1;
-  return f8_form(rows, groups, along_k != 0, N, f8_blocks(K), scale_type == BNN_SCALE_F32, type == BNN_F32, units);
+  return f8_form(rows, groups, along_k != 0, N, f8_blocks(K), scale_type == BNN_SCALE_F32, type != BNN_BF16, units);
 }

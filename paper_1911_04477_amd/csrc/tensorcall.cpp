@@ -644,6 +644,9 @@ at::Tensor made_scales(const at::Tensor *t, int64_t rows, int64_t K, const at::T
 at::Tensor made(const at::Tensor *t, at::IntArrayRef sizes, at::ScalarType type, const at::Tensor &on) {
   return t ? *t : at::empty(sizes, on.options().dtype(type));
 }
+int product_type(const at::Tensor &out, Args &v) {  // with the next argument, a choice of sums
+  return float_type(out.scalar_type()) | v.small();
+}
 PyObject *result(PyObject *status, const at::Tensor &t) {
   if (!status || PyLong_AsLong(status) != BNN_OK) return status;
   Py_DECREF(status);
@@ -669,8 +672,8 @@ PyObject *quant_f8(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-PyObject *linear_f8(PyObject *, PyObject *const *args, Py_ssize_t n) {  // a, a_scale, b, b_scale, bias, out -> status
-  return guarded(args, n, 6, [](Args &v) {
+PyObject *linear_f8(PyObject *, PyObject *const *args, Py_ssize_t n) {  // a, a_scale, b, b_scale, bias, out, sums -> status
+  return guarded(args, n, 7, [](Args &v) {
     const at::Tensor &ta = v.tensor(), &tsa = v.tensor(), &tb = v.tensor(), &tsb = v.tensor();
     if (ta.dim() != 2 || tb.dim() != 2) throw Other();
     const int64_t M = ta.size(0), K = ta.size(1), N = tb.size(0);
@@ -680,7 +683,7 @@ PyObject *linear_f8(PyObject *, PyObject *const *args, Py_ssize_t n) {  // a, a_
     if (tbias) present(*tbias, kFloat);
     const float *const bias = vector(tbias, N);
     const at::Tensor &out = v.tensor();
-    const int code = float_type(out.scalar_type());
+    const int code = product_type(out, v);
     const Matrix y = present_matrix(out, out.scalar_type(), M, N);
     return launch([&](void *s) {
       return lib.linear_f8(a.p, a.ld, sa.p, sa.ld, b.q.p, b.q.ld, b.s.p, b.wide, b.s.ld, b.per, bias, M, N, K, y.p, code, y.ld, s);
@@ -688,15 +691,15 @@ PyObject *linear_f8(PyObject *, PyObject *const *args, Py_ssize_t n) {  // a, a_
   });
 }
 
-PyObject *expert_linear_f8(PyObject *, PyObject *const *args, Py_ssize_t n) {  // a, a_scale, offsets, b, b_scale, out -> status
-  return guarded(args, n, 6, [](Args &v) {
+PyObject *expert_linear_f8(PyObject *, PyObject *const *args, Py_ssize_t n) {  // a, a_scale, offsets, b, b_scale, out, sums -> status
+  return guarded(args, n, 7, [](Args &v) {
     const at::Tensor &ta = v.tensor(), &tsa = v.tensor(), &to = v.tensor(), &tb = v.tensor(), &tsb = v.tensor(), &out = v.tensor();
     if (ta.dim() != 2 || tb.dim() != 3) throw Other();
     const int64_t S = ta.size(0), K = ta.size(1), E = tb.size(0), N = tb.size(1);
     const Padded a = f8_values(ta, -1, S, K), sa = f8_scales(tsa, -1, S, K);
     const Weight b = f8_weight(tb, tsb, E, N, K);
     const int32_t *const offsets = whole<int32_t>(&to, kInt, {E + 1});
-    const int code = float_type(out.scalar_type());
+    const int code = product_type(out, v);
     const Matrix y = present_matrix(out, out.scalar_type(), S, N);
     return launch([&](void *s) {
       return lib.expert_linear(a.p, a.ld, sa.p, sa.ld, offsets, E, b.q.p, b.q.ld, b.q.between, b.s.p, b.wide, b.s.ld, b.s.between, b.per, S, N,
@@ -705,14 +708,14 @@ PyObject *expert_linear_f8(PyObject *, PyObject *const *args, Py_ssize_t n) {  /
   });
 }
 
-PyObject *expert_linear_f8_dw(PyObject *, PyObject *const *args, Py_ssize_t n) {  // a, a_scale, b, b_scale, offsets, out -> status
-  return guarded(args, n, 6, [](Args &v) {
+PyObject *expert_linear_f8_dw(PyObject *, PyObject *const *args, Py_ssize_t n) {  // a, a_scale, b, b_scale, offsets, out, sums -> status
+  return guarded(args, n, 7, [](Args &v) {
     const at::Tensor &ta = v.tensor(), &tsa = v.tensor(), &tb = v.tensor(), &tsb = v.tensor(), &to = v.tensor(), &out = v.tensor();
     if (ta.dim() != 2 || tb.dim() != 2 || to.dim() != 1 || to.size(0) < 1) throw Other();
     const int64_t N = ta.size(0), S = ta.size(1), K = tb.size(0), E = to.size(0) - 1;
     const Padded a = f8_values(ta, -1, N, S), sa = f8_scales(tsa, -1, N, S), b = f8_values(tb, -1, K, S), sb = f8_scales(tsb, -1, K, S);
     const int32_t *const offsets = whole<int32_t>(&to, kInt, {E + 1});
-    const int code = float_type(out.scalar_type());
+    const int code = product_type(out, v);
     const Padded dw = padded(present(out, out.scalar_type()), E, N, K, K, 1);
     return launch([&](void *s) {
       return lib.expert_linear_dw(a.p, a.ld, sa.p, sa.ld, b.p, b.ld, sb.p, sb.ld, offsets, E, N, K, S, dw.p, code, dw.ld, dw.between, s);
