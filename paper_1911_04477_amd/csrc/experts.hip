@@ -265,6 +265,7 @@ __global__ __launch_bounds__(MAXT) void combine_backward_kernel(CombineBackwardP
   const int threads = BLOCK ? blockDim.x : 64, tid = BLOCK ? threadIdx.x : threadIdx.x & 63;
   const int64_t tokens = BLOCK ? p.T : (p.T + 3) / 4, block = wide_block();
   if (block >= tokens) {
+    if (!p.dys) return;  // nothing to clear: left over in a grid of more than 2^20 workgroups (wide_grid)
     const int64_t first = (block - tokens) * 64, own = first + (threadIdx.x & 63);
     const float none[8] = {};
     for (uint64_t left = __ballot(own < p.S && p.rows[min(own, p.S - 1)] == -1); left; left &= left - 1) {  // one look at all 64
