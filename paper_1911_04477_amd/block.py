@@ -86,6 +86,13 @@ class GatedProjections:
         return {"dwg": dwg, "dwu": dwu, **B.bnn_norm_gate_backward(b, r, dn, dr_out, **given)}
 
 
+def _choices(x: torch.Tensor, experts: torch.Tensor) -> Tuple[int, int]:
+    """Tokens and choices of each.  Slots of tokens that x does not have would be left as they were, without an error of their own."""
+    if x.dim() != 2 or experts.dim() != 2 or x.shape[0] != experts.shape[0]:
+        raise ValueError(f"x [T, D] and experts [T, choices] expected, got {list(x.shape)} and {list(experts.shape)}")
+    return experts.shape[0], experts.shape[1]
+
+
 class ExpertBlock8:
     """w1 [E, 2 F, D] (gate and up projections one below the other), w2 [E, D, F]: fp32, bf16 or fp16, quantised here once to e4m3
     in blocks of 128 x 128.  Any number of tokens from one to `tokens`, `choices` experts each; a pass allocates nothing where it is
@@ -109,7 +116,7 @@ class ExpertBlock8:
     def forward(self, x: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor,
                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x [T, D], experts [T, choices] int32 or int64 (outside 0 .. E - 1: none), weights [T, choices] fp32 -> [T, D]."""
-        T, k = experts.shape
+        T, k = _choices(x, experts)
         if T > self.tokens or k != self.choices:
             raise ValueError(f"made for {self.tokens} tokens of {self.choices} choices")
         S = T * k
@@ -134,7 +141,7 @@ class ExpertLayer:
 
     def forward(self, x: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor) -> torch.Tensor:
         """x [T, D], experts [T, k], weights [T, k] fp32 -> [T, D]."""
-        k = experts.shape[1]
+        _, k = _choices(x, experts)
         offsets, rows, places = B.bnn_expert_sort(experts, self.w2.shape[0], align=B.F8_BLOCK)
         (w1, w1t), (w2, w2t) = B.bnn_quant_weight_f8(self.w1), B.bnn_quant_weight_f8(self.w2)
         gu = B.bnn_expert_linear_f8(*B.bnn_quant_blocks_f8(x, rows=rows, k=k), offsets, *w1, dtype=x.dtype, fast=self.fast)

@@ -1,0 +1,28 @@
+"""What the layers of experts refuse before any call: tokens without choices, or choices of tokens that there are not.  No GPU."""
+import pytest
+import torch
+
+from paper_1911_04477_amd import block
+
+T, k, D = 6, 2, 8
+
+
+def layers():
+    served = object.__new__(block.ExpertBlock8)
+    served.E, served.D, served.F, served.tokens, served.choices, served.fast = 3, D, 4, 64, k, False
+    return served, block.ExpertLayer(torch.zeros((3, 8, D)), torch.zeros((3, D, 4)))
+
+
+@pytest.mark.parametrize("x,experts", [((T - 1, D), (T, k)), ((T + 1, D), (T, k)), ((0, D), (T, k)), ((T, D), (T * k,)), ((T * D,), (T, k)),
+                                       ((1, T, D), (T, k))], ids=str)
+def test_tokens_and_choices_have_to_belong_together(x, experts):
+    for layer in layers():
+        with pytest.raises(ValueError, match="expected, got"):
+            layer.forward(torch.zeros(x), torch.zeros(experts, dtype=torch.int32), torch.zeros((T, k)))
+
+
+def test_more_tokens_than_room():
+    served, _ = layers()
+    for t, n in ((65, k), (64, k + 1)):
+        with pytest.raises(ValueError, match="made for"):
+            served.forward(torch.zeros((t, D)), torch.zeros((t, n), dtype=torch.int32), torch.zeros((t, n)))
