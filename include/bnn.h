@@ -439,7 +439,8 @@ BNN_API int64_t bnn_f8_scale_bytes(int64_t K); /* ceil(K / 128) up to a multiple
  *   x [T, D]; positions without a slot are zeros, and so is the rest of the last block.  S at most 2^22 - 128; T > 0 where S > 0.
  * bnn_quant_weight_f8 -- weights w [experts, N, K] (expert_ld elements between experts) in blocks of 128 x 128: `out` as they lie, q [N,
  *   K] and scales [ceil(N / 128), ceil(K / 128)], `turned` q [K, N] and scales [ceil(K / 128), ceil(N / 128)]; either may be NULL.  The
- *   structs are HOST structs; ld and expert_ld in bytes, scale_ld and scale_expert_ld too.  N and K at most 2^22.
+ *   structs are HOST structs; ld and expert_ld in bytes, scale_ld and scale_expert_ld too.  N and K at most 2^22, rows of the results (K of
+ *   `out`, N of `turned`) at most 2^22 - 128, as products take them.
  */
 typedef struct {
   uint8_t *q;
@@ -472,7 +473,8 @@ BNN_API bnn_status bnn_quant_weight_f8(const void *w, int type, int64_t experts,
  * bnn_expert_linear_f8_dw -- the gradients of those weights, dw[e] [N, K] = sum over the expert's positions s of a[n,s] * b[k,s], a [N,
  *   S] and b [K, S] from bnn_quant_columns_f8 of the gradient and of the rows; offsets multiples of 128 (bnn_expert_sort with
  *   align 128).  Experts without rows get zeros.
- * M, S, N below 2^31 - 256, K at most 2^22, at most 65535 experts (BNN_ERR_UNSUPPORTED beyond).
+ * M, S, N below 2^31 - 256, K (in the last, S) at most 2^22 - 128, since strides are below 2^22, at most 65535 experts (BNN_ERR_UNSUPPORTED
+ *   beyond).
  */
 BNN_API bnn_status bnn_linear_f8(const uint8_t *a, int64_t lda, const uint8_t *a_scale, int64_t a_scale_ld, const uint8_t *b,
                                  int64_t ldb, const void *b_scale, int b_scale_type, int64_t b_scale_ld, int b_scale_rows,

@@ -57,6 +57,9 @@ __device__ __forceinline__ void f8_store_block(const float (&v)[8], uint8_t *q, 
   if ((c & 127) == 0) scale[c >> 7] = (uint8_t)byte;
 }
 
+// The longest row that products take: whole blocks at a stride below 2^22.
+constexpr int64_t F8_MOST_K = (1 << 22) - F8_BLOCK;
+
 // What operands in this form have to be: rows of whole blocks on 16 bytes, offsets inside a tile of 256 rows in 32 bits.
 inline bnn_status f8_check(const void *q, int64_t ld, const void *scale, int64_t scale_ld, int64_t K, bool products = true) {
   if (ld < f8_row_bytes(K) || scale_ld < f8_scale_bytes(K)) return BNN_ERR_STRIDE;

@@ -198,7 +198,7 @@ extern "C" bnn_status bnn_linear_f8(const uint8_t *a, int64_t lda, const uint8_t
   F8Operands p = {};
   if (M < 0 || N < 0 || K <= 0 || f8_type(p, type) != BNN_OK) return BNN_ERR_SHAPE;
   if (ldy < N) return BNN_ERR_STRIDE;
-  if (M > F8_MOST || N > F8_MOST || K > (1 << 22)) return BNN_ERR_UNSUPPORTED;
+  if (M > F8_MOST || N > F8_MOST || K > F8_MOST_K) return BNN_ERR_UNSUPPORTED;
   if (M == 0 || N == 0) return BNN_OK;
   bnn_status st = f8_check(a, lda, a_scale, a_scale_ld, K);
   if (st == BNN_OK) st = f8_weight(p, b, ldb, b_scale, b_scale_type, b_scale_ld, b_scale_rows, N, K);
@@ -220,7 +220,7 @@ extern "C" bnn_status bnn_expert_linear_f8(const uint8_t *a, int64_t lda, const 
   F8Operands p = {};
   if (S < 0 || N < 0 || K <= 0 || experts < 0 || f8_type(p, type) != BNN_OK) return BNN_ERR_SHAPE;
   if (ldy < N) return BNN_ERR_STRIDE;
-  if (S > F8_MOST || N > F8_MOST || K > (1 << 22) || experts > 65535) return BNN_ERR_UNSUPPORTED;
+  if (S > F8_MOST || N > F8_MOST || K > F8_MOST_K || experts > 65535) return BNN_ERR_UNSUPPORTED;
   if (S == 0 || N == 0 || experts == 0) return BNN_OK;
   bnn_status st = f8_check(a, lda, a_scale, a_scale_ld, K);
   if (st == BNN_OK) st = f8_weight(p, b, ldb, b_scale, b_scale_type, b_scale_ld, b_scale_rows, N, K);
@@ -246,7 +246,7 @@ extern "C" bnn_status bnn_expert_linear_f8_dw(const uint8_t *a, int64_t lda, con
   F8Operands p = {};
   if (S < 0 || N < 0 || K < 0 || experts < 0 || f8_type(p, type) != BNN_OK) return BNN_ERR_SHAPE;
   if (dw_ld < K || (experts > 1 && N > 0 && dw_expert_ld / N < dw_ld)) return BNN_ERR_STRIDE;
-  if (S > (1 << 22) - F8_BLOCK || N > F8_MOST || K > F8_MOST || experts > 65535) return BNN_ERR_UNSUPPORTED;
+  if (S > F8_MOST_K || N > F8_MOST || K > F8_MOST || experts > 65535) return BNN_ERR_UNSUPPORTED;
   if (N == 0 || K == 0 || experts == 0) return BNN_OK;
   if (S > 0) {  // else every group is empty, and the result 0
     bnn_status st = f8_check(a, lda, a_scale, a_scale_ld, S);

@@ -243,7 +243,7 @@ extern "C" bnn_status bnn_quant_columns_f8(const void *x, int type, int64_t T, i
   using namespace bnn;
   if (T < 0 || S < 0 || D <= 0 || !float_type(type) || (rows ? k < 1 : S != T)) return BNN_ERR_SHAPE;
   if (x_ld < D) return BNN_ERR_STRIDE;
-  if (!f8_sizes_fit(T, k, S, D, rows) || S > (1 << 22) - 128) return BNN_ERR_UNSUPPORTED;
+  if (!f8_sizes_fit(T, k, S, D, rows) || S > F8_MOST_K) return BNN_ERR_UNSUPPORTED;
   if (S == 0) return BNN_OK;
   const bnn_status st = f8_check(q, q_ld, scale, scale_ld, S, false);
   if (st != BNN_OK) return st;
@@ -269,7 +269,7 @@ extern "C" bnn_status bnn_quant_weight_f8(const void *w, int type, int64_t exper
   using namespace bnn;
   if (experts < 0 || N <= 0 || K <= 0 || !float_type(type)) return BNN_ERR_SHAPE;
   if (w_ld < K || (experts > 1 && expert_ld < 0)) return BNN_ERR_STRIDE;
-  if (experts > 65535 || N > (1 << 22) || K > (1 << 22)) return BNN_ERR_UNSUPPORTED;
+  if (experts > 65535 || N > (1 << 22) || K > (1 << 22) || (out && K > F8_MOST_K) || (turned && N > F8_MOST_K)) return BNN_ERR_UNSUPPORTED;
   if (experts == 0) return BNN_OK;
   if (!w || (!out && !turned)) return BNN_ERR_NULL;
   QuantWeightParams p = {w, w_ld, expert_ld, (int)N, (int)K, {}, {}};
