@@ -11,15 +11,15 @@ namespace bnn {
 // Which kernel takes a product: that of few rows, or the tiles with the least time by what a round of them was measured to take, in us, with
 // k of b blocks: start + block * b.  one: a compute unit has one tile at a time; two: it has two.  A last round of few tiles takes 0.55 of a round and
 // more (f8_form; 8192 x 4096 to 2048, one round, 61 us, to 2304, a ninth more tiles, 95).  Over 84 sizes drawn at random the form taken is
-// on average 3 % slower than the best of them.  Measured with fast sums in bf16, scales powers of two (exact sums, fp32 results, in brackets), us:
-//   rows x columns x k     256x256    256x128    128x128    the same, short k    128x128, one    128x64    64x64    64x32
-//   64 x 4096 x 4096          40         28         25                             20              13        12       8.6
-//   256 x 4096 x 4096         46         29         27                             21              15        12      15.7
-//   512 x 4096 x 4096         46         29         27                             22              15        19      29.5
-//   1000 x 3001 x 2321        33         20       17.6 (31)     17.3 (26.5)        15 (24)         20 (25)   18 (25)  32
-//   2048 x 4096 x 4096        50 (81)    36 (61)    38 (63)       41 (85)          50 (80)         60        67
-//   8192 x 8192 x 2048       146        178        186 (267)     188 (277)        243             246       287
-//   8192 x 4096 x 512         38 (65)    35 (67)    33 (63)       29 (58)          42 (85)         39 (66)   59
+// on average 3 % slower than the best of them.  Measured in bf16, scales powers of two, fast sums (exact ones in brackets), us:
+//   rows x columns x k     256x256    256x128    128x128    the same, short k    128x128, one    128x64    64x64      64x32
+//   64 x 4096 x 4096       37 (67)       24      23 (31)        22 (27)              17         12 (18)   10 (17)    8.5 (10)
+//   256 x 4096 x 4096      41 (69)       27      24 (32)        23 (27)              18         14 (19)   11 (17)    16 (18)
+//   512 x 4096 x 4096      41 (69)       27      24 (33)        23 (28)              18         14 (21)   16 (24)    29 (35)
+//   1000 x 3001 x 2321     30 (48)       19      17 (23)        16 (20)              13.5       19 (25)   16 (23)    32 (38)
+//   2048 x 4096 x 4096     42 (74)       34      34 (59)        34 (60)              39         52 (78)   54 (85)   110 (133)
+//   8192 x 8192 x 2048    124 (205)     138     134 (226)      137 (233)            166        302 (368) 261 (368)
+//   8192 x 4096 x 512      30 (41)       32      29 (39)        28 (39)              39         63 (76)   55 (65)
 // 128 x 128 tiles come in three: two a unit of four waves each, two a unit of eight waves, whose starts and ends hide each other's better (short
 // k), and one a unit with four steps in LDS.  256 x 256 tiles also come with their last round in quarters (launch_f8_rest).
 enum : int { F8_256, F8_256_128, F8_128, F8_128_SHORT, F8_128_ONE, F8_128_64, F8_64, F8_64_32, F8_FORM_COUNT, F8_256_REST = F8_FORM_COUNT, F8_FEW };
@@ -44,9 +44,13 @@ constexpr F8Cost F8_QUARTERS = {3.5f, 0.58f, 0, 0}, F8_QUARTERS_EXACT = {5, 0.82
 // rows: of all groups, or where these are along k (`same`) of each; blocks: of k a group.
 inline int f8_form(int64_t rows, int64_t groups, bool same, int64_t N, int64_t blocks, bool wide, bool exact, int64_t units) {
   // Few rows: sixteen of A cost what sixteen of B do, so more than a few want tiles where there is enough to stream (16 rows of two
-  // experts, 8192 x 4096 each: 18 us, on 64 x 64 tiles 14), and fewer columns than units can keep busy want k split (one row, 4096 x 4096: 6.0, 11).
+  // experts, 8192 x 4096 each: 17 us, on 64 x 64 tiles with fast sums 13), and fewer columns than units can keep busy want k split (one row, 4096 x
+  // 4096: 6.0, 11).  Exact sums cost tiles more, fp32 scales on top of them more still, so that up to 8 and 12 rows stay here where the weights are
+  // long (exact, few rows and 64 x 64 tiles, 4096 x 4096: 8 rows of each of 8 experts 33 and 40 us, with fp32 scales 12 rows 36 and 42; 16 rows of each
+  // of 4 experts, 8192 x 4096, 54 and 34).  Below 16 MB either takes as long, give or take a microsecond or two.
   const int64_t each = same ? rows : (rows - 1) / groups + 1, columns = groups * ((N - 1) / 16 + 1);
-  if (each <= 4 || (each <= 16 && columns <= 2 * units)) return F8_FEW;
+  const int64_t few = !exact || groups * N * blocks < (16 << 20) / F8_BLOCK ? 4 : wide ? 12 : 8;
+  if (each <= few || (each <= 16 && columns <= 2 * units)) return F8_FEW;
   int best = F8_64;
   double least = 1e30;
   for (int f = 0; f < F8_FORM_COUNT; ++f) {
@@ -89,8 +93,8 @@ bnn_status launch_f8_tile(F8Operands p, hipStream_t s) {
 }
 
 // 256 x 256 tiles as far as they fill rounds of the units, and where few are left for a last one, quarters of those in a launch behind: these take
-// a third of its time (8192 x 4096 to 2304: 95 us as 256 x 256, 87 as 128 x 128, 76 so; 8192 rows of eight experts of uneven parts to 2048: 108,
-// 106, 92; fp32 results 168, 143, 133).  How many there are of groups of rows, the kernels find for themselves.
+// a third of its time (fast sums: 8192 x 4096 to 2304 95 us as 256 x 256, 87 as 128 x 128, 76 so; 8192 rows of eight experts of uneven parts to
+// 2048 108, 106, 92; exact 163, 134, 126).  How many there are of groups of rows, the kernels find for themselves.
 template <class E, bool EXACT>
 bnn_status launch_f8_rest(F8Operands p, hipStream_t s) {
   p.units = device_cu_count();
