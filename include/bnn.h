@@ -423,7 +423,8 @@ BNN_API bnn_status bnn_gated_ff_backward(const void *x, int64_t x_ld, const void
  *   on their elements' size (at least 4).
  *   Values that are not numbers are NaN in e4m3 too, infinities become NaN; neither counts for a block's scale.
  *   No result of these calls shares memory with what the call reads, or with another of its results.
- *   Products take scales from elsewhere with p from -100 to 119; the quantisers give these and, for values from 448 * 2^119 on, 120.
+ *   Products take scales from elsewhere with p from -100 to 119; the quantisers give these and, for values from 448 * 2^119 on, 120. (In a
+ *   product 256 * 2^120, which values from 248 * 2^120 on become, is an infinity.)
  */
 typedef enum { BNN_SCALE_E8M0 = 0, BNN_SCALE_F32 = 1 } bnn_scale_type;
 typedef enum { BNN_FAST_SUMS = 16 } bnn_sums; /* added to BNN_BF16: bnn_linear_f8 */
@@ -465,7 +466,8 @@ BNN_API bnn_status bnn_quant_weight_f8(const void *w, int type, int64_t experts,
  *   of its products' magnitudes before it is rounded: for normal values by 1.5e-5 in the 2-norm, a hundredth of what bf16's rounding costs, but
  *   by many of its steps where a sum cancels.  Calls of few rows take no part in it, so a row's bits depend on how many rows a call has.
  *   a [M, K] with its scales.  b [N, K]; b_scale_rows rows of it share a row of scales: 1, or 128 (bnn_quant_weight_f8).
- *   b_scale_type BNN_SCALE_E8M0, or BNN_SCALE_F32: fp32 scales, any value, b_scale_rows 128, rows of ceil(K / 128).  bias fp32 or NULL.
+ *   b_scale_type BNN_SCALE_E8M0, or BNN_SCALE_F32: fp32 scales, any value, b_scale_rows 128, rows of ceil(K / 128); a block's sum times
+ *   a_scale is rounded to fp32, and has to be in its range, before its scale of b multiplies it.  bias fp32 or NULL.
  *   A training step: y from x and w; dx from bnn_quant_blocks_f8 of dy and `turned` of w; dw from bnn_quant_columns_f8 of dy and x.
  * bnn_expert_linear_f8 -- the same for rows sorted by expert: rows offsets[e] .. offsets[e + 1] - 1 of a [S, K] times b[e], of
  *   [experts, N, K] (b_expert_ld bytes, b_scale_expert_ld scales between experts).  offsets [experts + 1] int32, ascending, as

@@ -1,12 +1,13 @@
 // Matrix-core product of two row-major operands in e4m3 with a scale for each block of 128 values (f8.h),
 //   y[m][n] = sum over blocks of scaleA[m][b] * scaleB[n][b] * (sum over the block's k of A[m][k] * B[n][k]),
-// fp32 sums.  A step of 128 bytes of k is one block.  Scales that are powers of two go into the matrix instruction as bytes;
-// fp32 scales of B, one for 128 rows and a block, multiply a block's sums on the vector unit (the rows' scale is
-// in them by then), which fits into the shadow of the matrix instructions: 16 multiply-adds for two of them.
+// fp32 sums.  A step of 128 bytes of k is one block.  Scales that are powers of two go into the matrix instruction as bytes, or into the widening;
+// fp32 scales of B, one for 128 rows and a block, multiply a block's sums on the vector unit (the rows' scale is in them by then).  These
+// multiply-adds, 16 for two matrix instructions (eight where sums are EXACT), come behind all products of a step and are not hidden by them, and a
+// block's own sums take as many registers as the tile's, so that tiles are 256 x 128 at most: 8192^3 in bf16 1060 us for 715, with FAST sums 740 for 459.
 //
 // Sums are EXACT: values go to bf16 on their way into the 16-bit matrix instruction, times their scales; no digit is lost, and sums are fp32's.
 //
-// bf16 results may be asked for with FAST sums, at twice the rate (8192^3 433 to 478 us, EXACT 760): the 8-bit matrix instruction is exact in single
+// bf16 results may be asked for with FAST sums, up to twice as fast (8192^3 444 to 483 us, EXACT 715): the 8-bit matrix instruction is exact in single
 // products and adds up groups of them in fp32, but of the products of eight consecutive k it keeps no bits below 2^-13 of the largest.  A
 // result is off by less than 2^-10 of the sum of its products' magnitudes, for normal values by 1.5e-5 of itself in the 2-norm, whatever the length:
 // a hundredth of what rounding it to bf16 costs, but more where terms cancel; and where a result is quantised again, values next to
@@ -218,7 +219,7 @@ __device__ __forceinline__ void f8_interleave() {
 // all 64 banks (with r % 8 a read takes twice as long); behind them for each row the
 // four bytes of scales that hold the step's.  WGM x WGN waves of 32 x 32 blocks; KG such groups of waves take the blocks of k in turn, KG
 // of them a step, and their sums meet in the end: small tiles, one a compute unit, are bound by what a step does one after the other
-// (64 x 4096 by 4096 on 64 x 32 tiles 9.9 us with one group, 8.6 with four).
+// (64 x 4096 by 4096 on 64 x 32 tiles, FAST, 9.9 us with one group, 8.6 with four).
 template <int BM, int BN, int WGM, int WGN, int KG, int STAGES, bool WIDE>
 struct F8Tile {
   static constexpr int WAVES = WGM * WGN, ROWS = BM + BN, SCALED = WIDE ? BM : ROWS, LOADS_A = BM / 8 / WAVES, LOADS_ROWS = ROWS / 8 / WAVES,
@@ -557,7 +558,7 @@ __device__ __forceinline__ void f8_tile_product(const F8Operands &p, char *const
       const u32x4 v = *reinterpret_cast<const u32x4 *>(from);
       if (m >= t.M || n >= t.N) continue;
       E *to = reinterpret_cast<E *>(t.y) + m * p.ldy + n;
-      if (n + PER <= t.N) {  // results of large tiles past the caches (8192 x 4096 to 4096 122 -> 119 us)
+      if (n + PER <= t.N) {  // results of large tiles past the caches (8192 x 4096 to 4096, FAST, 122 -> 119 us)
         if constexpr (BM * BN >= 128 * 128) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any *>(to));
         else *reinterpret_cast<u32x4_any *>(to) = v;
       } else
