@@ -104,6 +104,8 @@ class ExpertBlock8:
         (self.E, self.D, self.F), self.act, self.tokens, self.choices, self.fast = w2.shape, act, tokens, choices, fast
         if w1.shape != (self.E, 2 * self.F, self.D):
             raise ValueError(f"w1: [{self.E}, {2 * self.F}, {self.D}] expected")
+        if fast and dtype != torch.bfloat16:
+            raise ValueError("fast: sums of bf16 only")
         (self.w1, _), (self.w2, _) = (B.bnn_quant_weight_f8(w, turned=False) for w in (w1, w2))
         dev, S = w1.device, tokens * choices
         self.offsets = torch.empty((self.E + 1,), dtype=torch.int32, device=dev)

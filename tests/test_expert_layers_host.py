@@ -26,3 +26,9 @@ def test_more_tokens_than_room():
     for t, n in ((65, k), (64, k + 1)):
         with pytest.raises(ValueError, match="made for"):
             served.forward(torch.zeros((t, D)), torch.zeros((t, n), dtype=torch.int32), torch.zeros((t, n)))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_fast_sums_are_bf16s(dtype):
+    with pytest.raises(ValueError, match="bf16 only"):
+        block.ExpertBlock8(torch.zeros((3, 8, D)), torch.zeros((3, D, 4)), tokens=4, choices=k, dtype=dtype, fast=True)
