@@ -46,10 +46,13 @@ inline int f8_form(int64_t rows, int64_t groups, bool same, int64_t N, int64_t b
   // Few rows: sixteen of A cost what sixteen of B do, so more than a few want tiles where there is enough to stream (16 rows of two
   // experts, 8192 x 4096 each: 17 us, on 64 x 64 tiles with fast sums 13), and fewer columns than units can keep busy want k split (one row, 4096 x
   // 4096: 6.0, 11).  Exact sums cost tiles more, fp32 scales on top of them more still, so that up to 8 and 12 rows stay here where the weights are
-  // long (exact, few rows and 64 x 64 tiles, 4096 x 4096: 8 rows of each of 8 experts 33 and 40 us, with fp32 scales 12 rows 36 and 42; 16 rows of each
-  // of 4 experts, 8192 x 4096, 54 and 34).  Below 16 MB either takes as long, give or take a microsecond or two.
+  // long (exact, few rows and 64 x 64 tiles: 8 rows, 16384 x 4096, 15.4 and 17.2 us, with fp32 scales 12 rows 17 and 26); below 16 MB either takes as
+  // long, give or take a microsecond or two.  Rows of experts are uneven, and an expert's weights are read once for 16 rows: 128 rows of 16 experts,
+  // 4096 x 4096, take 59 and 73 evenly spread, 60 and 50 where every expert has a quarter of what the one of half its rank has, so 8 rows on
+  // average stay with fp32 scales only (64 rows of 8 experts, 33 and 42).
   const int64_t each = same ? rows : (rows - 1) / groups + 1, columns = groups * ((N - 1) / 16 + 1);
-  const int64_t few = !exact || groups * N * blocks < (16 << 20) / F8_BLOCK ? 4 : wide ? 12 : 8;
+  const bool uneven = groups > 1 && !same, streamed = groups * N * blocks >= (16 << 20) / F8_BLOCK;
+  const int64_t few = !exact || !streamed ? 4 : uneven ? (wide ? 8 : 4) : wide ? 12 : 8;
   if (each <= few || (each <= 16 && columns <= 2 * units)) return F8_FEW;
   int best = F8_64;
   double least = 1e30;

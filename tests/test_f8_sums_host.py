@@ -21,9 +21,10 @@ def test_types_of_results(type, status):
 @pytest.mark.parametrize("type", [F32, BF16, F16])
 @pytest.mark.parametrize("kind", [0, 1])
 def test_few_rows(type, kind):
-    """Up to 4 rows an expert are few; with exact sums (for this call all types but bf16) and 16 MB of weights up to 8, with fp32 scales 12."""
+    """Up to 4 rows, on average of the experts, are few; with exact sums (for this call all types but bf16) and 16 MB of weights up to 8, with fp32
+    scales 12; of experts, which have uneven rows, 4 and 8."""
     form = lambda rows, experts, N, K: B.lib().bnn_testing_f8_form(rows, experts, 0, N, K, kind, type, 256)
-    most = 4 if type == BF16 else 12 if kind else 8
-    for experts, N, K in ((8, 4096, 4096), (1, 16384, 4096), (4, 8192, 512)):  # the last: 16 MB
-        assert form(experts * most, experts, N, K) == 9 != form(experts * most + 1, experts, N, K)
-    assert form(4 * 4, 4, 8192, 384) == 9 != form(4 * 4 + 1, 4, 8192, 384)
+    for experts, N, K, most in ((8, 4096, 4096, (4, 8)), (1, 16384, 4096, (8, 12)), (4, 8192, 512, (4, 8)), (1, 32768, 512, (8, 12)),
+                                (4, 8192, 384, (4, 4)), (1, 32768, 384, (4, 4))):  # 16 MB, and less
+        n = experts * (4 if type == BF16 else most[kind])
+        assert form(n, experts, N, K) == 9 != form(n + 1, experts, N, K)
